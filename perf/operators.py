@@ -304,8 +304,7 @@ def run(s):
             return {"h": A.gated_forward(s["x"], s["wg"], s["wu"], case["act"], out=s["h"])}
         saved = A.gated_saved(s["x"], s["wg"])
         h = A.gated_forward(s["x"], s["wg"], s["wu"], case["act"], out=s["h"], saved=saved)
-        dx, dwg, dwu = A.gated_backward(s["dh"], s["x"], s["wg"], s["wu"], saved, case["act"], dx=s["dx"], dwg=s["dwg"],
-                                        dwu=s["dwu"])
+        dx, dwg, dwu = A.gated_backward(s["dh"], s["x"], s["wg"], s["wu"], saved, dx=s["dx"], dwg=s["dwg"], dwu=s["dwu"])
         return {"h": h, "dx": dx, "dwg": dwg, "dwu": dwu}
     r = A.token_logprobs(s["logits"], s["tokens"], top=case["top"])
     out = {"logp": r.logp, "entropy": r.entropy}
