@@ -402,6 +402,97 @@ int antdt_dense_aggregate_adam(float* p, float* m, float* v, const float* const*
                                double beta2, double eps, int64_t step, void* stream);
 
 /*
+ * Operators on sequences of tokens (ids of items, one row each, not pooled): what a model that reads a
+ * user's history and answers with an item needs next to the ranking model.  Context-free: they work on the
+ * caller's buffers alone, enqueue their kernels on `stream`, allocate nothing and keep nothing between calls.
+ * Common to all of them:
+ *  - matrices are row-major, `ld...` elements from one row to the next, at least the row's length; any alignment
+ *    of the element type is accepted (16-byte aligned rows are read and written 16 bytes at a time) unless said
+ *    otherwise.  Buffers must not overlap unless said otherwise.
+ *  - dtype: ANTDT_F32 or ANTDT_BF16.  All arithmetic is fp32; results are rounded once, to nearest even.
+ *  - a token outside [0, V) is padding: it has no row and no gradient.
+ *  - empty shapes are legal and enqueue what is left to do (usually nothing); their buffers may be NULL.
+ *  - `workspace`: DEVICE, 256-byte aligned, of at least the size that the matching ..._bytes call reports (0: may be
+ *    NULL).  It holds nothing between calls and needs no clearing; calls that overlap need one each.
+ *  - INVALID_ARG, naming the argument, before anything is enqueued.
+ */
+
+/*
+ * A dropout, for antdt_dropout and the calls that apply one on the way.  Column c of row r is dropped where 16-bit lot
+ * c mod 8 of Philox4x32-10 (Salmon et al., SC'11; counter (c / 8, r, r >> 32, call), key seed + *step; lots in the order of
+ * the output words, low half first) is below t = round(65536 p); otherwise it is multiplied by 65536 / (65536 - t), so
+ * that the expected value is kept to the last bit.  The mask is never stored: the gradient's pass forms it again
+ * from the same four values.
+ */
+typedef struct antdt_dropout_spec {
+  float p;               /* probability of being dropped, 0..1 (1: everything) */
+  uint32_t call;         /* which of a step's dropouts this is */
+  uint64_t seed;
+  const uint64_t* step;  /* DEVICE, added to seed when the kernel runs (a captured graph draws anew when it changes); NULL: 0 */
+} antdt_dropout_spec;
+
+/* y = residual + dropout(x), or dropout(x) when residual is NULL.  x, residual, y: DEVICE [rows, cols] of `dtype`; y may be x or
+ * residual (with the same ld).  The gradient with respect to x is antdt_dropout of that with respect to y, without a residual. */
+int antdt_dropout(const void* x, int64_t ldx, const void* residual, int64_t ldr, int64_t rows, int64_t cols,
+                  int32_t dtype, const antdt_dropout_spec* drop, void* y, int64_t ldy, void* stream);
+
+/* out[n, :] = scale * dropout(table[tokens[n], :]), zeros for padding.  table: DEVICE [V, D] of `dtype`; tokens: DEVICE int32 [N];
+ * out: DEVICE [N, D] of `out_dtype`.  drop (HOST, may be NULL: none) has a row per n.  V, N < 2^31 - 1, D < 2^24. */
+int antdt_token_lookup(const void* table, int64_t ldt, int64_t V, int64_t D, int32_t dtype, const int32_t* tokens, int64_t N,
+                       float scale, const antdt_dropout_spec* drop, void* out, int64_t ldo, int32_t out_dtype, void* stream);
+
+/* The gradient of the table: grad[v, :] = sum over n with tokens[n] == v of scale * dropout(dy[n, :]), added up in an order that
+ * depends on the tokens alone.  dy: DEVICE [N, D] of `dtype`; grad: DEVICE fp32 [V, D], every row written, or, with accumulate
+ * != 0, the sums added to the rows that tokens name and no other row touched. */
+int antdt_token_gradient_bytes(int64_t N, int64_t V, int64_t D, size_t* bytes);
+int antdt_token_gradient(const void* dy, int64_t lddy, int32_t dtype, const int32_t* tokens, int64_t N, float scale,
+                         const antdt_dropout_spec* drop, float* grad, int64_t ldg, int64_t V, int64_t D, int32_t accumulate,
+                         void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Gated feed-forward block: h = act(x Wg) * (x Wu), both projections, the activation and the product in one kernel.
+ * x: DEVICE [N, K], Wg, Wu: DEVICE [K, H] (ldw both), h: DEVICE [N, H], all of `dtype`.  K, H >= 1; of bf16, K, H and every ld are
+ * multiples of 8 and the buffers 16-byte aligned (ANTDT_UNSUPPORTED otherwise).  K, H < 2^20, ld < 2^21; N max(K, H) and
+ * 2 K H below 2^36.
+ * saved: DEVICE buffer of antdt_gated_saved_bytes, 256-byte aligned, filled with what antdt_gated_backward needs, or NULL.
+ */
+enum { ANTDT_ACT_SILU = 0, ANTDT_ACT_GELU = 1 /* g * Phi(g), by erf */, ANTDT_ACT_RELU = 2, ANTDT_ACT_SIGMOID = 3 };
+int antdt_gated_saved_bytes(int64_t N, int64_t H, int32_t dtype, size_t* bytes);
+int antdt_gated_forward_bytes(int64_t N, int64_t K, int64_t H, int32_t dtype, size_t* bytes);
+int antdt_gated_forward(const void* x, int64_t ldx, const void* wg, const void* wu, int64_t ldw, int64_t N, int64_t K, int64_t H,
+                        int32_t dtype, int32_t act, void* h, int64_t ldh, void* saved, void* workspace, size_t workspace_bytes,
+                        void* stream);
+/* Its gradients, from dh = that of h: dx [N, K] (or NULL), dwg and dwu [K, H] (lddw both; both or neither NULL), of `dtype`.  x, Wg, Wu
+ * and saved as antdt_gated_forward was given and left them. */
+int antdt_gated_backward_bytes(int64_t N, int64_t K, int64_t H, int32_t dtype, size_t* bytes);
+int antdt_gated_backward(const void* dh, int64_t lddh, const void* x, int64_t ldx, const void* wg, const void* wu, int64_t ldw,
+                         int64_t N, int64_t K, int64_t H, int32_t dtype, const void* saved, void* dx, int64_t lddx, void* dwg,
+                         void* dwu, int64_t lddw, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Log probabilities under rows of logits (DEVICE [N, V] of `dtype`; -infinity = not allowed), p = softmax of the row:
+ *   logp        fp32 [N]         log p[tokens[n]]; 0 for padding.  NULL, as tokens, when not wanted
+ *   entropy     fp32 [N]         -sum p log p (terms of p = 0 are 0).  May be NULL
+ *   stats       fp32 [N, 4]      for antdt_token_logprobs_gradient: largest logit, log of the sum of exp(logit - largest), entropy, 0.
+ *                                May be NULL
+ *   top_logp    fp32 [N, top]    the `top` largest log probabilities, descending, and
+ *   top_index   int32 [N, top]   their columns, equal logits by the lower column; 0 <= top <= min(V, ANTDT_MAX_TOP)
+ * A row without an allowed column (all -infinity): logp and top_logp -infinity, entropy 0.  A row with a NaN or +infinity: NaN, its
+ * NaN counted largest in top_index.  1 <= V < 2^31.
+ */
+#define ANTDT_MAX_TOP 64
+int antdt_token_logprobs_bytes(int64_t N, int64_t V, int32_t top, size_t* bytes);
+int antdt_token_logprobs(const void* logits, int64_t ld, int64_t N, int64_t V, int32_t dtype, const int32_t* tokens, float* logp,
+                         float* entropy, float* stats, int32_t top, float* top_logp, int32_t* top_index, void* workspace,
+                         size_t workspace_bytes, void* stream);
+/* d_logits[n, j] = d_logp[n] * ([j == tokens[n]] - p_j) - d_entropy[n] * p_j * (log p_j + entropy), of `dtype`; a row without an allowed
+ * column and (in the first term) padding give zeros.  d_logp (with tokens), d_entropy: DEVICE fp32 [N], either may be NULL.
+ * d_logits may be logits (with the same ld). */
+int antdt_token_logprobs_gradient(const void* logits, int64_t ld, int64_t N, int64_t V, int32_t dtype, const int32_t* tokens,
+                                  const float* stats, const float* d_logp, const float* d_entropy, void* d_logits, int64_t ldd,
+                                  void* stream);
+
+/*
  * Plain streaming copy dst[i] = src[i], i < n (measurement aid, not part of the iteration): the
  * bandwidth this kernel reaches on a large buffer is the practical ceiling that the memory-bound
  * kernels of the iteration are compared with, and its known traffic (4n bytes read, 4n written)

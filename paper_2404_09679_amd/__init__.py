@@ -20,3 +20,15 @@ from .binding import (  # noqa: F401
     plan_accumulation,
     stream_copy,
 )
+from .tokens import (  # noqa: F401
+    Dropout,
+    LogProbs,
+    dropout,
+    gated_backward,
+    gated_forward,
+    gated_saved,
+    token_gradient,
+    token_logprobs,
+    token_logprobs_gradient,
+    token_lookup,
+)

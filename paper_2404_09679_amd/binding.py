@@ -27,6 +27,9 @@ EXPORTS = [
     "antdt_set_eager_weight_gradients", "antdt_set_library_streams",
     "antdt_dds_create", "antdt_dds_destroy", "antdt_dds_num_shards", "antdt_dds_fetch", "antdt_dds_report_done",
     "antdt_dds_release_worker", "antdt_dds_shard", "antdt_dds_counts", "antdt_simulate_bsp",
+    "antdt_dropout", "antdt_token_lookup", "antdt_token_gradient_bytes", "antdt_token_gradient",
+    "antdt_gated_saved_bytes", "antdt_gated_forward_bytes", "antdt_gated_forward", "antdt_gated_backward_bytes",
+    "antdt_gated_backward", "antdt_token_logprobs_bytes", "antdt_token_logprobs", "antdt_token_logprobs_gradient",
 ]
 
 
@@ -55,6 +58,10 @@ class SimConfig(C.Structure):
                 ("policy", C.c_int32), ("backup_b", C.c_int32), ("decide_every", C.c_double),
                 ("L_trans", C.c_double), ("L_per", C.c_double), ("lam", C.c_double), ("restart_cost", C.c_double),
                 ("max_iterations", C.c_int64)]
+
+
+class DropoutSpec(C.Structure):
+    _fields_ = [("p", C.c_float), ("call", C.c_uint32), ("seed", C.c_uint64), ("step", C.c_void_p)]
 
 
 class SimResult(C.Structure):
@@ -116,6 +123,20 @@ def _load():
                                             C.POINTER(C.c_double)]
     lib.antdt_expand_accumulation.argtypes = [i32, C.POINTER(i32), C.POINTER(i64), C.POINTER(i32), i32,
                                               C.POINTER(i64), C.POINTER(i32), C.POINTER(i32)]
+    size, drop = C.POINTER(C.c_size_t), C.POINTER(DropoutSpec)
+    lib.antdt_dropout.argtypes = [vp, i64, vp, i64, i64, i64, i32, drop, vp, i64, vp]
+    lib.antdt_token_lookup.argtypes = [vp, i64, i64, i64, i32, vp, i64, f32, drop, vp, i64, i32, vp]
+    lib.antdt_token_gradient_bytes.argtypes = [i64, i64, i64, size]
+    lib.antdt_token_gradient.argtypes = [vp, i64, i32, vp, i64, f32, drop, vp, i64, i64, i64, i32, vp, C.c_size_t, vp]
+    lib.antdt_gated_saved_bytes.argtypes = [i64, i64, i32, size]
+    lib.antdt_gated_forward_bytes.argtypes = [i64, i64, i64, i32, size]
+    lib.antdt_gated_forward.argtypes = [vp, i64, vp, vp, i64, i64, i64, i64, i32, i32, vp, i64, vp, vp, C.c_size_t, vp]
+    lib.antdt_gated_backward_bytes.argtypes = [i64, i64, i64, i32, size]
+    lib.antdt_gated_backward.argtypes = [vp, i64, vp, i64, vp, vp, i64, i64, i64, i64, i32, vp, vp, i64, vp, vp, i64, vp,
+                                         C.c_size_t, vp]
+    lib.antdt_token_logprobs_bytes.argtypes = [i64, i64, i32, size]
+    lib.antdt_token_logprobs.argtypes = [vp, i64, i64, i64, i32, vp, vp, vp, vp, i32, vp, vp, vp, C.c_size_t, vp]
+    lib.antdt_token_logprobs_gradient.argtypes = [vp, i64, i64, i64, i32, vp, vp, vp, vp, vp, i64, vp]
     return lib
 
 

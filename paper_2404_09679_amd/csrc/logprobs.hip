@@ -1,0 +1,495 @@
+// Log probabilities of given tokens under rows of logits, with entropy and top alternatives, and the gradient of the logits.
+// With m the largest logit of a row, s = sum e^(x - m) and q = sum e^(x - m) (x - m):
+//   log p_j = (x_j - m) - log s,   H = log s - q / s,
+// all three kept up in one pass (a new maximum scales s and q), so that a row is read once; bound by memory.
+#include <algorithm>
+
+#include "ops.h"
+
+namespace antdt {
+namespace {
+
+constexpr int LP_THREADS = 512, LP_WAVES = LP_THREADS / 64;
+constexpr int LP_LIST = 1024;           // candidates kept for the top
+constexpr float NEG_INF = -__builtin_inff();
+
+struct LpArgs {
+  const void* x;
+  int64_t ld, N, V;
+  const int32_t* tokens;
+  float* logp;
+  float* entropy;
+  float4* stats;
+  float* top_logp;
+  int32_t* top_index;
+  int32_t top, pieces;
+  float4* part;       // [N, pieces] m, s, q
+  uint64_t* part_top; // [N, pieces, top]
+};
+
+// A logit and its column as one number: larger values first, NaN above all, equal values by the lower column; never 0 or all ones.
+__device__ __forceinline__ uint64_t rank_key(float x, uint32_t col) {
+  const uint32_t u = __float_as_uint(x == 0.0f ? 0.0f : x);
+  const uint32_t o = x != x ? 0xFFFFFFF0u : (u >> 31) ? ~u : u | 0x80000000u;
+  return (uint64_t)o << 32 | (uint32_t)~col;
+}
+__device__ __forceinline__ float key_value(uint64_t k) {
+  const uint32_t o = (uint32_t)(k >> 32);
+  return __uint_as_float((o >> 31) ? o & 0x7FFFFFFFu : ~o);   // (NaN stays one)
+}
+__device__ __forceinline__ int32_t key_column(uint64_t k) { return (int32_t) ~(uint32_t)k; }
+
+// A NaN, or two infinities, make s a NaN, and it stays one.
+struct Softmax {
+  float m = NEG_INF, s = 0.0f, q = 0.0f;
+  // what logits are taken relative to
+  static __device__ __forceinline__ float base(float m) { return m == NEG_INF ? 0.0f : m; }
+  __device__ __forceinline__ void raise(float to) {
+    if (to > m) {
+      if (m != NEG_INF) {
+        const float d = m - to, r = __expf(d);
+        q = r == 0.0f ? 0.0f : r * (q + d * s);
+        s *= r;
+      }
+      m = to;
+    }
+  }
+  // x <= m
+  __device__ __forceinline__ void add(float x) {
+    const float d = x - base(m), e = __expf(d);
+    s += e;
+    q += e == 0.0f ? 0.0f : e * d;
+  }
+  __device__ __forceinline__ void join(float m2, float s2, float q2) {
+    if (m2 > m) {
+      const float d = base(m) - m2, r = m == NEG_INF ? 0.0f : __expf(d);
+      q = (r == 0.0f ? 0.0f : r * (q + d * s)) + q2;
+      s = s * r + s2;
+      m = m2;
+    } else {
+      const float d = base(m2) - base(m), r = m2 == NEG_INF ? 0.0f : __expf(d);
+      q += r == 0.0f ? 0.0f : r * (q2 + d * s2);
+      s += s2 * r;
+    }
+  }
+};
+
+// Columns [c0, c1) of a row in the thread's share: up to the first 16-byte boundary and from the last on one by one, 16 bytes at a
+// time in between.  f(values, first column, how many), columns of a thread ascending.
+template <typename T>
+struct RowWalk {
+  static constexpr int VN = 16 / sizeof(T);
+  const T* row;
+  int64_t c0, c1, body, vecs;   // first whole vector's column, whole vectors
+  __device__ __forceinline__ RowWalk(const T* row_, int64_t c0_, int64_t c1_) : row(row_), c0(c0_), c1(c1_) {
+    const int off = (int)((reinterpret_cast<uintptr_t>(row + c0) & 15) / sizeof(T));
+    body = min(c1, c0 + (off ? VN - off : 0));
+    vecs = (c1 - body) / VN;
+  }
+  static __device__ __forceinline__ void unpack(const uint4& w, float (&v)[VN]) {
+    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if constexpr (VN == 4) {
+        v[e] = __uint_as_float(u[e]);
+      } else {
+        v[2 * e] = __uint_as_float(u[e] << 16);
+        v[2 * e + 1] = __uint_as_float(u[e] & 0xFFFF0000u);
+      }
+    }
+  }
+  template <typename F>
+  __device__ __forceinline__ void one(int64_t c, F&& f) const {
+    float v[VN];
+    v[0] = to_f32(row[c]);
+#pragma unroll
+    for (int e = 1; e < VN; ++e) v[e] = NEG_INF;
+    f(v, c, 1);
+  }
+  template <int THREADS, typename F>
+  __device__ __forceinline__ void each(int tid, F&& f) const {
+    if (c0 + tid < body) one(c0 + tid, f);
+    constexpr int U = 4;
+    const uint4* p = reinterpret_cast<const uint4*>(row + body);
+    int64_t i = tid;
+    for (; i + (U - 1) * THREADS < vecs; i += U * THREADS) {
+      uint4 w[U];
+#pragma unroll
+      for (int q = 0; q < U; ++q) w[q] = p[i + q * THREADS];
+#pragma unroll
+      for (int q = 0; q < U; ++q) {
+        float v[VN];
+        unpack(w[q], v);
+        f(v, body + (i + q * THREADS) * VN, VN);
+      }
+    }
+    for (; i < vecs; i += THREADS) {
+      float v[VN];
+      unpack(p[i], v);
+      f(v, body + i * VN, VN);
+    }
+    const int64_t c = body + vecs * VN + tid;
+    if (c < c1) one(c, f);
+  }
+};
+
+__device__ __forceinline__ uint64_t shfl_xor64(uint64_t x, int o) {
+  const uint32_t lo = __shfl_xor((uint32_t)x, o, 64), hi = __shfl_xor((uint32_t)(x >> 32), o, 64);
+  return (uint64_t)hi << 32 | lo;
+}
+
+struct LpLds {
+  uint64_t list[LP_LIST];
+  uint64_t best[LP_WAVES * 64];
+  uint64_t threshold;
+  int count;
+  float m[LP_WAVES], s[LP_WAVES], q[LP_WAVES];
+};
+
+// The block's sums from its threads'.
+__device__ __forceinline__ Softmax block_softmax(LpLds& lds, Softmax x) {
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const float m = __shfl_xor(x.m, o, 64), s = __shfl_xor(x.s, o, 64), q = __shfl_xor(x.q, o, 64);
+    x.join(m, s, q);
+  }
+  if (lane == 0) {
+    lds.m[w] = x.m; lds.s[w] = x.s; lds.q[w] = x.q;
+  }
+  __syncthreads();
+  Softmax r;
+  for (int i = 0; i < (int)(blockDim.x >> 6); ++i) r.join(lds.m[i], lds.s[i], lds.q[i]);
+  return r;
+}
+
+// The k largest keys, in order, to out(rank, key).  `mine`: the largest key of this thread's share; rescan(f) calls f(key) for every
+// key of the share.  The threads go into G >= k groups: the smallest of the groups' largest keys has k keys at or above it, and few more
+// (about G ln G of evenly spread ones); those are listed and ranked.  More than the list holds, or `exact`: the largest key below
+// the last one, k times over.  At least k keys exist.
+template <typename Rescan, typename Out>
+__device__ __forceinline__ void block_top(LpLds& lds, int k, uint64_t mine, bool exact, Rescan&& rescan, Out&& out) {
+  const int tid = threadIdx.x, lane = tid & 63, waves = blockDim.x >> 6;
+  int G = 8;
+  while (G < k) G <<= 1;   // k <= 64
+  uint64_t b = mine;
+  for (int o = G; o < 64; o <<= 1) b = max(b, shfl_xor64(b, o));
+  __syncthreads();         // (lds.best may still be read)
+  lds.best[tid] = b;       // lanes 0 .. G - 1 of every wavefront
+  if (tid == 0) lds.count = 0;
+  __syncthreads();
+  if (tid < 64) {
+    uint64_t t = ~0ull;
+    if (lane < G) {
+      t = 0;
+      for (int w = 0; w < waves; ++w) t = max(t, lds.best[w * 64 + lane]);
+    }
+    for (int o = 1; o < 64; o <<= 1) t = min(t, shfl_xor64(t, o));
+    if (tid == 0) lds.threshold = t;
+  }
+  __syncthreads();
+  const uint64_t threshold = lds.threshold;
+  if (!exact && mine != 0 && mine >= threshold)
+    rescan([&](uint64_t key) {
+      if (key >= threshold) {
+        const int at = atomicAdd(&lds.count, 1);   // (in any order: ranked below)
+        if (at < LP_LIST) lds.list[at] = key;
+      }
+    });
+  __syncthreads();
+  const int n = lds.count;
+  if (!exact && n <= LP_LIST) {
+    for (int i = tid; i < n; i += blockDim.x) {
+      const uint64_t key = lds.list[i];
+      int above = 0;
+      for (int j = 0; j < n; ++j) above += lds.list[j] > key;
+      if (above < k) out(above, key);
+    }
+    return;
+  }
+  uint64_t last = ~0ull;
+  for (int r = 0; r < k; ++r) {
+    uint64_t t = 0;
+    rescan([&](uint64_t key) {
+      if (key < last) t = max(t, key);
+    });
+    for (int o = 1; o < 64; o <<= 1) t = max(t, shfl_xor64(t, o));
+    __syncthreads();
+    if (lane == 0) lds.best[tid >> 6] = t;
+    __syncthreads();
+    for (int w = 0; w < waves; ++w) t = max(t, lds.best[w]);
+    if (tid == 0) out(r, t);
+    last = t;
+  }
+}
+
+// A row's results from its sums (by one thread).
+__device__ __forceinline__ void write_row_stats(const LpArgs& a, int64_t row, const Softmax& t, float log_s) {
+  const bool none = t.m == NEG_INF && t.s == 0.0f;
+  const float h = none ? 0.0f : log_s - t.q / t.s;
+  if (a.entropy) a.entropy[row] = h;
+  if (a.stats) a.stats[row] = make_float4(t.m, log_s, h, 0.0f);
+}
+__device__ __forceinline__ float log_prob(const Softmax& t, float log_s, float x) {
+  return t.m == NEG_INF && t.s == 0.0f ? NEG_INF : (x - Softmax::base(t.m)) - log_s;
+}
+template <typename T>
+__device__ __forceinline__ void write_logp(const LpArgs& a, int64_t row, const Softmax& t, float log_s) {
+  if (!a.logp) return;
+  const int64_t tok = a.tokens[row];
+  a.logp[row] = tok >= 0 && tok < a.V ? log_prob(t, log_s, to_f32(reinterpret_cast<const T*>(a.x)[row * a.ld + tok])) : 0.0f;
+}
+
+// A block per row, or per piece of one: its sums and top then go to memory for lp_join_kernel.
+template <typename T, bool TOP>
+__global__ __launch_bounds__(LP_THREADS) void lp_kernel(LpArgs a) {
+  __shared__ LpLds lds;
+  const int64_t row = blockIdx.x / a.pieces;
+  const int piece = (int)(blockIdx.x - row * a.pieces), tid = threadIdx.x;
+  const RowWalk<T> walk(reinterpret_cast<const T*>(a.x) + row * a.ld, a.V * piece / a.pieces, a.V * (piece + 1) / a.pieces);
+  constexpr int VN = RowWalk<T>::VN;
+  Softmax t;
+  int64_t best = 0;   // column of the thread's first largest logit
+  bool any = false;
+  walk.template each<LP_THREADS>(tid, [&](const float (&v)[VN], int64_t c, int n) {
+    float vm = v[0];
+#pragma unroll
+    for (int e = 1; e < VN; ++e) vm = fmaxf(vm, v[e]);
+    if (vm > t.m || (TOP && !any)) {
+      if (TOP) {
+        best = c;
+        for (int e = VN - 1; e >= 0; --e)
+          if (e < n && v[e] == vm) best = c + e;
+        any = true;
+      }
+      t.raise(vm);
+    }
+#pragma unroll
+    for (int e = 0; e < VN; ++e)
+      if (e < n) t.add(v[e]);
+  });
+  const float mine = t.m;
+  t = block_softmax(lds, t);
+  const float log_s = logf(t.s);
+  if constexpr (TOP) {
+    const int64_t at = (row * a.pieces + piece) * a.top;
+    block_top(
+        lds, a.top, any ? rank_key(mine, (uint32_t)best) : 0, t.s != t.s,
+        [&](auto&& f) {
+          walk.template each<LP_THREADS>(tid, [&](const float (&v)[VN], int64_t c, int n) {
+#pragma unroll
+            for (int e = 0; e < VN; ++e)
+              if (e < n) f(rank_key(v[e], (uint32_t)(c + e)));
+          });
+        },
+        [&](int r, uint64_t key) {
+          if (a.pieces > 1) {
+            a.part_top[at + r] = key;
+          } else {
+            a.top_logp[at + r] = log_prob(t, log_s, key_value(key));
+            a.top_index[at + r] = key_column(key);
+          }
+        });
+  }
+  if (tid == 0) {
+    if (a.pieces > 1) {
+      a.part[blockIdx.x] = make_float4(t.m, t.s, t.q, 0.0f);
+    } else {
+      write_row_stats(a, row, t, log_s);
+      write_logp<T>(a, row, t, log_s);
+    }
+  }
+}
+
+// The pieces of a row put together: a block per row.
+constexpr int JOIN_KEYS = 4096;   // pieces * top at most
+template <typename T>
+__global__ __launch_bounds__(LP_THREADS) void lp_join_kernel(LpArgs a) {
+  __shared__ LpLds lds;
+  const int64_t row = blockIdx.x;
+  const int tid = threadIdx.x;
+  Softmax t;
+  for (int p = tid; p < a.pieces; p += LP_THREADS) {
+    const float4 v = a.part[row * a.pieces + p];
+    t.join(v.x, v.y, v.z);
+  }
+  t = block_softmax(lds, t);
+  const float log_s = logf(t.s);
+  if (a.top > 0) {
+    const uint64_t* keys = a.part_top + row * a.pieces * a.top;
+    const int n = a.pieces * a.top;
+    uint64_t mine = 0;
+    for (int i = tid; i < n; i += LP_THREADS) mine = max(mine, keys[i]);
+    block_top(
+        lds, a.top, mine, false,
+        [&](auto&& f) {
+          for (int i = tid; i < n; i += LP_THREADS) f(keys[i]);
+        },
+        [&](int r, uint64_t key) {
+          a.top_logp[row * a.top + r] = log_prob(t, log_s, key_value(key));
+          a.top_index[row * a.top + r] = key_column(key);
+        });
+  }
+  if (tid == 0) {
+    write_row_stats(a, row, t, log_s);
+    write_logp<T>(a, row, t, log_s);
+  }
+}
+
+// Pieces of a row: with fewer rows than the chip holds blocks, until they fill it, but no shorter than a block's threads have
+// two vectors each to read.
+int lp_pieces(int64_t N, int64_t V, int32_t top) {
+  if (N >= 512) return 1;
+  int64_t p = std::min(div_up(1024, std::max<int64_t>(N, 1)), V / 4096);
+  if (top > 0) p = std::min<int64_t>(p, JOIN_KEYS / top);
+  return (int)std::max<int64_t>(p, 1);
+}
+
+// ------------------------------------------------------------- gradient
+struct LpGradArgs {
+  const void* x;
+  void* dx;
+  int64_t ld, ldd, N, V;
+  const int32_t* tokens;
+  const float4* stats;
+  const float* d_logp;
+  const float* d_entropy;
+  int64_t pieces, piece;   // columns of a piece
+};
+constexpr int LG_THREADS = 256;
+
+template <typename T, bool SAME>   // SAME: both rows reach a 16-byte boundary at the same column
+__global__ __launch_bounds__(LG_THREADS) void lp_grad_kernel(LpGradArgs a) {
+  constexpr int VN = RowWalk<T>::VN;
+  for (int64_t id = blockIdx.x; id < a.N * a.pieces; id += gridDim.x) {
+    const int64_t row = id / a.pieces, c0 = (id - row * a.pieces) * a.piece, c1 = min(c0 + a.piece, a.V);
+    const float4 st = a.stats[row];
+    int64_t tok = -1;
+    float ga = 0.0f;
+    if (a.d_logp) {
+      tok = a.tokens[row];
+      ga = tok >= 0 && tok < a.V ? a.d_logp[row] : 0.0f;
+    }
+    const float gb = a.d_entropy ? a.d_entropy[row] : 0.0f;
+    const bool none = (st.x == NEG_INF && st.y == NEG_INF) || (ga == 0.0f && gb == 0.0f);
+    T* out = reinterpret_cast<T*>(a.dx) + row * a.ldd;
+    auto grad = [&](float x, int64_t c) {
+      const float lp = (x - st.x) - st.y, p = __expf(lp);
+      float g = ga * ((c == tok ? 1.0f : 0.0f) - p);
+      if (gb != 0.0f) g -= p == 0.0f ? 0.0f : gb * p * (lp + st.z);
+      return none ? 0.0f : g;
+    };
+    const RowWalk<T> walk(reinterpret_cast<const T*>(a.x) + row * a.ld, c0, c1);
+    if constexpr (SAME) {
+      walk.template each<LG_THREADS>(threadIdx.x, [&](const float (&v)[VN], int64_t c, int n) {
+        if (n == 1) {
+          out[c] = from_f32<T>(grad(v[0], c));
+        } else {
+          float g[VN];
+#pragma unroll
+          for (int e = 0; e < VN; ++e) g[e] = grad(v[e], c + e);
+          if constexpr (VN == 4) *reinterpret_cast<float4*>(out + c) = make_float4(g[0], g[1], g[2], g[3]);
+          else *reinterpret_cast<uint4*>(out + c) = make_uint4(f2bf2(g[0], g[1]), f2bf2(g[2], g[3]), f2bf2(g[4], g[5]), f2bf2(g[6], g[7]));
+        }
+      });
+    } else {
+      for (int64_t c = c0 + threadIdx.x; c < c1; c += LG_THREADS) out[c] = from_f32<T>(grad(to_f32(walk.row[c]), c));
+    }
+  }
+}
+
+}  // namespace
+}  // namespace antdt
+
+using namespace antdt;
+
+static int lp_sizes(const char* call, int64_t N, int64_t V, int32_t top) {
+  if (N < 0 || N >= INT32_MAX / 4 || V < 1 || V >= INT32_MAX) return op_fail(ANTDT_INVALID_ARG, "%s: N or V out of range", call);
+  if (top < 0 || top > ANTDT_MAX_TOP || top > V) return op_fail(ANTDT_INVALID_ARG, "%s: top must be 0 .. min(V, %d)", call, ANTDT_MAX_TOP);
+  return ANTDT_OK;
+}
+static size_t lp_bytes(int64_t N, int64_t V, int32_t top) {
+  const int64_t p = lp_pieces(N, V, top);
+  return N == 0 || p == 1 ? 0 : (size_t)(N * p) * (sizeof(float4) + 8 * (size_t)top);
+}
+
+extern "C" {
+
+int antdt_token_logprobs_bytes(int64_t N, int64_t V, int32_t top, size_t* bytes) {
+  const char* call = "antdt_token_logprobs_bytes";
+  if (!bytes) return op_fail(ANTDT_INVALID_ARG, "%s: bytes is null", call);
+  OP_TRY(lp_sizes(call, N, V, top));
+  *bytes = lp_bytes(N, V, top);
+  return ANTDT_OK;
+}
+
+int antdt_token_logprobs(const void* logits, int64_t ld, int64_t N, int64_t V, int32_t dtype, const int32_t* tokens, float* logp, float* entropy,
+                         float* stats, int32_t top, float* top_logp, int32_t* top_index, void* workspace, size_t workspace_bytes, void* stream) {
+  const char* call = "antdt_token_logprobs";
+  if (!op_dtype(dtype)) return op_fail(ANTDT_INVALID_ARG, "%s: dtype", call);
+  OP_TRY(lp_sizes(call, N, V, top));
+  OP_TRY(op_matrix(call, "logits", logits, N, V, ld, op_size(dtype)));
+  if (N == 0) return ANTDT_OK;
+  if (logp) OP_TRY(op_matrix(call, "tokens", tokens, N, 1, 1, 4));
+  if (logp) OP_TRY(op_matrix(call, "logp", logp, N, 1, 1, 4));
+  if (entropy) OP_TRY(op_matrix(call, "entropy", entropy, N, 1, 1, 4));
+  if (stats) OP_TRY(op_matrix(call, "stats", stats, N, 4, 4, 16));
+  if (top) OP_TRY(op_matrix(call, "top_logp", top_logp, N, top, top, 4));
+  if (top) OP_TRY(op_matrix(call, "top_index", top_index, N, top, top, 4));
+  OP_TRY(op_workspace(call, workspace, workspace_bytes, lp_bytes(N, V, top)));
+  LpArgs a = {};
+  a.x = logits; a.ld = ld; a.N = N; a.V = V; a.tokens = tokens; a.logp = logp; a.entropy = entropy;
+  a.stats = reinterpret_cast<float4*>(stats); a.top_logp = top_logp; a.top_index = top_index; a.top = top;
+  a.pieces = lp_pieces(N, V, top);
+  if (a.pieces > 1) {
+    a.part = reinterpret_cast<float4*>(workspace);
+    a.part_top = reinterpret_cast<uint64_t*>(a.part + N * a.pieces);
+  }
+  const hipStream_t s = (hipStream_t)stream;
+  const dim3 grid((unsigned)(N * a.pieces));
+  if (dtype == ANTDT_F32) {
+    if (top) hipLaunchKernelGGL((lp_kernel<float, true>), grid, dim3(LP_THREADS), 0, s, a);
+    else hipLaunchKernelGGL((lp_kernel<float, false>), grid, dim3(LP_THREADS), 0, s, a);
+  } else {
+    if (top) hipLaunchKernelGGL((lp_kernel<bf16_t, true>), grid, dim3(LP_THREADS), 0, s, a);
+    else hipLaunchKernelGGL((lp_kernel<bf16_t, false>), grid, dim3(LP_THREADS), 0, s, a);
+  }
+  OP_TRY(op_hip(call, hipGetLastError()));
+  if (a.pieces > 1) {
+    if (dtype == ANTDT_F32) hipLaunchKernelGGL(lp_join_kernel<float>, dim3((unsigned)N), dim3(LP_THREADS), 0, s, a);
+    else hipLaunchKernelGGL(lp_join_kernel<bf16_t>, dim3((unsigned)N), dim3(LP_THREADS), 0, s, a);
+  }
+  return op_hip(call, hipGetLastError());
+}
+
+int antdt_token_logprobs_gradient(const void* logits, int64_t ld, int64_t N, int64_t V, int32_t dtype, const int32_t* tokens, const float* stats,
+                                  const float* d_logp, const float* d_entropy, void* d_logits, int64_t ldd, void* stream) {
+  const char* call = "antdt_token_logprobs_gradient";
+  if (!op_dtype(dtype)) return op_fail(ANTDT_INVALID_ARG, "%s: dtype", call);
+  OP_TRY(lp_sizes(call, N, V, 0));
+  OP_TRY(op_matrix(call, "logits", logits, N, V, ld, op_size(dtype)));
+  OP_TRY(op_matrix(call, "d_logits", d_logits, N, V, ldd, op_size(dtype)));
+  OP_TRY(op_matrix(call, "stats", stats, N, 4, 4, 16));
+  if (d_logp) OP_TRY(op_matrix(call, "d_logp", d_logp, N, 1, 1, 4));
+  if (d_logp) OP_TRY(op_matrix(call, "tokens", tokens, N, 1, 1, 4));
+  if (d_entropy) OP_TRY(op_matrix(call, "d_entropy", d_entropy, N, 1, 1, 4));
+  if (N == 0) return ANTDT_OK;
+  LpGradArgs a = {};
+  a.x = logits; a.dx = d_logits; a.ld = ld; a.ldd = ldd; a.N = N; a.V = V; a.tokens = tokens;
+  a.stats = reinterpret_cast<const float4*>(stats); a.d_logp = d_logp; a.d_entropy = d_entropy;
+  a.piece = 8192; a.pieces = div_up(V, a.piece);
+  const int64_t size = op_size(dtype);
+  const bool same = ((reinterpret_cast<uintptr_t>(logits) ^ reinterpret_cast<uintptr_t>(d_logits)) & 15) == 0 && ((ld - ldd) * size) % 16 == 0;
+  const dim3 grid((unsigned)std::min<int64_t>(N * a.pieces, 1 << 20));
+  const hipStream_t s = (hipStream_t)stream;
+  if (dtype == ANTDT_F32) {
+    if (same) hipLaunchKernelGGL((lp_grad_kernel<float, true>), grid, dim3(LG_THREADS), 0, s, a);
+    else hipLaunchKernelGGL((lp_grad_kernel<float, false>), grid, dim3(LG_THREADS), 0, s, a);
+  } else {
+    if (same) hipLaunchKernelGGL((lp_grad_kernel<bf16_t, true>), grid, dim3(LG_THREADS), 0, s, a);
+    else hipLaunchKernelGGL((lp_grad_kernel<bf16_t, false>), grid, dim3(LG_THREADS), 0, s, a);
+  }
+  return op_hip(call, hipGetLastError());
+}
+
+}  // extern "C"

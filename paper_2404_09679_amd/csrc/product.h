@@ -1,0 +1,200 @@
+// Block-level matrix products of the gated feed-forward block, of bf16 or fp32 operands, on the gfx950 matrix cores:
+//
+//   acc[b][i][j] += sum_{k < len} A(m, k) * B_b(n, k),   b < NB
+//
+// with the operands of mfma.h (contiguous or strided along the contraction), moved to LDS the same way, STAGES deep.  With NB = 2 one tile of
+// A is multiplied with a tile of each of two matrices, whose columns a wavefront holds side by side.
+//   bf16: v_mfma_f32_32x32x16_bf16, 64 contraction slots a stage.
+//   fp32: v_mfma_f32_32x32x2_f32 (fp32 products and sums), 32 slots a stage; a lane's four slots of a step are four MFMAs.
+#pragma once
+
+#include "mfma.h"
+
+namespace antdt {
+
+typedef float f32x4v __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ void load_lds4(const void* src, uint32_t lds) {
+  asm volatile("s_nop 0\n\tglobal_load_lds_dword %1, off" ::"{m0}"(lds), "v"(src) : "memory");
+}
+__device__ __forceinline__ void load_lds4(const void* base, uint32_t off, uint32_t lds) {
+  asm volatile("s_nop 0\n\tglobal_load_lds_dword %1, %2" ::"{m0}"(lds), "v"(off), "s"(base) : "memory");
+}
+
+// BR rows x 128 bytes of contraction slots of one operand.  PIECE: bytes that a lane moves at a time, 16 or (fp32 rows of any alignment and
+// length) 4.
+template <typename T, int BR, bool STRIDED, int PIECE>
+struct ProductTile;
+
+template <int BR, bool STRIDED>
+struct ProductTile<bf16_t, BR, STRIDED, 16> {
+  typedef OperandTile<BR, 64, STRIDED> Base;
+  typedef bf16x8 Fragment;
+  static constexpr int BK = 64, STEP = 16, BYTES = Base::BYTES, PIECES = Base::SLOTS;
+  static __device__ __forceinline__ void piece(int slot, int64_t ld, int rows, int r0, uint32_t& off, int& k) {
+    const int r = slot / Base::PITCH, c = (slot % Base::PITCH) ^ Base::swizzle(r);
+    if (!STRIDED) {
+      k = c * 8;
+      off = (uint32_t)(min(r, rows - 1 - r0) * ld + k) * 2;
+    } else {
+      k = r;
+      off = (uint32_t)(r * ld + min(c * 8, ((rows - 1) & ~7) - r0)) * 2;
+    }
+  }
+  static __device__ __forceinline__ Fragment fragment(const char* tile, int r0, int kk, int lane) { return Base::fragment(tile, r0, kk, lane); }
+  static __device__ __forceinline__ void multiply(const Fragment& a, const Fragment& b, f32x16& acc) {
+    acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(b, a, acc, 0, 0, 0);
+  }
+};
+
+template <int BR, bool STRIDED, int PIECE>
+struct ProductTile<float, BR, STRIDED, PIECE> {
+  typedef f32x4v Fragment;
+  static constexpr int BK = 32, STEP = 8, BYTES = BR * BK * 4, PIECES = BYTES / PIECE;
+  static constexpr int PITCH = STRIDED ? BR / 4 : BK / 4;   // 16-byte slots per LDS row
+  // Contiguous operands are read 16 bytes down a column of slots; strided ones a word from 32 neighbours of a row.
+  static __device__ __forceinline__ int swizzle(int r) { return STRIDED ? 0 : (r >> 1) & 7; }
+  static __device__ __forceinline__ void piece(int at, int64_t ld, int rows, int r0, uint32_t& off, int& k) {
+    const int slot = PIECE == 16 ? at : at >> 2, e = PIECE == 16 ? 0 : at & 3;
+    const int r = slot / PITCH, c = ((slot % PITCH) ^ swizzle(r)) * 4 + e;
+    if (!STRIDED) {
+      k = c;
+      off = (uint32_t)(min(r, rows - 1 - r0) * ld + k) * 4;
+    } else {
+      k = r;
+      off = (uint32_t)(r * ld + min(c, (PIECE == 16 ? (rows - 1) & ~3 : rows - 1) - r0)) * 4;
+    }
+  }
+  // Contraction slots kk + 4 (lane / 32) + e, e < 4, of row r0 + lane % 32.
+  static __device__ __forceinline__ Fragment fragment(const char* tile, int r0, int kk, int lane) {
+    const int r = r0 + (lane & 31), k = kk + 4 * (lane >> 5);
+    if (!STRIDED) return *reinterpret_cast<const Fragment*>(tile + (r * PITCH + ((k >> 2) ^ swizzle(r))) * 16);
+    const float* p = reinterpret_cast<const float*>(tile) + k * BR + r;
+    return Fragment{p[0], p[BR], p[2 * BR], p[3 * BR]};
+  }
+  static __device__ __forceinline__ void multiply(const Fragment& a, const Fragment& b, f32x16& acc) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(b[e], a[e], acc, 0, 0, 0);
+  }
+};
+
+// One operand: its matrix, rows that exist, first row of the tile.
+struct Operand {
+  const void* x;
+  int64_t ld;
+  int rows, r0;
+};
+
+// WR x WC wavefronts of TM x (NB TN) MFMA tiles each.  Element e of acc[b][i][j] in a lane: row m = 32 i + lane % 32 of the wavefront's tile,
+// column 32 j + 8 (e / 4) + 4 (lane / 32) + e % 4 of B_b's.
+template <typename T, int NB, int TM, int TN, int WR, int WC, int STAGES, bool A_STRIDED, bool B_STRIDED, int PIECE>
+struct TileProduct {
+  static constexpr int THREADS = 64 * WR * WC, BM = 32 * TM * WR, BN = 32 * TN * WC;
+  typedef ProductTile<T, BM, A_STRIDED, PIECE> TA;
+  typedef ProductTile<T, BN, B_STRIDED, PIECE> TB;
+  static constexpr int BK = TA::BK, STEP = TA::STEP;
+  static constexpr int STAGE_BYTES = TA::BYTES + NB * TB::BYTES, LDS_BYTES = STAGES * STAGE_BYTES;
+  static constexpr int VA = TA::PIECES / THREADS, VB = TB::PIECES / THREADS;
+  static_assert(VA * THREADS == TA::PIECES && VB * THREADS == TB::PIECES, "tile / thread count");
+  typedef f32x16 Acc[NB][TM][TN];
+
+  static __device__ __forceinline__ void load(const char* base, uint32_t off, uint32_t lds) {
+    if constexpr (PIECE == 16) load_lds16(base, off, lds);
+    else load_lds4(base, off, lds);
+  }
+  static __device__ __forceinline__ void load(const char* src, uint32_t lds) {
+    if constexpr (PIECE == 16) load_lds16(src, lds);
+    else load_lds4(src, lds);
+  }
+  static __device__ __forceinline__ const char* origin(const Operand& o, bool strided) {
+    return reinterpret_cast<const char*>(o.x) + (strided ? (int64_t)o.r0 : (int64_t)o.r0 * o.ld) * (int64_t)sizeof(T);
+  }
+
+  // Every wavefront of the block calls it alike; `len` contraction slots (of bf16, a multiple of 8 unless both operands are strided).  The
+  // LDS is free when it returns.
+  static __device__ __forceinline__ void run(const Operand& a, const Operand (&b)[NB], int len, char* lds, Acc& acc) {
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wr = wave / WC, wc = wave % WC;
+    const uint32_t lds0 = lds_address(lds) + wave * (64 * PIECE);
+    uint32_t oa[VA], ob[VB];
+    int ka[VA], kb[VB];
+#pragma unroll
+    for (int i = 0; i < VA; ++i) TA::piece(tid + i * THREADS, a.ld, a.rows, a.r0, oa[i], ka[i]);
+#pragma unroll
+    for (int i = 0; i < VB; ++i) TB::piece(tid + i * THREADS, b[0].ld, b[0].rows, b[0].r0, ob[i], kb[i]);
+    const char* pa = origin(a, A_STRIDED);
+    const char* pb[NB];
+#pragma unroll
+    for (int q = 0; q < NB; ++q) pb[q] = origin(b[q], B_STRIDED);
+    const int64_t step_a = (A_STRIDED ? a.ld * BK : BK) * (int64_t)sizeof(T), step_b = (B_STRIDED ? b[0].ld * BK : BK) * (int64_t)sizeof(T);
+    const int nk = (len + BK - 1) / BK;
+
+    int left = len;
+    uint32_t fill = lds0;
+    auto issue = [&]() {
+      if (left >= BK) {
+#pragma unroll
+        for (int i = 0; i < VA; ++i) load(pa, oa[i], fill + i * (THREADS * PIECE));
+#pragma unroll
+        for (int q = 0; q < NB; ++q)
+#pragma unroll
+          for (int i = 0; i < VB; ++i) load(pb[q], ob[i], fill + TA::BYTES + q * TB::BYTES + i * (THREADS * PIECE));
+      } else {
+        const char* zero = reinterpret_cast<const char*>(mfma_zero16);
+#pragma unroll
+        for (int i = 0; i < VA; ++i) load(ka[i] < left ? pa + oa[i] : zero, fill + i * (THREADS * PIECE));
+#pragma unroll
+        for (int q = 0; q < NB; ++q)
+#pragma unroll
+          for (int i = 0; i < VB; ++i) load(kb[i] < left ? pb[q] + ob[i] : zero, fill + TA::BYTES + q * TB::BYTES + i * (THREADS * PIECE));
+      }
+      pa += step_a;
+#pragma unroll
+      for (int q = 0; q < NB; ++q) pb[q] += step_b;
+      left -= BK;
+      fill = fill == lds0 + (STAGES - 1) * STAGE_BYTES ? lds0 : fill + STAGE_BYTES;
+    };
+    constexpr int PER_STAGE = VA + NB * VB;
+#pragma unroll
+    for (int t = 0; t < STAGES - 1; ++t)
+      if (t < nk) issue();
+    uint32_t read = 0;
+    for (int t = 0; t < nk; ++t) {
+      if (t + STAGES - 2 < nk) wait_loads<(STAGES - 2) * PER_STAGE>();
+      else wait_loads<0>();
+      block_barrier();
+      const char* la = lds + read;
+      const char* lb = la + TA::BYTES;
+      constexpr int Q = BK / STEP;
+      typename TA::Fragment af[2][TM];
+      typename TB::Fragment bf[2][NB][TN];
+      auto fetch = [&](int q, int to) {
+#pragma unroll
+        for (int i = 0; i < TM; ++i) af[to][i] = TA::fragment(la, (wr * TM + i) * 32, q * STEP, lane);
+#pragma unroll
+        for (int s = 0; s < NB; ++s)
+#pragma unroll
+          for (int j = 0; j < TN; ++j) bf[to][s][j] = TB::fragment(lb + s * TB::BYTES, (wc * TN + j) * 32, q * STEP, lane);
+      };
+      fetch(0, 0);
+#pragma unroll
+      for (int q = 0; q < Q; ++q) {
+        if (q + 1 < Q) fetch(q + 1, (q + 1) & 1);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+          for (int s = 0; s < NB; ++s)
+#pragma unroll
+            for (int j = 0; j < TN; ++j) TA::multiply(af[q & 1][i], bf[q & 1][s][j], acc[s][i][j]);
+        __builtin_amdgcn_sched_barrier(0);
+        if (q == 0 && left > 0) issue();
+      }
+      read = read == (STAGES - 1) * STAGE_BYTES ? 0 : read + STAGE_BYTES;
+    }
+    block_barrier();
+  }
+};
+
+}  // namespace antdt
