@@ -44,35 +44,42 @@ struct Softmax {
   float m = NEG_INF, s = 0.0f, q = 0.0f;
   // what logits are taken relative to
   static __device__ __forceinline__ float base(float m) { return m == NEG_INF ? 0.0f : m; }
-  __device__ __forceinline__ void raise(float to) {
-    if (to > m) {
-      if (m != NEG_INF) {
-        const float d = m - to, r = __expf(d);
-        q = r == 0.0f ? 0.0f : r * (q + d * s);
-        s *= r;
-      }
-      m = to;
-    }
+  // The sums relative to `to` >= m.
+  __device__ __forceinline__ void rescale(float to) {
+    const float d = base(m) - base(to), r = m == NEG_INF ? 0.0f : __expf(d);
+    q = r == 0.0f ? 0.0f : r * (q + d * s);
+    s *= r;
+    m = to;
   }
-  // x <= m
+  // x <= m.  FINITE: not -infinity.
+  template <bool FINITE>
   __device__ __forceinline__ void add(float x) {
     const float d = x - base(m), e = __expf(d);
     s += e;
-    q += e == 0.0f ? 0.0f : e * d;
+    q += FINITE || e != 0.0f ? e * d : 0.0f;
   }
-  __device__ __forceinline__ void join(float m2, float s2, float q2) {
-    if (m2 > m) {
-      const float d = base(m) - m2, r = m == NEG_INF ? 0.0f : __expf(d);
-      q = (r == 0.0f ? 0.0f : r * (q + d * s)) + q2;
-      s = s * r + s2;
-      m = m2;
+  // n logits.
+  template <int n>
+  __device__ __forceinline__ void add_all(const float (&v)[n]) {
+    float lo = v[0];
+#pragma unroll
+    for (int e = 1; e < n; ++e) lo = fminf(lo, v[e]);
+    if (lo > NEG_INF) {
+#pragma unroll
+      for (int e = 0; e < n; ++e) add<true>(v[e]);
     } else {
-      const float d = base(m2) - base(m), r = m2 == NEG_INF ? 0.0f : __expf(d);
-      q += r == 0.0f ? 0.0f : r * (q2 + d * s2);
-      s += s2 * r;
+#pragma unroll
+      for (int e = 0; e < n; ++e) add<false>(v[e]);
     }
   }
 };
+template <int n>
+__device__ __forceinline__ float largest(const float (&v)[n]) {
+  float m = v[0];
+#pragma unroll
+  for (int e = 1; e < n; ++e) m = fmaxf(m, v[e]);
+  return m;
+}
 
 // Columns [c0, c1) of a row in the thread's share: up to the first 16-byte boundary and from the last on one by one, 16 bytes at a
 // time in between.  f(values, first column, how many), columns of a thread ascending.
@@ -98,38 +105,55 @@ struct RowWalk {
       }
     }
   }
-  template <typename F>
-  __device__ __forceinline__ void one(int64_t c, F&& f) const {
-    float v[VN];
-    v[0] = to_f32(row[c]);
-#pragma unroll
-    for (int e = 1; e < VN; ++e) v[e] = NEG_INF;
-    f(v, c, 1);
-  }
+  // f(values, first column, how many): columns of a thread ascending.
   template <int THREADS, typename F>
   __device__ __forceinline__ void each(int tid, F&& f) const {
-    if (c0 + tid < body) one(c0 + tid, f);
-    constexpr int U = 4;
+    batches<THREADS>(
+        tid,
+        [&](const float (&v)[U * VN], int64_t c) {
+#pragma unroll
+          for (int q = 0; q < U; ++q) {
+            float x[VN];
+#pragma unroll
+            for (int e = 0; e < VN; ++e) x[e] = v[q * VN + e];
+            f(x, c + (int64_t)q * THREADS * VN, VN);
+          }
+        },
+        f);
+  }
+  // The same, U vectors at a time where there are as many: g(values, first column), the vectors THREADS of them apart.
+  static constexpr int U = 4;
+  template <int THREADS, typename G, typename F>
+  __device__ __forceinline__ void batches(int tid, G&& g, F&& f) const {
+    float v[VN];
+    auto one = [&](int64_t c) {
+      v[0] = to_f32(row[c]);
+#pragma unroll
+      for (int e = 1; e < VN; ++e) v[e] = NEG_INF;
+      f(v, c, 1);
+    };
+    if (c0 + tid < body) one(c0 + tid);
     const uint4* p = reinterpret_cast<const uint4*>(row + body);
     int64_t i = tid;
     for (; i + (U - 1) * THREADS < vecs; i += U * THREADS) {
       uint4 w[U];
+      float x[U * VN];
 #pragma unroll
       for (int q = 0; q < U; ++q) w[q] = p[i + q * THREADS];
 #pragma unroll
       for (int q = 0; q < U; ++q) {
-        float v[VN];
         unpack(w[q], v);
-        f(v, body + (i + q * THREADS) * VN, VN);
+#pragma unroll
+        for (int e = 0; e < VN; ++e) x[q * VN + e] = v[e];
       }
+      g(x, body + i * VN);
     }
     for (; i < vecs; i += THREADS) {
-      float v[VN];
       unpack(p[i], v);
       f(v, body + i * VN, VN);
     }
     const int64_t c = body + vecs * VN + tid;
-    if (c < c1) one(c, f);
+    if (c < c1) one(c);
   }
 };
 
@@ -146,21 +170,30 @@ struct LpLds {
   float m[LP_WAVES], s[LP_WAVES], q[LP_WAVES];
 };
 
-// The block's sums from its threads'.
+// The block's sums from its threads': the largest logit first, then every thread's sums relative to it, added up.
 __device__ __forceinline__ Softmax block_softmax(LpLds& lds, Softmax x) {
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, waves = blockDim.x >> 6;
+  float m = x.m;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+  if (lane == 0) lds.m[w] = m;
+  __syncthreads();
+  for (int i = 0; i < waves; ++i) m = fmaxf(m, lds.m[i]);
+  x.rescale(m);
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
-    const float m = __shfl_xor(x.m, o, 64), s = __shfl_xor(x.s, o, 64), q = __shfl_xor(x.q, o, 64);
-    x.join(m, s, q);
+    x.s += __shfl_xor(x.s, o, 64);
+    x.q += __shfl_xor(x.q, o, 64);
   }
   if (lane == 0) {
-    lds.m[w] = x.m; lds.s[w] = x.s; lds.q[w] = x.q;
+    lds.s[w] = x.s; lds.q[w] = x.q;
   }
   __syncthreads();
-  Softmax r;
-  for (int i = 0; i < (int)(blockDim.x >> 6); ++i) r.join(lds.m[i], lds.s[i], lds.q[i]);
-  return r;
+  x.s = x.q = 0.0f;
+  for (int i = 0; i < waves; ++i) {
+    x.s += lds.s[i]; x.q += lds.q[i];
+  }
+  return x;
 }
 
 // The k largest keys, in order, to out(rank, key).  `mine`: the largest key of this thread's share; rescan(f) calls f(key) for every
@@ -246,28 +279,43 @@ __global__ __launch_bounds__(LP_THREADS) void lp_kernel(LpArgs a) {
   __shared__ LpLds lds;
   const int64_t row = blockIdx.x / a.pieces;
   const int piece = (int)(blockIdx.x - row * a.pieces), tid = threadIdx.x;
-  const RowWalk<T> walk(reinterpret_cast<const T*>(a.x) + row * a.ld, a.V * piece / a.pieces, a.V * (piece + 1) / a.pieces);
-  constexpr int VN = RowWalk<T>::VN;
+  typedef RowWalk<T> W;
+  const W walk(reinterpret_cast<const T*>(a.x) + row * a.ld, a.V * piece / a.pieces, a.V * (piece + 1) / a.pieces);
+  constexpr int VN = W::VN;
   Softmax t;
   int64_t best = 0;   // column of the thread's first largest logit
   bool any = false;
-  walk.template each<LP_THREADS>(tid, [&](const float (&v)[VN], int64_t c, int n) {
-    float vm = v[0];
+  walk.template batches<LP_THREADS>(
+      tid,
+      [&](const float (&v)[W::U * VN], int64_t c) {
+        const float vm = largest(v);
+        if (vm > t.m || (TOP && !any)) {
+          if (TOP) {
+            best = c;
 #pragma unroll
-    for (int e = 1; e < VN; ++e) vm = fmaxf(vm, v[e]);
-    if (vm > t.m || (TOP && !any)) {
-      if (TOP) {
-        best = c;
-        for (int e = VN - 1; e >= 0; --e)
-          if (e < n && v[e] == vm) best = c + e;
-        any = true;
-      }
-      t.raise(vm);
-    }
+            for (int e = W::U * VN - 1; e >= 0; --e)
+              if (v[e] == vm) best = c + (int64_t)(e / VN) * (LP_THREADS * VN) + e % VN;
+            any = true;
+          }
+          t.rescale(fmaxf(vm, t.m));
+        }
+        t.add_all(v);
+      },
+      [&](const float (&v)[VN], int64_t c, int n) {
+        const float vm = largest(v);
+        if (vm > t.m || (TOP && !any)) {
+          if (TOP) {
+            best = c;
 #pragma unroll
-    for (int e = 0; e < VN; ++e)
-      if (e < n) t.add(v[e]);
-  });
+            for (int e = VN - 1; e >= 0; --e)
+              if (e < n && v[e] == vm) best = c + e;
+            any = true;
+          }
+          t.rescale(fmaxf(vm, t.m));
+        }
+        if (n == VN) t.add_all(v);
+        else t.template add<false>(v[0]);
+      });
   const float mine = t.m;
   t = block_softmax(lds, t);
   const float log_s = logf(t.s);
@@ -311,7 +359,12 @@ __global__ __launch_bounds__(LP_THREADS) void lp_join_kernel(LpArgs a) {
   Softmax t;
   for (int p = tid; p < a.pieces; p += LP_THREADS) {
     const float4 v = a.part[row * a.pieces + p];
-    t.join(v.x, v.y, v.z);
+    Softmax o;
+    o.m = v.x; o.s = v.y; o.q = v.z;
+    const float m = fmaxf(t.m, o.m);
+    t.rescale(m);
+    o.rescale(m);
+    t.s += o.s; t.q += o.q;
   }
   t = block_softmax(lds, t);
   const float log_s = logf(t.s);
@@ -339,8 +392,7 @@ __global__ __launch_bounds__(LP_THREADS) void lp_join_kernel(LpArgs a) {
 // Pieces of a row: with fewer rows than the chip holds blocks, until they fill it, but no shorter than a block's threads have
 // two vectors each to read.
 int lp_pieces(int64_t N, int64_t V, int32_t top) {
-  if (N >= 512) return 1;
-  int64_t p = std::min(div_up(1024, std::max<int64_t>(N, 1)), V / 4096);
+  int64_t p = std::min(512 / std::max<int64_t>(N, 1), V / 4096);
   if (top > 0) p = std::min<int64_t>(p, JOIN_KEYS / top);
   return (int)std::max<int64_t>(p, 1);
 }

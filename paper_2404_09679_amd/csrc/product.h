@@ -4,8 +4,8 @@
 //
 // with the operands of mfma.h (contiguous or strided along the contraction), moved to LDS the same way, STAGES deep.  With NB = 2 one tile of
 // A is multiplied with a tile of each of two matrices, whose columns a wavefront holds side by side.
-//   bf16: v_mfma_f32_32x32x16_bf16, 64 contraction slots a stage.
-//   fp32: v_mfma_f32_32x32x2_f32 (fp32 products and sums), 32 slots a stage; a lane's four slots of a step are four MFMAs.
+//   bf16: v_mfma_f32_32x32x16_bf16.
+//   fp32: v_mfma_f32_32x32x2_f32 (fp32 products and sums); a lane's four slots of a step are four MFMAs.
 #pragma once
 
 #include "mfma.h"
@@ -21,18 +21,20 @@ __device__ __forceinline__ void load_lds4(const void* base, uint32_t off, uint32
   asm volatile("s_nop 0\n\tglobal_load_lds_dword %1, %2" ::"{m0}"(lds), "v"(off), "s"(base) : "memory");
 }
 
-// BR rows x 128 bytes of contraction slots of one operand.  PIECE: bytes that a lane moves at a time, 16 or (fp32 rows of any alignment and
+// BR rows x BK contraction slots of one operand.  PIECE: bytes that a lane moves at a time, 16 or (fp32 rows of any alignment and
 // length) 4.
-template <typename T, int BR, bool STRIDED, int PIECE>
+template <typename T, int BR, int BK, bool STRIDED, int PIECE>
 struct ProductTile;
 
-template <int BR, bool STRIDED>
-struct ProductTile<bf16_t, BR, STRIDED, 16> {
-  typedef OperandTile<BR, 64, STRIDED> Base;
+template <int BR, int BK, bool STRIDED>
+struct ProductTile<bf16_t, BR, BK, STRIDED, 16> {
+  typedef OperandTile<BR, BK, STRIDED> Base;
   typedef bf16x8 Fragment;
-  static constexpr int BK = 64, STEP = 16, BYTES = Base::BYTES, PIECES = Base::SLOTS;
+  static constexpr int STEP = 16, BYTES = Base::BYTES, PIECES = Base::SLOTS, PITCH = Base::PITCH;
+  // (four 16-byte slots a row: rows 4 apart would meet in the same banks)
+  static __device__ __forceinline__ int swizzle(int r) { return !STRIDED && PITCH == 4 ? (r >> 2) & 3 : Base::swizzle(r); }
   static __device__ __forceinline__ void piece(int slot, int64_t ld, int rows, int r0, uint32_t& off, int& k) {
-    const int r = slot / Base::PITCH, c = (slot % Base::PITCH) ^ Base::swizzle(r);
+    const int r = slot / PITCH, c = (slot % PITCH) ^ swizzle(r);
     if (!STRIDED) {
       k = c * 8;
       off = (uint32_t)(min(r, rows - 1 - r0) * ld + k) * 2;
@@ -41,18 +43,26 @@ struct ProductTile<bf16_t, BR, STRIDED, 16> {
       off = (uint32_t)(r * ld + min(c * 8, ((rows - 1) & ~7) - r0)) * 2;
     }
   }
-  static __device__ __forceinline__ Fragment fragment(const char* tile, int r0, int kk, int lane) { return Base::fragment(tile, r0, kk, lane); }
+  static __device__ __forceinline__ Fragment fragment(const char* tile, int r0, int kk, int lane) {
+    if constexpr (!STRIDED && PITCH == 4) {
+      const int r = r0 + (lane & 31), c = (kk >> 3) + (lane >> 5);
+      return *reinterpret_cast<const bf16x8*>(tile + (r * PITCH + (c ^ swizzle(r))) * 16);
+    } else {
+      return Base::fragment(tile, r0, kk, lane);
+    }
+  }
   static __device__ __forceinline__ void multiply(const Fragment& a, const Fragment& b, f32x16& acc) {
     acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(b, a, acc, 0, 0, 0);
   }
 };
 
-template <int BR, bool STRIDED, int PIECE>
-struct ProductTile<float, BR, STRIDED, PIECE> {
+template <int BR, int BK, bool STRIDED, int PIECE>
+struct ProductTile<float, BR, BK, STRIDED, PIECE> {
   typedef f32x4v Fragment;
-  static constexpr int BK = 32, STEP = 8, BYTES = BR * BK * 4, PIECES = BYTES / PIECE;
+  static constexpr int STEP = 8, BYTES = BR * BK * 4, PIECES = BYTES / PIECE;
   static constexpr int PITCH = STRIDED ? BR / 4 : BK / 4;   // 16-byte slots per LDS row
   // Contiguous operands are read 16 bytes down a column of slots; strided ones a word from 32 neighbours of a row.
+  static_assert(BK == 32, "eight slots a row");
   static __device__ __forceinline__ int swizzle(int r) { return STRIDED ? 0 : (r >> 1) & 7; }
   static __device__ __forceinline__ void piece(int at, int64_t ld, int rows, int r0, uint32_t& off, int& k) {
     const int slot = PIECE == 16 ? at : at >> 2, e = PIECE == 16 ? 0 : at & 3;
@@ -87,12 +97,13 @@ struct Operand {
 
 // WR x WC wavefronts of TM x (NB TN) MFMA tiles each.  Element e of acc[b][i][j] in a lane: row m = 32 i + lane % 32 of the wavefront's tile,
 // column 32 j + 8 (e / 4) + 4 (lane / 32) + e % 4 of B_b's.
-template <typename T, int NB, int TM, int TN, int WR, int WC, int STAGES, bool A_STRIDED, bool B_STRIDED, int PIECE>
+template <typename T, int NB, int TM, int TN, int WR, int WC, int BK, int STAGES, bool A_STRIDED, bool B_STRIDED, int PIECE>
 struct TileProduct {
-  static constexpr int THREADS = 64 * WR * WC, BM = 32 * TM * WR, BN = 32 * TN * WC;
-  typedef ProductTile<T, BM, A_STRIDED, PIECE> TA;
-  typedef ProductTile<T, BN, B_STRIDED, PIECE> TB;
-  static constexpr int BK = TA::BK, STEP = TA::STEP;
+  static constexpr int SLOTS = BK, NB_ = NB, TM_ = TM, TN_ = TN, WC_ = WC, WAVES = WR * WC;
+  static constexpr int THREADS = 64 * WAVES, BM = 32 * TM * WR, BN = 32 * TN * WC;
+  typedef ProductTile<T, BM, BK, A_STRIDED, PIECE> TA;
+  typedef ProductTile<T, BN, BK, B_STRIDED, PIECE> TB;
+  static constexpr int STEP = TA::STEP;
   static constexpr int STAGE_BYTES = TA::BYTES + NB * TB::BYTES, LDS_BYTES = STAGES * STAGE_BYTES;
   static constexpr int VA = TA::PIECES / THREADS, VB = TB::PIECES / THREADS;
   static_assert(VA * THREADS == TA::PIECES && VB * THREADS == TB::PIECES, "tile / thread count");
@@ -128,7 +139,7 @@ struct TileProduct {
 #pragma unroll
     for (int q = 0; q < NB; ++q) pb[q] = origin(b[q], B_STRIDED);
     const int64_t step_a = (A_STRIDED ? a.ld * BK : BK) * (int64_t)sizeof(T), step_b = (B_STRIDED ? b[0].ld * BK : BK) * (int64_t)sizeof(T);
-    const int nk = (len + BK - 1) / BK;
+    const int nk = len > 0 ? (len + BK - 1) / BK : 0;
 
     int left = len;
     uint32_t fill = lds0;

@@ -152,7 +152,7 @@ __global__ __launch_bounds__(256) void token_sum_kernel(GradArgs a, bool vec_gra
   int run = a.key[p0];
   bool came_in = p0 > 0 && a.key[p0 - 1] == run;
   float sum[8] = {};
-  constexpr int U = 4;
+  constexpr int U = 8;
   for (int64_t p = p0; p < p1 && run < a.V; p += U) {
     int k[U], at[U];
     float x[U][8];
@@ -193,8 +193,9 @@ __global__ __launch_bounds__(256) void token_sum_kernel(GradArgs a, bool vec_gra
   else write_row<ACCUMULATE>(a, run, c, n, vec_grad, sum);
 }
 
-// Runs over several chunks: those over a few are added up by the lanes of the chunk where they start, the others by the whole block.
-constexpr int JOIN_THREADS = 1024, JOIN_FEW = 12;
+// Runs over several chunks: those over up to JOIN_FEW more are added up by the lanes of the chunk where they start, the others by the whole
+// block.  (Bound by the chains of loads: how far a run goes is asked by all lanes at once.)
+constexpr int JOIN_THREADS = 1024, JOIN_FEW = 32;
 template <bool ACCUMULATE>
 __global__ __launch_bounds__(JOIN_THREADS) void token_join_kernel(GradArgs a, bool vec_grad) {
   extern __shared__ float part[];   // [groups][8 lanes]
@@ -205,25 +206,39 @@ __global__ __launch_bounds__(JOIN_THREADS) void token_join_kernel(GradArgs a, bo
   const int n = (int)max(min((int64_t)8, a.D - c), (int64_t)0);
   if (threadIdx.x == 0) n_many = 0;
   __syncthreads();
-  // chunks behind j that begin inside the run
+  // the chunk behind j begins inside the run
   auto begins_in = [&](int64_t i, int run) { return i < a.chunks && a.key[i * a.chunk] == run; };
+  // slot 0 of U chunks, `step` apart, up to `end`, added to sum
+  constexpr int U = 8;
+  auto add = [&](int64_t i, int64_t step, int64_t end, float (&sum)[8]) {
+    float x[U][8];
+#pragma unroll
+    for (int q = 0; q < U; ++q) load8<4>(a.partial + min(i + q * step, end - 1) * 2 * a.ldp + c, 8, x[q]);
+#pragma unroll
+    for (int q = 0; q < U; ++q)
+      if (i + q * step < end) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum[e] += x[q][e];
+      }
+  };
   const int64_t j = (int64_t)blockIdx.x * groups + g;
-  const int64_t end = (j + 1) * a.chunk;   // behind the chunk
-  if (j < a.chunks && end < a.N) {
-    const int run = a.key[end - 1];
+  const int64_t behind = (j + 1) * a.chunk;
+  if (j < a.chunks && behind < a.N) {
+    const int run = a.key[behind - 1];
     const int64_t p0 = j * a.chunk;
-    if (run < a.V && a.key[end] == run && !(a.key[p0] == run && p0 > 0 && a.key[p0 - 1] == run)) {
-      if (begins_in(j + 1 + JOIN_FEW, run)) {
+    if (run < a.V && a.key[behind] == run && !(a.key[p0] == run && p0 > 0 && a.key[p0 - 1] == run)) {
+      int more = 0, got = lanes;   // chunks that begin inside the run
+      while (got == lanes && more <= JOIN_FEW) {
+        const uint64_t yes = __ballot(begins_in(j + 1 + more + lane, run)) >> (threadIdx.x & 63 & ~(lanes - 1));
+        got = __popcll(lanes == 64 ? yes : yes & ((1ull << lanes) - 1));
+        more += got;
+      }
+      if (more > JOIN_FEW) {
         if (lane == 0) many[atomicAdd(&n_many, 1)] = (int)j;   // (in any order: each is summed by itself)
       } else if (n > 0) {
         float sum[8];
         load8<4>(a.partial + (j * 2 + 1) * a.ldp + c, 8, sum);
-        for (int64_t i = j + 1; begins_in(i, run); ++i) {
-          float x[8];
-          load8<4>(a.partial + i * 2 * a.ldp + c, 8, x);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) sum[e] += x[e];
-        }
+        for (int64_t i = j + 1; i <= j + more; i += U) add(i, 1, j + more + 1, sum);
         write_row<ACCUMULATE>(a, run, c, n, vec_grad, sum);
       }
     }
@@ -232,27 +247,16 @@ __global__ __launch_bounds__(JOIN_THREADS) void token_join_kernel(GradArgs a, bo
   for (int m = 0; m < n_many; ++m) {
     const int64_t from = many[m];
     const int run = a.key[(from + 1) * a.chunk - 1];
-    int64_t lo = from + 1, hi = a.chunks;   // chunks lo .. begin inside the run, hi .. do not
-    while (hi - lo > 1) {
-      const int64_t mid = (lo + hi) / 2;
-      if (begins_in(mid, run)) lo = mid;
-      else hi = mid;
+    int64_t lo = from + 1, hi = a.chunks;   // the first chunk that does not begin inside the run is in [lo, hi]
+    while (lo < hi) {
+      const int64_t step = (hi - lo + 63) / 64, at = lo + ((threadIdx.x & 63) + 1) * step - 1;
+      const int in = __popcll(__ballot(at < hi && begins_in(at, run)));
+      hi = min(hi, lo + (in + 1) * step - 1);
+      lo += in * step;
     }
     float sum[8] = {};
-    if (n > 0) {
-      constexpr int U = 8;
-      for (int64_t i = from + 1 + g; i < hi; i += U * groups) {
-        float x[U][8];
-#pragma unroll
-        for (int q = 0; q < U; ++q) load8<4>(a.partial + min(i + (int64_t)q * groups, hi - 1) * 2 * a.ldp + c, 8, x[q]);
-#pragma unroll
-        for (int q = 0; q < U; ++q)
-          if (i + q * groups < hi) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) sum[e] += x[q][e];
-          }
-      }
-    }
+    if (n > 0)
+      for (int64_t i = from + 1 + g; i < hi; i += U * groups) add(i, groups, hi, sum);
     store8<4>(part + threadIdx.x * 8, 8, sum);
     __syncthreads();
     if (g == 0 && n > 0) {
@@ -281,8 +285,8 @@ GradPlan grad_plan(int64_t N, int64_t V, int64_t D) {
   p.tiles = (int32_t)div_up(N, ANTDT_SORT_TILE);
   p.lanes_log2 = row_lanes_log2(D, 6);
   p.ldp = div_up(D, 8) * 8;
-  // Chunks short enough that half a million threads find work, long enough that few partial sums are written.
-  p.chunk = (int32_t)std::max<int64_t>(8, div_up(N << p.lanes_log2, 1 << 19));
+  // Chunks short enough that 2^18 threads find work, long enough that few partial sums are written.
+  p.chunk = (int32_t)std::max<int64_t>(8, div_up(N << p.lanes_log2, 1 << 18));
   p.chunks = (int32_t)div_up(N, p.chunk);
   size_t at = 0;
   auto take = [&](size_t bytes) {
