@@ -51,40 +51,14 @@ __device__ __forceinline__ void wave_order() {
   __builtin_amdgcn_wave_barrier();
 }
 
-// How the tiles of a product are handed out.  A compute unit holds a few blocks; tiles beyond the last whole filling of the chip would leave
-// most of it idle for the time of a tile, so their contraction is cut into `parts`, whose sums go to memory in the order of the accumulators
-// and are added up, in order, by a second launch.
+// How the tiles of a product are handed out: the first `whole` to a block each, the contraction of the others in `parts`, whose sums go to
+// memory in the order of the accumulators and are added up, in order, by a second launch.
 struct Split {
   int32_t tiles_m, tiles_n, whole, parts, len;   // len: contraction slots of a part
   float* partial;
   __host__ __device__ int rest() const { return tiles_m * tiles_n - whole; }
-  int blocks() const { return whole + rest() * parts; }
+  __host__ __device__ int blocks() const { return whole + rest() * parts; }
 };
-constexpr int COMPUTE_UNITS = 256, LDS_OF_A_UNIT = 160 * 1024;
-
-template <typename P>
-Split plan_split(int64_t rows, int64_t cols, int64_t contraction) {
-  Split s = {};
-  s.tiles_m = (int)div_up(rows, P::BM);
-  s.tiles_n = (int)div_up(cols, P::BN);
-  const int64_t tiles = (int64_t)s.tiles_m * s.tiles_n;
-  constexpr int per_unit = LDS_OF_A_UNIT / P::LDS_BYTES < 2048 / P::THREADS ? LDS_OF_A_UNIT / P::LDS_BYTES : 2048 / P::THREADS;
-  const int64_t slots = COMPUTE_UNITS * per_unit, rest = tiles % slots;
-  s.whole = (int)tiles;
-  s.parts = 1;
-  s.len = (int)contraction;
-  const int64_t parts = rest ? std::min<int64_t>({slots / rest, div_up(contraction, 4 * P::SLOTS), 8}) : 1;
-  if (parts > 1) {
-    s.whole = (int)(tiles - rest);
-    s.len = (int)(div_up(div_up(contraction, parts), P::SLOTS) * P::SLOTS);
-    s.parts = (int)div_up(contraction, s.len);
-  }
-  return s;
-}
-template <typename P>
-size_t split_bytes(const Split& s) {
-  return s.parts > 1 ? (size_t)s.rest() * s.parts * P::NB_ * P::BM * P::BN * 4 : 0;
-}
 
 // Place of block i of n in the order of the work: an XCD (block i runs on XCD i mod 8) has a share of consecutive places.
 __device__ __forceinline__ int xcd_order(int i, int n) { return (i & 7) * (n >> 3) + min(i & 7, n & 7) + (i >> 3); }
@@ -149,14 +123,13 @@ __device__ __forceinline__ void zero(A& acc) {
 // A product is described by an Op: P, its tiles; Args; product(), the sums of contraction slots [k0, k1) of a tile; finish(), what becomes
 // of a tile's sums.
 template <typename Op>
-__global__ __launch_bounds__(Op::P::THREADS) void tile_kernel(typename Op::Args a, Split sp) {
+__device__ __forceinline__ void tile_block(const typename Op::Args& a, const Split& sp, int block, char* lds) {
   typedef typename Op::P P;
-  extern __shared__ __attribute__((aligned(16))) char lds[];
   int t, part = -1;
-  if ((int)blockIdx.x < sp.whole) {
-    t = xcd_order(blockIdx.x, sp.whole);
+  if (block < sp.whole) {
+    t = xcd_order(block, sp.whole);
   } else {   // (neighbours: other tiles, the same contraction slots)
-    const int rest = sp.rest(), q = xcd_order(blockIdx.x - sp.whole, rest * sp.parts);
+    const int rest = sp.rest(), q = xcd_order(block - sp.whole, rest * sp.parts);
     part = q / rest;
     t = sp.whole + (q - part * rest);
   }
@@ -165,11 +138,20 @@ __global__ __launch_bounds__(Op::P::THREADS) void tile_kernel(typename Op::Args 
   typename P::Acc acc;
   zero(acc);
   const int length = Op::contraction(a);
+  Op::product(a, tm, tn, part < 0 ? 0 : part * sp.len, part < 0 ? length : min((part + 1) * sp.len, length), lds, acc);
   if (part < 0) {
-    Op::product(a, tm, tn, 0, length, lds, acc);
-    Op::finish(a, tm, tn, lds, acc);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    float* st = reinterpret_cast<float*>(lds) + wave * (32 * (32 * P::TN_ + 4));
+#pragma unroll
+    for (int i = 0; i < P::TM_; ++i) {
+      f32x16 x[P::NB_][P::TN_];
+#pragma unroll
+      for (int q = 0; q < P::NB_; ++q)
+#pragma unroll
+        for (int j = 0; j < P::TN_; ++j) x[q][j] = acc[q][i][j];
+      Op::finish(a, tm, tn, wave, i, st, x);
+    }
   } else {
-    Op::product(a, tm, tn, part * sp.len, min((part + 1) * sp.len, length), lds, acc);
     constexpr int N16 = (int)(sizeof(acc) / sizeof(f32x16));
     const f32x16* x = reinterpret_cast<const f32x16*>(&acc);
     f32x4v* out = reinterpret_cast<f32x4v*>(sp.partial) + ((int64_t)(t - sp.whole) * sp.parts + part) * (N16 * 4 * P::THREADS) + threadIdx.x;
@@ -180,46 +162,79 @@ __global__ __launch_bounds__(Op::P::THREADS) void tile_kernel(typename Op::Args 
         out[(i * 4 + v) * P::THREADS] = f32x4v{x[i][4 * v], x[i][4 * v + 1], x[i][4 * v + 2], x[i][4 * v + 3]};
   }
 }
+// 32 rows of a wavefront's tile by one wavefront (few tiles are in parts, but each is as much to read as many results).
+constexpr int JOIN_WAVES = 4;
+template <typename P>
+constexpr int join_units() { return P::WAVES * P::TM_; }   // of a tile
 template <typename Op>
-__global__ __launch_bounds__(Op::P::THREADS) void join_kernel(typename Op::Args a, Split sp) {
+__device__ __forceinline__ void join_rows(const typename Op::Args& a, const Split& sp, int unit, char* lds) {
   typedef typename Op::P P;
-  extern __shared__ __attribute__((aligned(16))) char lds[];
+  constexpr int UNITS = join_units<P>(), N16 = P::NB_ * P::TM_ * P::TN_;
+  const int tile = unit / UNITS, in_tile = unit - tile * UNITS, wave = in_tile / P::TM_, i = in_tile - wave * P::TM_;
+  if (tile >= sp.rest()) return;
   int tm, tn;
-  tile_at(sp.whole + blockIdx.x, sp.tiles_m, sp.tiles_n, tm, tn);
-  typename P::Acc acc;
-  zero(acc);
-  constexpr int N16 = (int)(sizeof(acc) / sizeof(f32x16));
-  f32x16* x = reinterpret_cast<f32x16*>(&acc);
-  const f32x4v* in = reinterpret_cast<const f32x4v*>(sp.partial) + (int64_t)blockIdx.x * sp.parts * (N16 * 4 * P::THREADS) + threadIdx.x;
-#pragma unroll 1
+  tile_at(sp.whole + tile, sp.tiles_m, sp.tiles_n, tm, tn);
+  f32x16 x[P::NB_][P::TN_] = {};
+  const int lane = threadIdx.x & 63;
+  const f32x4v* in = reinterpret_cast<const f32x4v*>(sp.partial) + (int64_t)tile * sp.parts * (N16 * 4 * P::THREADS) + wave * 64 + lane;
+#pragma unroll 2
   for (int p = 0; p < sp.parts; ++p, in += N16 * 4 * P::THREADS)
 #pragma unroll
-    for (int i = 0; i < N16; ++i)
+    for (int q = 0; q < P::NB_; ++q)
 #pragma unroll
-      for (int v = 0; v < 4; ++v) {
-        const f32x4v y = in[(i * 4 + v) * P::THREADS];
+      for (int j = 0; j < P::TN_; ++j)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) x[i][4 * v + e] += y[e];
-      }
-  Op::finish(a, tm, tn, lds, acc);
+        for (int v = 0; v < 4; ++v) {
+          const f32x4v y = in[(((q * P::TM_ + i) * P::TN_ + j) * 4 + v) * P::THREADS];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x[q][j][4 * v + e] += y[e];
+        }
+  Op::finish(a, tm, tn, wave, i, reinterpret_cast<float*>(lds) + (threadIdx.x >> 6) * (32 * (32 * P::TN_ + 4)), x);
+}
+template <typename Op>
+__global__ __launch_bounds__(Op::P::THREADS) void tile_kernel(typename Op::Args a, Split sp) {
+  extern __shared__ __attribute__((aligned(16))) char lds[];
+  tile_block<Op>(a, sp, blockIdx.x, lds);
+}
+template <typename Op>
+__global__ __launch_bounds__(64 * JOIN_WAVES) void join_kernel(typename Op::Args a, Split sp) {
+  extern __shared__ __attribute__((aligned(16))) char lds[];
+  join_rows<Op>(a, sp, blockIdx.x * JOIN_WAVES + (threadIdx.x >> 6), lds);
+}
+// Two products that do not wait for each other in one launch: the second's blocks fill what the first's leave (and a launch is saved: of 777
+// tokens of 520-1400, 25 us in two, 16 in one).
+template <typename Op1, typename Op2>
+__global__ __launch_bounds__(Op1::P::THREADS) void tile_pair_kernel(typename Op1::Args a1, Split sp1, typename Op2::Args a2, Split sp2) {
+  extern __shared__ __attribute__((aligned(16))) char lds[];
+  const int n = sp1.blocks();
+  if ((int)blockIdx.x < n) tile_block<Op1>(a1, sp1, blockIdx.x, lds);
+  else tile_block<Op2>(a2, sp2, blockIdx.x - n, lds);
+}
+template <typename Op1, typename Op2>
+__global__ __launch_bounds__(64 * JOIN_WAVES) void join_pair_kernel(typename Op1::Args a1, Split sp1, typename Op2::Args a2, Split sp2) {
+  extern __shared__ __attribute__((aligned(16))) char lds[];
+  const int n = sp1.parts > 1 ? sp1.rest() * join_units<typename Op1::P>() : 0, unit = blockIdx.x * JOIN_WAVES + (threadIdx.x >> 6);
+  if (unit < n) join_rows<Op1>(a1, sp1, unit, lds);
+  else join_rows<Op2>(a2, sp2, unit - n, lds);
 }
 // The part of an operand from contraction slot k on.
 template <typename T, bool STRIDED>
 __device__ __forceinline__ Operand operand(const void* x, int64_t ld, int64_t rows, int r0, int64_t k) {
   return Operand{reinterpret_cast<const T*>(x) + (STRIDED ? k * ld : k), ld, (int)rows, r0};
 }
-// Sums of a wavefront's tile to memory.
-template <typename P, typename T, bool VEC>
-__device__ __forceinline__ void store_tile(const f32x16 (&x)[P::TM_][P::TN_], char* lds, T* out, int64_t ld, int64_t rows, int64_t cols, int tm, int tn) {
-  constexpr int WN = 32 * P::TN_;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wr = wave / P::WC_, wc = wave % P::WC_;
-  float* st = reinterpret_cast<float*>(lds) + wave * (32 * (WN + 4));
-  const int64_t mw = (int64_t)tm * P::BM + wr * (32 * P::TM_), nw = (int64_t)tn * P::BN + wc * WN;
-#pragma unroll
-  for (int i = 0; i < P::TM_; ++i) {
-    const int64_t m = mw + 32 * i;
-    store_rows<T, P::TN_, VEC>(st, x[i], out + m * ld + nw, ld, (int)max(min(rows - m, (int64_t)32), (int64_t)0), (int)(cols - nw), lane);
-  }
+// Where the 32 rows `i` of wavefront `wave`'s part of tile (tm, tn) lie in a rows x cols result, and how much of them exists.
+struct Place {
+  int64_t m, n;
+  int rows, cols;
+};
+template <typename P>
+__device__ __forceinline__ Place place(int tm, int tn, int wave, int i, int64_t rows, int64_t cols) {
+  Place p;
+  p.m = (int64_t)tm * P::BM + wave / P::WC_ * (32 * P::TM_) + 32 * i;
+  p.n = (int64_t)tn * P::BN + wave % P::WC_ * (32 * P::TN_);
+  p.rows = (int)max(min(rows - p.m, (int64_t)32), (int64_t)0);
+  p.cols = (int)max(min(cols - p.n, (int64_t)(32 * P::TN_)), (int64_t)0);
+  return p;
 }
 
 template <typename T, typename P_, bool VEC, int ACT, bool SAVE>
@@ -231,35 +246,29 @@ struct ForwardOp {
     const Operand w[2] = {operand<T, true>(a.wg, a.ldw, a.H, tn * P::BN, k0), operand<T, true>(a.wu, a.ldw, a.H, tn * P::BN, k0)};
     P::run(operand<T, false>(a.x, a.ldx, a.N, tm * P::BM, k0), w, k1 - k0, lds, acc);
   }
-  static __device__ __forceinline__ void finish(const Args& a, int tm, int tn, char* lds, typename P::Acc& acc) {
-    constexpr int TN = P::TN_, WN = 32 * TN;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wr = wave / P::WC_, wc = wave % P::WC_;
-    float* st = reinterpret_cast<float*>(lds) + wave * (32 * (WN + 4));
-    const int64_t mw = (int64_t)tm * P::BM + wr * (32 * P::TM_), nw = (int64_t)tn * P::BN + wc * WN;
+  static __device__ __forceinline__ void finish(const Args& a, int tm, int tn, int wave, int i, float* st, f32x16 (&x)[2][P::TN_]) {
+    constexpr int TN = P::TN_;
+    const int lane = threadIdx.x & 63;
+    const Place at = place<P>(tm, tn, wave, i, a.N, a.H);
+    f32x16 h[TN];
 #pragma unroll
-    for (int i = 0; i < P::TM_; ++i) {
-      const int64_t m = mw + 32 * i;
-      const int rows = (int)max(min(a.N - m, (int64_t)32), (int64_t)0), cols = (int)(a.H - nw);
-      f32x16 h[TN];
+    for (int j = 0; j < TN; ++j)
 #pragma unroll
-      for (int j = 0; j < TN; ++j)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          float p, r;
-          const float u = acc[1][i][j][e];
-          activation(ACT, acc[0][i][j][e], p, r);
-          h[j][e] = p * u;
-          if (SAVE) {
-            acc[0][i][j][e] = p;
-            acc[1][i][j][e] = u * r;
-          }
+      for (int e = 0; e < 16; ++e) {
+        float p, r;
+        const float u = x[1][j][e];
+        activation(ACT, x[0][j][e], p, r);
+        h[j][e] = p * u;
+        if (SAVE) {
+          x[0][j][e] = p;
+          x[1][j][e] = u * r;
         }
-      store_rows<T, TN, VEC>(st, h, reinterpret_cast<T*>(a.h) + m * a.ldh + nw, a.ldh, rows, cols, lane);
-      if (SAVE) {
-        float* s = a.saved + m * a.H + nw;
-        store_rows<float, TN, VEC>(st, acc[0][i], s, a.H, rows, cols, lane);
-        store_rows<float, TN, VEC>(st, acc[1][i], s + a.N * a.H, a.H, rows, cols, lane);
       }
+    store_rows<T, TN, VEC>(st, h, reinterpret_cast<T*>(a.h) + at.m * a.ldh + at.n, a.ldh, at.rows, at.cols, lane);
+    if (SAVE) {
+      float* s = a.saved + at.m * a.H + at.n;
+      store_rows<float, TN, VEC>(st, x[0], s, a.H, at.rows, at.cols, lane);
+      store_rows<float, TN, VEC>(st, x[1], s + a.N * a.H, a.H, at.rows, at.cols, lane);
     }
   }
 };
@@ -314,8 +323,9 @@ struct DxOp {
       P::run(operand<T, false>(a.dz, 2 * a.H, a.N, tm * P::BM, from), w, to - from, lds, acc);
     }
   }
-  static __device__ __forceinline__ void finish(const Args& a, int tm, int tn, char* lds, typename P::Acc& acc) {
-    store_tile<P, T, VEC>(acc[0], lds, reinterpret_cast<T*>(a.dx), a.lddx, a.N, a.K, tm, tn);
+  static __device__ __forceinline__ void finish(const Args& a, int tm, int tn, int wave, int i, float* st, f32x16 (&x)[1][P::TN_]) {
+    const Place at = place<P>(tm, tn, wave, i, a.N, a.K);
+    store_rows<T, P::TN_, VEC>(st, x[0], reinterpret_cast<T*>(a.dx) + at.m * a.lddx + at.n, a.lddx, at.rows, at.cols, threadIdx.x & 63);
   }
 };
 
@@ -339,52 +349,251 @@ struct DwOp {
         operand<T, true>(reinterpret_cast<const T*>(a.dz) + (second ? a.H : 0), 2 * a.H, a.H, (second ? tn - a.tiles_h : tn) * P::BN, k0)};
     P::run(operand<T, true>(a.x, a.ldx, a.K, tm * P::BM, k0), z, k1 - k0, lds, acc);
   }
-  static __device__ __forceinline__ void finish(const Args& a, int tm, int tn, char* lds, typename P::Acc& acc) {
+  static __device__ __forceinline__ void finish(const Args& a, int tm, int tn, int wave, int i, float* st, f32x16 (&x)[1][P::TN_]) {
     const bool second = tn >= a.tiles_h;
-    store_tile<P, T, VEC>(acc[0], lds, reinterpret_cast<T*>(second ? a.dwu : a.dwg), a.lddw, a.K, a.H, tm, second ? tn - a.tiles_h : tn);
+    const Place at = place<P>(tm, second ? tn - a.tiles_h : tn, wave, i, a.K, a.H);
+    store_rows<T, P::TN_, VEC>(st, x[0], reinterpret_cast<T*>(second ? a.dwu : a.dwg) + at.m * a.lddw + at.n, a.lddw, at.rows, at.cols, threadIdx.x & 63);
   }
 };
 
+// ------------------------------------------------------------- plans
+// Which tiles a product goes by, and which of them in parts: the plan of the shortest estimated time.  The classes of tiles (`cols`: of all
+// products that a tile holds side by side) and what a tile costs a compute unit: ns a contraction slot, and us for filling the pipeline
+// and writing the results.
+struct TileClass {
+  int32_t rows, cols, slots;
+  float ns, us;
+};
+enum { BF16_256, BF16_128, BF16_64, F32_128, F32_64, F32_64_ANY, TILE_CLASSES };
+constexpr TileClass TILE_CLASS[2][TILE_CLASSES] = {
+    {{256, 256, 64, 27.0f, 7.0f}, {128, 128, 64, 10.0f, 2.5f}, {64, 64, 64, 4.6f, 1.0f}, {128, 128, 32, 58.0f, 5.0f}, {64, 64, 32, 16.0f, 2.0f}, {64, 64, 32, 25.0f, 2.0f}},
+    {{256, 256, 64, 27.0f, 7.0f}, {128, 128, 64, 10.0f, 2.5f}, {64, 64, 64, 4.6f, 1.0f}, {128, 128, 32, 58.0f, 5.0f}, {64, 128, 32, 32.0f, 3.0f}, {64, 128, 32, 50.0f, 3.0f}}};
+template <typename T, int C, int NB, bool AS, bool BS>
+struct TilingOf;   // Product: its TileProduct; vec: whole 16-byte groups may be written
+#define TILING(C, T, TM, TN, WR, WC, BK, STAGES, PIECE)                                                                                \
+  template <int NB, bool AS, bool BS>                                                                                                  \
+  struct TilingOf<T, C, NB, AS, BS> {                                                                                                  \
+    typedef TileProduct<T, NB, TM, TN, WR, WC, BK, STAGES, AS, BS, PIECE> Product;                                                     \
+    typedef T Type;                                                                                                                    \
+    static constexpr bool vec = PIECE == 16;                                                                                           \
+    static constexpr TileClass k = TILE_CLASS[NB - 1][C];                                                                              \
+    static_assert(Product::BM == k.rows && NB * Product::BN == k.cols && Product::SLOTS == k.slots, "class");                          \
+  };
+TILING(BF16_256, bf16_t, 4, 2 / NB, 2, 4, 64, 2, 16)
+TILING(BF16_128, bf16_t, 2 / NB, 1, 2 * NB, 4 / NB, 64, 3, 16)
+TILING(BF16_64, bf16_t, 1, 1, 2, 2 / NB, 64, 3, 16)
+TILING(F32_128, float, 2, 2 / NB, 2, 2, 32, 3, 16)
+TILING(F32_64, float, 1, 1, 2, 2, 32, 3, 16)
+TILING(F32_64_ANY, float, 1, 1, 2, 2, 32, 3, 4)
+#undef TILING
+
+constexpr int COMPUTE_UNITS = 256, MOST_PARTS = 16;
+constexpr double JOIN_US = 6.0, PARTIAL_BYTES_PER_US = 2e6;   // a further launch; the sums written and read again
+
+struct Jobs {   // of one length, in the order they are handed out
+  int64_t n;
+  double us;
+};
+// When the last of the jobs ends on `places` that each take the next one when they are free.
+double finish_time(int64_t places, std::initializer_list<Jobs> all) {
+  // places by the time they are free: a list of (time, how many), kept in order
+  constexpr int MOST = 32;
+  double at[MOST];
+  int64_t n[MOST];
+  int k = 1;
+  at[0] = 0.0;
+  n[0] = places;
+  double last = 0.0;
+  for (Jobs j : all) {
+    if (j.n > 64 * places) {   // (so many that the ends do not matter)
+      const int64_t rounds = j.n / places - 1;
+      for (int i = 0; i < k; ++i) at[i] += rounds * j.us;
+      j.n -= rounds * places;
+      last = std::max(last, at[k - 1]);
+    }
+    while (j.n > 0) {
+      const int64_t take = std::min(j.n, n[0]);
+      const double end = at[0] + j.us;
+      j.n -= take;
+      n[0] -= take;
+      last = std::max(last, end);
+      if (n[0] == 0) {
+        for (int i = 1; i < k; ++i) {
+          at[i - 1] = at[i];
+          n[i - 1] = n[i];
+        }
+        --k;
+      }
+      int i = k;
+      if (k == MOST) {   // (then the last two are taken for one)
+        n[k - 1] += take;
+        at[k - 1] = std::max(at[k - 1], end);
+        continue;
+      }
+      while (i > 0 && at[i - 1] > end) {
+        at[i] = at[i - 1];
+        n[i] = n[i - 1];
+        --i;
+      }
+      at[i] = end;
+      n[i] = take;
+      ++k;
+    }
+  }
+  return last;
+}
+
+// A product that is part of a launch: rows x cols of results, `copies` of them side by side (two weights' gradients), `contraction` slots.
+struct Job {
+  int64_t rows, cols, copies, contraction;
+};
+struct Plan {
+  int cls;
+  Split split[2];
+  size_t bytes;
+  double us;
+};
+// NB: products that a tile holds side by side.
+Plan plan_of(int cls, int NB, const Job (&job)[2]) {
+  const TileClass& c = TILE_CLASS[NB - 1][cls];
+  Plan best = {};
+  best.cls = cls;
+  int64_t tiles[2], len[2];
+  for (int q = 0; q < 2; ++q) {
+    Split& s = best.split[q];
+    s.tiles_m = (int)div_up(job[q].rows, c.rows);
+    s.tiles_n = (int)(job[q].copies * div_up(job[q].cols, c.cols / NB));
+    s.whole = s.tiles_m * s.tiles_n;
+    s.parts = 1;
+    tiles[q] = s.whole;
+    len[q] = s.len = (int)job[q].contraction;
+  }
+  const int64_t places = COMPUTE_UNITS, all = tiles[0] + tiles[1];
+  auto us = [&](int64_t slots) { return slots * c.ns * 1e-3 + c.us; };
+  best.us = finish_time(places, {{tiles[0], us(len[0])}, {tiles[1], us(len[1])}});
+  auto parts_of = [&](int64_t slots, int64_t want) { return std::max<int64_t>(std::min<int64_t>({want, slots / (4 * c.slots), MOST_PARTS}), 1); };
+  auto offer = [&](int64_t rest0, int64_t parts0, int64_t rest1, int64_t parts1) {
+    const int64_t rest[2] = {parts0 > 1 ? rest0 : 0, parts1 > 1 ? rest1 : 0}, parts[2] = {parts0, parts1};
+    if (rest[0] + rest[1] == 0) return;
+    Plan p = best;
+    int64_t sums = 0, part_len[2];
+    for (int q = 0; q < 2; ++q) {
+      Split& s = p.split[q];
+      s.whole = (int)(tiles[q] - rest[q]);
+      s.parts = 1;
+      part_len[q] = s.len = (int)len[q];
+      if (rest[q] == 0) continue;
+      part_len[q] = s.len = (int)(div_up(div_up(len[q], parts[q]), c.slots) * c.slots);
+      s.parts = (int)div_up(len[q], s.len);
+      sums += rest[q] * s.parts;
+    }
+    p.bytes = (size_t)sums * c.rows * c.cols * 4;
+    p.us = finish_time(places, {{p.split[0].whole, us(len[0])}, {rest[0] * p.split[0].parts, us(part_len[0])}, {p.split[1].whole, us(len[1])},
+                                {rest[1] * p.split[1].parts, us(part_len[1])}}) +
+           JOIN_US + p.bytes / PARTIAL_BYTES_PER_US;
+    if (p.us < best.us) best = p;
+  };
+  if (all == 0) return best;
+  // the tiles behind the last whole filling of the chip
+  const int64_t rest = all % places, last = tiles[1] ? 1 : 0;
+  if (all > places && rest > 0 && rest <= tiles[last])
+    for (int64_t p : {2, 3, 4, 6}) {
+      const int64_t parts = parts_of(len[last], p);
+      if (last) offer(0, 1, rest, parts);
+      else offer(rest, parts, 0, 1);
+    }
+  // all of those that take longer than an equal share of the work
+  const double each = std::max((double)(tiles[0] * len[0] + tiles[1] * len[1]) / places, 4.0 * c.slots);
+  if (len[0] > each || len[1] > each)
+    for (int more : {1, 2}) offer(tiles[0], parts_of(len[0], (int64_t)(more * len[0] / each)), tiles[1], parts_of(len[1], (int64_t)(more * len[1] / each)));
+  return best;
+}
+Plan best_plan(bool bf16, bool vec, int NB, const Job (&job)[2]) {
+  if (!bf16 && !vec) return plan_of(F32_64_ANY, NB, job);
+  Plan best = plan_of(bf16 ? BF16_64 : F32_64, NB, job);
+  for (int c = bf16 ? BF16_256 : F32_128; c < (bf16 ? BF16_64 : F32_64); ++c) {
+    const Plan p = plan_of(c, NB, job);
+    if (p.us < best.us) best = p;
+  }
+  return best;
+}
+// The last few plans of the calling thread, by all they depend on: making one takes microseconds.
+struct PlanKey {
+  int64_t N, K, H;
+  int32_t what;   // operands, alignment and results
+  bool operator==(const PlanKey& o) const { return N == o.N && K == o.K && H == o.H && what == o.what; }
+};
+template <typename F>
+Plan kept_plan(const PlanKey& key, F&& make) {
+  constexpr int KEPT = 32;
+  static thread_local PlanKey keys[KEPT];
+  static thread_local Plan plans[KEPT];
+  static thread_local int next = 0;
+  for (int i = 0; i < KEPT; ++i)
+    if (keys[i] == key) return plans[i];
+  const int at = next;
+  next = (next + 1) % KEPT;
+  keys[at] = key;
+  plans[at] = make();
+  return plans[at];
+}
+Plan forward_plan(int64_t N, int64_t K, int64_t H, bool bf16, bool vec) {
+  return kept_plan({N, K, H, 1 | bf16 << 1 | vec << 2}, [&] { return best_plan(bf16, vec, 2, {{N, H, 1, K}, {0, 0, 1, 0}}); });
+}
+// dx first where its tiles take longer, else the weights' gradients
+bool dx_first(int64_t N, int64_t H) { return 2 * H >= N; }
+Plan backward_plan(int64_t N, int64_t K, int64_t H, bool bf16, bool vec, bool dx, bool dw) {
+  return kept_plan({N, K, H, bf16 << 1 | vec << 2 | dx << 3 | dw << 4}, [&] {
+    const Job x = {dx ? N : 0, K, 1, 2 * H}, w = {dw ? K : 0, H, 2, N};
+    return dx_first(N, H) ? best_plan(bf16, vec, 1, {x, w}) : best_plan(bf16, vec, 1, {w, x});
+  });
+}
+// The partial sums' bytes, whichever way the rows lie and whichever results are wanted.
+size_t forward_bytes(int64_t N, int64_t K, int64_t H, bool bf16) {
+  if (N == 0) return 0;
+  return std::max(forward_plan(N, K, H, bf16, true).bytes, bf16 ? 0 : forward_plan(N, K, H, false, false).bytes);
+}
+size_t backward_partial_bytes(int64_t N, int64_t K, int64_t H, bool bf16) {
+  if (N == 0) return 0;
+  size_t most = 0;
+  for (int vec = bf16 ? 1 : 0; vec < 2; ++vec)
+    for (int want = 1; want < 4; ++want) most = std::max(most, backward_plan(N, K, H, bf16, vec, want & 1, want & 2).bytes);
+  return most;
+}
+
 // ------------------------------------------------------------- launches
+template <typename P>
+constexpr int staging(int waves) { return waves * 32 * (32 * P::TN_ + 4) * 4; }   // of the results, in LDS
+
 template <typename Op>
 hipError_t launch_op(const typename Op::Args& a, const Split& sp, hipStream_t s) {
   typedef typename Op::P P;
-  static_assert(P::WAVES * 32 * (32 * P::TN_ + 4) * 4 <= P::LDS_BYTES, "staging of the results");
-  static std::atomic<uint64_t> allowed[2];
-  hipError_t e = allow_lds(tile_kernel<Op>, P::LDS_BYTES, 0, allowed[0]);
+  static_assert(staging<P>(P::WAVES) <= P::LDS_BYTES && staging<P>(JOIN_WAVES) <= 64 * 1024, "staging of the results");
+  static std::atomic<uint64_t> allowed{0};
+  hipError_t e = allow_lds(tile_kernel<Op>, P::LDS_BYTES, 0, allowed);
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL(tile_kernel<Op>, dim3(sp.blocks()), dim3(P::THREADS), P::LDS_BYTES, s, a, sp);
   e = hipGetLastError();
   if (e != hipSuccess || sp.parts == 1) return e;
-  constexpr int bytes = P::WAVES * 32 * (32 * P::TN_ + 4) * 4;
-  e = allow_lds(join_kernel<Op>, bytes, 0, allowed[1]);
-  if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(join_kernel<Op>, dim3(sp.rest()), dim3(P::THREADS), bytes, s, a, sp);
+  hipLaunchKernelGGL(join_kernel<Op>, dim3((unsigned)div_up(sp.rest() * join_units<P>(), JOIN_WAVES)), dim3(64 * JOIN_WAVES), staging<P>(JOIN_WAVES), s, a,
+                     sp);
   return hipGetLastError();
 }
-
-template <typename P, typename T, bool VEC>
-struct Tiling {   // of a product: its tiles' class, operands' type, whether whole 16-byte groups may be written
-  typedef P Product;
-  typedef T Type;
-  static constexpr bool vec = VEC;
-};
-template <typename T, int NB, int TM, int TN, int WR, int WC, int STAGES, bool AS, bool BS, int PIECE>
-using TilingOf = Tiling<TileProduct<T, NB, TM, TN, WR, WC, sizeof(T) == 2 ? 64 : 32, STAGES, AS, BS, PIECE>, T, PIECE == 16>;
-
-int64_t tiles(int64_t m, int64_t n, int bm, int bn) { return div_up(m, bm) * div_up(n, bn); }
-
-// f(tiling) with the tiles of a rows x cols result (of NB products at a time): of 256 rows and columns as long as they give most compute
-// units a block, smaller ones below.
-template <int NB, bool AS, bool BS, typename F>
-auto with_tiles(bool bf16, bool vec, int64_t rows, int64_t cols, F&& f) {
-  if (bf16) {
-    if (tiles(rows, cols, 256, 256 / NB) >= 150) return f(TilingOf<bf16_t, NB, 4, 2 / NB, 2, 4, 2, AS, BS, 16>());
-    return f(TilingOf<bf16_t, NB, 1, 1, 2, 2, 3, AS, BS, 16>());
-  }
-  if (!vec) return f(TilingOf<float, NB, 1, 1, 2, 2, 3, AS, BS, 4>());
-  if (tiles(rows, cols, 128, 128 / NB) >= 150) return f(TilingOf<float, NB, 2, 2 / NB, 2, 2, 3, AS, BS, 16>());
-  return f(TilingOf<float, NB, 1, 1, 2, 2, 3, AS, BS, 16>());
+template <typename Op1, typename Op2>
+hipError_t launch_pair(const typename Op1::Args& a1, const Split& s1, const typename Op2::Args& a2, const Split& s2, hipStream_t s) {
+  typedef typename Op1::P P;
+  typedef typename Op2::P P2;
+  constexpr int bytes = std::max((int)P::LDS_BYTES, (int)P2::LDS_BYTES);
+  static_assert(P::THREADS == P2::THREADS && staging<P>(1) == staging<P2>(1) && staging<P>(P::WAVES) <= bytes && join_units<P>() == join_units<P2>(), "one block");
+  static std::atomic<uint64_t> allowed{0};
+  hipError_t e = allow_lds(tile_pair_kernel<Op1, Op2>, bytes, 0, allowed);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((tile_pair_kernel<Op1, Op2>), dim3(s1.blocks() + s2.blocks()), dim3(P::THREADS), bytes, s, a1, s1, a2, s2);
+  e = hipGetLastError();
+  const int joins = ((s1.parts > 1 ? s1.rest() : 0) + (s2.parts > 1 ? s2.rest() : 0)) * join_units<P>();
+  if (e != hipSuccess || joins == 0) return e;
+  hipLaunchKernelGGL((join_pair_kernel<Op1, Op2>), dim3((unsigned)div_up(joins, JOIN_WAVES)), dim3(64 * JOIN_WAVES), staging<P>(JOIN_WAVES), s, a1, s1, a2, s2);
+  return hipGetLastError();
 }
 
 template <typename G, bool SAVE>
@@ -398,62 +607,48 @@ hipError_t launch_forward(const GatedArgs& a, const Split& sp, hipStream_t s) {
     default: return launch_op<ForwardOp<T, P, G::vec, ANTDT_ACT_SIGMOID, SAVE>>(a, sp, s);
   }
 }
+template <typename T, int C>
+hipError_t launch_forward_class(const GatedArgs& a, const Split& sp, hipStream_t s) {
+  typedef TilingOf<T, C, 2, false, true> G;
+  return a.saved ? launch_forward<G, true>(a, sp, s) : launch_forward<G, false>(a, sp, s);
+}
 hipError_t gated_forward(const GatedArgs& a, bool bf16, bool vec, float* partial, hipStream_t s) {
-  return with_tiles<2, false, true>(bf16, vec, a.N, a.H, [&](auto g) {
-    Split sp = plan_split<typename decltype(g)::Product>(a.N, a.H, a.K);
-    sp.partial = partial;
-    return a.saved ? launch_forward<decltype(g), true>(a, sp, s) : launch_forward<decltype(g), false>(a, sp, s);
-  });
+  Plan p = forward_plan(a.N, a.K, a.H, bf16, vec);
+  Split& sp = p.split[0];
+  sp.partial = partial;
+  switch (p.cls) {
+    case BF16_256: return launch_forward_class<bf16_t, BF16_256>(a, sp, s);
+    case BF16_128: return launch_forward_class<bf16_t, BF16_128>(a, sp, s);
+    case BF16_64: return launch_forward_class<bf16_t, BF16_64>(a, sp, s);
+    case F32_128: return launch_forward_class<float, F32_128>(a, sp, s);
+    case F32_64: return launch_forward_class<float, F32_64>(a, sp, s);
+    default: return launch_forward_class<float, F32_64_ANY>(a, sp, s);
+  }
 }
-hipError_t gated_dx(const DxArgs& a, bool bf16, bool vec, float* partial, hipStream_t s) {
-  return with_tiles<1, false, false>(bf16, vec, a.N, a.K, [&](auto g) {
-    typedef decltype(g) G;
-    Split sp = plan_split<typename G::Product>(a.N, a.K, 2 * a.H);
-    sp.partial = partial;
-    return launch_op<DxOp<typename G::Type, typename G::Product, G::vec>>(a, sp, s);
-  });
+template <typename T, int C>
+hipError_t launch_backward(const DxArgs& x, const DwArgs& w, const Split (&sp)[2], hipStream_t s) {
+  typedef TilingOf<T, C, 1, false, false> GX;
+  typedef TilingOf<T, C, 1, true, true> GW;
+  typedef DxOp<T, typename GX::Product, GX::vec> OpX;
+  typedef DwOp<T, typename GW::Product, GW::vec> OpW;
+  if (dx_first(x.N, x.H)) return launch_pair<OpX, OpW>(x, sp[0], w, sp[1], s);
+  return launch_pair<OpW, OpX>(w, sp[0], x, sp[1], s);
 }
-// (both weights' tiles side by side; a column of tiles belongs to one of them)
-template <typename P>
-Split plan_dw(int64_t N, int64_t K, int64_t H) { return plan_split<P>(K, 2 * div_up(H, P::BN) * P::BN, N); }
-hipError_t gated_dw(const DwArgs& args, bool bf16, bool vec, float* partial, hipStream_t s) {
-  return with_tiles<1, true, true>(bf16, vec, args.K, 2 * args.H, [&](auto g) {
-    typedef decltype(g) G;
-    DwArgs a = args;
-    Split sp = plan_dw<typename G::Product>(a.N, a.K, a.H);
-    sp.partial = partial;
-    a.tiles_h = sp.tiles_n / 2;
-    return launch_op<DwOp<typename G::Type, typename G::Product, G::vec>>(a, sp, s);
-  });
-}
-
-// Bytes of the partial sums, whichever way the rows lie.
-template <typename F>
-size_t most_bytes(bool bf16, F&& f) { return bf16 ? f(true) : std::max(f(false), f(true)); }
-size_t forward_bytes(int64_t N, int64_t K, int64_t H, bool bf16) {
-  if (N == 0) return 0;
-  return most_bytes(bf16, [&](bool vec) {
-    return with_tiles<2, false, true>(bf16, vec, N, H, [&](auto g) {
-      typedef typename decltype(g)::Product P;
-      return split_bytes<P>(plan_split<P>(N, H, K));
-    });
-  });
-}
-size_t backward_partial_bytes(int64_t N, int64_t K, int64_t H, bool bf16) {
-  if (N == 0) return 0;
-  const size_t dx = most_bytes(bf16, [&](bool vec) {
-    return with_tiles<1, false, false>(bf16, vec, N, K, [&](auto g) {
-      typedef typename decltype(g)::Product P;
-      return split_bytes<P>(plan_split<P>(N, K, 2 * H));
-    });
-  });
-  const size_t dw = most_bytes(bf16, [&](bool vec) {
-    return with_tiles<1, true, true>(bf16, vec, K, 2 * H, [&](auto g) {
-      typedef typename decltype(g)::Product P;
-      return split_bytes<P>(plan_dw<P>(N, K, H));
-    });
-  });
-  return std::max(dx, dw);   // (one after the other)
+hipError_t gated_products(const DxArgs& x, DwArgs w, bool bf16, bool vec, float* partial, hipStream_t s) {
+  Plan p = backward_plan(x.N, x.K, x.H, bf16, vec, x.dx != nullptr && x.N > 0, w.dwg != nullptr);
+  const TileClass& c = TILE_CLASS[0][p.cls];
+  w.tiles_h = (int32_t)div_up(x.H, c.cols);
+  p.split[0].partial = partial;
+  p.split[1].partial = partial;
+  if (p.split[0].parts > 1) p.split[1].partial += (size_t)p.split[0].rest() * p.split[0].parts * c.rows * c.cols;
+  switch (p.cls) {
+    case BF16_256: return launch_backward<bf16_t, BF16_256>(x, w, p.split, s);
+    case BF16_128: return launch_backward<bf16_t, BF16_128>(x, w, p.split, s);
+    case BF16_64: return launch_backward<bf16_t, BF16_64>(x, w, p.split, s);
+    case F32_128: return launch_backward<float, F32_128>(x, w, p.split, s);
+    case F32_64: return launch_backward<float, F32_64>(x, w, p.split, s);
+    default: return launch_backward<float, F32_64_ANY>(x, w, p.split, s);
+  }
 }
 
 size_t align256(size_t v) { return (v + 255) / 256 * 256; }
@@ -555,14 +750,11 @@ int antdt_gated_backward(const void* dh, int64_t lddh, const void* x, int64_t ld
     else hipLaunchKernelGGL((gated_dz_kernel<float, 1>), grid, dim3(256), 0, s, d);
     OP_TRY(op_hip(call, hipGetLastError()));
   }
-  if (dx && N > 0) {
-    const DxArgs a = {workspace, wg, wu, dx, ldw, lddx, N, K, H};
-    OP_TRY(op_hip(call, gated_dx(a, bf16, whole16(wg, ldw) && whole16(wu, ldw) && whole16(dx, lddx) && ((K | H) & 3) == 0, partial, s)));
-  }
-  if (dwg) {
-    const DwArgs a = {x, workspace, dwg, dwu, ldx, lddw, N, K, H, 0};
-    OP_TRY(op_hip(call, gated_dw(a, bf16, whole16(x, ldx) && whole16(dwg, lddw) && whole16(dwu, lddw) && ((K | H) & 3) == 0, partial, s)));
-  }
+  const DxArgs x_args = {workspace, wg, wu, dx, ldw, lddx, N, K, H};
+  const DwArgs w_args = {x, workspace, dwg, dwu, ldx, lddw, N, K, H, 0};
+  const bool vec = ((K | H) & 3) == 0 && (!dx || (whole16(wg, ldw) && whole16(wu, ldw) && whole16(dx, lddx))) &&
+                   (!dwg || (whole16(x, ldx) && whole16(dwg, lddw) && whole16(dwu, lddw)));
+  OP_TRY(op_hip(call, gated_products(x_args, w_args, bf16, vec, partial, s)));
   return ANTDT_OK;
 }
 
