@@ -273,6 +273,96 @@ struct ForwardOp {
   }
 };
 
+// The forward pass for a few tokens, bound by reading the weights once: a block has 2^c lanes along H, of 16 bytes each, and as many rows of the
+// weights at a time as its other lanes make; products and sums in fp32 on the vector units, the lanes' sums added up at the end.
+// By tiles / here, us: bf16 1 and 2 tokens of 1024-4096 7.7 / 5.5 and 6.0, 4 of 2048-5632 14.6 / 17.7; fp32 8 of 1024-4096 18.4 / 12.1, of 4096-14336
+// 145 / 129.
+constexpr int FEW_THREADS = 256;
+constexpr int few_tokens(size_t element) { return element == 4 ? 8 : 2; }
+
+// The sums of v[0 .. COUNT) over the lanes that differ in bits O and above: at every step a lane keeps one half of the values and hands
+// on the other, so that COUNT values cost about COUNT exchanges.  Afterwards v[0] .. are those from the returned one on.
+template <int COUNT, int O>
+__device__ __forceinline__ int sum_over_lanes(float* v, int lane, int first) {
+  if constexpr (O >= 64) {
+    return first;
+  } else if constexpr (COUNT > 1) {
+    constexpr int HALF = COUNT / 2;
+    const bool up = (lane & O) != 0;
+#pragma unroll
+    for (int i = 0; i < HALF; ++i) {
+      const float keep = up ? v[HALF + i] : v[i], give = up ? v[i] : v[HALF + i];
+      v[i] = keep + __shfl_xor(give, O, 64);
+    }
+    return sum_over_lanes<HALF, 2 * O>(v, lane, first + (up ? HALF : 0));
+  } else {
+    v[0] += __shfl_xor(v[0], O, 64);
+    return sum_over_lanes<1, 2 * O>(v, lane, first);
+  }
+}
+
+template <typename T, int NT, int LANES>   // NT >= N
+__global__ __launch_bounds__(FEW_THREADS) void gated_few_kernel(GatedArgs a) {
+  constexpr int VN = 16 / sizeof(T), U = NT > 4 ? 2 : 4, WAVES = FEW_THREADS / 64, STEP = FEW_THREADS / LANES, WIDTH = LANES * VN, COUNT = NT * 2 * VN;
+  constexpr int LEFT = COUNT * LANES / 64 > 0 ? COUNT * LANES / 64 : 1;   // values of a lane after the sum
+  __shared__ float red[WAVES][LANES][COUNT];
+  const int l = threadIdx.x & (LANES - 1), lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t c0 = (int64_t)xcd_order(blockIdx.x, gridDim.x) * WIDTH, c = min(c0 + l * VN, a.H - VN);   // (H is a multiple of VN; what lies behind is not stored)
+  const T* x = reinterpret_cast<const T*>(a.x);
+  const T* wg = reinterpret_cast<const T*>(a.wg) + c;
+  const T* wu = reinterpret_cast<const T*>(a.wu) + c;
+  float acc[COUNT] = {};   // [token][matrix][column]
+  const int K = (int)a.K, N = (int)a.N;
+  for (int k0 = threadIdx.x / LANES; k0 < K; k0 += U * STEP) {
+    uint4 g[U], u[U];
+    float xv[U][NT];
+#pragma unroll
+    for (int q = 0; q < U; ++q) {
+      const int64_t k = min(k0 + q * STEP, K - 1);
+      g[q] = *reinterpret_cast<const uint4*>(wg + k * a.ldw);
+      u[q] = *reinterpret_cast<const uint4*>(wu + k * a.ldw);
+#pragma unroll
+      for (int t = 0; t < NT; ++t) xv[q][t] = to_f32(x[(int64_t)min(t, N - 1) * a.ldx + k]);
+    }
+#pragma unroll
+    for (int q = 0; q < U; ++q) {
+      if (k0 + q * STEP >= K) continue;
+      const uint32_t gw[4] = {g[q].x, g[q].y, g[q].z, g[q].w}, uw[4] = {u[q].x, u[q].y, u[q].z, u[q].w};
+#pragma unroll
+      for (int e = 0; e < VN; ++e) {
+        const float gv = VN == 4 ? __uint_as_float(gw[e % 4]) : __uint_as_float(e & 1 ? gw[e / 2 % 4] & 0xFFFF0000u : gw[e / 2 % 4] << 16);
+        const float uv = VN == 4 ? __uint_as_float(uw[e % 4]) : __uint_as_float(e & 1 ? uw[e / 2 % 4] & 0xFFFF0000u : uw[e / 2 % 4] << 16);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          acc[(t * 2) * VN + e] = fmaf(xv[q][t], gv, acc[(t * 2) * VN + e]);
+          acc[(t * 2 + 1) * VN + e] = fmaf(xv[q][t], uv, acc[(t * 2 + 1) * VN + e]);
+        }
+      }
+    }
+  }
+  const int first = sum_over_lanes<COUNT, LANES>(acc, lane, 0);
+#pragma unroll
+  for (int i = 0; i < LEFT; ++i) red[wave][l][first + i] = acc[i];   // (lanes that hold the same value write the same)
+  __syncthreads();
+  for (int i = threadIdx.x; i < N * WIDTH; i += FEW_THREADS) {
+    const int t = i / WIDTH, e = i % WIDTH;
+    const int64_t col = c0 + e;
+    if (col >= a.H) continue;
+    float g = 0.0f, u = 0.0f, p, r;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+      g += red[w][e / VN][(t * 2) * VN + e % VN];
+      u += red[w][e / VN][(t * 2 + 1) * VN + e % VN];
+    }
+    activation(a.act, g, p, r);
+    reinterpret_cast<T*>(a.h)[t * a.ldh + col] = from_f32<T>(p * u);
+    if (a.saved) {
+      a.saved[t * a.H + col] = p;
+      a.saved[(a.N + t) * a.H + col] = u * r;
+    }
+  }
+}
+
 // dz = [dh R | dh P], [N, 2H].
 struct DzArgs {
   const void* dh;
@@ -551,7 +641,7 @@ Plan backward_plan(int64_t N, int64_t K, int64_t H, bool bf16, bool vec, bool dx
 // The partial sums' bytes, whichever way the rows lie and whichever results are wanted.
 size_t forward_bytes(int64_t N, int64_t K, int64_t H, bool bf16) {
   if (N == 0) return 0;
-  return std::max(forward_plan(N, K, H, bf16, true).bytes, bf16 ? 0 : forward_plan(N, K, H, false, false).bytes);
+  return std::max(N <= few_tokens(bf16 ? 2 : 4) ? 0 : forward_plan(N, K, H, bf16, true).bytes, bf16 ? 0 : forward_plan(N, K, H, false, false).bytes);
 }
 size_t backward_partial_bytes(int64_t N, int64_t K, int64_t H, bool bf16) {
   if (N == 0) return 0;
@@ -607,12 +697,33 @@ hipError_t launch_forward(const GatedArgs& a, const Split& sp, hipStream_t s) {
     default: return launch_op<ForwardOp<T, P, G::vec, ANTDT_ACT_SIGMOID, SAVE>>(a, sp, s);
   }
 }
+template <typename T, int LANES>
+hipError_t launch_few(const GatedArgs& a, hipStream_t s) {
+  const dim3 grid((unsigned)div_up(a.H, LANES * (16 / (int)sizeof(T))));
+  if (a.N == 1) hipLaunchKernelGGL((gated_few_kernel<T, 1, LANES>), grid, dim3(FEW_THREADS), 0, s, a);
+  else if (a.N == 2) hipLaunchKernelGGL((gated_few_kernel<T, 2, LANES>), grid, dim3(FEW_THREADS), 0, s, a);
+  else if constexpr (few_tokens(sizeof(T)) > 2) {
+    if (a.N <= 4) hipLaunchKernelGGL((gated_few_kernel<T, 4, LANES>), grid, dim3(FEW_THREADS), 0, s, a);
+    else hipLaunchKernelGGL((gated_few_kernel<T, 8, LANES>), grid, dim3(FEW_THREADS), 0, s, a);
+  }
+  return hipGetLastError();
+}
+// Lanes along H: as many (128 bytes of a row at most) as leave 150 blocks.  1 token, 2 / 4 / 8 lanes, us: bf16 1024-4096 5.5 / 5.4 / 7.3,
+// 2048-5632 16.3 / 13.8 / 19.0, 4096-14336 8 lanes 39.2, 4 44.5; fp32 2048-5632 4 lanes 22.6, 8 18.2.
+template <typename T>
+hipError_t launch_few(const GatedArgs& a, hipStream_t s) {
+  constexpr int VN = 16 / sizeof(T), ENOUGH = 150;
+  if (a.H / (8 * VN) >= ENOUGH) return launch_few<T, 8>(a, s);
+  if (a.H / (4 * VN) >= ENOUGH) return launch_few<T, 4>(a, s);
+  return launch_few<T, 2>(a, s);
+}
 template <typename T, int C>
 hipError_t launch_forward_class(const GatedArgs& a, const Split& sp, hipStream_t s) {
   typedef TilingOf<T, C, 2, false, true> G;
   return a.saved ? launch_forward<G, true>(a, sp, s) : launch_forward<G, false>(a, sp, s);
 }
 hipError_t gated_forward(const GatedArgs& a, bool bf16, bool vec, float* partial, hipStream_t s) {
+  if (vec && a.N <= few_tokens(bf16 ? 2 : 4)) return bf16 ? launch_few<bf16_t>(a, s) : launch_few<float>(a, s);
   Plan p = forward_plan(a.N, a.K, a.H, bf16, vec);
   Split& sp = p.split[0];
   sp.partial = partial;
@@ -710,7 +821,7 @@ int antdt_gated_forward(const void* x, int64_t ldx, const void* wg, const void* 
   if (N == 0) return ANTDT_OK;
   OP_TRY(op_workspace(call, workspace, workspace_bytes, forward_bytes(N, K, H, dtype == ANTDT_BF16)));
   const GatedArgs a = {x, wg, wu, h, reinterpret_cast<float*>(saved), ldx, ldw, ldh, N, K, H, act};
-  const bool vec = whole16(x, ldx) && whole16(wg, ldw) && whole16(wu, ldw) && whole16(h, ldh) && ((K | H) & 3) == 0;
+  const bool vec = dtype == ANTDT_BF16 || (whole16(x, ldx) && whole16(wg, ldw) && whole16(wu, ldw) && whole16(h, ldh) && ((K | H) & 3) == 0);
   return op_hip(call, gated_forward(a, dtype == ANTDT_BF16, vec, reinterpret_cast<float*>(workspace), (hipStream_t)stream));
 }
 

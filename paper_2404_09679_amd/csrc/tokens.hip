@@ -4,6 +4,7 @@
 #include <utility>
 
 #include "ops.h"
+#include "sort.h"
 
 namespace antdt {
 namespace {
@@ -75,10 +76,10 @@ hipError_t launch_rows(RowsArgs a, int quantum, hipStream_t s) {
 
 // ------------------------------------------------------------- gradient of the table
 // grad[v, :] = scale * sum over the n with tokens[n] == v of dropout(dy[n, :]).  The positions are sorted by token (stable, so a
-// row's sum is in the order of the sequence); the sorted list is cut into chunks of C positions, and L lanes walk a chunk, 8
-// columns each, adding up dy rows and writing a row whenever the token changes.  A run of one token over several chunks leaves a
-// partial sum per chunk: slot 0 of a chunk for a run that came in from the chunk before, slot 1 for one that starts in it and goes on;
-// the chunk where it starts adds them up in a second launch.
+// row's sum is in the order of the sequence).  L lanes walk C positions of the sorted list, 8 columns each, adding up dy rows and
+// writing a row whenever the token changes; a block has 256 / L such walks behind each other and puts the ends of its walks together in LDS.
+// A run of one token over several blocks leaves a partial sum per block: slot 0 for a run that came in from the block before, slot 1
+// for one that starts in it and goes on; a second launch adds them up.
 struct GradArgs {
   const int32_t* key;     // tokens ascending, padding (V) last
   const int32_t* pay;     // their positions
@@ -86,32 +87,70 @@ struct GradArgs {
   float* grad;
   float* partial;         // [chunks, 2, ldp]
   int64_t lddy, ldg, ldp, N, V, D;
-  int32_t chunk, chunks, lanes_log2;
+  int32_t walk, chunk, chunks, lanes_log2;   // positions of a walk and of a block, blocks
   float scale;
   DropArgs drop;
 };
 
+// What clears the gradient (of the rows that no token names; the others are written again).
+struct ClearArgs {
+  float* grad;
+  int64_t ldg, rows, cols;
+  int32_t whole;   // 16 bytes at a time, rows without gaps
+};
+template <int THREADS>
+__device__ __forceinline__ void clear_rows(const ClearArgs& a, int block, int blocks) {
+  const int64_t first = (int64_t)block * THREADS + threadIdx.x, step = (int64_t)blocks * THREADS;
+  if (a.whole) {
+    const int64_t n = a.rows * a.cols / 4;
+    for (int64_t i = first; i < n; i += step) reinterpret_cast<float4*>(a.grad)[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  } else {
+    for (int64_t r = first >> 6; r < a.rows; r += step >> 6)
+      for (int64_t c = first & 63; c < a.cols; c += 64) a.grad[r * a.ldg + c] = 0.0f;
+  }
+}
+
 // Keys and positions of the sort; further blocks clear the gradient.
-__global__ __launch_bounds__(256) void token_keys_kernel(const int32_t* tokens, int32_t* key, int32_t* pay, int N, int V, int key_blocks,
-                                                         float* grad, int64_t ldg, int64_t D, bool vec) {
-  if ((int)blockIdx.x < key_blocks) {
-    const int i = blockIdx.x * 256 + threadIdx.x;
-    if (i < N) {
-      const int t = tokens[i];
-      key[i] = t >= 0 && t < V ? t : V;
-      pay[i] = i;
-    }
+__global__ __launch_bounds__(256) void token_keys_kernel(const int32_t* tokens, int32_t* key, int32_t* pay, int N, int V, int key_blocks, ClearArgs clear) {
+  if ((int)blockIdx.x >= key_blocks) {
+    clear_rows<256>(clear, blockIdx.x - key_blocks, gridDim.x - key_blocks);
     return;
   }
-  const int64_t first = (int64_t)(blockIdx.x - key_blocks) * 256 + threadIdx.x, step = (int64_t)(gridDim.x - key_blocks) * 256;
-  if (vec) {   // rows without gaps, as one array
-    const int64_t n = (int64_t)V * D / 4;
-    for (int64_t i = first; i < n; i += step) reinterpret_cast<float4*>(grad)[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-  } else {
-    const int64_t rows = V;
-    for (int64_t r = first >> 6; r < rows; r += step >> 6)
-      for (int64_t c = first & 63; c < D; c += 64) grad[r * ldg + c] = 0.0f;
+  const int i = blockIdx.x * 256 + threadIdx.x;
+  if (i < N) {
+    const int t = tokens[i];
+    key[i] = t >= 0 && t < V ? t : V;
+    pay[i] = i;
   }
+}
+// The same and the whole sort, of as many tokens as one block sorts (the first; 3001 tokens: launches of 5.5 and 8.2 us in one of 9).
+template <int IT>
+__global__ __launch_bounds__(SMALL_THREADS) void token_sort_kernel(const int32_t* tokens, int32_t* key_in, int32_t* pay_in, int32_t* key, int32_t* pay, int N,
+                                                                   int V, int passes, int rb, ClearArgs clear) {
+  __shared__ SmallSortLds lds;
+  extern __shared__ int32_t stage[];
+  if (blockIdx.x > 0) {
+    clear_rows<SMALL_THREADS>(clear, blockIdx.x - 1, gridDim.x - 1);
+    return;
+  }
+  for (int i = threadIdx.x; i < N; i += SMALL_THREADS) {
+    const int t = tokens[i];
+    key_in[i] = t >= 0 && t < V ? t : V;
+    pay_in[i] = i;
+  }
+  __syncthreads();   // (read by other threads of the block)
+  sort_small_field<IT>(lds, stage, key_in, pay_in, key, pay, N, passes, rb);
+}
+template <int IT>
+hipError_t launch_token_sort(const int32_t* tokens, const SortBuffers& sb, int N, int V, const SortPlan& sp, int clear_blocks, const ClearArgs& clear,
+                             hipStream_t s) {
+  static std::atomic<uint64_t> allowed{0};
+  constexpr int bytes = SMALL_THREADS * IT * 4;
+  const hipError_t e = allow_lds(token_sort_kernel<IT>, bytes, (int)sizeof(SmallSortLds), allowed);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(token_sort_kernel<IT>, dim3(1 + clear_blocks), dim3(SMALL_THREADS), bytes, s, tokens, sb.key[1], sb.pay[1], sb.key[0], sb.pay[0], N, V,
+                     sp.passes, sp.radix_bits, clear);
+  return hipGetLastError();
 }
 
 template <bool ACCUMULATE>
@@ -138,63 +177,107 @@ __device__ __forceinline__ void write_row(const GradArgs& a, int v, int64_t c, i
 
 template <typename T, int Q, bool DROP, bool ACCUMULATE>
 __global__ __launch_bounds__(256) void token_sum_kernel(GradArgs a, bool vec_grad) {
-  const int lane = threadIdx.x & ((1 << a.lanes_log2) - 1);
-  const int64_t j = ((int64_t)blockIdx.x << (8 - a.lanes_log2)) + (threadIdx.x >> a.lanes_log2);
+  // of the walks of the block: the sum of the run that came in and of the one that goes on, and whether there is the one, whether it is
+  // the whole walk and goes on, and whether there is the other
+  __shared__ float sums[2][256][8];
+  __shared__ uint8_t came[256], through[256], starts[256];
+  const int lanes = 1 << a.lanes_log2, walks = 256 >> a.lanes_log2;
+  const int lane = threadIdx.x & (lanes - 1), g = threadIdx.x >> a.lanes_log2;
   const int64_t c = 8 * (((int64_t)blockIdx.y << a.lanes_log2) + lane);
-  if (j >= a.chunks || c >= a.D) return;
-  const int64_t p0 = j * a.chunk, p1 = min(p0 + a.chunk, a.N);
-  const int n = (int)min((int64_t)8, a.D - c);
+  const int64_t p0 = (int64_t)blockIdx.x * a.chunk + (int64_t)g * a.walk, p1 = min(p0 + a.walk, a.N);
+  const int n = (int)max(min((int64_t)8, a.D - c), (int64_t)0);
   const DropKey dk(a.drop);
   const float scale = a.scale * a.drop.factor;
   const T* dy = reinterpret_cast<const T*>(a.dy) + c;
-  float* slots = a.partial + j * 2 * a.ldp + c;
 
-  int run = a.key[p0];
-  bool came_in = p0 > 0 && a.key[p0 - 1] == run;
-  float sum[8] = {};
-  constexpr int U = 8;
-  for (int64_t p = p0; p < p1 && run < a.V; p += U) {
-    int k[U], at[U];
-    float x[U][8];
+  bool has_in = false, is_through = false, has_out = false;
+  int run = (int)a.V;
+  if (p0 < a.N) {
+    run = a.key[p0];
+    has_in = run < a.V && p0 > 0 && a.key[p0 - 1] == run;
+    bool in = has_in;
+    float sum[8] = {};
+    if (n > 0) {
+      constexpr int U = 8;
+      for (int64_t p = p0; p < p1 && run < a.V; p += U) {
+        int k[U], at[U];
+        float x[U][8];
 #pragma unroll
-    for (int q = 0; q < U; ++q) {
-      const int64_t i = min(p + q, p1 - 1);
-      k[q] = a.key[i];
-      at[q] = a.pay[i];
+        for (int q = 0; q < U; ++q) {
+          const int64_t i = min(p + q, p1 - 1);
+          k[q] = a.key[i];
+          at[q] = a.pay[i];
+        }
+#pragma unroll
+        for (int q = 0; q < U; ++q) load8<Q>(dy + (int64_t)at[q] * a.lddy, n, x[q]);
+#pragma unroll
+        for (int q = 0; q < U; ++q) {
+          if (p + q >= p1 || run >= a.V) continue;
+          if (k[q] != run) {
+            if (in) store8<4>(sums[0][threadIdx.x], 8, sum);
+            else write_row<ACCUMULATE>(a, run, c, n, vec_grad, sum);
+            in = false;
+            run = k[q];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum[e] = 0.0f;
+            if (run >= a.V) continue;
+          }
+          if (DROP) {
+            drop8(a.drop, dk, at[q], (uint32_t)(c >> 3), scale, x[q]);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum[e] += x[q][e];
+          } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum[e] = fmaf(x[q][e], scale, sum[e]);
+          }
+        }
+      }
+    } else {   // (a lane without columns: the flags alone)
+      run = a.key[p1 - 1];
+      in = has_in && run == a.key[p0];
     }
-#pragma unroll
-    for (int q = 0; q < U; ++q) load8<Q>(dy + (int64_t)at[q] * a.lddy, n, x[q]);
-#pragma unroll
-    for (int q = 0; q < U; ++q) {
-      if (p + q >= p1 || run >= a.V) continue;
-      if (k[q] != run) {
-        if (came_in) store8<4>(slots, 8, sum);
-        else write_row<ACCUMULATE>(a, run, c, n, vec_grad, sum);
-        came_in = false;
-        run = k[q];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) sum[e] = 0.0f;
-        if (run >= a.V) continue;
-      }
-      if (DROP) {
-        drop8(a.drop, dk, at[q], (uint32_t)(c >> 3), scale, x[q]);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) sum[e] += x[q][e];
-      } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) sum[e] = fmaf(x[q][e], scale, sum[e]);
-      }
+    if (run < a.V) {
+      const bool goes_on = p1 < a.N && a.key[p1] == run;
+      is_through = in && goes_on;
+      has_out = !in && goes_on;
+      if (in) store8<4>(sums[0][threadIdx.x], 8, sum);
+      else if (goes_on) store8<4>(sums[1][threadIdx.x], 8, sum);
+      else if (n > 0) write_row<ACCUMULATE>(a, run, c, n, vec_grad, sum);
     }
   }
-  if (run >= a.V) return;
-  const bool goes_on = p1 < a.N && a.key[p1] == run;
-  if (came_in) store8<4>(slots, 8, sum);
-  else if (goes_on) store8<4>(slots + a.ldp, 8, sum);
-  else write_row<ACCUMULATE>(a, run, c, n, vec_grad, sum);
+  if (lane == 0) {
+    came[g] = has_in; through[g] = is_through; starts[g] = has_out;
+  }
+  __syncthreads();
+  float* slots = a.partial + (int64_t)blockIdx.x * 2 * a.ldp + c;
+  // the sums of the walks from q on that belong to the run, added to sum; whether it goes on behind the block
+  auto follow = [&](int q, float (&sum)[8]) {
+    for (; q < walks; ++q) {
+      if (!came[q]) return false;
+      float x[8];
+      load8<4>(sums[0][q * lanes + lane], 8, x);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sum[e] += x[e];
+      if (!through[q]) return false;
+    }
+    return true;
+  };
+  float sum[8];
+  if (has_out && n > 0) {
+    load8<4>(sums[1][threadIdx.x], 8, sum);
+    if (follow(g + 1, sum)) store8<4>(slots + a.ldp, 8, sum);
+    else write_row<ACCUMULATE>(a, run, c, n, vec_grad, sum);
+  }
+  if (g == 0 && has_in && n > 0) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sum[e] = 0.0f;
+    follow(0, sum);
+    store8<4>(slots, 8, sum);
+  }
 }
 
-// Runs over several chunks: those over up to JOIN_FEW more are added up by the lanes of the chunk where they start, the others by the whole
-// block.  (Bound by the chains of loads: how far a run goes is asked by all lanes at once.)
+// Runs over several blocks of the first launch (`chunks` here): those over up to JOIN_FEW more are added up by the lanes of the chunk where
+// they start, the others by a whole block.  (Bound by the chains of loads: how far a run goes is asked by all lanes at once.)
 constexpr int JOIN_THREADS = 1024, JOIN_FEW = 32;
 template <bool ACCUMULATE>
 __global__ __launch_bounds__(JOIN_THREADS) void token_join_kernel(GradArgs a, bool vec_grad) {
@@ -272,7 +355,7 @@ __global__ __launch_bounds__(JOIN_THREADS) void token_join_kernel(GradArgs a, bo
 
 // How the gradient's workspace is laid out.
 struct GradPlan {
-  int32_t passes, radix_bits, tiles, chunk, chunks, lanes_log2;
+  int32_t passes, radix_bits, tiles, walk, chunk, chunks, lanes_log2;
   int64_t ldp;
   size_t key[2], pay[2], hist, digit_total, partial, bytes;
 };
@@ -285,8 +368,9 @@ GradPlan grad_plan(int64_t N, int64_t V, int64_t D) {
   p.tiles = (int32_t)div_up(N, ANTDT_SORT_TILE);
   p.lanes_log2 = row_lanes_log2(D, 6);
   p.ldp = div_up(D, 8) * 8;
-  // Chunks short enough that 2^18 threads find work, long enough that few partial sums are written.
-  p.chunk = (int32_t)std::max<int64_t>(8, div_up(N << p.lanes_log2, 1 << 18));
+  // Walks short enough that 2^18 threads find work, long enough that not most of them end inside a run.
+  p.walk = (int32_t)std::max<int64_t>(8, div_up(N << p.lanes_log2, 1 << 18));
+  p.chunk = p.walk * (256 >> p.lanes_log2);
   p.chunks = (int32_t)div_up(N, p.chunk);
   size_t at = 0;
   auto take = [&](size_t bytes) {
@@ -307,9 +391,8 @@ GradPlan grad_plan(int64_t N, int64_t V, int64_t D) {
 
 template <typename T, int Q, bool DROP>
 hipError_t launch_token_sums(const GradArgs& a, bool accumulate, bool vec_grad, hipStream_t s) {
-  const int groups = 256 >> a.lanes_log2;
   const unsigned slices = (unsigned)div_up(a.D, (int64_t)8 << a.lanes_log2);
-  const dim3 grid((unsigned)div_up(a.chunks, groups), slices), join((unsigned)div_up(a.chunks, JOIN_THREADS >> a.lanes_log2), slices);
+  const dim3 grid((unsigned)a.chunks, slices), join((unsigned)div_up(a.chunks, JOIN_THREADS >> a.lanes_log2), slices);
   constexpr int bytes = JOIN_THREADS * 8 * 4;
   if (accumulate) hipLaunchKernelGGL((token_sum_kernel<T, Q, DROP, true>), grid, dim3(256), 0, s, a, vec_grad);
   else hipLaunchKernelGGL((token_sum_kernel<T, Q, DROP, false>), grid, dim3(256), 0, s, a, vec_grad);
@@ -413,21 +496,15 @@ int antdt_token_gradient(const void* dy, int64_t lddy, int32_t dtype, const int3
   const hipStream_t s = (hipStream_t)stream;
   char* ws = reinterpret_cast<char*>(workspace);
   auto ints = [&](size_t at) { return reinterpret_cast<int32_t*>(ws + at); };
-  int32_t *key1 = N ? ints(pl.key[1]) : nullptr, *pay1 = N ? ints(pl.pay[1]) : nullptr;
-  const int key_blocks = (int)div_up(N, 256);
   const bool whole = ldg == D && D % 4 == 0 && (reinterpret_cast<uintptr_t>(grad) & 15) == 0;
-  const int clear_blocks = accumulate ? 0 : (int)std::min<int64_t>(whole ? div_up(V * D, 4096) : div_up(V, 4), 8192);
-  hipLaunchKernelGGL(token_keys_kernel, dim3(key_blocks + clear_blocks), dim3(256), 0, s, tokens, key1, pay1, (int)N, (int)V, key_blocks, grad, ldg, D,
-                     whole);
-  OP_TRY(op_hip(call, hipGetLastError()));
-  if (N == 0) return ANTDT_OK;
+  const ClearArgs clear = {grad, ldg, V, D, whole};
+  const int64_t clear_blocks = accumulate ? 0 : std::min<int64_t>(whole ? div_up(V * D, 4096) : div_up(V, 4), 8192);
 
   SortPlan sp = {};
   sp.F = 1; sp.passes = pl.passes; sp.radix_bits = pl.radix_bits; sp.total_tiles = pl.tiles; sp.rows = V + 1; sp.samples = N; sp.width = D;
   SortBuffers sb = {};
-  sb.ids = key1; sb.pay0 = pay1;   // (read by the first pass, written by the second)
-  sb.key[0] = ints(pl.key[0]); sb.key[1] = key1; sb.pay[0] = ints(pl.pay[0]); sb.pay[1] = pay1;
-  sb.hist = reinterpret_cast<uint32_t*>(ws + pl.hist); sb.digit_total = reinterpret_cast<uint32_t*>(ws + pl.digit_total);
+  sb.key[1] = N ? ints(pl.key[1]) : nullptr; sb.pay[1] = N ? ints(pl.pay[1]) : nullptr;
+  sb.ids = sb.key[1]; sb.pay0 = sb.pay[1];   // (read by the first pass, written by the second)
   FieldPtr fp = {};
   TileBase tb = {};
   for (int f = 1; f <= ANTDT_MAX_FIELDS; ++f) {
@@ -435,12 +512,31 @@ int antdt_token_gradient(const void* dy, int64_t lddy, int32_t dtype, const int3
     tb.t[f] = pl.tiles;
   }
   int sorted = 0;
-  OP_TRY(op_hip(call, launch_sort(sp, sb, fp, tb, nullptr, s, &sorted)));
+  const int items = N ? small_sort_items(1, fp) : 0;
+  if (items) {
+    sb.key[0] = ints(pl.key[0]); sb.pay[0] = ints(pl.pay[0]);
+    const int blocks = (int)div_up(clear_blocks, SMALL_THREADS / 256);
+    switch (items) {
+      case 2: OP_TRY(op_hip(call, launch_token_sort<2>(tokens, sb, (int)N, (int)V, sp, blocks, clear, s))); break;
+      case 4: OP_TRY(op_hip(call, launch_token_sort<4>(tokens, sb, (int)N, (int)V, sp, blocks, clear, s))); break;
+      case 8: OP_TRY(op_hip(call, launch_token_sort<8>(tokens, sb, (int)N, (int)V, sp, blocks, clear, s))); break;
+      default: OP_TRY(op_hip(call, launch_token_sort<16>(tokens, sb, (int)N, (int)V, sp, blocks, clear, s))); break;
+    }
+  } else {
+    const int key_blocks = (int)div_up(N, 256);
+    hipLaunchKernelGGL(token_keys_kernel, dim3((unsigned)(key_blocks + clear_blocks)), dim3(256), 0, s, tokens, sb.key[1], sb.pay[1], (int)N, (int)V,
+                       key_blocks, clear);
+    OP_TRY(op_hip(call, hipGetLastError()));
+    if (N == 0) return ANTDT_OK;
+    sb.key[0] = ints(pl.key[0]); sb.pay[0] = ints(pl.pay[0]);
+    sb.hist = reinterpret_cast<uint32_t*>(ws + pl.hist); sb.digit_total = reinterpret_cast<uint32_t*>(ws + pl.digit_total);
+    OP_TRY(op_hip(call, launch_sort(sp, sb, fp, tb, nullptr, s, &sorted)));
+  }
 
   a.key = sb.key[sorted]; a.pay = sb.pay[sorted];
   a.dy = dy; a.grad = grad; a.partial = reinterpret_cast<float*>(ws + pl.partial);
   a.lddy = lddy; a.ldg = ldg; a.ldp = pl.ldp; a.N = N; a.V = V; a.D = D;
-  a.chunk = pl.chunk; a.chunks = pl.chunks; a.lanes_log2 = pl.lanes_log2; a.scale = scale;
+  a.walk = pl.walk; a.chunk = pl.chunk; a.chunks = pl.chunks; a.lanes_log2 = pl.lanes_log2; a.scale = scale;
   const int q = row_quantum(D, op_size(dtype), {{dy, lddy}});
   const bool vec_grad = row_quantum(D, 4, {{grad, ldg}}) >= 4;
   hipError_t e;
