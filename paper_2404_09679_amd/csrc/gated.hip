@@ -96,10 +96,10 @@ __device__ __forceinline__ void store_rows(float* st, const f32x16 (&x)[TN], T* 
       if (VEC) {   // (a whole group exists)
         const float4 a = *reinterpret_cast<const float4*>(s);
         if constexpr (sizeof(T) == 4) {
-          *reinterpret_cast<float4*>(o) = a;
+          store16<false>(o, bits4(a.x, a.y, a.z, a.w));
         } else {
           const float4 b = *reinterpret_cast<const float4*>(s + 4);
-          *reinterpret_cast<uint4*>(o) = make_uint4(f2bf2(a.x, a.y), f2bf2(a.z, a.w), f2bf2(b.x, b.y), f2bf2(b.z, b.w));
+          store16<false>(o, make_uint4(f2bf2(a.x, a.y), f2bf2(a.z, a.w), f2bf2(b.x, b.y), f2bf2(b.z, b.w)));
         }
       } else {
 #pragma unroll
@@ -377,9 +377,9 @@ __global__ __launch_bounds__(256) void gated_dz_kernel(DzArgs a) {
     const int64_t r = i / per_row, c = (i - r * per_row) * 8;
     const int cols = (int)min((int64_t)8, a.H - c);
     float d[8], p[8], q[8];
-    load8<Q>(reinterpret_cast<const T*>(a.dh) + r * a.lddh + c, cols, d);
-    load8<Q>(a.saved + r * a.H + c, cols, p);
-    load8<Q>(a.saved + (a.N + r) * a.H + c, cols, q);
+    load8<Q, true>(reinterpret_cast<const T*>(a.dh) + r * a.lddh + c, cols, d);
+    load8<Q, true>(a.saved + r * a.H + c, cols, p);
+    load8<Q, true>(a.saved + (a.N + r) * a.H + c, cols, q);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       p[e] *= d[e];

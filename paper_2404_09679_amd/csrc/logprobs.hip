@@ -3,6 +3,7 @@
 //   log p_j = (x_j - m) - log s,   H = log s - q / s,
 // all three kept up in one pass (a new maximum scales s and q), so that a row is read once; bound by memory.
 #include <algorithm>
+#include <type_traits>
 
 #include "ops.h"
 
@@ -12,6 +13,11 @@ namespace {
 constexpr int LP_THREADS = 512, LP_WAVES = LP_THREADS / 64;
 constexpr int LP_LIST = 1024;           // candidates kept for the top
 constexpr float NEG_INF = -__builtin_inff();
+
+// Logits of more bytes than this are read, and their gradient written, without being kept in the last-level cache (256 MB), which they would
+// leave before they are used again.  Kept / not, us, another buffer every time: forward and gradient of 128 / 192 / 256 / 400 MB 80 / 74, 118 / 106,
+// 154 / 137, 235 / 212; with the gradient read by what follows 100 / 114, 160 / 161, 212 / 205, 320 / 311.
+constexpr int64_t STREAM_BYTES = 192 << 20;
 
 struct LpArgs {
   const void* x;
@@ -23,6 +29,7 @@ struct LpArgs {
   float* top_logp;
   int32_t* top_index;
   int32_t top, pieces;
+  int64_t piece;      // columns of one (the last may have fewer)
   float4* part;       // [N, pieces] m, s, q
   uint64_t* part_top; // [N, pieces, top]
 };
@@ -83,7 +90,7 @@ __device__ __forceinline__ float largest(const float (&v)[n]) {
 
 // Columns [c0, c1) of a row in the thread's share: up to the first 16-byte boundary and from the last on one by one, 16 bytes at a
 // time in between.  f(values, first column, how many), columns of a thread ascending.
-template <typename T>
+template <typename T, bool STREAM>
 struct RowWalk {
   static constexpr int VN = 16 / sizeof(T);
   const T* row;
@@ -122,7 +129,7 @@ struct RowWalk {
         f);
   }
   // The same, U vectors at a time where there are as many: g(values, first column), the vectors THREADS of them apart.
-  static constexpr int U = 4;
+  static constexpr int U = 2;
   template <int THREADS, typename G, typename F>
   __device__ __forceinline__ void batches(int tid, G&& g, F&& f) const {
     float v[VN];
@@ -135,18 +142,30 @@ struct RowWalk {
     if (c0 + tid < body) one(c0 + tid);
     const uint4* p = reinterpret_cast<const uint4*>(row + body);
     int64_t i = tid;
-    for (; i + (U - 1) * THREADS < vecs; i += U * THREADS) {
-      uint4 w[U];
-      float x[U * VN];
+    constexpr int64_t LAST = (U - 1) * THREADS;
+    if (i + LAST < vecs) {   // the next vectors are requested before these are worked on
+      uint4 w[U], next[U];
 #pragma unroll
-      for (int q = 0; q < U; ++q) w[q] = p[i + q * THREADS];
+      for (int q = 0; q < U; ++q) w[q] = load16<STREAM>(p + i + q * THREADS);
+      while (true) {
+        const bool more = i + U * THREADS + LAST < vecs;
+        if (more) {
 #pragma unroll
-      for (int q = 0; q < U; ++q) {
-        unpack(w[q], v);
+          for (int q = 0; q < U; ++q) next[q] = load16<STREAM>(p + i + (U + q) * THREADS);
+        }
+        float x[U * VN];
 #pragma unroll
-        for (int e = 0; e < VN; ++e) x[q * VN + e] = v[e];
+        for (int q = 0; q < U; ++q) {
+          unpack(w[q], v);
+#pragma unroll
+          for (int e = 0; e < VN; ++e) x[q * VN + e] = v[e];
+        }
+        g(x, body + i * VN);
+        i += U * THREADS;
+        if (!more) break;
+#pragma unroll
+        for (int q = 0; q < U; ++q) w[q] = next[q];
       }
-      g(x, body + i * VN);
     }
     for (; i < vecs; i += THREADS) {
       unpack(p[i], v);
@@ -241,6 +260,7 @@ __device__ __forceinline__ void block_top(LpLds& lds, int k, uint64_t mine, bool
     return;
   }
   uint64_t last = ~0ull;
+#pragma unroll 1
   for (int r = 0; r < k; ++r) {
     uint64_t t = 0;
     rescan([&](uint64_t key) {
@@ -274,13 +294,13 @@ __device__ __forceinline__ void write_logp(const LpArgs& a, int64_t row, const S
 }
 
 // A block per row, or per piece of one: its sums and top then go to memory for lp_join_kernel.
-template <typename T, bool TOP>
+template <typename T, bool TOP, bool STREAM>
 __global__ __launch_bounds__(LP_THREADS) void lp_kernel(LpArgs a) {
   __shared__ LpLds lds;
-  const int64_t row = blockIdx.x / a.pieces;
+  const int64_t row = a.pieces == 1 ? blockIdx.x : blockIdx.x / (unsigned)a.pieces;
   const int piece = (int)(blockIdx.x - row * a.pieces), tid = threadIdx.x;
-  typedef RowWalk<T> W;
-  const W walk(reinterpret_cast<const T*>(a.x) + row * a.ld, a.V * piece / a.pieces, a.V * (piece + 1) / a.pieces);
+  typedef RowWalk<T, STREAM> W;
+  const W walk(reinterpret_cast<const T*>(a.x) + row * a.ld, piece * a.piece, min((piece + 1) * a.piece, a.V));
   constexpr int VN = W::VN;
   Softmax t;
   int64_t best = 0;   // column of the thread's first largest logit
@@ -410,9 +430,9 @@ struct LpGradArgs {
 };
 constexpr int LG_THREADS = 256;
 
-template <typename T, bool SAME>   // SAME: both rows reach a 16-byte boundary at the same column
+template <typename T, bool SAME, bool STREAM>   // SAME: both rows reach a 16-byte boundary at the same column
 __global__ __launch_bounds__(LG_THREADS) void lp_grad_kernel(LpGradArgs a) {
-  constexpr int VN = RowWalk<T>::VN;
+  constexpr int VN = 16 / sizeof(T);
   for (int64_t id = blockIdx.x; id < a.N * a.pieces; id += gridDim.x) {
     const int64_t row = id / a.pieces, c0 = (id - row * a.pieces) * a.piece, c1 = min(c0 + a.piece, a.V);
     const float4 st = a.stats[row];
@@ -431,7 +451,7 @@ __global__ __launch_bounds__(LG_THREADS) void lp_grad_kernel(LpGradArgs a) {
       if (gb != 0.0f) g -= p == 0.0f ? 0.0f : gb * p * (lp + st.z);
       return none ? 0.0f : g;
     };
-    const RowWalk<T> walk(reinterpret_cast<const T*>(a.x) + row * a.ld, c0, c1);
+    const RowWalk<T, false> walk(reinterpret_cast<const T*>(a.x) + row * a.ld, c0, c1);
     if constexpr (SAME) {
       walk.template each<LG_THREADS>(threadIdx.x, [&](const float (&v)[VN], int64_t c, int n) {
         if (n == 1) {
@@ -440,8 +460,8 @@ __global__ __launch_bounds__(LG_THREADS) void lp_grad_kernel(LpGradArgs a) {
           float g[VN];
 #pragma unroll
           for (int e = 0; e < VN; ++e) g[e] = grad(v[e], c + e);
-          if constexpr (VN == 4) *reinterpret_cast<float4*>(out + c) = make_float4(g[0], g[1], g[2], g[3]);
-          else *reinterpret_cast<uint4*>(out + c) = make_uint4(f2bf2(g[0], g[1]), f2bf2(g[2], g[3]), f2bf2(g[4], g[5]), f2bf2(g[6], g[7]));
+          if constexpr (VN == 4) store16<STREAM>(out + c, bits4(g[0], g[1], g[2], g[3]));
+          else store16<STREAM>(out + c, make_uint4(f2bf2(g[0], g[1]), f2bf2(g[2], g[3]), f2bf2(g[4], g[5]), f2bf2(g[6], g[7])));
         }
       });
     } else {
@@ -493,19 +513,26 @@ int antdt_token_logprobs(const void* logits, int64_t ld, int64_t N, int64_t V, i
   a.x = logits; a.ld = ld; a.N = N; a.V = V; a.tokens = tokens; a.logp = logp; a.entropy = entropy;
   a.stats = reinterpret_cast<float4*>(stats); a.top_logp = top_logp; a.top_index = top_index; a.top = top;
   a.pieces = lp_pieces(N, V, top);
+  a.piece = div_up(V, a.pieces);   // (at least 4096 columns and at most 512 pieces: the last is not shorter than `top`)
   if (a.pieces > 1) {
     a.part = reinterpret_cast<float4*>(workspace);
     a.part_top = reinterpret_cast<uint64_t*>(a.part + N * a.pieces);
   }
   const hipStream_t s = (hipStream_t)stream;
   const dim3 grid((unsigned)(N * a.pieces));
-  if (dtype == ANTDT_F32) {
-    if (top) hipLaunchKernelGGL((lp_kernel<float, true>), grid, dim3(LP_THREADS), 0, s, a);
-    else hipLaunchKernelGGL((lp_kernel<float, false>), grid, dim3(LP_THREADS), 0, s, a);
-  } else {
-    if (top) hipLaunchKernelGGL((lp_kernel<bf16_t, true>), grid, dim3(LP_THREADS), 0, s, a);
-    else hipLaunchKernelGGL((lp_kernel<bf16_t, false>), grid, dim3(LP_THREADS), 0, s, a);
-  }
+  const bool far = N * V * op_size(dtype) > STREAM_BYTES;
+  auto go = [&](auto t, auto with_top) {
+    typedef decltype(t) T;
+    constexpr bool TOP = decltype(with_top)::value;
+    if (far) hipLaunchKernelGGL((lp_kernel<T, TOP, true>), grid, dim3(LP_THREADS), 0, s, a);
+    else hipLaunchKernelGGL((lp_kernel<T, TOP, false>), grid, dim3(LP_THREADS), 0, s, a);
+  };
+  auto typed = [&](auto t) {
+    if (top) go(t, std::true_type());
+    else go(t, std::false_type());
+  };
+  if (dtype == ANTDT_F32) typed(0.0f);
+  else typed((bf16_t)0);
   OP_TRY(op_hip(call, hipGetLastError()));
   if (a.pieces > 1) {
     if (dtype == ANTDT_F32) hipLaunchKernelGGL(lp_join_kernel<float>, dim3((unsigned)N), dim3(LP_THREADS), 0, s, a);
@@ -534,13 +561,15 @@ int antdt_token_logprobs_gradient(const void* logits, int64_t ld, int64_t N, int
   const bool same = ((reinterpret_cast<uintptr_t>(logits) ^ reinterpret_cast<uintptr_t>(d_logits)) & 15) == 0 && ((ld - ldd) * size) % 16 == 0;
   const dim3 grid((unsigned)std::min<int64_t>(N * a.pieces, 1 << 20));
   const hipStream_t s = (hipStream_t)stream;
-  if (dtype == ANTDT_F32) {
-    if (same) hipLaunchKernelGGL((lp_grad_kernel<float, true>), grid, dim3(LG_THREADS), 0, s, a);
-    else hipLaunchKernelGGL((lp_grad_kernel<float, false>), grid, dim3(LG_THREADS), 0, s, a);
-  } else {
-    if (same) hipLaunchKernelGGL((lp_grad_kernel<bf16_t, true>), grid, dim3(LG_THREADS), 0, s, a);
-    else hipLaunchKernelGGL((lp_grad_kernel<bf16_t, false>), grid, dim3(LG_THREADS), 0, s, a);
-  }
+  const bool far = N * V * size > STREAM_BYTES;
+  auto go = [&](auto t) {
+    typedef decltype(t) T;
+    if (same && far) hipLaunchKernelGGL((lp_grad_kernel<T, true, true>), grid, dim3(LG_THREADS), 0, s, a);
+    else if (same) hipLaunchKernelGGL((lp_grad_kernel<T, true, false>), grid, dim3(LG_THREADS), 0, s, a);
+    else hipLaunchKernelGGL((lp_grad_kernel<T, false, false>), grid, dim3(LG_THREADS), 0, s, a);
+  };
+  if (dtype == ANTDT_F32) go(0.0f);
+  else go((bf16_t)0);
   return op_hip(call, hipGetLastError());
 }
 

@@ -60,27 +60,53 @@ inline int row_quantum(int64_t cols, int64_t size, std::initializer_list<std::pa
   return q;
 }
 
+// 16 or 8 bytes from or to memory; STREAM: not kept in the caches beyond this use.
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+template <bool STREAM>
+__device__ __forceinline__ uint4 load16(const void* p) {
+  const u32x4* q = reinterpret_cast<const u32x4*>(p);
+  const u32x4 v = STREAM ? __builtin_nontemporal_load(q) : *q;
+  return make_uint4(v.x, v.y, v.z, v.w);
+}
+template <bool STREAM>
+__device__ __forceinline__ uint2 load8b(const void* p) {
+  const u32x2* q = reinterpret_cast<const u32x2*>(p);
+  const u32x2 v = STREAM ? __builtin_nontemporal_load(q) : *q;
+  return make_uint2(v.x, v.y);
+}
+template <bool STREAM>
+__device__ __forceinline__ void store16(void* p, uint4 w) {
+  const u32x4 v = {w.x, w.y, w.z, w.w};
+  if (STREAM) __builtin_nontemporal_store(v, reinterpret_cast<u32x4*>(p));
+  else *reinterpret_cast<u32x4*>(p) = v;
+}
+__device__ __forceinline__ uint4 bits4(float a, float b, float c, float d) {
+  return make_uint4(__float_as_uint(a), __float_as_uint(b), __float_as_uint(c), __float_as_uint(d));
+}
+
 // v[0 .. n) from p, n <= 8 columns of which Q at a time exist.
-template <int Q, typename T>
+template <int Q, bool STREAM = false, typename T>
 __device__ __forceinline__ void load8(const T* p, int n, float (&v)[8]) {
   if constexpr (Q == 1) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = e < n ? to_f32(p[e]) : 0.0f;
   } else if constexpr (sizeof(T) == 4) {
-    const float4 a = *reinterpret_cast<const float4*>(p);
-    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
-    float4 b = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    if (Q == 8 || n > 4) b = *reinterpret_cast<const float4*>(p + 4);
-    v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+    const uint4 a = load16<STREAM>(p);
+    uint4 b = make_uint4(0, 0, 0, 0);
+    if (Q == 8 || n > 4) b = load16<STREAM>(p + 4);
+    const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(w[e]);
   } else {
     uint4 a = make_uint4(0, 0, 0, 0);
     if constexpr (Q == 8) {
-      a = *reinterpret_cast<const uint4*>(p);
+      a = load16<STREAM>(p);
     } else {
-      const uint2 x = *reinterpret_cast<const uint2*>(p);
+      const uint2 x = load8b<STREAM>(p);
       a.x = x.x; a.y = x.y;
       if (n > 4) {
-        const uint2 y = *reinterpret_cast<const uint2*>(p + 4);
+        const uint2 y = load8b<STREAM>(p + 4);
         a.z = y.x; a.w = y.y;
       }
     }
@@ -92,19 +118,19 @@ __device__ __forceinline__ void load8(const T* p, int n, float (&v)[8]) {
     }
   }
 }
-template <int Q, typename T>
+template <int Q, bool STREAM = false, typename T>
 __device__ __forceinline__ void store8(T* p, int n, const float (&v)[8]) {
   if constexpr (Q == 1) {
 #pragma unroll
     for (int e = 0; e < 8; ++e)
       if (e < n) p[e] = from_f32<T>(v[e]);
   } else if constexpr (sizeof(T) == 4) {
-    *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
-    if (Q == 8 || n > 4) *reinterpret_cast<float4*>(p + 4) = make_float4(v[4], v[5], v[6], v[7]);
+    store16<STREAM>(p, bits4(v[0], v[1], v[2], v[3]));
+    if (Q == 8 || n > 4) store16<STREAM>(p + 4, bits4(v[4], v[5], v[6], v[7]));
   } else {
     const uint4 a = make_uint4(f2bf2(v[0], v[1]), f2bf2(v[2], v[3]), f2bf2(v[4], v[5]), f2bf2(v[6], v[7]));
     if constexpr (Q == 8) {
-      *reinterpret_cast<uint4*>(p) = a;
+      store16<STREAM>(p, a);
     } else {
       *reinterpret_cast<uint2*>(p) = make_uint2(a.x, a.y);
       if (n > 4) *reinterpret_cast<uint2*>(p + 4) = make_uint2(a.z, a.w);

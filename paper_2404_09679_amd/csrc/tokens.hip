@@ -103,7 +103,7 @@ __device__ __forceinline__ void clear_rows(const ClearArgs& a, int block, int bl
   const int64_t first = (int64_t)block * THREADS + threadIdx.x, step = (int64_t)blocks * THREADS;
   if (a.whole) {
     const int64_t n = a.rows * a.cols / 4;
-    for (int64_t i = first; i < n; i += step) reinterpret_cast<float4*>(a.grad)[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    for (int64_t i = first; i < n; i += step) store16<false>(a.grad + 4 * i, make_uint4(0, 0, 0, 0));
   } else {
     for (int64_t r = first >> 6; r < a.rows; r += step >> 6)
       for (int64_t c = first & 63; c < a.cols; c += 64) a.grad[r * a.ldg + c] = 0.0f;
@@ -209,7 +209,7 @@ __global__ __launch_bounds__(256) void token_sum_kernel(GradArgs a, bool vec_gra
           at[q] = a.pay[i];
         }
 #pragma unroll
-        for (int q = 0; q < U; ++q) load8<Q>(dy + (int64_t)at[q] * a.lddy, n, x[q]);
+        for (int q = 0; q < U; ++q) load8<Q, true>(dy + (int64_t)at[q] * a.lddy, n, x[q]);
 #pragma unroll
         for (int q = 0; q < U; ++q) {
           if (p + q >= p1 || run >= a.V) continue;
