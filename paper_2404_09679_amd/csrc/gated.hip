@@ -24,14 +24,15 @@ struct GatedArgs {
   int32_t act;
 };
 
-__device__ __forceinline__ float logistic(float x) { return 1.0f / (1.0f + __expf(-x)); }
+// (the reciprocal by one instruction, off by a unit at most: a correctly rounded quotient takes ten)
+__device__ __forceinline__ float logistic(float x) { return __builtin_amdgcn_rcpf(1.0f + __expf(-x)); }
 
 // p = act(g), r = act'(g).
 __device__ __forceinline__ void activation(int act, float g, float& p, float& r) {
   if (act == ANTDT_ACT_SILU) {
     const float s = logistic(g);
     p = g * s;
-    r = s * (1.0f + g * (1.0f - s));
+    r = fmaf(p, 1.0f - s, s);
   } else if (act == ANTDT_ACT_GELU) {
     const float cdf = 0.5f * (1.0f + erff(g * 0.70710678f));
     p = g * cdf;
@@ -451,13 +452,13 @@ struct DwOp {
 // products that a tile holds side by side) and what a tile costs a compute unit: ns a contraction slot, and us for filling the pipeline
 // and writing the results.
 struct TileClass {
-  int32_t rows, cols, slots;
+  int32_t rows, cols, slots, at_once;   // at_once: blocks that a compute unit's LDS holds
   float ns, us;
 };
-enum { BF16_256, BF16_128, BF16_64, F32_128, F32_64, F32_64_ANY, TILE_CLASSES };
+enum { BF16_256, BF16_128, BF16_64, F32_64, F32_64_ANY, TILE_CLASSES };
 constexpr TileClass TILE_CLASS[2][TILE_CLASSES] = {
-    {{256, 256, 64, 27.0f, 7.0f}, {128, 128, 64, 10.0f, 2.5f}, {64, 64, 64, 4.6f, 1.0f}, {128, 128, 32, 58.0f, 5.0f}, {64, 64, 32, 16.0f, 2.0f}, {64, 64, 32, 25.0f, 2.0f}},
-    {{256, 256, 64, 27.0f, 7.0f}, {128, 128, 64, 10.0f, 2.5f}, {64, 64, 64, 4.6f, 1.0f}, {128, 128, 32, 58.0f, 5.0f}, {64, 128, 32, 32.0f, 3.0f}, {64, 128, 32, 50.0f, 3.0f}}};
+    {{256, 256, 64, 1, 27.0f, 7.0f}, {128, 128, 64, 1, 10.0f, 2.5f}, {64, 64, 64, 3, 4.6f, 1.0f}, {64, 64, 32, 3, 16.0f, 2.0f}, {64, 64, 32, 3, 25.0f, 2.0f}},
+    {{256, 256, 64, 1, 27.0f, 7.0f}, {128, 128, 64, 1, 10.0f, 2.5f}, {64, 64, 64, 3, 4.6f, 1.0f}, {64, 128, 32, 2, 32.0f, 3.0f}, {64, 128, 32, 2, 50.0f, 3.0f}}};
 template <typename T, int C, int NB, bool AS, bool BS>
 struct TilingOf;   // Product: its TileProduct; vec: whole 16-byte groups may be written
 #define TILING(C, T, TM, TN, WR, WC, BK, STAGES, PIECE)                                                                                \
@@ -467,12 +468,12 @@ struct TilingOf;   // Product: its TileProduct; vec: whole 16-byte groups may be
     typedef T Type;                                                                                                                    \
     static constexpr bool vec = PIECE == 16;                                                                                           \
     static constexpr TileClass k = TILE_CLASS[NB - 1][C];                                                                              \
-    static_assert(Product::BM == k.rows && NB * Product::BN == k.cols && Product::SLOTS == k.slots, "class");                          \
+    static_assert(Product::BM == k.rows && NB * Product::BN == k.cols && Product::SLOTS == k.slots &&                                  \
+                      160 * 1024 / Product::LDS_BYTES == k.at_once, "class");                                                          \
   };
 TILING(BF16_256, bf16_t, 4, 2 / NB, 2, 4, 64, 2, 16)
 TILING(BF16_128, bf16_t, 2 / NB, 1, 2 * NB, 4 / NB, 64, 3, 16)
 TILING(BF16_64, bf16_t, 1, 1, 2, 2 / NB, 64, 3, 16)
-TILING(F32_128, float, 2, 2 / NB, 2, 2, 32, 3, 16)
 TILING(F32_64, float, 1, 1, 2, 2, 32, 3, 16)
 TILING(F32_64_ANY, float, 1, 1, 2, 2, 32, 3, 4)
 #undef TILING
@@ -533,6 +534,20 @@ double finish_time(int64_t places, std::initializer_list<Jobs> all) {
   return last;
 }
 
+// The same for jobs that all find a place at once: they are dealt out in turn, and a compute unit works on its jobs together.  0 where more
+// than that are waiting.
+double dealt_out(int at_once, std::initializer_list<Jobs> all) {
+  int64_t n = 0;
+  for (const Jobs& j : all) n += j.n;
+  if (at_once == 1 || n > COMPUTE_UNITS * at_once) return 0.0;
+  double unit[COMPUTE_UNITS] = {}, last = 0.0;
+  int64_t at = 0;
+  for (const Jobs& j : all)
+    for (int64_t i = 0; i < j.n; ++i) unit[at++ % COMPUTE_UNITS] += j.us;
+  for (double u : unit) last = std::max(last, u);
+  return last;
+}
+
 // A product that is part of a launch: rows x cols of results, `copies` of them side by side (two weights' gradients), `contraction` slots.
 struct Job {
   int64_t rows, cols, copies, contraction;
@@ -559,8 +574,9 @@ Plan plan_of(int cls, int NB, const Job (&job)[2]) {
     len[q] = s.len = (int)job[q].contraction;
   }
   const int64_t places = COMPUTE_UNITS, all = tiles[0] + tiles[1];
+  auto end = [&](std::initializer_list<Jobs> jobs) { return std::max(finish_time(places, jobs), dealt_out(c.at_once, jobs)); };
   auto us = [&](int64_t slots) { return slots * c.ns * 1e-3 + c.us; };
-  best.us = finish_time(places, {{tiles[0], us(len[0])}, {tiles[1], us(len[1])}});
+  best.us = end({{tiles[0], us(len[0])}, {tiles[1], us(len[1])}});
   auto parts_of = [&](int64_t slots, int64_t want) { return std::max<int64_t>(std::min<int64_t>({want, slots / (4 * c.slots), MOST_PARTS}), 1); };
   auto offer = [&](int64_t rest0, int64_t parts0, int64_t rest1, int64_t parts1) {
     const int64_t rest[2] = {parts0 > 1 ? rest0 : 0, parts1 > 1 ? rest1 : 0}, parts[2] = {parts0, parts1};
@@ -578,7 +594,7 @@ Plan plan_of(int cls, int NB, const Job (&job)[2]) {
       sums += rest[q] * s.parts;
     }
     p.bytes = (size_t)sums * c.rows * c.cols * 4;
-    p.us = finish_time(places, {{p.split[0].whole, us(len[0])}, {rest[0] * p.split[0].parts, us(part_len[0])}, {p.split[1].whole, us(len[1])},
+    p.us = end({{p.split[0].whole, us(len[0])}, {rest[0] * p.split[0].parts, us(part_len[0])}, {p.split[1].whole, us(len[1])},
                                 {rest[1] * p.split[1].parts, us(part_len[1])}}) +
            JOIN_US + p.bytes / PARTIAL_BYTES_PER_US;
     if (p.us < best.us) best = p;
@@ -600,8 +616,9 @@ Plan plan_of(int cls, int NB, const Job (&job)[2]) {
 }
 Plan best_plan(bool bf16, bool vec, int NB, const Job (&job)[2]) {
   if (!bf16 && !vec) return plan_of(F32_64_ANY, NB, job);
-  Plan best = plan_of(bf16 ? BF16_64 : F32_64, NB, job);
-  for (int c = bf16 ? BF16_256 : F32_128; c < (bf16 ? BF16_64 : F32_64); ++c) {
+  if (!bf16) return plan_of(F32_64, NB, job);
+  Plan best = plan_of(BF16_256, NB, job);
+  for (int c : {BF16_128, BF16_64}) {
     const Plan p = plan_of(c, NB, job);
     if (p.us < best.us) best = p;
   }
@@ -731,7 +748,6 @@ hipError_t gated_forward(const GatedArgs& a, bool bf16, bool vec, float* partial
     case BF16_256: return launch_forward_class<bf16_t, BF16_256>(a, sp, s);
     case BF16_128: return launch_forward_class<bf16_t, BF16_128>(a, sp, s);
     case BF16_64: return launch_forward_class<bf16_t, BF16_64>(a, sp, s);
-    case F32_128: return launch_forward_class<float, F32_128>(a, sp, s);
     case F32_64: return launch_forward_class<float, F32_64>(a, sp, s);
     default: return launch_forward_class<float, F32_64_ANY>(a, sp, s);
   }
@@ -756,7 +772,6 @@ hipError_t gated_products(const DxArgs& x, DwArgs w, bool bf16, bool vec, float*
     case BF16_256: return launch_backward<bf16_t, BF16_256>(x, w, p.split, s);
     case BF16_128: return launch_backward<bf16_t, BF16_128>(x, w, p.split, s);
     case BF16_64: return launch_backward<bf16_t, BF16_64>(x, w, p.split, s);
-    case F32_128: return launch_backward<float, F32_128>(x, w, p.split, s);
     case F32_64: return launch_backward<float, F32_64>(x, w, p.split, s);
     default: return launch_backward<float, F32_64_ANY>(x, w, p.split, s);
   }

@@ -144,27 +144,28 @@ struct RowWalk {
     int64_t i = tid;
     constexpr int64_t LAST = (U - 1) * THREADS;
     if (i + LAST < vecs) {   // the next vectors are requested before these are worked on
-      uint4 w[U], next[U];
+      struct {
+        uint4 v[U];
+      } w, next = {};
 #pragma unroll
-      for (int q = 0; q < U; ++q) w[q] = load16<STREAM>(p + i + q * THREADS);
+      for (int q = 0; q < U; ++q) w.v[q] = load16<STREAM>(p + i + q * THREADS);
       while (true) {
         const bool more = i + U * THREADS + LAST < vecs;
         if (more) {
 #pragma unroll
-          for (int q = 0; q < U; ++q) next[q] = load16<STREAM>(p + i + (U + q) * THREADS);
+          for (int q = 0; q < U; ++q) next.v[q] = load16<STREAM>(p + i + (U + q) * THREADS);
         }
         float x[U * VN];
 #pragma unroll
         for (int q = 0; q < U; ++q) {
-          unpack(w[q], v);
+          unpack(w.v[q], v);
 #pragma unroll
           for (int e = 0; e < VN; ++e) x[q * VN + e] = v[e];
         }
         g(x, body + i * VN);
         i += U * THREADS;
         if (!more) break;
-#pragma unroll
-        for (int q = 0; q < U; ++q) w[q] = next[q];
+        w = next;
       }
     }
     for (; i < vecs; i += THREADS) {
