@@ -12,6 +12,7 @@ namespace {
 
 constexpr int LP_THREADS = 512, LP_WAVES = LP_THREADS / 64;
 constexpr int LP_LIST = 1024;           // candidates kept for the top
+constexpr int64_t ROWS_OF_A_LAUNCH = 1 << 22;   // (2^32 threads are the most)
 constexpr float NEG_INF = -__builtin_inff();
 
 // Logits of more bytes than this are read, and their gradient written, without being kept in the last-level cache (256 MB), which they would
@@ -31,7 +32,7 @@ struct LpArgs {
   int32_t top, pieces;
   int64_t piece;      // columns of one (the last may have fewer)
   float4* part;       // [N, pieces] m, s, q
-  uint64_t* part_top; // [N, pieces, top]
+  uint64_t* part_top; // [N, top, pieces]
 };
 
 // A logit and its column as one number: larger values first, NaN above all, equal values by the lower column; never 0 or all ones.
@@ -88,11 +89,11 @@ __device__ __forceinline__ float largest(const float (&v)[n]) {
   return m;
 }
 
-// Columns [c0, c1) of a row in the thread's share: up to the first 16-byte boundary and from the last on one by one, 16 bytes at a
-// time in between.  f(values, first column, how many), columns of a thread ascending.
-template <typename T, bool STREAM>
+// Columns [c0, c1) of a row, shared out among THREADS threads: up to the first 16-byte boundary and from the last on one by one, 16 bytes
+// (a vector) at a time in between.
+template <typename T, int THREADS, bool STREAM>
 struct RowWalk {
-  static constexpr int VN = 16 / sizeof(T);
+  static constexpr int VN = 16 / sizeof(T), U = 2;
   const T* row;
   int64_t c0, c1, body, vecs;   // first whole vector's column, whole vectors
   __device__ __forceinline__ RowWalk(const T* row_, int64_t c0_, int64_t c1_) : row(row_), c0(c0_), c1(c1_) {
@@ -100,7 +101,7 @@ struct RowWalk {
     body = min(c1, c0 + (off ? VN - off : 0));
     vecs = (c1 - body) / VN;
   }
-  static __device__ __forceinline__ void unpack(const uint4& w, float (&v)[VN]) {
+  static __device__ __forceinline__ void unpack(const uint4& w, float* v) {
     const uint32_t u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
@@ -112,41 +113,19 @@ struct RowWalk {
       }
     }
   }
-  // f(values, first column, how many): columns of a thread ascending.
-  template <int THREADS, typename F>
-  __device__ __forceinline__ void each(int tid, F&& f) const {
-    batches<THREADS>(
-        tid,
-        [&](const float (&v)[U * VN], int64_t c) {
-#pragma unroll
-          for (int q = 0; q < U; ++q) {
-            float x[VN];
-#pragma unroll
-            for (int e = 0; e < VN; ++e) x[e] = v[q * VN + e];
-            f(x, c + (int64_t)q * THREADS * VN, VN);
-          }
-        },
-        f);
-  }
-  // The same, U vectors at a time where there are as many: g(values, first column), the vectors THREADS of them apart.
-  static constexpr int U = 2;
-  template <int THREADS, typename G, typename F>
-  __device__ __forceinline__ void batches(int tid, G&& g, F&& f) const {
-    float v[VN];
-    auto one = [&](int64_t c) {
-      v[0] = to_f32(row[c]);
-#pragma unroll
-      for (int e = 1; e < VN; ++e) v[e] = NEG_INF;
-      f(v, c, 1);
-    };
-    if (c0 + tid < body) one(c0 + tid);
+  // The thread's share, columns ascending: U vectors at a time, THREADS of them apart, to batch(words, first column) as long as there are as
+  // many, else vector(words, first column), single columns to one(value, column).
+  struct Words {
+    uint4 v[U];
+  };
+  template <typename B, typename V, typename O>
+  __device__ __forceinline__ void each(int tid, B&& batch, V&& vector, O&& one) const {
+    if (c0 + tid < body) one(to_f32(row[c0 + tid]), c0 + tid);
     const uint4* p = reinterpret_cast<const uint4*>(row + body);
     int64_t i = tid;
     constexpr int64_t LAST = (U - 1) * THREADS;
     if (i + LAST < vecs) {   // the next vectors are requested before these are worked on
-      struct {
-        uint4 v[U];
-      } w, next = {};
+      Words w, next = {};
 #pragma unroll
       for (int q = 0; q < U; ++q) w.v[q] = load16<STREAM>(p + i + q * THREADS);
       while (true) {
@@ -155,25 +134,36 @@ struct RowWalk {
 #pragma unroll
           for (int q = 0; q < U; ++q) next.v[q] = load16<STREAM>(p + i + (U + q) * THREADS);
         }
-        float x[U * VN];
-#pragma unroll
-        for (int q = 0; q < U; ++q) {
-          unpack(w.v[q], v);
-#pragma unroll
-          for (int e = 0; e < VN; ++e) x[q * VN + e] = v[e];
-        }
-        g(x, body + i * VN);
+        batch(w, body + i * VN);
         i += U * THREADS;
         if (!more) break;
         w = next;
       }
     }
-    for (; i < vecs; i += THREADS) {
-      unpack(p[i], v);
-      f(v, body + i * VN, VN);
+#pragma unroll 1
+    for (; i < vecs; i += THREADS) vector(p[i], body + i * VN);
+    const int64_t c = body + vecs * VN + tid;
+    if (c < c1) one(to_f32(row[c]), c);
+  }
+  // f(value, column) for the same share, in little code.
+  template <typename F>
+  __device__ __forceinline__ void again(int tid, F&& f) const {
+    if (c0 + tid < body) f(to_f32(row[c0 + tid]), c0 + tid);
+#pragma unroll 1
+    for (int64_t i = tid; i < vecs; i += THREADS) {
+      float v[VN];
+      unpack(reinterpret_cast<const uint4*>(row + body)[i], v);
+#pragma unroll
+      for (int e = 0; e < VN; ++e) f(v[e], body + i * VN + e);
     }
     const int64_t c = body + vecs * VN + tid;
-    if (c < c1) one(c);
+    if (c < c1) f(to_f32(row[c]), c);
+  }
+  // The same for another share, every THREADS-th column.
+  template <typename F>
+  __device__ __forceinline__ void each_column(int tid, F&& f) const {
+#pragma unroll 1
+    for (int64_t c = c0 + tid; c < c1; c += THREADS) f(to_f32(row[c]), c);
   }
 };
 
@@ -186,7 +176,7 @@ struct LpLds {
   uint64_t list[LP_LIST];
   uint64_t best[LP_WAVES * 64];
   uint64_t threshold;
-  int count;
+  int count, digit, above;
   float m[LP_WAVES], s[LP_WAVES], q[LP_WAVES];
 };
 
@@ -216,64 +206,119 @@ __device__ __forceinline__ Softmax block_softmax(LpLds& lds, Softmax x) {
   return x;
 }
 
-// The k largest keys, in order, to out(rank, key).  `mine`: the largest key of this thread's share; rescan(f) calls f(key) for every
-// key of the share.  The threads go into G >= k groups: the smallest of the groups' largest keys has k keys at or above it, and few more
-// (about G ln G of evenly spread ones); those are listed and ranked.  More than the list holds, or `exact`: the largest key below
-// the last one, k times over.  At least k keys exist.
+// A key with at least k of the block's keys at or above it, and at most `most` (>= k) if they differ: the digits of the k-th largest
+// from the highest on, until few enough remain.  each(f): f(key) for the thread's keys.
+template <typename Each>
+__device__ __forceinline__ uint64_t key_at_rank(LpLds& lds, int k, int most, Each&& each) {
+  const int tid = threadIdx.x, lane = tid & 63;
+  uint32_t* hist = reinterpret_cast<uint32_t*>(lds.best);   // [256]
+  uint64_t prefix = 0;
+  int kept = 0;   // keys above the prefix's
+  for (int shift = 56; shift >= 0; shift -= 8) {
+    __syncthreads();
+    if (tid < 256) hist[tid] = 0;
+    __syncthreads();
+    each([&](uint64_t key) {
+      if (key != 0 && (shift == 56 || (key >> (shift + 8)) == (prefix >> (shift + 8)))) atomicAdd(&hist[(key >> shift) & 255], 1u);
+    });
+    __syncthreads();
+    if (tid < 64) {   // digits 4 lane .. + 3; sums from the highest digit on
+      uint32_t c[4], mine = 0;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        c[q] = hist[4 * lane + q];
+        mine += c[q];
+      }
+      uint32_t up = mine;   // of this lane's digits and those above
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        const uint32_t other = __shfl_down(up, o, 64);
+        up += lane + o < 64 ? other : 0;
+      }
+      const uint32_t want = (uint32_t)(k - kept);
+      uint32_t run = up - mine;
+      if (run < want && up >= want) {   // (one lane; none if there are fewer keys than k)
+#pragma unroll
+        for (int q = 3; q >= 0; --q) {
+          if (run + c[q] >= want && run < want) {
+            lds.digit = 4 * lane + q;
+            lds.above = (int)run;
+            lds.count = (int)c[q];
+          }
+          run += c[q];
+        }
+      }
+      if (lane == 0 && up < want) {
+        lds.digit = 0; lds.above = (int)up; lds.count = 0;
+      }
+    }
+    __syncthreads();
+    prefix |= (uint64_t)lds.digit << shift;
+    kept += lds.above;
+    if (kept + lds.count <= most) break;
+  }
+  return prefix;
+}
+
+// The k largest keys, in order, to out(rank, key).  `mine`: the largest key of this thread's share; rescan(f, t) calls f(key) for every
+// key of the share that is at least t (and may for others).  The k-th largest of the threads' largest keys is a threshold that k keys reach, and few
+// more; up to FEW_TOP it is found by taking the largest away k - 1 times, above (roughly) digit by digit.  What reaches it is listed and
+// ranked; if that is more than the list holds, or `exact`, the threshold comes from all keys.  At least k keys exist.
+// (The threshold has to be close: a thread with a second key above it goes through its whole share again.  With the least of the largest
+// keys of 8 groups of threads, about 22 keys at k = 5, 4096 x 50000 bf16 took 182 us.)
+constexpr int FEW_TOP = 6;
 template <typename Rescan, typename Out>
 __device__ __forceinline__ void block_top(LpLds& lds, int k, uint64_t mine, bool exact, Rescan&& rescan, Out&& out) {
-  const int tid = threadIdx.x, lane = tid & 63, waves = blockDim.x >> 6;
-  int G = 8;
-  while (G < k) G <<= 1;   // k <= 64
-  uint64_t b = mine;
-  for (int o = G; o < 64; o <<= 1) b = max(b, shfl_xor64(b, o));
-  __syncthreads();         // (lds.best may still be read)
-  lds.best[tid] = b;       // lanes 0 .. G - 1 of every wavefront
-  if (tid == 0) lds.count = 0;
-  __syncthreads();
-  if (tid < 64) {
-    uint64_t t = ~0ull;
-    if (lane < G) {
-      t = 0;
-      for (int w = 0; w < waves; ++w) t = max(t, lds.best[w * 64 + lane]);
-    }
-    for (int o = 1; o < 64; o <<= 1) t = min(t, shfl_xor64(t, o));
-    if (tid == 0) lds.threshold = t;
-  }
-  __syncthreads();
-  const uint64_t threshold = lds.threshold;
-  if (!exact && mine != 0 && mine >= threshold)
-    rescan([&](uint64_t key) {
-      if (key >= threshold) {
-        const int at = atomicAdd(&lds.count, 1);   // (in any order: ranked below)
-        if (at < LP_LIST) lds.list[at] = key;
-      }
-    });
-  __syncthreads();
-  const int n = lds.count;
-  if (!exact && n <= LP_LIST) {
-    for (int i = tid; i < n; i += blockDim.x) {
-      const uint64_t key = lds.list[i];
-      int above = 0;
-      for (int j = 0; j < n; ++j) above += lds.list[j] > key;
-      if (above < k) out(above, key);
-    }
-    return;
-  }
-  uint64_t last = ~0ull;
+  const int tid = threadIdx.x, lane = tid & 63;
+  uint64_t threshold = 0;
+  if (k <= FEW_TOP) {
+    __syncthreads();         // (lds.best may still be read)
+    lds.best[tid] = mine;
+    __syncthreads();
+    if (tid < 64) {
+      uint64_t x[LP_WAVES], t = 0;
+#pragma unroll
+      for (int w = 0; w < LP_WAVES; ++w) x[w] = lds.best[w * 64 + lane];
 #pragma unroll 1
-  for (int r = 0; r < k; ++r) {
-    uint64_t t = 0;
-    rescan([&](uint64_t key) {
-      if (key < last) t = max(t, key);
-    });
-    for (int o = 1; o < 64; o <<= 1) t = max(t, shfl_xor64(t, o));
+      for (int r = 0; r < k; ++r) {
+        t = 0;
+#pragma unroll
+        for (int w = 0; w < LP_WAVES; ++w) t = max(t, x[w]);
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) t = max(t, shfl_xor64(t, o));
+#pragma unroll
+        for (int w = 0; w < LP_WAVES; ++w) x[w] = x[w] == t ? 0 : x[w];
+      }
+      if (tid == 0) lds.threshold = t;
+    }
     __syncthreads();
-    if (lane == 0) lds.best[tid >> 6] = t;
+    threshold = lds.threshold;
+  } else if (!exact) {
+    threshold = key_at_rank(lds, k, k + k / 4, [&](auto&& f) { f(mine); });
+  }
+  for (bool all = exact;; all = true) {
+    if (all) threshold = key_at_rank(lds, k, LP_LIST, [&](auto&& f) { rescan(f, (uint64_t)0); });
     __syncthreads();
-    for (int w = 0; w < waves; ++w) t = max(t, lds.best[w]);
-    if (tid == 0) out(r, t);
-    last = t;
+    if (tid == 0) lds.count = 0;
+    __syncthreads();
+    if (mine >= threshold || all)
+      rescan(
+          [&](uint64_t key) {
+            if (key != 0 && key >= threshold) {
+              const int at = atomicAdd(&lds.count, 1);   // (in any order: ranked below)
+              if (at < LP_LIST) lds.list[at] = key;
+            }
+          },
+          all ? (uint64_t)0 : threshold);
+    __syncthreads();
+    if (all || lds.count <= LP_LIST) break;
+  }
+  const int n = min(lds.count, LP_LIST);
+  for (int i = tid; i < n; i += blockDim.x) {
+    const uint64_t key = lds.list[i];
+    int above = 0;
+    for (int j = 0; j < n; ++j) above += lds.list[j] > key;
+    if (above < k) out(above, key);
   }
 }
 
@@ -296,67 +341,92 @@ __device__ __forceinline__ void write_logp(const LpArgs& a, int64_t row, const S
 
 // A block per row, or per piece of one: its sums and top then go to memory for lp_join_kernel.
 template <typename T, bool TOP, bool STREAM>
-__global__ __launch_bounds__(LP_THREADS) void lp_kernel(LpArgs a) {
+__global__ __launch_bounds__(LP_THREADS, 6) void lp_kernel(LpArgs a) {
   __shared__ LpLds lds;
   const int64_t row = a.pieces == 1 ? blockIdx.x : blockIdx.x / (unsigned)a.pieces;
   const int piece = (int)(blockIdx.x - row * a.pieces), tid = threadIdx.x;
-  typedef RowWalk<T, STREAM> W;
+  typedef RowWalk<T, LP_THREADS, STREAM> W;
   const W walk(reinterpret_cast<const T*>(a.x) + row * a.ld, piece * a.piece, min((piece + 1) * a.piece, a.V));
-  constexpr int VN = W::VN;
+  constexpr int VN = W::VN, U = W::U;
   Softmax t;
-  int64_t best = 0;   // column of the thread's first largest logit
-  bool any = false;
-  walk.template batches<LP_THREADS>(
+  // of the thread: the group of logits that holds its first largest one, kept in LDS (a single one at the front), and the largest of the
+  // other groups' largest
+  __shared__ uint4 held[TOP ? U : 1][TOP ? LP_THREADS : 1];
+  int64_t group = 0;
+  int held_n = 0;   // logits in it
+  float second = NEG_INF;
+  auto note = [&](float vm, int64_t c, int n, auto&& words) {
+    if (vm > t.m || (TOP && held_n == 0)) {
+      if (TOP) {
+        second = t.m;
+        words();
+        group = c;
+        held_n = n;
+      }
+      t.rescale(fmaxf(vm, t.m));
+    } else if (TOP) {
+      second = fmaxf(second, vm);
+    }
+  };
+  walk.each(
       tid,
-      [&](const float (&v)[W::U * VN], int64_t c) {
-        const float vm = largest(v);
-        if (vm > t.m || (TOP && !any)) {
-          if (TOP) {
-            best = c;
+      [&](const typename W::Words& w, int64_t c) {
+        float v[U * VN];
 #pragma unroll
-            for (int e = W::U * VN - 1; e >= 0; --e)
-              if (v[e] == vm) best = c + (int64_t)(e / VN) * (LP_THREADS * VN) + e % VN;
-            any = true;
-          }
-          t.rescale(fmaxf(vm, t.m));
-        }
+        for (int q = 0; q < U; ++q) W::unpack(w.v[q], v + q * VN);
+        note(largest(v), c, U * VN, [&] {
+#pragma unroll
+          for (int q = 0; q < U; ++q) held[q][tid] = w.v[q];
+        });
         t.add_all(v);
       },
-      [&](const float (&v)[VN], int64_t c, int n) {
-        const float vm = largest(v);
-        if (vm > t.m || (TOP && !any)) {
-          if (TOP) {
-            best = c;
-#pragma unroll
-            for (int e = VN - 1; e >= 0; --e)
-              if (e < n && v[e] == vm) best = c + e;
-            any = true;
-          }
-          t.rescale(fmaxf(vm, t.m));
-        }
-        if (n == VN) t.add_all(v);
-        else t.template add<false>(v[0]);
+      [&](const uint4& w, int64_t c) {
+        float v[VN];
+        W::unpack(w, v);
+        note(largest(v), c, VN, [&] { held[0][tid] = w; });
+        t.add_all(v);
+      },
+      [&](float x, int64_t c) {
+        note(x, c, 1, [&] { *reinterpret_cast<T*>(&held[0][tid]) = from_f32<T>(x); });
+        t.template add<false>(x);
       });
-  const float mine = t.m;
+  const float top_value = t.m;
   t = block_softmax(lds, t);
   const float log_s = logf(t.s);
   if constexpr (TOP) {
-    const int64_t at = (row * a.pieces + piece) * a.top;
+    // the group held, value by value: f(value, which)
+    auto each_held = [&](auto&& f) {
+#pragma unroll 1
+      for (int i = 0; i < held_n; ++i) f(to_f32(reinterpret_cast<const T*>(&held[i / VN][tid])[i % VN]), i);
+    };
+    auto held_column = [&](int i) { return (uint32_t)(group + (int64_t)(i / VN) * (LP_THREADS * VN) + i % VN); };
+    int first = U * VN;
+    each_held([&](float x, int i) { first = x == top_value ? min(first, i) : first; });
+    const uint64_t mine = held_n ? rank_key(top_value, held_column(first)) : 0;   // (of a row with a NaN any number: not asked for)
     block_top(
-        lds, a.top, any ? rank_key(mine, (uint32_t)best) : 0, t.s != t.s,
-        [&](auto&& f) {
-          walk.template each<LP_THREADS>(tid, [&](const float (&v)[VN], int64_t c, int n) {
-#pragma unroll
-            for (int e = 0; e < VN; ++e)
-              if (e < n) f(rank_key(v[e], (uint32_t)(c + e)));
-          });
+        lds, a.top, mine, t.s != t.s,
+        [&](auto&& f, uint64_t least) {
+          if (least == 0) {
+            walk.each_column(tid, [&](float x, int64_t c) { f(rank_key(x, (uint32_t)c)); });
+            return;
+          }
+          const float at_least = key_value(least);
+          if (rank_key(second, 0) < least) {   // none reaches it in the other groups
+            each_held([&](float x, int i) {
+              if (x >= at_least) f(rank_key(x, held_column(i)));
+            });
+          } else {
+            walk.again(tid, [&](float x, int64_t c) {
+              if (x >= at_least) f(rank_key(x, (uint32_t)c));
+            });
+          }
         },
         [&](int r, uint64_t key) {
-          if (a.pieces > 1) {
-            a.part_top[at + r] = key;
+          if (a.pieces > 1) {   // (rank by rank: neighbours are of other pieces, so that every group of lp_join_kernel has a large one)
+            a.part_top[(row * a.top + r) * a.pieces + piece] = key;
           } else {
-            a.top_logp[at + r] = log_prob(t, log_s, key_value(key));
-            a.top_index[at + r] = key_column(key);
+            a.top_logp[row * a.top + r] = log_prob(t, log_s, key_value(key));
+            a.top_index[row * a.top + r] = key_column(key);
           }
         });
   }
@@ -396,7 +466,7 @@ __global__ __launch_bounds__(LP_THREADS) void lp_join_kernel(LpArgs a) {
     for (int i = tid; i < n; i += LP_THREADS) mine = max(mine, keys[i]);
     block_top(
         lds, a.top, mine, false,
-        [&](auto&& f) {
+        [&](auto&& f, uint64_t) {
           for (int i = tid; i < n; i += LP_THREADS) f(keys[i]);
         },
         [&](int r, uint64_t key) {
@@ -452,19 +522,24 @@ __global__ __launch_bounds__(LG_THREADS) void lp_grad_kernel(LpGradArgs a) {
       if (gb != 0.0f) g -= p == 0.0f ? 0.0f : gb * p * (lp + st.z);
       return none ? 0.0f : g;
     };
-    const RowWalk<T, false> walk(reinterpret_cast<const T*>(a.x) + row * a.ld, c0, c1);
+    typedef RowWalk<T, LG_THREADS, false> W;
+    const W walk(reinterpret_cast<const T*>(a.x) + row * a.ld, c0, c1);
     if constexpr (SAME) {
-      walk.template each<LG_THREADS>(threadIdx.x, [&](const float (&v)[VN], int64_t c, int n) {
-        if (n == 1) {
-          out[c] = from_f32<T>(grad(v[0], c));
-        } else {
-          float g[VN];
+      auto vector = [&](const uint4& w, int64_t c) {
+        float g[VN];
+        W::unpack(w, g);
 #pragma unroll
-          for (int e = 0; e < VN; ++e) g[e] = grad(v[e], c + e);
-          if constexpr (VN == 4) store16<STREAM>(out + c, bits4(g[0], g[1], g[2], g[3]));
-          else store16<STREAM>(out + c, make_uint4(f2bf2(g[0], g[1]), f2bf2(g[2], g[3]), f2bf2(g[4], g[5]), f2bf2(g[6], g[7])));
-        }
-      });
+        for (int e = 0; e < VN; ++e) g[e] = grad(g[e], c + e);
+        if constexpr (VN == 4) store16<STREAM>(out + c, bits4(g[0], g[1], g[2], g[3]));
+        else store16<STREAM>(out + c, make_uint4(f2bf2(g[0], g[1]), f2bf2(g[2], g[3]), f2bf2(g[4], g[5]), f2bf2(g[6], g[7])));
+      };
+      walk.each(
+          threadIdx.x,
+          [&](const typename W::Words& w, int64_t c) {
+#pragma unroll
+            for (int q = 0; q < W::U; ++q) vector(w.v[q], c + (int64_t)q * (LG_THREADS * VN));
+          },
+          vector, [&](float x, int64_t c) { out[c] = from_f32<T>(grad(x, c)); });
     } else {
       for (int64_t c = c0 + threadIdx.x; c < c1; c += LG_THREADS) out[c] = from_f32<T>(grad(to_f32(walk.row[c]), c));
     }
@@ -520,20 +595,29 @@ int antdt_token_logprobs(const void* logits, int64_t ld, int64_t N, int64_t V, i
     a.part_top = reinterpret_cast<uint64_t*>(a.part + N * a.pieces);
   }
   const hipStream_t s = (hipStream_t)stream;
-  const dim3 grid((unsigned)(N * a.pieces));
   const bool far = N * V * op_size(dtype) > STREAM_BYTES;
-  auto go = [&](auto t, auto with_top) {
+  auto go = [&](auto t, auto with_top, const LpArgs& rows) {
     typedef decltype(t) T;
     constexpr bool TOP = decltype(with_top)::value;
-    if (far) hipLaunchKernelGGL((lp_kernel<T, TOP, true>), grid, dim3(LP_THREADS), 0, s, a);
-    else hipLaunchKernelGGL((lp_kernel<T, TOP, false>), grid, dim3(LP_THREADS), 0, s, a);
+    const dim3 grid((unsigned)(rows.N * rows.pieces));
+    if (far) hipLaunchKernelGGL((lp_kernel<T, TOP, true>), grid, dim3(LP_THREADS), 0, s, rows);
+    else hipLaunchKernelGGL((lp_kernel<T, TOP, false>), grid, dim3(LP_THREADS), 0, s, rows);
   };
-  auto typed = [&](auto t) {
-    if (top) go(t, std::true_type());
-    else go(t, std::false_type());
+  auto typed = [&](auto t, const LpArgs& rows) {
+    if (top) go(t, std::true_type(), rows);
+    else go(t, std::false_type(), rows);
   };
-  if (dtype == ANTDT_F32) typed(0.0f);
-  else typed((bf16_t)0);
+  for (int64_t r = 0; r < N; r += ROWS_OF_A_LAUNCH) {
+    LpArgs rows = a;
+    rows.N = std::min(ROWS_OF_A_LAUNCH, N - r);
+    rows.x = reinterpret_cast<const char*>(a.x) + r * ld * op_size(dtype);
+    if (logp) { rows.tokens += r; rows.logp += r; }
+    if (entropy) rows.entropy += r;
+    if (stats) rows.stats += r;
+    if (top) { rows.top_logp += r * top; rows.top_index += r * top; }
+    if (dtype == ANTDT_F32) typed(0.0f, rows);
+    else typed((bf16_t)0, rows);
+  }
   OP_TRY(op_hip(call, hipGetLastError()));
   if (a.pieces > 1) {
     if (dtype == ANTDT_F32) hipLaunchKernelGGL(lp_join_kernel<float>, dim3((unsigned)N), dim3(LP_THREADS), 0, s, a);

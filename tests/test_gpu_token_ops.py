@@ -357,6 +357,19 @@ def test_top_of_equal_and_of_unevenly_spread_logits(dtype, V):
     assert np.array_equal(host(r.top_index).astype(np.int64), f["top_index"])
 
 
+@pytest.mark.parametrize("top", [1, 6, 7, 16, 17, 32, 64])
+@pytest.mark.parametrize("N,V", [(2, 64), (3, 3001), (1, 40000), (513, 70)])
+def test_how_many_of_the_top(N, V, top):
+    """Every way to find the threshold, over one block and over pieces, with logits that differ and with many that do not."""
+    rng = np.random.default_rng(V + top)
+    x = np.concatenate([rng.normal(size=(N, V)), np.round(rng.normal(size=(N, V)))])
+    x[-1, : V // 2] = -np.inf
+    dx = strided(x, "f32", 1, 0)
+    r = A.token_logprobs(dx, None, top)
+    f = F.logprobs(host(dx), np.zeros(2 * N, np.int64), top)
+    assert np.array_equal(host(r.top_index).astype(np.int64), f["top_index"])
+
+
 @pytest.mark.parametrize("V", [300, 40000])
 def test_logprobs_of_rows_with_what_is_not_finite(V):
     x = torch.randn(4, V, device=DEV)
@@ -436,6 +449,22 @@ def test_operators_on_another_stream_and_in_a_graph():
         assert all(torch.equal(x, y) for x, y in zip(outs, w))
         assert torch.equal(step()[0], w[0])                    # eager work between the replays
         torch.cuda.synchronize()
+
+
+def test_next_item_example_learns():
+    """examples/next_item.py: the operators in one training step, and the answer to a single user."""
+    import importlib.util
+    import os
+    at = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "next_item.py")
+    spec = importlib.util.spec_from_file_location("next_item", at)
+    m = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(m)
+    model, loss = m.train(steps=60, items=200, width=64, hidden=256, n=2048)
+    assert loss[0] > 4 and loss[-1] < 0.5 * loss[0], (loss[0], loss[-1])
+    again = m.train(steps=3, items=200, width=64, hidden=256, n=2048)[1]
+    assert again[0] == loss[0]
+    items, p = model.answer(5, top=3)
+    assert len(items) == 3 and p[0] >= p[1] >= p[2] > 0 and sum(p) <= 1 + 1e-4
 
 
 def test_refusals_of_tensors():
