@@ -164,7 +164,7 @@ __device__ __forceinline__ void tile_block(const typename Op::Args& a, const Spl
   }
 }
 // 32 rows of a wavefront's tile by one wavefront (few tiles are in parts, but each is as much to read as many results).
-constexpr int JOIN_WAVES = 4;
+constexpr int JOIN_WAVES = 2;
 template <typename P>
 constexpr int join_units() { return P::WAVES * P::TM_; }   // of a tile
 template <typename Op>

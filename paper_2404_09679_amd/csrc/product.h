@@ -141,6 +141,8 @@ struct TileProduct {
     const int64_t step_a = (A_STRIDED ? a.ld * BK : BK) * (int64_t)sizeof(T), step_b = (B_STRIDED ? b[0].ld * BK : BK) * (int64_t)sizeof(T);
     const int nk = len > 0 ? (len + BK - 1) / BK : 0;
 
+    constexpr int PER_STAGE = VA + NB * VB, Q = BK / STEP;
+    static_assert(Q % 2 == 0, "the fragments' two buffers in turn, over the stages too");
     int left = len;
     uint32_t fill = lds0;
     auto issue = [&]() {
@@ -166,32 +168,48 @@ struct TileProduct {
       left -= BK;
       fill = fill == lds0 + (STAGES - 1) * STAGE_BYTES ? lds0 : fill + STAGE_BYTES;
     };
-    constexpr int PER_STAGE = VA + NB * VB;
+    constexpr int LDS_READS_DONE = 0xC07F;   // lgkmcnt(0) alone
+    typename TA::Fragment af[2][TM];
+    typename TB::Fragment bf[2][NB][TN];
+    auto fetch = [&](const char* la, int q, int to) {
+      const char* lb = la + TA::BYTES;
 #pragma unroll
-    for (int t = 0; t < STAGES - 1; ++t)
-      if (t < nk) issue();
-    uint32_t read = 0;
-    for (int t = 0; t < nk; ++t) {
+      for (int i = 0; i < TM; ++i) af[to][i] = TA::fragment(la, (wr * TM + i) * 32, q * STEP, lane);
+#pragma unroll
+      for (int s = 0; s < NB; ++s)
+#pragma unroll
+        for (int j = 0; j < TN; ++j) bf[to][s][j] = TB::fragment(lb + s * TB::BYTES, (wc * TN + j) * 32, q * STEP, lane);
+    };
+    // Stage t is in LDS, and everybody's fragments of the stage before have been read.
+    auto arrived = [&](int t) {
       if (t + STAGES - 2 < nk) wait_loads<(STAGES - 2) * PER_STAGE>();
       else wait_loads<0>();
       block_barrier();
-      const char* la = lds + read;
-      const char* lb = la + TA::BYTES;
-      constexpr int Q = BK / STEP;
-      typename TA::Fragment af[2][TM];
-      typename TB::Fragment bf[2][NB][TN];
-      auto fetch = [&](int q, int to) {
+    };
 #pragma unroll
-        for (int i = 0; i < TM; ++i) af[to][i] = TA::fragment(la, (wr * TM + i) * 32, q * STEP, lane);
-#pragma unroll
-        for (int s = 0; s < NB; ++s)
-#pragma unroll
-          for (int j = 0; j < TN; ++j) bf[to][s][j] = TB::fragment(lb + s * TB::BYTES, (wc * TN + j) * 32, q * STEP, lane);
-      };
-      fetch(0, 0);
+    for (int t = 0; t < STAGES - 1; ++t)
+      if (t < nk) issue();
+    if (nk == 0) return;
+    arrived(0);
+    fetch(lds, 0, 0);
+    // (the last buffer is free from the start)
+    if (left > 0) issue();
+    uint32_t read = 0;
+    for (int t = 0; t < nk; ++t) {
 #pragma unroll
       for (int q = 0; q < Q; ++q) {
-        if (q + 1 < Q) fetch(q + 1, (q + 1) & 1);
+        if (q + 1 < Q) {
+          fetch(lds + read, q + 1, (q + 1) & 1);
+        } else {
+          // (said so that the compiler knows: else it waits for the fragments requested below before the multiplications)
+          __builtin_amdgcn_s_waitcnt(LDS_READS_DONE);
+          __builtin_amdgcn_sched_barrier(0);
+          if (t + 1 < nk) {
+          read = read == (STAGES - 1) * STAGE_BYTES ? 0 : read + STAGE_BYTES;
+          arrived(t + 1);
+          fetch(lds + read, 0, 0);
+          }
+        }
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int i = 0; i < TM; ++i)
@@ -200,9 +218,8 @@ struct TileProduct {
 #pragma unroll
             for (int j = 0; j < TN; ++j) TA::multiply(af[q & 1][i], bf[q & 1][s][j], acc[s][i][j]);
         __builtin_amdgcn_sched_barrier(0);
-        if (q == 0 && left > 0) issue();
+        if (q + 1 == Q && left > 0) issue();
       }
-      read = read == (STAGES - 1) * STAGE_BYTES ? 0 : read + STAGE_BYTES;
     }
     block_barrier();
   }
