@@ -332,12 +332,21 @@ __device__ __forceinline__ void write_row_stats(const LpArgs& a, int64_t row, co
 __device__ __forceinline__ float log_prob(const Softmax& t, float log_s, float x) {
   return t.m == NEG_INF && t.s == 0.0f ? NEG_INF : (x - Softmax::base(t.m)) - log_s;
 }
-template <typename T>
-__device__ __forceinline__ void write_logp(const LpArgs& a, int64_t row, const Softmax& t, float log_s) {
-  if (!a.logp) return;
-  const int64_t tok = a.tokens[row];
-  a.logp[row] = tok >= 0 && tok < a.V ? log_prob(t, log_s, to_f32(reinterpret_cast<const T*>(a.x)[row * a.ld + tok])) : 0.0f;
-}
+// The logit of the row's given token (asked for at the start: two loads behind each other).
+struct Given {
+  bool there = false;
+  float x = 0.0f;
+  template <typename T>
+  __device__ __forceinline__ void load(const LpArgs& a, const T* x_row, int64_t row) {
+    if (!a.logp) return;
+    const int64_t tok = a.tokens[row];
+    there = tok >= 0 && tok < a.V;
+    if (there) x = to_f32(x_row[tok]);
+  }
+  __device__ __forceinline__ void write(const LpArgs& a, int64_t row, const Softmax& t, float log_s) const {
+    if (a.logp) a.logp[row] = there ? log_prob(t, log_s, x) : 0.0f;
+  }
+};
 
 // A block per row, or per piece of one: its sums and top then go to memory for lp_join_kernel.
 template <typename T, bool TOP, bool STREAM>
@@ -347,6 +356,8 @@ __global__ __launch_bounds__(LP_THREADS, 6) void lp_kernel(LpArgs a) {
   const int piece = (int)(blockIdx.x - row * a.pieces), tid = threadIdx.x;
   typedef RowWalk<T, LP_THREADS, STREAM> W;
   const W walk(reinterpret_cast<const T*>(a.x) + row * a.ld, piece * a.piece, min((piece + 1) * a.piece, a.V));
+  Given given;
+  if (tid == 0 && a.pieces == 1) given.load(a, walk.row, row);
   constexpr int VN = W::VN, U = W::U;
   Softmax t;
   // of the thread: the group of logits that holds its first largest one, kept in LDS (a single one at the front), and the largest of the
@@ -435,55 +446,60 @@ __global__ __launch_bounds__(LP_THREADS, 6) void lp_kernel(LpArgs a) {
       a.part[blockIdx.x] = make_float4(t.m, t.s, t.q, 0.0f);
     } else {
       write_row_stats(a, row, t, log_s);
-      write_logp<T>(a, row, t, log_s);
+      given.write(a, row, t, log_s);
     }
   }
 }
 
 // The pieces of a row put together: a block per row.
-constexpr int JOIN_KEYS = 4096;   // pieces * top at most
+constexpr int JOIN_KEYS = 4096, JOIN_PIECES = LP_THREADS;   // pieces * top, pieces at most
 template <typename T>
 __global__ __launch_bounds__(LP_THREADS) void lp_join_kernel(LpArgs a) {
   __shared__ LpLds lds;
   const int64_t row = blockIdx.x;
   const int tid = threadIdx.x;
+  // (everything is asked for first: the block's time is that of its loads behind each other)
+  Given given;
+  if (tid == 0) given.load(a, reinterpret_cast<const T*>(a.x) + row * a.ld, row);
+  const int n = a.pieces * a.top;
+  uint64_t key[JOIN_KEYS / LP_THREADS];
+#pragma unroll
+  for (int i = 0; i < JOIN_KEYS / LP_THREADS; ++i) {
+    const int at = tid + i * LP_THREADS;
+    key[i] = at < n ? a.part_top[row * n + at] : 0;
+  }
   Softmax t;
-  for (int p = tid; p < a.pieces; p += LP_THREADS) {
-    const float4 v = a.part[row * a.pieces + p];
-    Softmax o;
-    o.m = v.x; o.s = v.y; o.q = v.z;
-    const float m = fmaxf(t.m, o.m);
-    t.rescale(m);
-    o.rescale(m);
-    t.s += o.s; t.q += o.q;
+  if (tid < a.pieces) {
+    const float4 v = a.part[row * a.pieces + tid];
+    t.m = v.x; t.s = v.y; t.q = v.z;
   }
   t = block_softmax(lds, t);
   const float log_s = logf(t.s);
   if (a.top > 0) {
-    const uint64_t* keys = a.part_top + row * a.pieces * a.top;
-    const int n = a.pieces * a.top;
     uint64_t mine = 0;
-    for (int i = tid; i < n; i += LP_THREADS) mine = max(mine, keys[i]);
+#pragma unroll
+    for (uint64_t k : key) mine = max(mine, k);
     block_top(
         lds, a.top, mine, false,
         [&](auto&& f, uint64_t) {
-          for (int i = tid; i < n; i += LP_THREADS) f(keys[i]);
+#pragma unroll
+          for (uint64_t k : key) f(k);
         },
-        [&](int r, uint64_t key) {
-          a.top_logp[row * a.top + r] = log_prob(t, log_s, key_value(key));
-          a.top_index[row * a.top + r] = key_column(key);
+        [&](int r, uint64_t k) {
+          a.top_logp[row * a.top + r] = log_prob(t, log_s, key_value(k));
+          a.top_index[row * a.top + r] = key_column(k);
         });
   }
   if (tid == 0) {
     write_row_stats(a, row, t, log_s);
-    write_logp<T>(a, row, t, log_s);
+    given.write(a, row, t, log_s);
   }
 }
 
 // Pieces of a row: with fewer rows than the chip holds blocks, until they fill it, but no shorter than a block's threads have
 // two vectors each to read.
 int lp_pieces(int64_t N, int64_t V, int32_t top) {
-  int64_t p = std::min(512 / std::max<int64_t>(N, 1), V / 4096);
+  int64_t p = std::min(JOIN_PIECES / std::max<int64_t>(N, 1), V / 4096);
   if (top > 0) p = std::min<int64_t>(p, JOIN_KEYS / top);
   return (int)std::max<int64_t>(p, 1);
 }
@@ -641,7 +657,10 @@ int antdt_token_logprobs_gradient(const void* logits, int64_t ld, int64_t N, int
   LpGradArgs a = {};
   a.x = logits; a.dx = d_logits; a.ld = ld; a.ldd = ldd; a.N = N; a.V = V; a.tokens = tokens;
   a.stats = reinterpret_cast<const float4*>(stats); a.d_logp = d_logp; a.d_entropy = d_entropy;
-  a.piece = 8192; a.pieces = div_up(V, a.piece);
+  // (fewer columns a block where that leaves compute units idle)
+  a.piece = 8192;
+  while (a.piece > 2048 && N * div_up(V, a.piece) < 2048) a.piece /= 2;
+  a.pieces = div_up(V, a.piece);
   const int64_t size = op_size(dtype);
   const bool same = ((reinterpret_cast<uintptr_t>(logits) ^ reinterpret_cast<uintptr_t>(d_logits)) & 15) == 0 && ((ld - ldd) * size) % 16 == 0;
   const dim3 grid((unsigned)std::min<int64_t>(N * a.pieces, 1 << 20));

@@ -223,18 +223,27 @@ def token_logprobs(logits: torch.Tensor, tokens: Optional[torch.Tensor] = None, 
     """Log probabilities of `tokens` under softmax(logits), the rows' entropies and their `top` largest log
     probabilities with their columns."""
     N, V, ld, dev = _matrix(logits, "logits")
-    ws, n = _workspace(workspace, _bytes("antdt_token_logprobs_bytes", N, V, top), logits)
-    f32 = torch.float32
-    stats, entropy = _new((N, 4), f32, logits), _new((N,), f32, logits)
-    tp = logp = lp = top_logp = top_index = tl = ti = None
-    if tokens is not None:
-        tp, logp = _vector(tokens, "tokens", N, torch.int32, dev), _new((N,), f32, logits)
-        lp = logp.data_ptr()
-    if top:
-        top_logp, top_index = _new((N, top), f32, logits), _new((N, top), torch.int32, logits)
-        tl, ti = top_logp.data_ptr(), top_index.data_ptr()
-    _check(lib.antdt_token_logprobs(logits.data_ptr(), ld, N, V, _DTYPES[logits.dtype], tp, lp, entropy.data_ptr(),
-                                    stats.data_ptr(), top, tl, ti, ws, n, _stream()))
+    n = _bytes("antdt_token_logprobs_bytes", N, V, top)
+    f32, given, k = torch.float32, tokens is not None, top if top > 0 else 0
+    tp = _vector(tokens, "tokens", N, torch.int32, dev) if given else None
+    # One block of memory for all results and, behind them, the workspace: an allocation costs as much as two views.
+    words = [4 * N, N, N if given else 0, k * N, k * N]
+    front = (sum(words) + 63) // 64 * 64
+    own = workspace is None
+    buf = _new((front + (n // 4 if own else 0),), f32, logits)
+    ws, n = (buf.data_ptr() + 4 * front, n) if own else _workspace(workspace, n, logits)
+    stats, entropy, logp, top_logp, top_index, _ = torch.unsafe_split_with_sizes(buf, words + [buf.shape[0] - sum(words)])
+    at = buf.data_ptr()
+    sp, ep, lp = at, at + 16 * N, at + 20 * N
+    tl = at + 4 * (words[0] + words[1] + words[2])
+    ti = tl + 4 * k * N
+    stats, logp = stats.view(N, 4), logp if given else None
+    if k:
+        top_logp, top_index = top_logp.view(N, k), top_index.view(torch.int32).view(N, k)
+    else:
+        top_logp = top_index = None
+    _check(lib.antdt_token_logprobs(logits.data_ptr(), ld, N, V, _DTYPES[logits.dtype], tp, lp if given else None, ep, sp, top,
+                                    tl, ti, ws, n, _stream()))
     return LogProbs(logp, entropy, stats, top_logp, top_index)
 
 
