@@ -35,12 +35,13 @@ struct LpArgs {
   uint64_t* part_top; // [N, top, pieces]
 };
 
-// A logit and its column as one number: larger values first, NaN above all, equal values by the lower column; never 0 or all ones.
-__device__ __forceinline__ uint64_t rank_key(float x, uint32_t col) {
+// A logit as a whole number: larger values first, NaN above all, equal values equal; never 0 or all ones.  And with its column, equal values by
+// the lower one.
+__device__ __forceinline__ uint32_t value_order(float x) {
   const uint32_t u = __float_as_uint(x == 0.0f ? 0.0f : x);
-  const uint32_t o = x != x ? 0xFFFFFFF0u : (u >> 31) ? ~u : u | 0x80000000u;
-  return (uint64_t)o << 32 | (uint32_t)~col;
+  return x != x ? 0xFFFFFFF0u : (u >> 31) ? ~u : u | 0x80000000u;
 }
+__device__ __forceinline__ uint64_t rank_key(float x, uint32_t col) { return (uint64_t)value_order(x) << 32 | (uint32_t)~col; }
 __device__ __forceinline__ float key_value(uint64_t k) {
   const uint32_t o = (uint32_t)(k >> 32);
   return __uint_as_float((o >> 31) ? o & 0x7FFFFFFFu : ~o);   // (NaN stays one)
@@ -167,14 +168,36 @@ struct RowWalk {
   }
 };
 
-__device__ __forceinline__ uint64_t shfl_xor64(uint64_t x, int o) {
-  const uint32_t lo = __shfl_xor((uint32_t)x, o, 64), hi = __shfl_xor((uint32_t)(x >> 32), o, 64);
-  return (uint64_t)hi << 32 | lo;
+// Over the 64 lanes, by DPP (exchanges through LDS took twice the block's whole sum): what all lanes then hold.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t dpp(uint32_t old, uint32_t x) {
+  return (uint32_t)__builtin_amdgcn_update_dpp((int)old, (int)x, CTRL, ROWS, 0xF, false);
+}
+template <typename Op>
+__device__ __forceinline__ uint32_t wave_reduce(uint32_t x, uint32_t none, Op&& op) {
+  x = op(x, dpp<0x111, 0xF>(none, x));   // rows of 16 lanes: one lane down, ...
+  x = op(x, dpp<0x112, 0xF>(none, x));
+  x = op(x, dpp<0x114, 0xF>(none, x));
+  x = op(x, dpp<0x118, 0xF>(none, x));   // ... eight
+  x = op(x, dpp<0x142, 0xA>(none, x));   // last lane of a row to the next row (rows 1 and 3)
+  x = op(x, dpp<0x143, 0xC>(none, x));   // lane 31 to rows 2 and 3
+  return (uint32_t)__builtin_amdgcn_readlane((int)x, 63);
+}
+__device__ __forceinline__ float wave_max(float x) {
+  return __uint_as_float(wave_reduce(__float_as_uint(x), __float_as_uint(NEG_INF), [](uint32_t a, uint32_t b) {
+    return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b)));
+  }));
+}
+__device__ __forceinline__ float wave_sum(float x) {
+  return __uint_as_float(wave_reduce(__float_as_uint(x), 0u, [](uint32_t a, uint32_t b) { return __float_as_uint(__uint_as_float(a) + __uint_as_float(b)); }));
+}
+__device__ __forceinline__ uint32_t wave_max(uint32_t x) {
+  return wave_reduce(x, 0u, [](uint32_t a, uint32_t b) { return max(a, b); });
 }
 
 struct LpLds {
   uint64_t list[LP_LIST];
-  uint64_t best[LP_WAVES * 64];
+  uint32_t best[LP_THREADS], column[LP_THREADS];
   uint64_t threshold;
   int count, digit, above;
   float m[LP_WAVES], s[LP_WAVES], q[LP_WAVES];
@@ -183,18 +206,13 @@ struct LpLds {
 // The block's sums from its threads': the largest logit first, then every thread's sums relative to it, added up.
 __device__ __forceinline__ Softmax block_softmax(LpLds& lds, Softmax x) {
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, waves = blockDim.x >> 6;
-  float m = x.m;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+  float m = wave_max(x.m);
   if (lane == 0) lds.m[w] = m;
   __syncthreads();
   for (int i = 0; i < waves; ++i) m = fmaxf(m, lds.m[i]);
   x.rescale(m);
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    x.s += __shfl_xor(x.s, o, 64);
-    x.q += __shfl_xor(x.q, o, 64);
-  }
+  x.s = wave_sum(x.s);
+  x.q = wave_sum(x.q);
   if (lane == 0) {
     lds.s[w] = x.s; lds.q[w] = x.q;
   }
@@ -206,12 +224,47 @@ __device__ __forceinline__ Softmax block_softmax(LpLds& lds, Softmax x) {
   return x;
 }
 
+// The 256 counters of digits, turned into the digit (counted from `last` on downwards) at which `want` keys are reached: lds.digit, how many
+// are in the digits before it (lds.above) and in it (lds.count; 0 if there are not as many keys).  By the first wavefront.
+__device__ __forceinline__ void digit_at_rank(LpLds& lds, const uint32_t* hist, uint32_t want, bool ascending) {
+  const int lane = threadIdx.x & 63;
+  uint32_t c[4], mine = 0;   // digits 4 lane .. + 3, in the order asked for
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const int at = 4 * lane + q;
+    c[q] = hist[ascending ? at : 255 - at];
+    mine += c[q];
+  }
+  uint32_t up = mine;   // of this lane's digits and those before
+  up += dpp<0x111, 0xF>(0, up);
+  up += dpp<0x112, 0xF>(0, up);
+  up += dpp<0x114, 0xF>(0, up);
+  up += dpp<0x118, 0xF>(0, up);
+  up += dpp<0x142, 0xA>(0, up);
+  up += dpp<0x143, 0xC>(0, up);
+  uint32_t run = up - mine;
+  if (run < want && up >= want) {   // (one lane; none if there are fewer keys)
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      if (run + c[q] >= want && run < want) {
+        lds.digit = ascending ? 4 * lane + q : 255 - (4 * lane + q);
+        lds.above = (int)run;
+        lds.count = (int)c[q];
+      }
+      run += c[q];
+    }
+  }
+  if (lane == 63 && up < want) {
+    lds.digit = ascending ? 255 : 0; lds.above = (int)up; lds.count = 0;
+  }
+}
+
 // A key with at least k of the block's keys at or above it, and at most `most` (>= k) if they differ: the digits of the k-th largest
 // from the highest on, until few enough remain.  each(f): f(key) for the thread's keys.
 template <typename Each>
 __device__ __forceinline__ uint64_t key_at_rank(LpLds& lds, int k, int most, Each&& each) {
-  const int tid = threadIdx.x, lane = tid & 63;
-  uint32_t* hist = reinterpret_cast<uint32_t*>(lds.best);   // [256]
+  const int tid = threadIdx.x;
+  uint32_t* hist = lds.best;   // [256]
   uint64_t prefix = 0;
   int kept = 0;   // keys above the prefix's
   for (int shift = 56; shift >= 0; shift -= 8) {
@@ -222,36 +275,7 @@ __device__ __forceinline__ uint64_t key_at_rank(LpLds& lds, int k, int most, Eac
       if (key != 0 && (shift == 56 || (key >> (shift + 8)) == (prefix >> (shift + 8)))) atomicAdd(&hist[(key >> shift) & 255], 1u);
     });
     __syncthreads();
-    if (tid < 64) {   // digits 4 lane .. + 3; sums from the highest digit on
-      uint32_t c[4], mine = 0;
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        c[q] = hist[4 * lane + q];
-        mine += c[q];
-      }
-      uint32_t up = mine;   // of this lane's digits and those above
-#pragma unroll
-      for (int o = 1; o < 64; o <<= 1) {
-        const uint32_t other = __shfl_down(up, o, 64);
-        up += lane + o < 64 ? other : 0;
-      }
-      const uint32_t want = (uint32_t)(k - kept);
-      uint32_t run = up - mine;
-      if (run < want && up >= want) {   // (one lane; none if there are fewer keys than k)
-#pragma unroll
-        for (int q = 3; q >= 0; --q) {
-          if (run + c[q] >= want && run < want) {
-            lds.digit = 4 * lane + q;
-            lds.above = (int)run;
-            lds.count = (int)c[q];
-          }
-          run += c[q];
-        }
-      }
-      if (lane == 0 && up < want) {
-        lds.digit = 0; lds.above = (int)up; lds.count = 0;
-      }
-    }
+    if (tid < 64) digit_at_rank(lds, hist, (uint32_t)(k - kept), false);
     __syncthreads();
     prefix |= (uint64_t)lds.digit << shift;
     kept += lds.above;
@@ -260,40 +284,72 @@ __device__ __forceinline__ uint64_t key_at_rank(LpLds& lds, int k, int most, Eac
   return prefix;
 }
 
-// The k largest keys, in order, to out(rank, key).  `mine`: the largest key of this thread's share; rescan(f, t) calls f(key) for every
-// key of the share that is at least t (and may for others).  The k-th largest of the threads' largest keys is a threshold that k keys reach, and few
-// more; up to FEW_TOP it is found by taking the largest away k - 1 times, above (roughly) digit by digit.  What reaches it is listed and
-// ranked; if that is more than the list holds, or `exact`, the threshold comes from all keys.  At least k keys exist.
+// The k largest keys, in order, to out(rank, key).  `mine`: the largest key of this thread's share, 0 without one; `highest`: the order of the
+// largest value of all; rescan(f, t) calls f(key) for every key of the share that is at least t (and may for others).  The k-th largest of the
+// threads' largest keys is a threshold that k keys reach, and few more.  It is found by counting the values by their distance from the largest, in
+// 64ths of a factor of two: where the k-th lies is near enough unless many are about as large, or it lies 16 times lower.  Then, and for one or
+// two, up to FEW_TOP by taking the largest values away until k are gone, else digit by digit.  (Us, 2000 x 10000 fp32, by distance / taken away /
+// by digits: top 5 24 / 27 / -, 8 25 / 29 / -, 17 27 / - / 32, 64 35 / - / 41.)  What reaches the threshold is listed and ranked; if
+// that is more than the list holds, or `exact`, the threshold comes from all keys.  At least k keys exist.
 // (The threshold has to be close: a thread with a second key above it goes through its whole share again.  With the least of the largest
 // keys of 8 groups of threads, about 22 keys at k = 5, 4096 x 50000 bf16 took 182 us.)
-constexpr int FEW_TOP = 6;
+constexpr int FEW_TOP = 6, NEAR_BITS = 17;
 template <typename Rescan, typename Out>
-__device__ __forceinline__ void block_top(LpLds& lds, int k, uint64_t mine, bool exact, Rescan&& rescan, Out&& out) {
+__device__ __forceinline__ void block_top(LpLds& lds, int k, uint64_t mine, uint32_t highest, bool exact, Rescan&& rescan, Out&& out) {
   const int tid = threadIdx.x, lane = tid & 63;
+  const uint32_t order = (uint32_t)(mine >> 32);
   uint64_t threshold = 0;
-  if (k <= FEW_TOP) {
+  bool found = exact;
+  if (!found && k > 2) {
+    uint32_t* hist = lds.best;
     __syncthreads();         // (lds.best may still be read)
-    lds.best[tid] = mine;
+    if (tid < 256) hist[tid] = 0;
+    __syncthreads();
+    if (mine != 0) atomicAdd(&hist[min((highest - order) >> NEAR_BITS, 255u)], 1u);
+    __syncthreads();
+    if (tid < 64) digit_at_rank(lds, hist, (uint32_t)k, true);
+    __syncthreads();
+    found = lds.digit < 255 && lds.above + lds.count <= k + 8 + k / 4;
+    const uint32_t below = (uint32_t)(lds.digit + 1) << NEAR_BITS;   // (not below the order of -infinity)
+    if (found) threshold = (uint64_t)max(highest - min(below, highest) + 1, 0x007FFFFFu) << 32;
+  }
+  if (!found && k <= FEW_TOP) {
+    __syncthreads();
+    lds.best[tid] = order;
+    lds.column[tid] = (uint32_t)mine;
     __syncthreads();
     if (tid < 64) {
-      uint64_t x[LP_WAVES], t = 0;
+      uint32_t x[LP_WAVES], t = 0, c = 0;
 #pragma unroll
       for (int w = 0; w < LP_WAVES; ++w) x[w] = lds.best[w * 64 + lane];
-#pragma unroll 1
-      for (int r = 0; r < k; ++r) {
-        t = 0;
+      // the largest of x, taken away, until `left` are gone; what is left of that is returned
+      auto take = [&](int left, uint32_t& last, int& before) {
+        while (left > 0) {
+          last = 0;
 #pragma unroll
-        for (int w = 0; w < LP_WAVES; ++w) t = max(t, x[w]);
+          for (int w = 0; w < LP_WAVES; ++w) last = max(last, x[w]);
+          last = wave_max(last);
+          if (last == 0) break;
+          before = left;
 #pragma unroll
-        for (int o = 1; o < 64; o <<= 1) t = max(t, shfl_xor64(t, o));
+          for (int w = 0; w < LP_WAVES; ++w) {
+            left -= __popcll(__ballot(x[w] == last));
+            x[w] = x[w] == last ? 0 : x[w];
+          }
+        }
+        return left;
+      };
+      int among = 0, ignored;
+      if (take(k, t, among) < 0) {   // more equal ones than are wanted: the first of their columns
 #pragma unroll
-        for (int w = 0; w < LP_WAVES; ++w) x[w] = x[w] == t ? 0 : x[w];
+        for (int w = 0; w < LP_WAVES; ++w) x[w] = lds.best[w * 64 + lane] == t ? lds.column[w * 64 + lane] : 0;
+        take(among, c, ignored);
       }
-      if (tid == 0) lds.threshold = t;
+      if (tid == 0) lds.threshold = (uint64_t)t << 32 | c;
     }
     __syncthreads();
     threshold = lds.threshold;
-  } else if (!exact) {
+  } else if (!found) {
     threshold = key_at_rank(lds, k, k + k / 4, [&](auto&& f) { f(mine); });
   }
   for (bool all = exact;; all = true) {
@@ -405,26 +461,31 @@ __global__ __launch_bounds__(LP_THREADS, 6) void lp_kernel(LpArgs a) {
   t = block_softmax(lds, t);
   const float log_s = logf(t.s);
   if constexpr (TOP) {
-    // the group held, value by value: f(value, which)
+    // the group held: f(value, column)
     auto each_held = [&](auto&& f) {
-#pragma unroll 1
-      for (int i = 0; i < held_n; ++i) f(to_f32(reinterpret_cast<const T*>(&held[i / VN][tid])[i % VN]), i);
+#pragma unroll
+      for (int q = 0; q < U; ++q) {
+        float v[VN];
+        W::unpack(held[q][tid], v);
+#pragma unroll
+        for (int e = 0; e < VN; ++e)
+          if (q * VN + e < held_n) f(v[e], (uint32_t)(group + (int64_t)q * (LP_THREADS * VN) + e));
+      }
     };
-    auto held_column = [&](int i) { return (uint32_t)(group + (int64_t)(i / VN) * (LP_THREADS * VN) + i % VN); };
-    int first = U * VN;
-    each_held([&](float x, int i) { first = x == top_value ? min(first, i) : first; });
-    const uint64_t mine = held_n ? rank_key(top_value, held_column(first)) : 0;   // (of a row with a NaN any number: not asked for)
+    uint32_t first = 0xFFFFFFFEu;
+    each_held([&](float x, uint32_t c) { first = x == top_value ? min(first, c) : first; });
+    const uint64_t mine = held_n ? rank_key(top_value, first) : 0;   // (of a row with a NaN any number: not asked for)
     block_top(
-        lds, a.top, mine, t.s != t.s,
+        lds, a.top, mine, value_order(t.m), t.s != t.s,
         [&](auto&& f, uint64_t least) {
           if (least == 0) {
             walk.each_column(tid, [&](float x, int64_t c) { f(rank_key(x, (uint32_t)c)); });
             return;
           }
           const float at_least = key_value(least);
-          if (rank_key(second, 0) < least) {   // none reaches it in the other groups
-            each_held([&](float x, int i) {
-              if (x >= at_least) f(rank_key(x, held_column(i)));
+          if (value_order(second) < (uint32_t)(least >> 32)) {   // none reaches it in the other groups
+            each_held([&](float x, uint32_t c) {
+              if (x >= at_least) f(rank_key(x, c));
             });
           } else {
             walk.again(tid, [&](float x, int64_t c) {
@@ -480,7 +541,7 @@ __global__ __launch_bounds__(LP_THREADS) void lp_join_kernel(LpArgs a) {
 #pragma unroll
     for (uint64_t k : key) mine = max(mine, k);
     block_top(
-        lds, a.top, mine, false,
+        lds, a.top, mine, t.s != t.s ? 0xFFFFFFF0u : value_order(t.m), false,
         [&](auto&& f, uint64_t) {
 #pragma unroll
           for (uint64_t k : key) f(k);
