@@ -250,9 +250,13 @@ __global__ __launch_bounds__(SAMPLE_KEYS) void sort_cuts_kernel(const int32_t* k
 // the other: every digit has copies of its counter, and the lanes take turns with them (42 M lookups of 21 bits: 60 / 102 / 121
 // us a pass with one counter, the keys more and more in order; 54 with eight, the blocks' loads and their latency).
 // BUCKETS: their numbers are the digits.
-template <bool BUCKETS>
+// CLEAR (of all three kernels): further blocks clear part of a matrix.
+template <bool BUCKETS, bool CLEAR = false>
 __global__ __launch_bounds__(SORT_THREADS) void sort_hist_kernel(const int32_t* keys, uint32_t* hist,
-                                                                 FieldPtr fp, TileBase tb, int F, int shift, int rb, BucketPlan bp) {
+                                                                 FieldPtr fp, TileBase tb, int F, int shift, int rb, BucketPlan bp, ClearOrNone<CLEAR> clear) {
+  if constexpr (CLEAR) {
+    if ((int)blockIdx.x >= clear.first) return clear_part<SORT_THREADS>(clear);
+  }
   constexpr int LOG_COUNTERS = 12, LOG_COPIES = 3;
   __shared__ uint32_t h[1 << LOG_COUNTERS];
   __shared__ typename std::conditional<BUCKETS, FieldBuckets, int>::type fb;
@@ -296,8 +300,12 @@ __global__ __launch_bounds__(SORT_THREADS) void sort_hist_kernel(const int32_t* 
 // block per field, a chain of loads for each digit, took 18.8 us for 204 tiles of 128 digits, now 11.6, and 11 for 80 of
 // 1024, now 7.5.
 constexpr int SCAN_THREADS = 1024, SCAN_DIGITS = 128;
-template <bool BUCKETS>
-__global__ __launch_bounds__(SCAN_THREADS) void sort_scan_kernel(uint32_t* hist, uint32_t* digit_total, TileBase tb, int rb, BucketPlan bp) {
+template <bool BUCKETS, bool CLEAR = false>
+__global__ __launch_bounds__(SCAN_THREADS) void sort_scan_kernel(uint32_t* hist, uint32_t* digit_total, TileBase tb, int rb, BucketPlan bp,
+                                                                 ClearOrNone<CLEAR> clear) {
+  if constexpr (CLEAR) {
+    if ((int)blockIdx.x >= clear.first) return clear_part<SCAN_THREADS>(clear);
+  }
   __shared__ uint32_t sums[SCAN_THREADS];
   const int nb = 1 << rb, digits = min(nb, SCAN_DIGITS), groups = nb / digits;
   const int f = (int)blockIdx.x / groups;
@@ -514,10 +522,13 @@ __device__ __forceinline__ void scatter_tile(ScatterLds& lds, const int32_t* key
   }
 }
 
-template <bool BUCKETS>
+template <bool BUCKETS, bool CLEAR = false>
 __global__ __launch_bounds__(SORT_THREADS, 8) void sort_scatter_kernel(
     const int32_t* keys_in, const int32_t* pay_in, int32_t* keys_out, int32_t* pay_out, int32_t* packed, const uint32_t* hist,
-    const uint32_t* digit_total, FieldPtr fp, TileBase tb, int F, int shift, int rb, BucketPlan bp) {
+    const uint32_t* digit_total, FieldPtr fp, TileBase tb, int F, int shift, int rb, BucketPlan bp, ClearOrNone<CLEAR> clear) {
+  if constexpr (CLEAR) {
+    if ((int)blockIdx.x >= clear.first) return clear_part<SORT_THREADS>(clear);
+  }
   __shared__ ScatterLds lds;
   __shared__ typename std::conditional<BUCKETS, FieldBuckets, int>::type fb;
   static_assert(4 * (sizeof(lds) + sizeof(fb)) <= 160 * 1024, "four blocks to fill a compute unit's places for wavefronts");
@@ -1510,25 +1521,40 @@ hipError_t launch_reduce_variant(const SegArgs& a, const FieldPtr& fp, const Til
 
 }  // namespace
 
+template <bool CLEAR>
 static hipError_t launch_sort_pass(const SortPlan& pl, const SortBuffers& sb, int pass, const FieldPtr& fp,
-                            const TileBase& tb, Profiler* prof, hipStream_t s) {
+                            const TileBase& tb, Profiler* prof, hipStream_t s, const ClearRows* clear) {
   const int shift = pass * pl.radix_bits;
   const int32_t* kin = pass == 0 ? sb.ids : sb.key[(pass - 1) & 1];
   const int32_t* pin = pass == 0 ? sb.pay0 : sb.pay[(pass - 1) & 1];
-  dim3 grid(tile_grid(pl.total_tiles));
+  const unsigned tiles = tile_grid(pl.total_tiles);
+  // the grid of launch `which` of the pass with the blocks that clear (the caller has cleared the first part)
+  auto with = [&](unsigned blocks, int which, int threads, ClearOrNone<CLEAR>& part) {
+    if constexpr (CLEAR) {
+      part = ClearPart{*clear, (int32_t)blocks, 1 + 3 * pass + which, 1 + 3 * pl.passes};
+      return dim3(blocks + clear_blocks(part, threads));
+    } else {
+      part = 0;
+      return dim3(blocks);
+    }
+  };
+  ClearOrNone<CLEAR> part;
   {
     ProfScope ps(prof, KID_SORT_HIST, s);
-    hipLaunchKernelGGL(sort_hist_kernel<false>, grid, dim3(SORT_THREADS), 0, s, kin, sb.hist, fp, tb, pl.F, shift, pl.radix_bits, BucketPlan());
+    const dim3 grid = with(tiles, 0, SORT_THREADS, part);
+    hipLaunchKernelGGL((sort_hist_kernel<false, CLEAR>), grid, dim3(SORT_THREADS), 0, s, kin, sb.hist, fp, tb, pl.F, shift, pl.radix_bits, BucketPlan(), part);
   }
   {
     ProfScope ps(prof, KID_SORT_SCAN, s);
     const int groups = std::max(1, (1 << pl.radix_bits) / SCAN_DIGITS);
-    hipLaunchKernelGGL(sort_scan_kernel<false>, dim3(pl.F * groups), dim3(SCAN_THREADS), 0, s, sb.hist, sb.digit_total, tb, pl.radix_bits, BucketPlan());
+    const dim3 grid = with(pl.F * groups, 1, SCAN_THREADS, part);
+    hipLaunchKernelGGL((sort_scan_kernel<false, CLEAR>), grid, dim3(SCAN_THREADS), 0, s, sb.hist, sb.digit_total, tb, pl.radix_bits, BucketPlan(), part);
   }
   {
     ProfScope ps(prof, KID_SORT_SCATTER, s);
-    hipLaunchKernelGGL(sort_scatter_kernel<false>, grid, dim3(SORT_THREADS), 0, s, kin, pin, sb.key[pass & 1],
-                       sb.pay[pass & 1], sb.key[0], sb.hist, sb.digit_total, fp, tb, pl.F, shift, pl.radix_bits, BucketPlan());
+    const dim3 grid = with(tiles, 2, SORT_THREADS, part);
+    hipLaunchKernelGGL((sort_scatter_kernel<false, CLEAR>), grid, dim3(SORT_THREADS), 0, s, kin, pin, sb.key[pass & 1],
+                       sb.pay[pass & 1], sb.key[0], sb.hist, sb.digit_total, fp, tb, pl.F, shift, pl.radix_bits, BucketPlan(), part);
   }
   return hipGetLastError();
 }
@@ -1585,17 +1611,17 @@ static hipError_t launch_sort_buckets(const SortPlan& pl, const SortBuffers& sb,
   {
     ProfScope ps(prof, KID_SORT_HIST, s);
     hipLaunchKernelGGL(sort_cuts_kernel, dim3(pl.F), dim3(SAMPLE_KEYS), 0, s, sb.ids, fp, bp);
-    hipLaunchKernelGGL(sort_hist_kernel<true>, grid, dim3(SORT_THREADS), 0, s, sb.ids, sb.hist, fp, tb, pl.F, 0, bp.rb, bp);
+    hipLaunchKernelGGL(sort_hist_kernel<true>, grid, dim3(SORT_THREADS), 0, s, sb.ids, sb.hist, fp, tb, pl.F, 0, bp.rb, bp, 0);
     ps.launches(2);
   }
   {
     ProfScope ps(prof, KID_SORT_SCAN, s);
     const int groups = std::max(1, (1 << bp.rb) / SCAN_DIGITS);
-    hipLaunchKernelGGL(sort_scan_kernel<true>, dim3(pl.F * groups), dim3(SCAN_THREADS), 0, s, sb.hist, sb.digit_total, tb, bp.rb, bp);
+    hipLaunchKernelGGL(sort_scan_kernel<true>, dim3(pl.F * groups), dim3(SCAN_THREADS), 0, s, sb.hist, sb.digit_total, tb, bp.rb, bp, 0);
   }
   ProfScope ps(prof, KID_SORT_SCATTER, s);
   hipLaunchKernelGGL(sort_scatter_kernel<true>, grid, dim3(SORT_THREADS), 0, s, sb.ids, sb.pay0, sb.key[0], sb.pay[0], sb.key[1], sb.hist,
-                     sb.digit_total, fp, tb, pl.F, 0, bp.rb, bp);
+                     sb.digit_total, fp, tb, pl.F, 0, bp.rb, bp, 0);
   const int large_blocks = std::min((bp.most_large + 7) / 8 * 8, 1024);   // (the others keep their XCDs)
   hipLaunchKernelGGL(sort_buckets_kernel, dim3(large_blocks + 8 * (((pl.F << bp.rb) + 7) / 8)), dim3(BUCKET_THREADS), 0, s, sb.key[1], sb.pay[1],
                      sb.key[0], sb.pay[0], sb.digit_total, fp, pl.F, large_blocks, bp);
@@ -1617,21 +1643,21 @@ bool sort_finds_samples(const SortPlan& pl, const SortBuffers& sb, const FieldPt
 }
 
 hipError_t launch_sort(const SortPlan& pl, const SortBuffers& sb, const FieldPtr& fp, const TileBase& tb, Profiler* prof, hipStream_t s,
-                       int* sorted_buf) {
+                       int* sorted_buf, const ClearRows* clear) {
   *sorted_buf = 0;
   if (pl.total_tiles == 0) return hipSuccess;
   // One block per field as long as a field fits one: two passes over 1000 / 9000 lookups of a field take 10 / 24 us, the
   // six launches 29 / 30 and the host four times as long.
-  switch (small_sort_items(pl.F, fp)) {
+  switch (clear ? 0 : small_sort_items(pl.F, fp)) {
     case 2: return launch_sort_small_items<2>(pl, sb, fp, prof, s);
     case 4: return launch_sort_small_items<4>(pl, sb, fp, prof, s);
     case 8: return launch_sort_small_items<8>(pl, sb, fp, prof, s);
     case 16: return launch_sort_small_items<16>(pl, sb, fp, prof, s);
   }
   BucketPlan bp = {};
-  if (plan_buckets(pl, sb, fp, bp)) return launch_sort_buckets(pl, sb, fp, tb, bp, prof, s);
+  if (!clear && plan_buckets(pl, sb, fp, bp)) return launch_sort_buckets(pl, sb, fp, tb, bp, prof, s);
   for (int p = 0; p < pl.passes; ++p) {
-    const hipError_t e = launch_sort_pass(pl, sb, p, fp, tb, prof, s);
+    const hipError_t e = clear ? launch_sort_pass<true>(pl, sb, p, fp, tb, prof, s, clear) : launch_sort_pass<false>(pl, sb, p, fp, tb, prof, s, nullptr);
     if (e != hipSuccess) return e;
   }
   *sorted_buf = (pl.passes - 1) & 1;

@@ -295,9 +295,11 @@ __device__ __forceinline__ void add_up_losses(const LossJob* job) {   // (the fi
 void plan_sort_pass(const SortPlan& pl, const SortBuffers& sb, const FieldPtr& fp, int pass, SortPass& sp);
 // Whether launch_sort can do without sample indices, and work them out of the bags' boundaries (of a whole batch).
 bool sort_finds_samples(const SortPlan& pl, const SortBuffers& sb, const FieldPtr& fp);
-// Sorts every field's lookups by row id (stable); the result is in key / pay [*sorted_buf].
+// Sorts every field's lookups by row id (stable); the result is in key / pay [*sorted_buf].  clear: rows of which the launches of a sort by passes
+// clear all parts of 1 + 3 passes but the first, which the caller does.
+struct ClearRows;
 hipError_t launch_sort(const SortPlan& pl, const SortBuffers& sb, const FieldPtr& fp, const TileBase& tb, Profiler* prof, hipStream_t s,
-                       int* sorted_buf);
+                       int* sorted_buf, const ClearRows* clear = nullptr);
 
 // Slots of the windows: window i of a field that starts at lookup p has slot p / 128 + i.  A field of n > 256 lookups has
 // ceil(n / 256) <= floor(n / 128) windows at most, so no two fields' windows meet and none lies past the last

@@ -8,6 +8,37 @@ namespace antdt {
 
 constexpr int MAX_BINS = 1024;
 
+// Rows of a matrix that are cleared by further blocks of launches that leave the memory idle: part `part` of `parts`, by the blocks from `first` on.
+struct ClearRows {
+  float* x;        // NULL: nothing to clear
+  int64_t ld, rows, cols;
+  int32_t whole;   // 16 bytes at a time, rows without gaps
+};
+struct ClearPart {
+  ClearRows rows;
+  int32_t first, part, parts;
+};
+inline int clear_blocks(const ClearPart& c, int threads) {
+  if (!c.rows.x) return 0;
+  const int64_t n = c.rows.rows * c.rows.cols / c.parts + 1;   // elements, 16 or more a thread
+  return (int)(n / (16 * threads) < 1 ? 1 : n / (16 * threads) > 2048 ? 2048 : n / (16 * threads));
+}
+template <int THREADS>
+__device__ __forceinline__ void clear_part(const ClearPart& c) {
+  const ClearRows& a = c.rows;
+  const int64_t first = ((int64_t)blockIdx.x - c.first) * THREADS + threadIdx.x, step = ((int64_t)gridDim.x - c.first) * THREADS;
+  if (a.whole) {
+    const int64_t n = a.rows * a.cols / 4, end = n * (c.part + 1) / c.parts;
+    for (int64_t i = n * c.part / c.parts + first; i < end; i += step) reinterpret_cast<float4*>(a.x)[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  } else {
+    const int64_t end = a.rows * (c.part + 1) / c.parts;
+    for (int64_t r = a.rows * c.part / c.parts + (first >> 6); r < end; r += step >> 6)
+      for (int64_t i = first & 63; i < a.cols; i += 64) a.x[r * a.ld + i] = 0.0f;
+  }
+}
+template <bool CLEAR>
+using ClearOrNone = typename std::conditional<CLEAR, ClearPart, int32_t>::type;
+
 __device__ __forceinline__ uint64_t lanemask_lt() {
   const unsigned lane = threadIdx.x & 63;
   return lane == 0 ? 0ull : (~0ull >> (64 - lane));

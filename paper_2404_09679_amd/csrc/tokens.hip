@@ -92,28 +92,10 @@ struct GradArgs {
   DropArgs drop;
 };
 
-// What clears the gradient (of the rows that no token names; the others are written again).
-struct ClearArgs {
-  float* grad;
-  int64_t ldg, rows, cols;
-  int32_t whole;   // 16 bytes at a time, rows without gaps
-};
-template <int THREADS>
-__device__ __forceinline__ void clear_rows(const ClearArgs& a, int block, int blocks) {
-  const int64_t first = (int64_t)block * THREADS + threadIdx.x, step = (int64_t)blocks * THREADS;
-  if (a.whole) {
-    const int64_t n = a.rows * a.cols / 4;
-    for (int64_t i = first; i < n; i += step) store16<false>(a.grad + 4 * i, make_uint4(0, 0, 0, 0));
-  } else {
-    for (int64_t r = first >> 6; r < a.rows; r += step >> 6)
-      for (int64_t c = first & 63; c < a.cols; c += 64) a.grad[r * a.ldg + c] = 0.0f;
-  }
-}
-
-// Keys and positions of the sort; further blocks clear the gradient.
-__global__ __launch_bounds__(256) void token_keys_kernel(const int32_t* tokens, int32_t* key, int32_t* pay, int N, int V, int key_blocks, ClearArgs clear) {
-  if ((int)blockIdx.x >= key_blocks) {
-    clear_rows<256>(clear, blockIdx.x - key_blocks, gridDim.x - key_blocks);
+// Keys and positions of the sort; further blocks clear their part of the gradient.
+__global__ __launch_bounds__(256) void token_keys_kernel(const int32_t* tokens, int32_t* key, int32_t* pay, int N, int V, ClearPart clear) {
+  if ((int)blockIdx.x >= clear.first) {
+    clear_part<256>(clear);
     return;
   }
   const int i = blockIdx.x * 256 + threadIdx.x;
@@ -126,11 +108,11 @@ __global__ __launch_bounds__(256) void token_keys_kernel(const int32_t* tokens, 
 // The same and the whole sort, of as many tokens as one block sorts (the first; 3001 tokens: launches of 5.5 and 8.2 us in one of 9).
 template <int IT>
 __global__ __launch_bounds__(SMALL_THREADS) void token_sort_kernel(const int32_t* tokens, int32_t* key_in, int32_t* pay_in, int32_t* key, int32_t* pay, int N,
-                                                                   int V, int passes, int rb, ClearArgs clear) {
+                                                                   int V, int passes, int rb, ClearPart clear) {
   __shared__ SmallSortLds lds;
   extern __shared__ int32_t stage[];
   if (blockIdx.x > 0) {
-    clear_rows<SMALL_THREADS>(clear, blockIdx.x - 1, gridDim.x - 1);
+    clear_part<SMALL_THREADS>(clear);
     return;
   }
   for (int i = threadIdx.x; i < N; i += SMALL_THREADS) {
@@ -142,14 +124,14 @@ __global__ __launch_bounds__(SMALL_THREADS) void token_sort_kernel(const int32_t
   sort_small_field<IT>(lds, stage, key_in, pay_in, key, pay, N, passes, rb);
 }
 template <int IT>
-hipError_t launch_token_sort(const int32_t* tokens, const SortBuffers& sb, int N, int V, const SortPlan& sp, int clear_blocks, const ClearArgs& clear,
-                             hipStream_t s) {
+hipError_t launch_token_sort(const int32_t* tokens, const SortBuffers& sb, int N, int V, const SortPlan& sp, const ClearRows& clear, hipStream_t s) {
   static std::atomic<uint64_t> allowed{0};
   constexpr int bytes = SMALL_THREADS * IT * 4;
   const hipError_t e = allow_lds(token_sort_kernel<IT>, bytes, (int)sizeof(SmallSortLds), allowed);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(token_sort_kernel<IT>, dim3(1 + clear_blocks), dim3(SMALL_THREADS), bytes, s, tokens, sb.key[1], sb.pay[1], sb.key[0], sb.pay[0], N, V,
-                     sp.passes, sp.radix_bits, clear);
+  const ClearPart part = {clear, 1, 0, 1};
+  hipLaunchKernelGGL(token_sort_kernel<IT>, dim3(1 + clear_blocks(part, SMALL_THREADS)), dim3(SMALL_THREADS), bytes, s, tokens, sb.key[1], sb.pay[1],
+                     sb.key[0], sb.pay[0], N, V, sp.passes, sp.radix_bits, part);
   return hipGetLastError();
 }
 
@@ -177,10 +159,10 @@ __device__ __forceinline__ void write_row(const GradArgs& a, int v, int64_t c, i
 
 template <typename T, int Q, bool DROP, bool ACCUMULATE>
 __global__ __launch_bounds__(256) void token_sum_kernel(GradArgs a, bool vec_grad) {
-  // of the walks of the block: the sum of the run that came in and of the one that goes on, and whether there is the one, whether it is
-  // the whole walk and goes on, and whether there is the other
+  // of the walks of the block: the sum of the run that came in and of the one that goes on, whether there is the one, and whether it is
+  // the whole walk and goes on
   __shared__ float sums[2][256][8];
-  __shared__ uint8_t came[256], through[256], starts[256];
+  __shared__ uint8_t came[256], through[256];
   const int lanes = 1 << a.lanes_log2, walks = 256 >> a.lanes_log2;
   const int lane = threadIdx.x & (lanes - 1), g = threadIdx.x >> a.lanes_log2;
   const int64_t c = 8 * (((int64_t)blockIdx.y << a.lanes_log2) + lane);
@@ -194,7 +176,8 @@ __global__ __launch_bounds__(256) void token_sum_kernel(GradArgs a, bool vec_gra
   int run = (int)a.V;
   if (p0 < a.N) {
     run = a.key[p0];
-    has_in = run < a.V && p0 > 0 && a.key[p0 - 1] == run;
+    const int before = a.key[max(p0 - 1, (int64_t)0)], behind = a.key[min(p1, a.N - 1)];   // (asked for here: one wait for all three)
+    has_in = run < a.V && p0 > 0 && before == run;
     bool in = has_in;
     float sum[8] = {};
     if (n > 0) {
@@ -237,7 +220,7 @@ __global__ __launch_bounds__(256) void token_sum_kernel(GradArgs a, bool vec_gra
       in = has_in && run == a.key[p0];
     }
     if (run < a.V) {
-      const bool goes_on = p1 < a.N && a.key[p1] == run;
+      const bool goes_on = p1 < a.N && behind == run;
       is_through = in && goes_on;
       has_out = !in && goes_on;
       if (in) store8<4>(sums[0][threadIdx.x], 8, sum);
@@ -246,7 +229,7 @@ __global__ __launch_bounds__(256) void token_sum_kernel(GradArgs a, bool vec_gra
     }
   }
   if (lane == 0) {
-    came[g] = has_in; through[g] = is_through; starts[g] = has_out;
+    came[g] = has_in; through[g] = is_through;
   }
   __syncthreads();
   float* slots = a.partial + (int64_t)blockIdx.x * 2 * a.ldp + c;
@@ -497,8 +480,7 @@ int antdt_token_gradient(const void* dy, int64_t lddy, int32_t dtype, const int3
   char* ws = reinterpret_cast<char*>(workspace);
   auto ints = [&](size_t at) { return reinterpret_cast<int32_t*>(ws + at); };
   const bool whole = ldg == D && D % 4 == 0 && (reinterpret_cast<uintptr_t>(grad) & 15) == 0;
-  const ClearArgs clear = {grad, ldg, V, D, whole};
-  const int64_t clear_blocks = accumulate ? 0 : std::min<int64_t>(whole ? div_up(V * D, 4096) : div_up(V, 4), 8192);
+  const ClearRows clear = {accumulate ? nullptr : grad, ldg, V, D, whole};
 
   SortPlan sp = {};
   sp.F = 1; sp.passes = pl.passes; sp.radix_bits = pl.radix_bits; sp.total_tiles = pl.tiles; sp.rows = V + 1; sp.samples = N; sp.width = D;
@@ -515,22 +497,26 @@ int antdt_token_gradient(const void* dy, int64_t lddy, int32_t dtype, const int3
   const int items = N ? small_sort_items(1, fp) : 0;
   if (items) {
     sb.key[0] = ints(pl.key[0]); sb.pay[0] = ints(pl.pay[0]);
-    const int blocks = (int)div_up(clear_blocks, SMALL_THREADS / 256);
     switch (items) {
-      case 2: OP_TRY(op_hip(call, launch_token_sort<2>(tokens, sb, (int)N, (int)V, sp, blocks, clear, s))); break;
-      case 4: OP_TRY(op_hip(call, launch_token_sort<4>(tokens, sb, (int)N, (int)V, sp, blocks, clear, s))); break;
-      case 8: OP_TRY(op_hip(call, launch_token_sort<8>(tokens, sb, (int)N, (int)V, sp, blocks, clear, s))); break;
-      default: OP_TRY(op_hip(call, launch_token_sort<16>(tokens, sb, (int)N, (int)V, sp, blocks, clear, s))); break;
+      case 2: OP_TRY(op_hip(call, launch_token_sort<2>(tokens, sb, (int)N, (int)V, sp, clear, s))); break;
+      case 4: OP_TRY(op_hip(call, launch_token_sort<4>(tokens, sb, (int)N, (int)V, sp, clear, s))); break;
+      case 8: OP_TRY(op_hip(call, launch_token_sort<8>(tokens, sb, (int)N, (int)V, sp, clear, s))); break;
+      default: OP_TRY(op_hip(call, launch_token_sort<16>(tokens, sb, (int)N, (int)V, sp, clear, s))); break;
     }
   } else {
-    const int key_blocks = (int)div_up(N, 256);
-    hipLaunchKernelGGL(token_keys_kernel, dim3((unsigned)(key_blocks + clear_blocks)), dim3(256), 0, s, tokens, sb.key[1], sb.pay[1], (int)N, (int)V,
-                       key_blocks, clear);
+    // A large gradient is cleared in parts beside all of the sort's launches, which leave the memory idle, a smaller one in this launch alone.  All
+    // at once / in parts, us: 131072 tokens of 200000 x 256 98 / 93, 100000 of 1000000 x 48 79 / 73, of 2000 x 256 56.5 / 57.8.
+    constexpr int64_t AT_ONCE = 32 << 20;
+    const bool in_parts = N > 0 && !accumulate && V * D * 4 > AT_ONCE;
+    const int parts = in_parts ? 1 + 3 * pl.passes : 1;
+    const ClearPart part = {clear, (int32_t)div_up(N, 256), 0, parts};
+    hipLaunchKernelGGL(token_keys_kernel, dim3((unsigned)(part.first + clear_blocks(part, 256))), dim3(256), 0, s, tokens, sb.key[1], sb.pay[1], (int)N,
+                       (int)V, part);
     OP_TRY(op_hip(call, hipGetLastError()));
     if (N == 0) return ANTDT_OK;
     sb.key[0] = ints(pl.key[0]); sb.pay[0] = ints(pl.pay[0]);
     sb.hist = reinterpret_cast<uint32_t*>(ws + pl.hist); sb.digit_total = reinterpret_cast<uint32_t*>(ws + pl.digit_total);
-    OP_TRY(op_hip(call, launch_sort(sp, sb, fp, tb, nullptr, s, &sorted)));
+    OP_TRY(op_hip(call, launch_sort(sp, sb, fp, tb, nullptr, s, &sorted, in_parts ? &clear : nullptr)));
   }
 
   a.key = sb.key[sorted]; a.pay = sb.pay[sorted];
