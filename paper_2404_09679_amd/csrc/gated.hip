@@ -457,8 +457,8 @@ struct TileClass {
 };
 enum { BF16_256, BF16_128, BF16_64, F32_64, F32_64_ANY, TILE_CLASSES };
 constexpr TileClass TILE_CLASS[2][TILE_CLASSES] = {
-    {{256, 256, 64, 1, 27.0f, 7.0f}, {128, 128, 64, 1, 10.0f, 2.5f}, {64, 64, 64, 3, 4.6f, 1.0f}, {64, 64, 32, 3, 16.0f, 2.0f}, {64, 64, 32, 3, 25.0f, 2.0f}},
-    {{256, 256, 64, 1, 27.0f, 7.0f}, {128, 128, 64, 1, 10.0f, 2.5f}, {64, 64, 64, 3, 4.6f, 1.0f}, {64, 128, 32, 2, 32.0f, 3.0f}, {64, 128, 32, 2, 50.0f, 3.0f}}};
+    {{256, 256, 32, 1, 27.0f, 7.0f}, {128, 128, 64, 1, 10.0f, 2.5f}, {64, 64, 64, 3, 4.6f, 1.0f}, {64, 64, 32, 3, 16.0f, 2.0f}, {64, 64, 32, 3, 25.0f, 2.0f}},
+    {{256, 256, 32, 1, 27.0f, 7.0f}, {128, 128, 64, 1, 10.0f, 2.5f}, {64, 64, 64, 3, 4.6f, 1.0f}, {64, 128, 32, 2, 32.0f, 3.0f}, {64, 128, 32, 2, 50.0f, 3.0f}}};
 template <typename T, int C, int NB, bool AS, bool BS>
 struct TilingOf;   // Product: its TileProduct; vec: whole 16-byte groups may be written
 #define TILING(C, T, TM, TN, WR, WC, BK, STAGES, PIECE)                                                                                \
@@ -471,7 +471,7 @@ struct TilingOf;   // Product: its TileProduct; vec: whole 16-byte groups may be
     static_assert(Product::BM == k.rows && NB * Product::BN == k.cols && Product::SLOTS == k.slots &&                                  \
                       160 * 1024 / Product::LDS_BYTES == k.at_once, "class");                                                          \
   };
-TILING(BF16_256, bf16_t, 4, 2 / NB, 2, 4, 64, 2, 16)
+TILING(BF16_256, bf16_t, 4, 4 / NB, 2, 2, 32, 4, 16)
 TILING(BF16_128, bf16_t, 2 / NB, 1, 2 * NB, 4 / NB, 64, 3, 16)
 TILING(BF16_64, bf16_t, 1, 1, 2, 2 / NB, 64, 3, 16)
 TILING(F32_64, float, 1, 1, 2, 2, 32, 3, 16)

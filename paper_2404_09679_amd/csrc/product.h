@@ -99,6 +99,7 @@ struct Operand {
 // column 32 j + 8 (e / 4) + 4 (lane / 32) + e % 4 of B_b's.
 template <typename T, int NB, int TM, int TN, int WR, int WC, int BK, int STAGES, bool A_STRIDED, bool B_STRIDED, int PIECE>
 struct TileProduct {
+  static constexpr bool INTERLEAVED = TM * NB * TN >= 16;
   static constexpr int SLOTS = BK, NB_ = NB, TM_ = TM, TN_ = TN, WC_ = WC, WAVES = WR * WC;
   static constexpr int THREADS = 64 * WAVES, BM = 32 * TM * WR, BN = 32 * TN * WC;
   typedef ProductTile<T, BM, BK, A_STRIDED, PIECE> TA;
@@ -180,6 +181,76 @@ struct TileProduct {
 #pragma unroll
         for (int j = 0; j < TN; ++j) bf[to][s][j] = TB::fragment(lb + s * TB::BYTES, (wc * TN + j) * 32, q * STEP, lane);
     };
+    if constexpr (INTERLEAVED) {
+      // One wavefront a SIMD: the next step's fragments and the next stages' loads go between the multiplications, one at a time.
+      constexpr int MF = TM * NB * TN, FR = TM + NB * TN, LOADS = PER_STAGE / Q;
+      static_assert(LOADS * Q == PER_STAGE && FR + 2 * LOADS <= MF && STAGES >= 3, "room between the multiplications");
+      auto fetch_one = [&](const char* la, int q, int to, int f) {
+        if (f < TM) af[to][f] = TA::fragment(la, (wr * TM + f) * 32, q * STEP, lane);
+        else bf[to][(f - TM) / TN][(f - TM) % TN] =
+            TB::fragment(la + TA::BYTES + (f - TM) / TN * TB::BYTES, (wc * TN + (f - TM) % TN) * 32, q * STEP, lane);
+      };
+      auto load_one = [&](auto kind, int i) {
+        const int q = i < VA ? 0 : (i - VA) / VB, j = i < VA ? i : (i - VA) % VB;
+        const char* base = i < VA ? pa : pb[q];
+        const uint32_t off = i < VA ? oa[j] : ob[j], to = fill + (i < VA ? 0 : TA::BYTES + q * TB::BYTES) + j * (THREADS * PIECE);
+        if constexpr (decltype(kind)::value == 1) load(base, off, to);
+        else load((i < VA ? ka[j] : kb[j]) < left ? base + off : reinterpret_cast<const char*>(mfma_zero16), to);
+      };
+#pragma unroll
+      for (int t = 0; t < STAGES - 1; ++t)
+        if (t < nk) issue();
+      if (nk == 0) return;
+      if (STAGES - 2 < nk) wait_loads<(STAGES - 2) * PER_STAGE>();
+      else wait_loads<0>();
+      block_barrier();
+      fetch(lds, 0, 0);
+      uint32_t read = 0;
+      int t = 0;
+      // Stage t, with the loads of stage t + STAGES - 1 (KIND 0: there is none; 1: a whole one; 2: the last one, partly filled).
+      auto stage = [&](auto kind) {
+        constexpr int KIND = decltype(kind)::value;
+        const uint32_t next = read == (STAGES - 1) * STAGE_BYTES ? 0 : read + STAGE_BYTES;
+#pragma unroll
+        for (int q = 0; q < Q; ++q) {
+          if (q + 1 == Q) {
+            __builtin_amdgcn_s_waitcnt(LDS_READS_DONE);
+            __builtin_amdgcn_sched_barrier(0);
+            if constexpr (KIND != 0) {
+              wait_loads<(STAGES - 3) * PER_STAGE + (Q - 1) * LOADS>();
+              block_barrier();
+            } else if (t + 1 < nk) {
+              wait_loads<0>();
+              block_barrier();
+            }
+          }
+          const char* from = lds + (q + 1 < Q ? read : next);   // (behind the last stage whatever lies there)
+#pragma unroll
+          for (int m = 0; m < MF; ++m) {
+            const int i = m / (NB * TN), sj = m % (NB * TN);
+            TA::multiply(af[q & 1][i], bf[q & 1][sj / TN][sj % TN], acc[sj / TN][i][sj % TN]);
+            __builtin_amdgcn_sched_barrier(0);
+            if (m < FR) fetch_one(from, q + 1 < Q ? q + 1 : 0, (q + 1) & 1, m);
+            else if (KIND != 0 && (m - FR) % 2 == 0 && (m - FR) / 2 < LOADS) load_one(kind, q * LOADS + (m - FR) / 2);
+            __builtin_amdgcn_sched_barrier(0);
+          }
+        }
+        if constexpr (KIND != 0) {
+          pa += step_a;
+#pragma unroll
+          for (int q = 0; q < NB; ++q) pb[q] += step_b;
+          left -= BK;
+          fill = fill == lds0 + (STAGES - 1) * STAGE_BYTES ? lds0 : fill + STAGE_BYTES;
+        }
+        read = next;
+        ++t;
+      };
+      while (left >= BK) stage(std::integral_constant<int, 1>());
+      if (left > 0) stage(std::integral_constant<int, 2>());
+      while (t < nk) stage(std::integral_constant<int, 0>());
+      block_barrier();
+      return;
+    }
     // Stage t is in LDS, and everybody's fragments of the stage before have been read.
     auto arrived = [&](int t) {
       if (t + STAGES - 2 < nk) wait_loads<(STAGES - 2) * PER_STAGE>();
