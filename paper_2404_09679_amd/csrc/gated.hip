@@ -163,7 +163,8 @@ __device__ __forceinline__ void tile_block(const typename Op::Args& a, const Spl
         out[(i * 4 + v) * P::THREADS] = f32x4v{x[i][4 * v], x[i][4 * v + 1], x[i][4 * v + 2], x[i][4 * v + 3]};
   }
 }
-// 32 rows of a wavefront's tile by one wavefront (few tiles are in parts, but each is as much to read as many results).
+// 32 rows of a wavefront's tile by one wavefront (few tiles are in parts, but each is as much to read as many results).  Blocks of two: 777
+// tokens of 520-1400, backward pass, blocks of four 27.5 us, so 24.8.
 constexpr int JOIN_WAVES = 2;
 template <typename P>
 constexpr int join_units() { return P::WAVES * P::TM_; }   // of a tile

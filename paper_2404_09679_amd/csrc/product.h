@@ -6,6 +6,13 @@
 // A is multiplied with a tile of each of two matrices, whose columns a wavefront holds side by side.
 //   bf16: v_mfma_f32_32x32x16_bf16.
 //   fp32: v_mfma_f32_32x32x2_f32 (fp32 products and sums); a lane's four slots of a step are four MFMAs.
+// What bounds it is LDS: a wavefront's tile of 128 x 64 reads 96 bytes a cycle of a compute unit at the matrix cores' full rate, and the loads write
+// another 32 of the 128 there are.  So
+//  - the first fragments of a stage are read before the last multiplications of the one before (read behind its barrier they cost a fifth of the
+//    time: 8192 x 2048 x 2 x 5632 336 us, so 327);
+//  - large bf16 tiles are four wavefronts of 128 x 128 (64 and 32 bytes a cycle), one a SIMD.  Nothing else then fills the matrix core while a
+//    wavefront issues reads and loads, so these go between its multiplications one at a time, stages of 32 slots, four deep: 322 us, and the
+//    backward pass's products with what goes before them 727 / 699.  (Not interleaved: 362 and 770.)
 #pragma once
 
 #include "mfma.h"
@@ -99,7 +106,7 @@ struct Operand {
 // column 32 j + 8 (e / 4) + 4 (lane / 32) + e % 4 of B_b's.
 template <typename T, int NB, int TM, int TN, int WR, int WC, int BK, int STAGES, bool A_STRIDED, bool B_STRIDED, int PIECE>
 struct TileProduct {
-  static constexpr bool INTERLEAVED = TM * NB * TN >= 16;
+  static constexpr bool INTERLEAVED = TM * NB * TN >= 16;   // (else there are other wavefronts on the SIMD, or the loads' latency bounds the block)
   static constexpr int SLOTS = BK, NB_ = NB, TM_ = TM, TN_ = TN, WC_ = WC, WAVES = WR * WC;
   static constexpr int THREADS = 64 * WAVES, BM = 32 * TM * WR, BN = 32 * TN * WC;
   typedef ProductTile<T, BM, BK, A_STRIDED, PIECE> TA;
@@ -182,7 +189,7 @@ struct TileProduct {
         for (int j = 0; j < TN; ++j) bf[to][s][j] = TB::fragment(lb + s * TB::BYTES, (wc * TN + j) * 32, q * STEP, lane);
     };
     if constexpr (INTERLEAVED) {
-      // One wavefront a SIMD: the next step's fragments and the next stages' loads go between the multiplications, one at a time.
+      // The next step's fragments, then the loads, between the multiplications.
       constexpr int MF = TM * NB * TN, FR = TM + NB * TN, LOADS = PER_STAGE / Q;
       static_assert(LOADS * Q == PER_STAGE && FR + 2 * LOADS <= MF && STAGES >= 3, "room between the multiplications");
       auto fetch_one = [&](const char* la, int q, int to, int f) {
@@ -214,9 +221,11 @@ struct TileProduct {
 #pragma unroll
         for (int q = 0; q < Q; ++q) {
           if (q + 1 == Q) {
+            // this wavefront has read stage t, and its loads of stage t + 1 are there: behind them only stage t + 2 and what went of t + 3
             __builtin_amdgcn_s_waitcnt(LDS_READS_DONE);
             __builtin_amdgcn_sched_barrier(0);
             if constexpr (KIND != 0) {
+              static_assert(STAGES == 4, "the stages behind it");
               wait_loads<(STAGES - 3) * PER_STAGE + (Q - 1) * LOADS>();
               block_barrier();
             } else if (t + 1 < nk) {
@@ -276,9 +285,9 @@ struct TileProduct {
           __builtin_amdgcn_s_waitcnt(LDS_READS_DONE);
           __builtin_amdgcn_sched_barrier(0);
           if (t + 1 < nk) {
-          read = read == (STAGES - 1) * STAGE_BYTES ? 0 : read + STAGE_BYTES;
-          arrived(t + 1);
-          fetch(lds + read, 0, 0);
+            read = read == (STAGES - 1) * STAGE_BYTES ? 0 : read + STAGE_BYTES;
+            arrived(t + 1);
+            fetch(lds + read, 0, 0);
           }
         }
         __builtin_amdgcn_sched_barrier(0);
