@@ -12,7 +12,7 @@ from typing import NamedTuple, Optional, Tuple
 
 import torch
 
-from .binding import BF16, F32, AntdtError, DropoutSpec, _stream, lib
+from .binding import BF16, F32, AntdtError, DropoutSpec, _raw_stream, lib
 
 ACTS = {"silu": 0, "gelu": 1, "relu": 2, "sigmoid": 3}
 _DTYPES = {torch.float32: F32, torch.bfloat16: BF16}
@@ -36,11 +36,9 @@ def _check(rc: int):
         raise AntdtError(rc, lib.antdt_last_error(None).decode())
 
 
-def _device(t: torch.Tensor, name: str) -> int:
-    index = t.get_device()
-    if index < 0:
-        raise ValueError(f"{name}: not on the device")
-    return index
+def _stream(device: int) -> int:
+    """Handle of torch's current stream of the operands' device."""
+    return _raw_stream(device) if _raw_stream is not None else torch.cuda.current_stream(device).cuda_stream
 
 
 def _rows(t: torch.Tensor, name: str, rows: int, cols: int, dtype: torch.dtype, device: int) -> int:
@@ -59,11 +57,16 @@ def _rows(t: torch.Tensor, name: str, rows: int, cols: int, dtype: torch.dtype, 
 
 def _matrix(t: torch.Tensor, name: str) -> Tuple[int, int, int, int]:
     """(rows, columns, leading dimension, device) of a call's first matrix."""
-    shape = t.shape
+    shape, s = t.shape, t.stride()
     if len(shape) != 2 or t.dtype not in _DTYPES:
         raise ValueError(f"{name}: a matrix of float32 or bfloat16, not {tuple(shape)} of {t.dtype}")
-    device = _device(t, name)
-    return shape[0], shape[1], _rows(t, name, shape[0], shape[1], t.dtype, device), device
+    device = t.get_device()
+    if device < 0:
+        raise ValueError(f"{name}: not on the device")
+    rows, cols = shape
+    if s[1] != 1 and cols > 1:
+        raise ValueError(f"{name}: columns of a row must be neighbours")
+    return rows, cols, s[0] if rows > 1 else max(s[0], cols), device
 
 
 def _vector(t: torch.Tensor, name: str, n: int, dtype: torch.dtype, device: int) -> int:
@@ -109,7 +112,7 @@ def dropout(x: torch.Tensor, drop: Dropout, residual: Optional[torch.Tensor] = N
         ldr, rp = _rows(residual, "residual", rows, cols, dt, dev), residual.data_ptr()
     ldo = _rows(out, "out", rows, cols, dt, dev)
     _check(lib.antdt_dropout(x.data_ptr(), ldx, rp, ldr, rows, cols, _DTYPES[dt], drop._ref, out.data_ptr(), ldo,
-                             _stream()))
+                             _stream(dev)))
     return out
 
 
@@ -126,7 +129,7 @@ def token_lookup(table: torch.Tensor, tokens: torch.Tensor, scale: float = 1.0, 
         raise ValueError(f"out: {odt}")
     ldo = _rows(out, "out", N, D, odt, dev)
     _check(lib.antdt_token_lookup(table.data_ptr(), ldt, V, D, _DTYPES[table.dtype], tp, N, scale,
-                                  None if dropout is None else dropout._ref, out.data_ptr(), ldo, _DTYPES[odt], _stream()))
+                                  None if dropout is None else dropout._ref, out.data_ptr(), ldo, _DTYPES[odt], _stream(dev)))
     return out
 
 
@@ -145,7 +148,7 @@ def token_gradient(dy: torch.Tensor, tokens: torch.Tensor, rows: int, scale: flo
     ws, n = _workspace(workspace, _bytes("antdt_token_gradient_bytes", N, rows, D), dy)
     _check(lib.antdt_token_gradient(dy.data_ptr(), ldd, _DTYPES[dy.dtype], tp, N, scale,
                                     None if dropout is None else dropout._ref, out.data_ptr(), ldg, rows, D,
-                                    1 if accumulate else 0, ws, n, _stream()))
+                                    1 if accumulate else 0, ws, n, _stream(dev)))
     return out
 
 
@@ -185,7 +188,7 @@ def gated_forward(x: torch.Tensor, wg: torch.Tensor, wu: torch.Tensor, act: str 
     ws, n = _workspace(workspace, _bytes("antdt_gated_forward_bytes", N, K, H, _DTYPES[dt]), x)
     _check(lib.antdt_gated_forward(x.data_ptr(), ldx, wg.data_ptr(), wu.data_ptr(), ldw, N, K, H, _DTYPES[dt], ACTS[act],
                                    out.data_ptr(), ldh, None if saved is None else _saved(saved, N, H, dt, dev), ws, n,
-                                   _stream()))
+                                   _stream(dev)))
     return out
 
 
@@ -206,7 +209,7 @@ def gated_backward(dh: torch.Tensor, x: torch.Tensor, wg: torch.Tensor, wu: torc
     ws, n = _workspace(workspace, _bytes("antdt_gated_backward_bytes", N, K, H, _DTYPES[dt]), x)
     _check(lib.antdt_gated_backward(dh.data_ptr(), ldd, x.data_ptr(), ldx, wg.data_ptr(), wu.data_ptr(), ldw, N, K, H,
                                     _DTYPES[dt], _saved(saved, N, H, dt, dev), dx.data_ptr(), lddx, dwg.data_ptr(),
-                                    dwu.data_ptr(), lddw, ws, n, _stream()))
+                                    dwu.data_ptr(), lddw, ws, n, _stream(dev)))
     return dx, dwg, dwu
 
 
@@ -243,7 +246,7 @@ def token_logprobs(logits: torch.Tensor, tokens: Optional[torch.Tensor] = None, 
     else:
         top_logp = top_index = None
     _check(lib.antdt_token_logprobs(logits.data_ptr(), ld, N, V, _DTYPES[logits.dtype], tp, lp if given else None, ep, sp, top,
-                                    tl, ti, ws, n, _stream()))
+                                    tl, ti, ws, n, _stream(dev)))
     return LogProbs(logp, entropy, stats, top_logp, top_index)
 
 
@@ -261,5 +264,5 @@ def token_logprobs_gradient(logits: torch.Tensor, tokens: Optional[torch.Tensor]
     _check(lib.antdt_token_logprobs_gradient(
         logits.data_ptr(), ld, N, V, _DTYPES[dt], None if tokens is None else _vector(tokens, "tokens", N, torch.int32, dev),
         stats.data_ptr(), None if d_logp is None else _vector(d_logp, "d_logp", N, f32, dev),
-        None if d_entropy is None else _vector(d_entropy, "d_entropy", N, f32, dev), out.data_ptr(), ldd, _stream()))
+        None if d_entropy is None else _vector(d_entropy, "d_entropy", N, f32, dev), out.data_ptr(), ldd, _stream(dev)))
     return out

@@ -482,3 +482,61 @@ def test_refusals_of_tensors():
                                          torch.zeros(12, 8, device=DEV).bfloat16())):
         with pytest.raises(A.AntdtError):
             call()
+
+
+@pytest.mark.parametrize("N,K,H", [(8192, 8, 2048), (8200, 32, 2056), (8192, 40, 2048), (8192, 72, 4096), (8192, 104, 2048), (8192, 136, 2048), (8, 8192, 4096),
+                                   (40, 4096, 8192)])
+def test_gated_with_few_contraction_slots(N, K, H):
+    """Large tiles whose products end before, at and behind the stages their pipeline is filled with."""
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(K)
+    x, wg, wu, dh = (torch.randn(*s, device=DEV, generator=gen).mul_(v).bfloat16()
+                     for s, v in (((N, K), 1), ((K, H), K ** -0.5), ((K, H), K ** -0.5), ((N, H), 1)))
+    saved = A.gated_saved(x, wg)
+    h = A.gated_forward(x, wg, wu, "sigmoid", saved=saved)
+    got = (h,) + A.gated_backward(dh, x, wg, wu, saved)
+    X, G, U, D = x.double(), wg.double(), wu.double(), dh.double()
+    s, u = torch.sigmoid(X @ G), X @ U
+    dg, du = D * u * s * (1 - s), D * s
+    want = (s * u, dg @ G.t().contiguous() + du @ U.t().contiguous(), X.t().contiguous() @ dg, X.t().contiguous() @ du)
+    for name, a, b in zip(("h", "dx", "dwg", "dwu"), got, want):
+        off = a.double() - b
+        for r in range(0, b.shape[0], 256):      # (a rounding of dz and one of the result)
+            for c in range(0, b.shape[1], 256):
+                assert float(off[r:r + 256, c:c + 256].norm()) <= 4 * F.HALF["bf16"] * float(b[r:r + 256, c:c + 256].norm()), (name, r, c)
+
+
+def test_logprobs_without_rows_and_with_a_workspace():
+    none = A.token_logprobs(torch.empty(0, 40, device=DEV), ints([]), 3)
+    assert none.logp.shape == (0,) and none.entropy.shape == (0,) and none.stats.shape == (0, 4)
+    assert none.top_logp.shape == (0, 3) and none.top_index.shape == (0, 3) and none.top_index.dtype == torch.int32
+    x = torch.randn(2, 100003, device=DEV)
+    want = A.token_logprobs(x, ints([5, -1]), 9)
+    given = A.token_logprobs(x, ints([5, -1]), 9, workspace=torch.full((1 << 20,), 255, dtype=torch.uint8, device=DEV))
+    for a, b in zip(want, given):
+        assert torch.equal(a, b) and a.is_contiguous()
+    with pytest.raises(A.AntdtError):
+        A.token_logprobs(x, None, 9, workspace=torch.empty(256, dtype=torch.uint8, device=DEV))
+    with pytest.raises(A.AntdtError):
+        A.token_logprobs(x, None, -1)
+
+
+@pytest.mark.parametrize("top", [3, 6, 9, 40])
+@pytest.mark.parametrize("V", [2000, 30000, 100000])
+def test_top_of_logits_far_apart_and_alike(top, V):
+    """Where the distance from the largest logit decides least: all of a row equal (and not allowed), one far above the rest, logits over the
+    type's whole range, negative ones, and values next to each other."""
+    rng = np.random.default_rng(V + top)
+    x = rng.normal(size=(8, V))
+    x[0] = -np.inf
+    x[1] = 7.25
+    x[2, V // 3] = 1e30
+    x[3] = np.sign(x[3]) * 10.0 ** rng.uniform(-37, 38, V)
+    x[4] = -np.abs(x[4]) * 1e-30
+    x[5] = 1 + rng.integers(0, 50, V) * 2.0 ** -23
+    x[6, rng.random(V) < 0.999] = -np.inf
+    x[7] = np.where(rng.random(V) < 0.5, torch.finfo(torch.float32).min, 0.0)
+    dx = strided(x, "f32", 1, 1)
+    f = F.logprobs(host(dx), np.zeros(8, np.int64), top)
+    r = A.token_logprobs(dx, None, top)
+    assert np.array_equal(host(r.top_index).astype(np.int64), f["top_index"])
