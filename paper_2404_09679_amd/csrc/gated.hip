@@ -279,7 +279,9 @@ struct ForwardOp {
 // weights at a time as its other lanes make; products and sums in fp32 on the vector units, the lanes' sums added up at the end.
 // By tiles / here, us: bf16 1 and 2 tokens of 1024-4096 7.7 / 5.5 and 6.0, 4 of 2048-5632 14.6 / 17.7; fp32 8 of 1024-4096 18.4 / 12.1, of 4096-14336
 // 145 / 129.
-constexpr int FEW_THREADS = 256;
+// Blocks of 256 / 512 / 1024 threads, other weights every time (the more loads under way the better): 1 token bf16 1024-4096 6.7 / 6.5 / 6.7, 2048-5632
+// 17.0 / 15.4 / 15.5, 4096-14336 53 / 47 / 51; fp32 8 of 2048-5632 53 / 35 / 28.
+constexpr int FEW_THREADS = 512;
 constexpr int few_tokens(size_t element) { return element == 4 ? 8 : 2; }
 
 // The sums of v[0 .. COUNT) over the lanes that differ in bits O and above: at every step a lane keeps one half of the values and hands
@@ -726,11 +728,15 @@ hipError_t launch_few(const GatedArgs& a, hipStream_t s) {
   }
   return hipGetLastError();
 }
-// Lanes along H: as many (128 bytes of a row at most) as leave 150 blocks.  1 token, 2 / 4 / 8 lanes, us: bf16 1024-4096 5.5 / 5.4 / 7.3,
-// 2048-5632 16.3 / 13.8 / 19.0, 4096-14336 8 lanes 39.2, 4 44.5; fp32 2048-5632 4 lanes 22.6, 8 18.2.
+// Lanes along H: as many (128 bytes of a row; of fp32 and up to four tokens 256) as leave 150 blocks.  1 token, us: bf16, blocks of 256 threads,
+// 2 / 4 / 8 lanes 1024-4096 5.5 / 5.4 / 7.3, 2048-5632 16.3 / 13.8 / 19.0; fp32 2048-5632 4 lanes 22.6, 8 18.2; of 512 threads, other weights every time,
+// 8 / 16 lanes fp32 4096-14336 101 / 80 (8 tokens 103 / 118), bf16 2048-5632 4 / 8 lanes 15.5 / 17.8.
 template <typename T>
 hipError_t launch_few(const GatedArgs& a, hipStream_t s) {
   constexpr int VN = 16 / sizeof(T), ENOUGH = 150;
+  if constexpr (sizeof(T) == 4) {
+    if (a.N <= 4 && a.H / (16 * VN) >= ENOUGH) return launch_few<T, 16>(a, s);
+  }
   if (a.H / (8 * VN) >= ENOUGH) return launch_few<T, 8>(a, s);
   if (a.H / (4 * VN) >= ENOUGH) return launch_few<T, 4>(a, s);
   return launch_few<T, 2>(a, s);

@@ -540,3 +540,19 @@ def test_top_of_logits_far_apart_and_alike(top, V):
     f = F.logprobs(host(dx), np.zeros(8, np.int64), top)
     r = A.token_logprobs(dx, None, top)
     assert np.array_equal(host(r.top_index).astype(np.int64), f["top_index"])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("N", [1, 2, 3, 4, 5, 8, 9])
+@pytest.mark.parametrize("K,H", [(48, 9736), (1104, 2408)])
+def test_gated_of_a_few_tokens_and_wide_blocks(N, K, H, dtype):
+    """The ways to share out a few tokens' columns, with columns behind the last whole share."""
+    rng = np.random.default_rng(N + H)
+    x, wg, wu, _ = gated_inputs(rng, N, K, H, dtype, 8, 8)
+    f = F.gated(host(x), host(wg), host(wu), "silu", F.HALF[dtype])
+    saved = A.gated_saved(x, wg)
+    h = A.gated_forward(x, wg, wu, "silu", saved=saved)
+    within(h, f["h"], f["eh"], "h")
+    p, r = saved.view(torch.float32).view(2, N, H)
+    within(p, f["p"], f["ep"], "act(g)")
+    within(r, f["u"] * f["r"], f["er"] * (np.abs(f["u"]) + f["eu"]) + np.abs(f["r"]) * f["eu"] + F.U32 * np.abs(f["u"] * f["r"]), "u act'(g)")
