@@ -56,9 +56,10 @@ __device__ __forceinline__ void wave_order() {
 // memory in the order of the accumulators and are added up, in order, by a second launch.
 struct Split {
   int32_t tiles_m, tiles_n, whole, parts, len;   // len: contraction slots of a part
+  int32_t halves;                                // the others by two blocks of half the rows each instead (see halves_kernel)
   float* partial;
   __host__ __device__ int rest() const { return tiles_m * tiles_n - whole; }
-  __host__ __device__ int blocks() const { return whole + rest() * parts; }
+  __host__ __device__ int blocks() const { return whole + rest() * (halves ? 2 : parts); }
 };
 
 // Place of block i of n in the order of the work: an XCD (block i runs on XCD i mod 8) has a share of consecutive places.
@@ -124,6 +125,21 @@ __device__ __forceinline__ void zero(A& acc) {
 // A product is described by an Op: P, its tiles; Args; product(), the sums of contraction slots [k0, k1) of a tile; finish(), what becomes
 // of a tile's sums.
 template <typename Op>
+__device__ __forceinline__ void finish_tile(const typename Op::Args& a, int tm, int tn, char* lds, const typename Op::P::Acc& acc) {
+  typedef typename Op::P P;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  float* st = reinterpret_cast<float*>(lds) + wave * (32 * (32 * P::TN_ + 4));
+#pragma unroll
+  for (int i = 0; i < P::TM_; ++i) {
+    f32x16 x[P::NB_][P::TN_];
+#pragma unroll
+    for (int q = 0; q < P::NB_; ++q)
+#pragma unroll
+      for (int j = 0; j < P::TN_; ++j) x[q][j] = acc[q][i][j];
+    Op::finish(a, tm, tn, wave, i, st, x);
+  }
+}
+template <typename Op>
 __device__ __forceinline__ void tile_block(const typename Op::Args& a, const Split& sp, int block, char* lds) {
   typedef typename Op::P P;
   int t, part = -1;
@@ -141,17 +157,7 @@ __device__ __forceinline__ void tile_block(const typename Op::Args& a, const Spl
   const int length = Op::contraction(a);
   Op::product(a, tm, tn, part < 0 ? 0 : part * sp.len, part < 0 ? length : min((part + 1) * sp.len, length), lds, acc);
   if (part < 0) {
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    float* st = reinterpret_cast<float*>(lds) + wave * (32 * (32 * P::TN_ + 4));
-#pragma unroll
-    for (int i = 0; i < P::TM_; ++i) {
-      f32x16 x[P::NB_][P::TN_];
-#pragma unroll
-      for (int q = 0; q < P::NB_; ++q)
-#pragma unroll
-        for (int j = 0; j < P::TN_; ++j) x[q][j] = acc[q][i][j];
-      Op::finish(a, tm, tn, wave, i, st, x);
-    }
+    finish_tile<Op>(a, tm, tn, lds, acc);
   } else {
     constexpr int N16 = (int)(sizeof(acc) / sizeof(f32x16));
     const f32x16* x = reinterpret_cast<const f32x16*>(&acc);
@@ -197,6 +203,31 @@ template <typename Op>
 __global__ __launch_bounds__(Op::P::THREADS) void tile_kernel(typename Op::Args a, Split sp) {
   extern __shared__ __attribute__((aligned(16))) char lds[];
   tile_block<Op>(a, sp, blockIdx.x, lds);
+}
+// Tiles of Op, and of those behind the last whole filling of the chip the upper and lower halves, tiles of Half.  The upper halves come first and the lower
+// ones last: that halves what the last filling costs, without partial sums, and from then on some compute units write the results of a tile (10 bytes an
+// element where they are saved) while others multiply.
+template <typename Op, typename Half>
+__global__ __launch_bounds__(Op::P::THREADS) void halves_kernel(typename Op::Args a, Split sp) {
+  extern __shared__ __attribute__((aligned(16))) char lds[];
+  const int rest = sp.rest(), block = blockIdx.x;
+  int tm, tn;
+  if (block >= rest && block < rest + sp.whole) {
+    typename Op::P::Acc acc;
+    zero(acc);
+    tile_at(xcd_order(block - rest, sp.whole), sp.tiles_m, sp.tiles_n, tm, tn);
+    Op::product(a, tm, tn, 0, Op::contraction(a), lds, acc);
+    finish_tile<Op>(a, tm, tn, lds, acc);
+  } else {
+    const int lower = block >= rest;
+    typename Half::P::Acc acc;
+    zero(acc);
+    tile_at(sp.whole + (lower ? block - sp.whole - rest : block), sp.tiles_m, sp.tiles_n, tm, tn);
+    tm = 2 * tm + lower;
+    if (tm * Half::P::BM >= Op::rows(a)) return;
+    Half::product(a, tm, tn, 0, Op::contraction(a), lds, acc);
+    finish_tile<Half>(a, tm, tn, lds, acc);
+  }
 }
 template <typename Op>
 __global__ __launch_bounds__(64 * JOIN_WAVES) void join_kernel(typename Op::Args a, Split sp) {
@@ -244,6 +275,7 @@ struct ForwardOp {
   typedef P_ P;
   typedef GatedArgs Args;
   static __device__ __forceinline__ int contraction(const Args& a) { return (int)a.K; }
+  static __device__ __forceinline__ int64_t rows(const Args& a) { return a.N; }
   static __device__ __forceinline__ void product(const Args& a, int tm, int tn, int k0, int k1, char* lds, typename P::Acc& acc) {
     const Operand w[2] = {operand<T, true>(a.wg, a.ldw, a.H, tn * P::BN, k0), operand<T, true>(a.wu, a.ldw, a.H, tn * P::BN, k0)};
     P::run(operand<T, false>(a.x, a.ldx, a.N, tm * P::BM, k0), w, k1 - k0, lds, acc);
@@ -482,6 +514,7 @@ TILING(F32_64_ANY, float, 1, 1, 2, 2, 32, 3, 4)
 #undef TILING
 
 constexpr int COMPUTE_UNITS = 256, MOST_PARTS = 16;
+constexpr double HALF_TILE = 0.75;   // of a tile's time
 constexpr double JOIN_US = 6.0, PARTIAL_BYTES_PER_US = 2e6;   // a further launch; the sums written and read again
 
 struct Jobs {   // of one length, in the order they are handed out
@@ -590,6 +623,7 @@ Plan plan_of(int cls, int NB, const Job (&job)[2]) {
       Split& s = p.split[q];
       s.whole = (int)(tiles[q] - rest[q]);
       s.parts = 1;
+      s.halves = 0;
       part_len[q] = s.len = (int)len[q];
       if (rest[q] == 0) continue;
       part_len[q] = s.len = (int)(div_up(div_up(len[q], parts[q]), c.slots) * c.slots);
@@ -611,6 +645,20 @@ Plan plan_of(int cls, int NB, const Job (&job)[2]) {
       if (last) offer(0, 1, rest, parts);
       else offer(rest, parts, 0, 1);
     }
+  // Those by halves.  Saving, in parts or whole / by halves, us: 8192 tokens of 2048-5632 (128 left over) 384 / 364, 6500 of 520-1704 (108) 55 / 45, 8192 of
+  // 1024-1408 (96) 70 / 61; of few the contraction's parts cost less: 5000 of 640-2048 (64) 44 / 48, 3000 of 1024-3200 (44) 58 / 62.
+  if (cls == BF16_256 && NB == 2 && rest > places / 4 && rest <= places / 2 && all > places) {
+    Plan p = best;
+    p.bytes = 0;
+    Split& s = p.split[0];
+    s.whole = (int)(all - rest);
+    s.parts = 1;
+    s.len = (int)len[0];
+    s.halves = 1;
+    const double half = HALF_TILE * us(len[0]);
+    p.us = end({{rest, half}, {s.whole, us(len[0])}, {rest, half}});
+    if (p.us < best.us) best = p;
+  }
   // all of those that take longer than an equal share of the work
   const double each = std::max((double)(tiles[0] * len[0] + tiles[1] * len[1]) / places, 4.0 * c.slots);
   if (len[0] > each || len[1] > each)
@@ -689,6 +737,17 @@ hipError_t launch_op(const typename Op::Args& a, const Split& sp, hipStream_t s)
                      sp);
   return hipGetLastError();
 }
+template <typename Op, typename Half>
+hipError_t launch_halves(const typename Op::Args& a, const Split& sp, hipStream_t s) {
+  typedef typename Op::P P;
+  static_assert(P::THREADS == Half::P::THREADS && P::BM == 2 * Half::P::BM && P::BN == Half::P::BN && P::LDS_BYTES >= Half::P::LDS_BYTES &&
+                    staging<typename Half::P>(P::WAVES) <= P::LDS_BYTES, "halves of the same tiles");
+  static std::atomic<uint64_t> allowed{0};
+  const hipError_t e = allow_lds(halves_kernel<Op, Half>, P::LDS_BYTES, 0, allowed);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((halves_kernel<Op, Half>), dim3(sp.blocks()), dim3(P::THREADS), P::LDS_BYTES, s, a, sp);
+  return hipGetLastError();
+}
 template <typename Op1, typename Op2>
 hipError_t launch_pair(const typename Op1::Args& a1, const Split& s1, const typename Op2::Args& a2, const Split& s2, hipStream_t s) {
   typedef typename Op1::P P;
@@ -706,15 +765,24 @@ hipError_t launch_pair(const typename Op1::Args& a1, const Split& s1, const type
   return hipGetLastError();
 }
 
-template <typename G, bool SAVE>
+template <typename G, int ACT, bool SAVE>
 hipError_t launch_forward(const GatedArgs& a, const Split& sp, hipStream_t s) {
   typedef typename G::Product P;
   typedef typename G::Type T;
+  typedef ForwardOp<T, P, G::vec, ACT, SAVE> Op;
+  if constexpr (G::k.rows == 256) {
+    typedef TileProduct<T, 2, 2, 2, 2, 2, 32, 4, false, true, 16> HalfP;
+    if (sp.halves) return launch_halves<Op, ForwardOp<T, HalfP, G::vec, ACT, SAVE>>(a, sp, s);
+  }
+  return launch_op<Op>(a, sp, s);
+}
+template <typename G, bool SAVE>
+hipError_t launch_forward(const GatedArgs& a, const Split& sp, hipStream_t s) {
   switch (a.act) {
-    case ANTDT_ACT_SILU: return launch_op<ForwardOp<T, P, G::vec, ANTDT_ACT_SILU, SAVE>>(a, sp, s);
-    case ANTDT_ACT_GELU: return launch_op<ForwardOp<T, P, G::vec, ANTDT_ACT_GELU, SAVE>>(a, sp, s);
-    case ANTDT_ACT_RELU: return launch_op<ForwardOp<T, P, G::vec, ANTDT_ACT_RELU, SAVE>>(a, sp, s);
-    default: return launch_op<ForwardOp<T, P, G::vec, ANTDT_ACT_SIGMOID, SAVE>>(a, sp, s);
+    case ANTDT_ACT_SILU: return launch_forward<G, ANTDT_ACT_SILU, SAVE>(a, sp, s);
+    case ANTDT_ACT_GELU: return launch_forward<G, ANTDT_ACT_GELU, SAVE>(a, sp, s);
+    case ANTDT_ACT_RELU: return launch_forward<G, ANTDT_ACT_RELU, SAVE>(a, sp, s);
+    default: return launch_forward<G, ANTDT_ACT_SIGMOID, SAVE>(a, sp, s);
   }
 }
 template <typename T, int LANES>

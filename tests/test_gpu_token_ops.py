@@ -556,3 +556,25 @@ def test_gated_of_a_few_tokens_and_wide_blocks(N, K, H, dtype):
     p, r = saved.view(torch.float32).view(2, N, H)
     within(p, f["p"], f["ep"], "act(g)")
     within(r, f["u"] * f["r"], f["er"] * (np.abs(f["u"]) + f["eu"]) + np.abs(f["r"]) * f["eu"] + F.U32 * np.abs(f["u"] * f["r"]), "u act'(g)")
+
+
+@pytest.mark.parametrize("N,K,H", [(8292, 512, 1160), (8192, 1024, 1408), (6500, 520, 1704), (2048, 2048, 4224)])
+def test_gated_with_a_partly_filled_last_round_of_tiles(N, K, H):
+    """More tiles than compute units: what is left over, by halves or in parts, row by row and column by column."""
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(N)
+    x, wg, wu = (torch.randn(*s, device=DEV, generator=gen).mul_(v).bfloat16() for s, v in (((N, K), 1), ((K, H), K ** -0.5), ((K, H), K ** -0.5)))
+    saved = A.gated_saved(x, wg)
+    saved.view(torch.float32).fill_(float("nan"))
+    out = torch.full((N, H), float("nan"), device=DEV).bfloat16()
+    h = A.gated_forward(x, wg, wu, "silu", out=out, saved=saved)
+    g, u = x.double() @ wg.double(), x.double() @ wu.double()
+    s = torch.sigmoid(g)
+    p, r = saved.view(torch.float32).view(2, N, H)
+    # sums of K products of random signs in fp32 are off by about sqrt(K) roundings; an element's by 16 times that at most, relative to the row's and column's norms
+    off = 16 * (K + 16) ** 0.5 * F.U32 * 1.2
+    for name, got, want in (("P", p, g * s), ("R", r, u * s * (1 + g * (1 - s)))):
+        assert bool(((got.double() - want).abs() <= off * (1 + want.abs()) * 8).all()), name
+    want = g * s * u
+    assert bool(((h.double() - want).abs() <= F.HALF["bf16"] * want.abs() + off * (1 + want.abs()) * 64).all())
+    assert torch.equal(A.gated_forward(x, wg, wu, "silu"), h)
