@@ -3,7 +3,8 @@
 // Forward: a block multiplies a tile of x with the same columns of Wg and Wu, so that a lane holds both projections of an element of
 // h and forms it in its registers; neither projection goes to memory.  For the backward pass it also stores
 //   P = act(g),  R = u act'(g)    (fp32: dg = dh R and du = dh P are then rounded once)
-// Backward: dz = [dh R | dh P] [N, 2H] (operands of the products, in the type of x), then
+// Backward: dz = [dh R | dh P] [N, 2H], rounded to the type of x (the matrix cores multiply bf16 operands; from exact dz the gradients would be off
+// by the results' own rounding, 0.0017 of their norm, so by 0.0023), then
 //   dx = dz [Wg | Wu]^T,   dWg = x^T dz[:, :H],   dWu = x^T dz[:, H:],
 // the weights, x and dz read as they lie in memory.
 #include <algorithm>
@@ -399,7 +400,8 @@ __global__ __launch_bounds__(FEW_THREADS) void gated_few_kernel(GatedArgs a) {
   }
 }
 
-// dz = [dh R | dh P], [N, 2H].
+// dz = [dh R | dh P], [N, 2H].  Bound by memory: 8192 x 5632 bf16 102 us (6.3 TB/s).  A launch of its own, because a product would form every element
+// again for each of its 8 or 22 tiles along the other side.
 struct DzArgs {
   const void* dh;
   const float* saved;
@@ -427,6 +429,7 @@ __global__ __launch_bounds__(256) void gated_dz_kernel(DzArgs a) {
   }
 }
 
+// The backward products of 8192 tokens of 2048-5632: 583-600 us in one launch (1.26-1.3 PFLOP/s; matrix cores busy 74 % of the cycles).
 // dx = dz [Wg | Wu]^T, a contraction over the columns of one and then of the other.
 struct DxArgs {
   const void* dz;

