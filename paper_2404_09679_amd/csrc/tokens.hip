@@ -263,7 +263,9 @@ __global__ __launch_bounds__(256) void token_sum_kernel(GradArgs a, bool vec_gra
 
 // Runs over several blocks of the first launch (`chunks` here): those over up to JOIN_FEW more are added up by the lanes of the chunk where
 // they start, the others by a whole block.  (Bound by the chains of loads: how far a run goes is asked by all lanes at once.)
-constexpr int JOIN_THREADS = 1024, JOIN_FEW = 32;
+// Lookup and gradient with blocks of 1024 / 512 / 256 / 128 threads, us: 131072 tokens of 200000 x 256 bf16 126.1 / 125.5 / 125.2 / 126.4, 100000 of 1000000 x
+// 32 fp32 98.5 / 94 / 90 / 89; JOIN_FEW 8 / 16 / 32 / 64 (1024 threads) 131.6 / 129.3 / 128.4 / 126.4 and 122.9 / 99.5 / 99.8 / 89.4 (of 256 no different).
+constexpr int JOIN_THREADS = 256, JOIN_FEW = 32;
 template <bool ACCUMULATE>
 __global__ __launch_bounds__(JOIN_THREADS) void token_join_kernel(GradArgs a, bool vec_grad) {
   extern __shared__ float part[];   // [groups][8 lanes]
