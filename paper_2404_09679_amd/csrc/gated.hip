@@ -207,7 +207,8 @@ __global__ __launch_bounds__(Op::P::THREADS) void tile_kernel(typename Op::Args 
 }
 // Tiles of Op, and of those behind the last whole filling of the chip the upper and lower halves, tiles of Half.  The upper halves come first and the lower
 // ones last: that halves what the last filling costs, without partial sums, and from then on some compute units write the results of a tile (10 bytes an
-// element where they are saved) while others multiply.
+// element where they are saved) while others multiply.  (The upper halves to four XCDs and the lower ones to the others, so that the blocks of an XCD stay at
+// the same contraction slots: 8192 tokens of 2048-5632 saving 378 / 382 us.)
 template <typename Op, typename Half>
 __global__ __launch_bounds__(Op::P::THREADS) void halves_kernel(typename Op::Args a, Split sp) {
   extern __shared__ __attribute__((aligned(16))) char lds[];
