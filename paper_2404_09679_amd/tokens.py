@@ -81,16 +81,18 @@ def _new(shape: Tuple[int, ...], dtype: torch.dtype, like: torch.Tensor) -> torc
     return torch.empty_strided(shape, (shape[1], 1) if len(shape) == 2 else (1,), dtype=dtype, device=like.device)
 
 
-def _workspace(workspace: Optional[torch.Tensor], nbytes: int, like: torch.Tensor) -> Tuple[Optional[int], int]:
-    """(address, bytes) of the caller's workspace, or of a new one; torch's blocks start at multiples of 512 bytes.  A new
-    one goes back to torch's allocator when the call returns, which hands it on in the order of the stream."""
+def _workspace(workspace: Optional[torch.Tensor], nbytes: int,
+               like: torch.Tensor) -> Tuple[Optional[torch.Tensor], Optional[int], int]:
+    """(tensor, address, bytes) of the caller's workspace, or of a new one; torch's blocks start at multiples of 512 bytes.
+    The caller holds on to the tensor until the kernels are enqueued: from then on torch's allocator hands a block that
+    is given back on in the order of the stream, before that to any thread."""
     if workspace is None:
         if nbytes == 0:
-            return None, 0
+            return None, None, 0
         workspace = _new((nbytes,), torch.uint8, like)
     elif workspace.device != like.device or not workspace.is_contiguous():
         raise ValueError("workspace: contiguous, on the operands' device")
-    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    return workspace, workspace.data_ptr(), workspace.numel() * workspace.element_size()
 
 
 @lru_cache(maxsize=4096)
@@ -145,7 +147,7 @@ def token_gradient(dy: torch.Tensor, tokens: torch.Tensor, rows: int, scale: flo
             raise ValueError("token_gradient: accumulate needs out")
         out = _new((rows, D), torch.float32, dy)
     ldg = _rows(out, "out", rows, D, torch.float32, dev)
-    ws, n = _workspace(workspace, _bytes("antdt_token_gradient_bytes", N, rows, D), dy)
+    held, ws, n = _workspace(workspace, _bytes("antdt_token_gradient_bytes", N, rows, D), dy)
     _check(lib.antdt_token_gradient(dy.data_ptr(), ldd, _DTYPES[dy.dtype], tp, N, scale,
                                     None if dropout is None else dropout._ref, out.data_ptr(), ldg, rows, D,
                                     1 if accumulate else 0, ws, n, _stream(dev)))
@@ -185,7 +187,7 @@ def gated_forward(x: torch.Tensor, wg: torch.Tensor, wu: torch.Tensor, act: str 
     if out is None:
         out = _new((N, H), dt, x)
     ldh = _rows(out, "out", N, H, dt, dev)
-    ws, n = _workspace(workspace, _bytes("antdt_gated_forward_bytes", N, K, H, _DTYPES[dt]), x)
+    held, ws, n = _workspace(workspace, _bytes("antdt_gated_forward_bytes", N, K, H, _DTYPES[dt]), x)
     _check(lib.antdt_gated_forward(x.data_ptr(), ldx, wg.data_ptr(), wu.data_ptr(), ldw, N, K, H, _DTYPES[dt], ACTS[act],
                                    out.data_ptr(), ldh, None if saved is None else _saved(saved, N, H, dt, dev), ws, n,
                                    _stream(dev)))
@@ -206,7 +208,7 @@ def gated_backward(dh: torch.Tensor, x: torch.Tensor, wg: torch.Tensor, wu: torc
     lddx, lddw = _rows(dx, "dx", N, K, dt, dev), _rows(dwg, "dwg", K, H, dt, dev)
     if _rows(dwu, "dwu", K, H, dt, dev) != lddw:
         raise ValueError("dwg and dwu: one leading dimension")
-    ws, n = _workspace(workspace, _bytes("antdt_gated_backward_bytes", N, K, H, _DTYPES[dt]), x)
+    held, ws, n = _workspace(workspace, _bytes("antdt_gated_backward_bytes", N, K, H, _DTYPES[dt]), x)
     _check(lib.antdt_gated_backward(dh.data_ptr(), ldd, x.data_ptr(), ldx, wg.data_ptr(), wu.data_ptr(), ldw, N, K, H,
                                     _DTYPES[dt], _saved(saved, N, H, dt, dev), dx.data_ptr(), lddx, dwg.data_ptr(),
                                     dwu.data_ptr(), lddw, ws, n, _stream(dev)))
@@ -234,7 +236,7 @@ def token_logprobs(logits: torch.Tensor, tokens: Optional[torch.Tensor] = None, 
     front = (sum(words) + 63) // 64 * 64
     own = workspace is None
     buf = _new((front + (n // 4 if own else 0),), f32, logits)
-    ws, n = (buf.data_ptr() + 4 * front, n) if own else _workspace(workspace, n, logits)
+    held, ws, n = (buf, buf.data_ptr() + 4 * front, n) if own else _workspace(workspace, n, logits)
     stats, entropy, logp, top_logp, top_index, _ = torch.unsafe_split_with_sizes(buf, words + [buf.shape[0] - sum(words)])
     at = buf.data_ptr()
     sp, ep, lp = at, at + 16 * N, at + 20 * N

@@ -1,0 +1,66 @@
+"""What tokens.py does around the calls of the library, without a GPU: tensors of the host that say they are on a device, and a boundary that
+records what it is given."""
+import weakref
+
+import pytest
+import torch
+
+A = pytest.importorskip("paper_2404_09679_amd", reason="build the library first (python paper_2404_09679_amd/build.py)")
+T = A.tokens
+
+
+class Boundary:
+    """In the library's place: every call is recorded, and `during` runs inside it."""
+
+    def __init__(self):
+        self.calls, self.during = [], lambda: None
+
+    def __getattr__(self, name):
+        def call(*args):
+            self.during()
+            self.calls.append((name, args))
+            return 0
+        return call
+
+
+@pytest.fixture
+def boundary(monkeypatch):
+    b = Boundary()
+    monkeypatch.setattr(T, "lib", b)
+    monkeypatch.setattr(T, "_bytes", lambda call, *sizes: 4096)
+    monkeypatch.setattr(T, "_stream", lambda device: 0)
+    monkeypatch.setattr(torch.Tensor, "get_device", lambda t: 0)
+    return b
+
+
+def calls(dtype=torch.float32):
+    """Every operator once, by name: a function that calls it."""
+    x, w, h = torch.zeros(4, 8, dtype=dtype), torch.zeros(8, 16, dtype=dtype), torch.zeros(4, 16, dtype=dtype)
+    t, f, saved = torch.zeros(4, dtype=torch.int32), torch.zeros(4), torch.zeros(4096, dtype=torch.uint8)
+    drop = A.Dropout(0.5, 1)
+    return {"antdt_dropout": lambda: A.dropout(x, drop, residual=x),
+            "antdt_token_lookup": lambda: A.token_lookup(x, t, dropout=drop),
+            "antdt_token_gradient": lambda: A.token_gradient(x, t, 5, dropout=drop),
+            "antdt_gated_forward": lambda: A.gated_forward(x, w, w, saved=saved),
+            "antdt_gated_backward": lambda: A.gated_backward(h, x, w, w, saved),
+            "antdt_token_logprobs": lambda: A.token_logprobs(x, t, 2),
+            "antdt_token_logprobs_gradient": lambda: A.token_logprobs_gradient(x, t, torch.zeros(4, 4), f, f)}
+
+
+@pytest.mark.parametrize("name", list(calls()))
+def test_buffers_live_until_the_call_returns(boundary, monkeypatch, name):
+    """Results and workspaces that a call makes: one that goes back to torch's allocator before the kernels are enqueued may be another
+    thread's by then."""
+    made, new = [], T._new
+
+    def noted(*args):
+        out = new(*args)
+        made.append(weakref.ref(out))
+        return out
+
+    seen = []
+    monkeypatch.setattr(T, "_new", noted)
+    boundary.during = lambda: seen.append([r() is not None for r in made])
+    calls()[name]()
+    assert [n for n, _ in boundary.calls] == [name]
+    assert made and seen == [[True] * len(made)]
