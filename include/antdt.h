@@ -404,7 +404,8 @@ int antdt_dense_aggregate_adam(float* p, float* m, float* v, const float* const*
 /*
  * Operators on sequences of tokens (ids of items, one row each, not pooled): what a model that reads a
  * user's history and answers with an item needs next to the ranking model.  Context-free: they work on the
- * caller's buffers alone, enqueue their kernels on `stream`, allocate nothing and keep nothing between calls.
+ * caller's buffers alone, enqueue their kernels on `stream`, allocate nothing and keep nothing between calls.  The calling
+ * thread's current device is the one that `stream` and the buffers belong to.
  * Common to all of them:
  *  - matrices are row-major, `ld...` elements from one row to the next, at least the row's length; any alignment
  *    of the element type is accepted (16-byte aligned rows are read and written 16 bytes at a time) unless said

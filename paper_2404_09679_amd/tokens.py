@@ -30,6 +30,12 @@ class Dropout:
                                  None if step is None else step.data_ptr())
         self._ref = C.byref(self._spec)
 
+    def _on(self, device: int):
+        """The spec for a call on `device`, which reads `step`."""
+        if self.step is not None and self.step.get_device() != device:
+            raise ValueError(f"Dropout: step is on {self.step.device}, the operands on device {device}")
+        return self._ref
+
 
 def _check(rc: int):
     if rc:
@@ -39,6 +45,19 @@ def _check(rc: int):
 def _stream(device: int) -> int:
     """Handle of torch's current stream of the operands' device."""
     return _raw_stream(device) if _raw_stream is not None else torch.cuda.current_stream(device).cuda_stream
+
+
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
+def _enqueue(device: int, call, *args):
+    """call(*args, stream) with the operands' device current: torch's default stream has the same handle on every device,
+    and kernels on it go to the current one."""
+    if _current_device() == device:
+        _check(call(*args, _stream(device)))
+    else:
+        with torch.cuda.device(device):
+            _check(call(*args, _stream(device)))
 
 
 def _rows(t: torch.Tensor, name: str, rows: int, cols: int, dtype: torch.dtype, device: int) -> int:
@@ -113,8 +132,8 @@ def dropout(x: torch.Tensor, drop: Dropout, residual: Optional[torch.Tensor] = N
     if residual is not None:
         ldr, rp = _rows(residual, "residual", rows, cols, dt, dev), residual.data_ptr()
     ldo = _rows(out, "out", rows, cols, dt, dev)
-    _check(lib.antdt_dropout(x.data_ptr(), ldx, rp, ldr, rows, cols, _DTYPES[dt], drop._ref, out.data_ptr(), ldo,
-                             _stream(dev)))
+    _enqueue(dev, lib.antdt_dropout, x.data_ptr(), ldx, rp, ldr, rows, cols, _DTYPES[dt], drop._on(dev),
+             out.data_ptr(), ldo)
     return out
 
 
@@ -130,8 +149,8 @@ def token_lookup(table: torch.Tensor, tokens: torch.Tensor, scale: float = 1.0, 
     if odt not in _DTYPES:
         raise ValueError(f"out: {odt}")
     ldo = _rows(out, "out", N, D, odt, dev)
-    _check(lib.antdt_token_lookup(table.data_ptr(), ldt, V, D, _DTYPES[table.dtype], tp, N, scale,
-                                  None if dropout is None else dropout._ref, out.data_ptr(), ldo, _DTYPES[odt], _stream(dev)))
+    _enqueue(dev, lib.antdt_token_lookup, table.data_ptr(), ldt, V, D, _DTYPES[table.dtype], tp, N, scale,
+             None if dropout is None else dropout._on(dev), out.data_ptr(), ldo, _DTYPES[odt])
     return out
 
 
@@ -148,9 +167,9 @@ def token_gradient(dy: torch.Tensor, tokens: torch.Tensor, rows: int, scale: flo
         out = _new((rows, D), torch.float32, dy)
     ldg = _rows(out, "out", rows, D, torch.float32, dev)
     held, ws, n = _workspace(workspace, _bytes("antdt_token_gradient_bytes", N, rows, D), dy)
-    _check(lib.antdt_token_gradient(dy.data_ptr(), ldd, _DTYPES[dy.dtype], tp, N, scale,
-                                    None if dropout is None else dropout._ref, out.data_ptr(), ldg, rows, D,
-                                    1 if accumulate else 0, ws, n, _stream(dev)))
+    _enqueue(dev, lib.antdt_token_gradient, dy.data_ptr(), ldd, _DTYPES[dy.dtype], tp, N, scale,
+             None if dropout is None else dropout._on(dev), out.data_ptr(), ldg, rows, D, 1 if accumulate else 0, ws,
+             n)
     return out
 
 
@@ -188,9 +207,8 @@ def gated_forward(x: torch.Tensor, wg: torch.Tensor, wu: torch.Tensor, act: str 
         out = _new((N, H), dt, x)
     ldh = _rows(out, "out", N, H, dt, dev)
     held, ws, n = _workspace(workspace, _bytes("antdt_gated_forward_bytes", N, K, H, _DTYPES[dt]), x)
-    _check(lib.antdt_gated_forward(x.data_ptr(), ldx, wg.data_ptr(), wu.data_ptr(), ldw, N, K, H, _DTYPES[dt], ACTS[act],
-                                   out.data_ptr(), ldh, None if saved is None else _saved(saved, N, H, dt, dev), ws, n,
-                                   _stream(dev)))
+    _enqueue(dev, lib.antdt_gated_forward, x.data_ptr(), ldx, wg.data_ptr(), wu.data_ptr(), ldw, N, K, H, _DTYPES[dt],
+             ACTS[act], out.data_ptr(), ldh, None if saved is None else _saved(saved, N, H, dt, dev), ws, n)
     return out
 
 
@@ -209,9 +227,9 @@ def gated_backward(dh: torch.Tensor, x: torch.Tensor, wg: torch.Tensor, wu: torc
     if _rows(dwu, "dwu", K, H, dt, dev) != lddw:
         raise ValueError("dwg and dwu: one leading dimension")
     held, ws, n = _workspace(workspace, _bytes("antdt_gated_backward_bytes", N, K, H, _DTYPES[dt]), x)
-    _check(lib.antdt_gated_backward(dh.data_ptr(), ldd, x.data_ptr(), ldx, wg.data_ptr(), wu.data_ptr(), ldw, N, K, H,
-                                    _DTYPES[dt], _saved(saved, N, H, dt, dev), dx.data_ptr(), lddx, dwg.data_ptr(),
-                                    dwu.data_ptr(), lddw, ws, n, _stream(dev)))
+    _enqueue(dev, lib.antdt_gated_backward, dh.data_ptr(), ldd, x.data_ptr(), ldx, wg.data_ptr(), wu.data_ptr(), ldw,
+             N, K, H, _DTYPES[dt], _saved(saved, N, H, dt, dev), dx.data_ptr(), lddx, dwg.data_ptr(), dwu.data_ptr(),
+             lddw, ws, n)
     return dx, dwg, dwu
 
 
@@ -247,8 +265,8 @@ def token_logprobs(logits: torch.Tensor, tokens: Optional[torch.Tensor] = None, 
         top_logp, top_index = top_logp.view(N, k), top_index.view(torch.int32).view(N, k)
     else:
         top_logp = top_index = None
-    _check(lib.antdt_token_logprobs(logits.data_ptr(), ld, N, V, _DTYPES[logits.dtype], tp, lp if given else None, ep, sp, top,
-                                    tl, ti, ws, n, _stream(dev)))
+    _enqueue(dev, lib.antdt_token_logprobs, logits.data_ptr(), ld, N, V, _DTYPES[logits.dtype], tp,
+             lp if given else None, ep, sp, top, tl, ti, ws, n)
     return LogProbs(logp, entropy, stats, top_logp, top_index)
 
 
@@ -263,8 +281,8 @@ def token_logprobs_gradient(logits: torch.Tensor, tokens: Optional[torch.Tensor]
     if out is None:
         out = _new((N, V), dt, logits)
     ldd = _rows(out, "out", N, V, dt, dev)
-    _check(lib.antdt_token_logprobs_gradient(
-        logits.data_ptr(), ld, N, V, _DTYPES[dt], None if tokens is None else _vector(tokens, "tokens", N, torch.int32, dev),
-        stats.data_ptr(), None if d_logp is None else _vector(d_logp, "d_logp", N, f32, dev),
-        None if d_entropy is None else _vector(d_entropy, "d_entropy", N, f32, dev), out.data_ptr(), ldd, _stream(dev)))
+    _enqueue(dev, lib.antdt_token_logprobs_gradient, logits.data_ptr(), ld, N, V, _DTYPES[dt],
+             None if tokens is None else _vector(tokens, "tokens", N, torch.int32, dev), stats.data_ptr(),
+             None if d_logp is None else _vector(d_logp, "d_logp", N, f32, dev),
+             None if d_entropy is None else _vector(d_entropy, "d_entropy", N, f32, dev), out.data_ptr(), ldd)
     return out

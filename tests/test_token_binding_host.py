@@ -1,6 +1,7 @@
 """What tokens.py does around the calls of the library, without a GPU: tensors of the host that say they are on a device, and a boundary that
 records what it is given."""
 import weakref
+from contextlib import contextmanager
 
 import pytest
 import torch
@@ -10,10 +11,10 @@ T = A.tokens
 
 
 class Boundary:
-    """In the library's place: every call is recorded, and `during` runs inside it."""
+    """In the library's place: every call is recorded, and `during` runs inside it.  `device` is the current one, `on` the tensors'."""
 
     def __init__(self):
-        self.calls, self.during = [], lambda: None
+        self.calls, self.during, self.device, self.on = [], lambda: None, 0, 0
 
     def __getattr__(self, name):
         def call(*args):
@@ -29,7 +30,16 @@ def boundary(monkeypatch):
     monkeypatch.setattr(T, "lib", b)
     monkeypatch.setattr(T, "_bytes", lambda call, *sizes: 4096)
     monkeypatch.setattr(T, "_stream", lambda device: 0)
-    monkeypatch.setattr(torch.Tensor, "get_device", lambda t: 0)
+    monkeypatch.setattr(T, "_current_device", lambda: b.device, raising=False)
+    monkeypatch.setattr(torch.Tensor, "get_device", lambda t: b.on)
+
+    @contextmanager
+    def device(index):
+        before, b.device = b.device, index
+        yield
+        b.device = before
+
+    monkeypatch.setattr(torch.cuda, "device", device)
     return b
 
 
@@ -64,3 +74,30 @@ def test_buffers_live_until_the_call_returns(boundary, monkeypatch, name):
     calls()[name]()
     assert [n for n, _ in boundary.calls] == [name]
     assert made and seen == [[True] * len(made)]
+
+
+@pytest.mark.parametrize("name", list(calls()))
+def test_kernels_go_to_the_operands_device(boundary, name):
+    """torch's default stream has the same handle on every device: which one is meant is the current device's."""
+    seen = []
+    boundary.during = lambda: seen.append(boundary.device)
+    for current, on in ((0, 0), (0, 1), (2, 0)):
+        boundary.device, boundary.on = current, on
+        calls()[name]()
+        assert seen.pop() == on and boundary.device == current
+
+
+def test_the_step_of_a_dropout_is_on_the_operands_device(boundary, monkeypatch):
+    """Its address goes into the kernel."""
+    monkeypatch.setattr(torch.Tensor, "is_cuda", True)
+    step = torch.zeros(1, dtype=torch.int64)
+    drop = A.Dropout(0.5, 1, step=step)
+    monkeypatch.setattr(torch.Tensor, "get_device", lambda t: 1 if t.dtype == torch.int64 else 0)
+    x, t = torch.zeros(4, 8), torch.zeros(4, dtype=torch.int32)
+    for call in (lambda: A.dropout(x, drop), lambda: A.token_lookup(x, t, dropout=drop), lambda: A.token_gradient(x, t, 5, dropout=drop)):
+        with pytest.raises(ValueError, match="step"):
+            call()
+    assert not boundary.calls
+    monkeypatch.setattr(torch.Tensor, "get_device", lambda t: 0)
+    A.dropout(x, drop)
+    assert len(boundary.calls) == 1
