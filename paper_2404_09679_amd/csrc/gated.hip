@@ -841,7 +841,7 @@ hipError_t launch_backward(const DxArgs& x, const DwArgs& w, const Split (&sp)[2
   return launch_pair<OpW, OpX>(w, sp[0], x, sp[1], s);
 }
 hipError_t gated_products(const DxArgs& x, DwArgs w, bool bf16, bool vec, float* partial, hipStream_t s) {
-  Plan p = backward_plan(x.N, x.K, x.H, bf16, vec, x.dx != nullptr && x.N > 0, w.dwg != nullptr);
+  Plan p = backward_plan(x.N, x.K, x.H, bf16, vec, x.dx != nullptr, w.dwg != nullptr);
   const TileClass& c = TILE_CLASS[0][p.cls];
   w.tiles_h = (int32_t)div_up(x.H, c.cols);
   p.split[0].partial = partial;
@@ -940,6 +940,7 @@ int antdt_gated_backward(const void* dh, int64_t lddh, const void* x, int64_t ld
   if (dwg) OP_TRY(gated_matrix(call, "x", x, N, K, ldx, dtype));
   if (dwg) OP_TRY(gated_matrix(call, "dwg", dwg, K, H, lddw, dtype));
   if (dwg) OP_TRY(gated_matrix(call, "dwu", dwu, K, H, lddw, dtype));
+  if (N == 0) dx = nullptr;   // (nothing of it; the weights' gradients are zeros)
   if (!dx && !dwg) return ANTDT_OK;
   if (N > 0 && (!saved || (reinterpret_cast<uintptr_t>(saved) & 255))) return op_fail(ANTDT_INVALID_ARG, "%s: saved is null or not 256-byte aligned", call);
   const bool bf16 = dtype == ANTDT_BF16;

@@ -1,0 +1,51 @@
+"""The operators on sequences of tokens at the borders of what they take, against their definitions in 64 bits (token_formulas.py)."""
+import ctypes as C
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2404_09679_amd as A
+import token_formulas as F
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+DT = {"f32": torch.float32, "bf16": torch.bfloat16}
+
+
+def host(t):
+    return t.double().cpu().numpy()
+
+
+def within(got, want, bound, what):
+    got = host(got) if torch.is_tensor(got) else got
+    bad = ~(np.abs(got - want) <= bound) & ~(got == want)
+    assert not bad.any(), (what, int(bad.sum()), np.argwhere(bad)[:3].tolist(), got[bad][:3], want[bad][:3])
+
+
+@pytest.mark.parametrize("N,K,H", [(1, 8, 16), (67, 200, 136), (777, 520, 328), (300, 1032, 2056)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_gated_backward_of_one_side(dtype, N, K, H):
+    """The gradient of x alone and those of the weights alone, which have plans of their own, in a workspace of the size reported."""
+    rng = np.random.default_rng(N + H)
+    x, wg, wu, dh = (torch.as_tensor(v).to(DEV, DT[dtype]) for v in (rng.normal(size=(N, K)), rng.normal(size=(K, H)) / K ** 0.5,
+                                                                     rng.normal(size=(K, H)) / K ** 0.5, rng.normal(size=(N, H))))
+    saved = A.gated_saved(x, wg)
+    A.gated_forward(x, wg, wu, "silu", saved=saved)
+    f = F.gated(host(x), host(wg), host(wu), "silu", F.HALF[dtype])
+    want = F.gated_gradients(host(x), host(wg), host(wu), host(dh), f, F.HALF[dtype])
+    code, n = {"f32": 0, "bf16": 1}[dtype], C.c_size_t()
+    assert A.lib.antdt_gated_backward_bytes(N, K, H, code, C.byref(n)) == 0
+    ws = torch.empty(n.value + 256, dtype=torch.uint8, device=DEV).fill_(255)
+    for dx, dw in ((True, False), (False, True)):
+        outs = [torch.full(s, 7.0, dtype=DT[dtype], device=DEV) for s in ((N, K), (K, H), (K, H))]
+        p = [t.data_ptr() if w else None for t, w in zip(outs, (dx, dw, dw))]
+        rc = A.lib.antdt_gated_backward(dh.data_ptr(), H, x.data_ptr(), K, wg.data_ptr(), wu.data_ptr(), H, N, K, H, code, saved.data_ptr(),
+                                        p[0], K, p[1], p[2], H, ws.data_ptr(), n.value, torch.cuda.current_stream().cuda_stream)
+        assert rc == 0
+        for name, t, w, (v, e) in zip(("dx", "dwg", "dwu"), outs, (dx, dw, dw), want):
+            if w:
+                within(t, v, e, (name, dx, dw))
+            else:
+                assert bool((t == 7).all())
+        assert bool((ws[n.value:] == 255).all())
