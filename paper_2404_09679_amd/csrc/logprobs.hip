@@ -60,7 +60,7 @@ struct Softmax {
     s *= r;
     m = to;
   }
-  // x <= m.  FINITE: not -infinity.
+  // x <= m.  FINITE: x - m is not -infinity (which the lowest finite logits are below a large one, too: terms of e = 0, not of NaN).
   template <bool FINITE>
   __device__ __forceinline__ void add(float x) {
     const float d = x - base(m), e = __expf(d);
@@ -73,7 +73,7 @@ struct Softmax {
     float lo = v[0];
 #pragma unroll
     for (int e = 1; e < n; ++e) lo = fminf(lo, v[e]);
-    if (lo > NEG_INF) {
+    if (lo - base(m) > NEG_INF) {
 #pragma unroll
       for (int e = 0; e < n; ++e) add<true>(v[e]);
     } else {

@@ -49,3 +49,30 @@ def test_gated_backward_of_one_side(dtype, N, K, H):
             else:
                 assert bool((t == 7).all())
         assert bool((ws[n.value:] == 255).all())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [8, 600, 20011])
+@pytest.mark.parametrize("top", [0, 3])
+def test_entropy_of_finite_logits_whose_differences_are_not(V, top, dtype):
+    """The lowest value of the type as a mask beside a large logit: their difference overflows, and the term is 0."""
+    rng = np.random.default_rng(V)
+    x = rng.normal(size=(6, V))
+    x[0], x[0, V // 2] = torch.finfo(DT[dtype]).min, 1e38
+    x[1, 0], x[1, 1] = torch.finfo(DT[dtype]).min, 1e38
+    x[2] = np.where(np.arange(V) % 2, -3e38, 3e38)
+    x[3] = np.sign(x[3]) * 10.0 ** rng.uniform(30, 38.4, V)
+    x[4] = torch.finfo(DT[dtype]).min
+    x[5, V - 1] = torch.finfo(DT[dtype]).max
+    dx = torch.as_tensor(x).to(DEV, DT[dtype])
+    f = F.logprobs(host(dx), np.zeros(6, np.int64), top)
+    r = A.token_logprobs(dx, None, top)
+    bound = F.U32 * (f["depth"] + 4 * (4 + f["entropy"] * f["depth"]))
+    within(r.entropy, f["entropy"], bound, "entropy")
+    within(r.stats[:, 2], f["entropy"], bound, "stats")
+    if top:
+        assert np.array_equal(host(r.top_index).astype(np.int64), f["top_index"])
+    b = rng.normal(size=6)
+    db = torch.as_tensor(b, dtype=torch.float32, device=DEV)
+    want, e = F.logprobs_gradient(f, np.full(6, -1), np.zeros(6), host(db))
+    within(A.token_logprobs_gradient(dx, None, r.stats, None, db), want, e + F.HALF[dtype] * (np.abs(want) + e) + 1e-38, "gradient")
