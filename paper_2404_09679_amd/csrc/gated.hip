@@ -41,10 +41,10 @@ __device__ __forceinline__ void activation(int act, float g, float& p, float& r)
   } else if (act == ANTDT_ACT_RELU) {
     p = g <= 0.0f ? 0.0f : g;   // (a NaN stays one)
     r = g > 0.0f ? 1.0f : 0.0f;
-  } else {
-    const float s = logistic(g);
-    p = s;
-    r = s * (1.0f - s);
+  } else {   // s (1 - s) from e^-|g|: 1 - s has no digits left where s is near 1
+    const float e = __expf(-fabsf(g)), t = __builtin_amdgcn_rcpf(1.0f + e);
+    p = g < 0.0f ? e * t : t;
+    r = e * t * t;
   }
 }
 

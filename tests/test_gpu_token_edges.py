@@ -76,3 +76,23 @@ def test_entropy_of_finite_logits_whose_differences_are_not(V, top, dtype):
     db = torch.as_tensor(b, dtype=torch.float32, device=DEV)
     want, e = F.logprobs_gradient(f, np.full(6, -1), np.zeros(6), host(db))
     within(A.token_logprobs_gradient(dx, None, r.stats, None, db), want, e + F.HALF[dtype] * (np.abs(want) + e) + 1e-38, "gradient")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N", [1, 2, 9])
+def test_slope_of_the_logistic_function_far_out(N, dtype):
+    """s (1 - s) where s is 1 in fp32, relative to its own size.  With u = 2^-24: the exponential of an argument of |g| is off by (2 |g| + 2) u, the
+    reciprocal of its sum with 1 by (|g| + 4) u, once in s and twice in the slope, and three products round."""
+    g = np.array([-30, 17.5, 24, 60, -17, 8.25, 0, 40, -1.5])[:N]
+    x = np.zeros((N, 8))
+    x[:, 0], x[:, 1] = g, 1
+    wg, wu = np.zeros((8, 16)), np.zeros((8, 16))
+    wg[0], wu[1] = np.where(np.arange(16) % 2, -1, 1), 1          # g or -g, and u = 1
+    x, wg, wu = (torch.as_tensor(v).to(DEV, DT[dtype]) for v in (x, wg, wu))
+    saved = A.gated_saved(x, wg)
+    A.gated_forward(x, wg, wu, "sigmoid", saved=saved)
+    p, r = saved.view(torch.float32).view(2, N, 16)
+    g = g[:, None] * np.where(np.arange(16) % 2, -1, 1)[None]
+    s, rest = 1 / (1 + np.exp(-g)), 1 / (1 + np.exp(g))
+    within(p, s, (3 * np.abs(g) + 8) * F.U32 * s, "s")
+    within(r, s * rest, (4 * np.abs(g) + 13) * F.U32 * s * rest, "slope")
