@@ -61,7 +61,8 @@ def _enqueue(device: int, call, *args):
 
 
 def _rows(t: torch.Tensor, name: str, rows: int, cols: int, dtype: torch.dtype, device: int) -> int:
-    """Leading dimension of a matrix argument, after the checks that the C boundary cannot make."""
+    """Leading dimension of a matrix argument (a single row's stride means nothing), after the checks that the C boundary
+    cannot make."""
     s, shape = t.stride(), t.shape
     if len(s) != 2 or shape[0] != rows or shape[1] != cols:
         raise ValueError(f"{name}: shape {tuple(shape)}, expected ({rows}, {cols})")
@@ -71,7 +72,7 @@ def _rows(t: torch.Tensor, name: str, rows: int, cols: int, dtype: torch.dtype, 
         raise ValueError(f"{name}: on {t.device}, expected device {device}")
     if s[1] != 1 and cols > 1:
         raise ValueError(f"{name}: columns of a row must be neighbours")
-    return s[0] if rows > 1 else max(s[0], cols)
+    return s[0] if rows > 1 else cols
 
 
 def _matrix(t: torch.Tensor, name: str) -> Tuple[int, int, int, int]:
@@ -85,7 +86,7 @@ def _matrix(t: torch.Tensor, name: str) -> Tuple[int, int, int, int]:
     rows, cols = shape
     if s[1] != 1 and cols > 1:
         raise ValueError(f"{name}: columns of a row must be neighbours")
-    return rows, cols, s[0] if rows > 1 else max(s[0], cols), device
+    return rows, cols, s[0] if rows > 1 else cols, device
 
 
 def _vector(t: torch.Tensor, name: str, n: int, dtype: torch.dtype, device: int) -> int:

@@ -96,3 +96,15 @@ def test_slope_of_the_logistic_function_far_out(N, dtype):
     s, rest = 1 / (1 + np.exp(-g)), 1 / (1 + np.exp(g))
     within(p, s, (3 * np.abs(g) + 8) * F.U32 * s, "s")
     within(r, s * rest, (4 * np.abs(g) + 13) * F.U32 * s * rest, "slope")
+
+
+def test_one_token_of_a_long_sequence():
+    """x [1, K] out of [1, T, K] with T K beyond the leading dimensions that are taken, for one row has none."""
+    T, K, H = 2100, 1024, 264
+    x = torch.randn(1, T, K, device=DEV).bfloat16()[:, -1]
+    wg, wu = (torch.randn(K, H, device=DEV).mul_(K ** -0.5).bfloat16() for _ in range(2))
+    saved, dh = A.gated_saved(x, wg), torch.randn(1, H, device=DEV).bfloat16()
+    h = A.gated_forward(x, wg, wu, saved=saved)
+    assert torch.equal(h, A.gated_forward(x.contiguous(), wg, wu))
+    for a, b in zip(A.gated_backward(dh, x, wg, wu, saved), A.gated_backward(dh, x.contiguous(), wg, wu, saved)):
+        assert torch.equal(a, b)

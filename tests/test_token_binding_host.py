@@ -101,3 +101,21 @@ def test_the_step_of_a_dropout_is_on_the_operands_device(boundary, monkeypatch):
     monkeypatch.setattr(torch.Tensor, "get_device", lambda t: 0)
     A.dropout(x, drop)
     assert len(boundary.calls) == 1
+
+
+def test_the_stride_of_a_single_row_is_no_leading_dimension(boundary):
+    """The last token of a long sequence, [1, T, K] sliced to [1, K]: its stride T K means nothing."""
+    x = torch.zeros(1, 2100, 1024, dtype=torch.bfloat16)[:, -1]
+    w = torch.zeros(1024, 16, dtype=torch.bfloat16)
+    assert x.stride(0) > 1 << 21
+    odd = torch.zeros(1, 16 + 3, dtype=torch.bfloat16)[:, :16]
+    out = A.gated_forward(x, w, w, out=odd)
+    name, args = boundary.calls.pop()
+    assert out is odd and name == "antdt_gated_forward" and args[1] == 1024 and args[11] == 16
+    A.token_lookup(torch.zeros(1, 9)[:, :5], torch.zeros(1, dtype=torch.int32))
+    name, args = boundary.calls.pop()
+    assert args[1] == 5 and args[10] == 5
+    A.token_logprobs_gradient(torch.zeros(1, 7), None, torch.zeros(1, 8)[:, :4], None, torch.zeros(1))
+    two = torch.zeros(2, 9)[:, :5]
+    A.dropout(two, A.Dropout(0.5, 1))
+    assert boundary.calls.pop()[1][1] == 9
