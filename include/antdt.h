@@ -453,8 +453,8 @@ int antdt_token_gradient(const void* dy, int64_t lddy, int32_t dtype, const int3
 /*
  * Gated feed-forward block: h = act(x Wg) * (x Wu), both projections, the activation and the product in one kernel.
  * x: DEVICE [N, K], Wg, Wu: DEVICE [K, H] (ldw both), h: DEVICE [N, H], all of `dtype`.  K, H >= 1; of bf16, K, H and every ld are
- * multiples of 8 and the buffers 16-byte aligned (ANTDT_UNSUPPORTED otherwise).  K, H < 2^20, ld < 2^21; N max(K, H) and
- * 2 K H below 2^36.
+ * multiples of 8 and the buffers 16-byte aligned (ANTDT_UNSUPPORTED otherwise).  K, H < 2^20, ld < 2^21; N max(K, H) (of fp32
+ * N max(K, 2 H)) and 2 K H, of N, K and H rounded up to multiples of 64, below 2^36.
  * saved: DEVICE buffer of antdt_gated_saved_bytes, 256-byte aligned, filled with what antdt_gated_backward needs, or NULL.
  */
 enum { ANTDT_ACT_SILU = 0, ANTDT_ACT_GELU = 1 /* g * Phi(g), by erf */, ANTDT_ACT_RELU = 2, ANTDT_ACT_SIGMOID = 3 };

@@ -864,8 +864,9 @@ int gated_sizes(const char* call, int64_t N, int64_t K, int64_t H, int32_t dtype
   if (!op_dtype(dtype)) return op_fail(ANTDT_INVALID_ARG, "%s: dtype", call);
   if (N < 0 || N >= INT32_MAX - 512 || K < 1 || K >= (1 << 20) || H < 1 || H >= (1 << 20))
     return op_fail(ANTDT_INVALID_ARG, "%s: N, K or H out of range", call);
-  const int64_t k = div_up(K, 64), h = div_up(H, 64);   // blocks of a launch, of 256 threads at least
-  if (std::max(div_up(N, 64) * std::max(k, h), 2 * k * h) >= (1 << 24)) return op_fail(ANTDT_INVALID_ARG, "%s: N, K or H out of range", call);
+  const int64_t k = div_up(K, 64), h = div_up(H, 64);   // blocks of a launch, of 256 threads at least (2^32 threads are the most)
+  const int64_t tiles = dtype == ANTDT_F32 ? std::max(k, div_up(H, 32)) : std::max(k, h);   // (of the forward pass in fp32: 64 x 32)
+  if (std::max(div_up(N, 64) * tiles, 2 * k * h) >= (1 << 24)) return op_fail(ANTDT_INVALID_ARG, "%s: N, K or H out of range", call);
   if (dtype == ANTDT_BF16 && ((K | H) & 7)) return op_fail(ANTDT_UNSUPPORTED, "%s: bf16 widths must be multiples of 8", call);
   return ANTDT_OK;
 }
