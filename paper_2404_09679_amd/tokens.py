@@ -174,9 +174,17 @@ def token_gradient(dy: torch.Tensor, tokens: torch.Tensor, rows: int, scale: flo
     return out
 
 
+def _width(w: torch.Tensor) -> int:
+    """Columns of what should be a matrix, to check it by."""
+    return w.shape[1] if len(w.shape) == 2 else 0
+
+
 def gated_saved(x: torch.Tensor, wg: torch.Tensor) -> torch.Tensor:
     """A buffer for what gated_forward leaves to gated_backward."""
-    return _new((_bytes("antdt_gated_saved_bytes", x.shape[0], wg.shape[1], _DTYPES[x.dtype]),), torch.uint8, x)
+    N, K, _, dev = _matrix(x, "x")
+    H = _width(wg)
+    _rows(wg, "wg", K, H, x.dtype, dev)
+    return _new((_bytes("antdt_gated_saved_bytes", N, H, _DTYPES[x.dtype]),), torch.uint8, x)
 
 
 def _saved(saved: torch.Tensor, N: int, H: int, dtype: torch.dtype, device: int) -> int:
@@ -188,7 +196,7 @@ def _saved(saved: torch.Tensor, N: int, H: int, dtype: torch.dtype, device: int)
 
 def _weights(wg: torch.Tensor, wu: torch.Tensor, K: int, dt: torch.dtype, dev: int) -> Tuple[int, int]:
     """(H, leading dimension) of the two weight matrices."""
-    H = wg.shape[-1]
+    H = _width(wg)
     ldw = _rows(wg, "wg", K, H, dt, dev)
     if _rows(wu, "wu", K, H, dt, dev) != ldw:
         raise ValueError("wg and wu: one leading dimension")

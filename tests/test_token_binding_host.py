@@ -119,3 +119,14 @@ def test_the_stride_of_a_single_row_is_no_leading_dimension(boundary):
     two = torch.zeros(2, 9)[:, :5]
     A.dropout(two, A.Dropout(0.5, 1))
     assert boundary.calls.pop()[1][1] == 9
+
+
+def test_refusals_of_the_gated_blocks_tensors(boundary):
+    x, w = torch.zeros(4, 8), torch.zeros(8, 16)
+    saved = torch.zeros(4096, dtype=torch.uint8)
+    for call in (lambda: A.gated_saved(x.half(), w), lambda: A.gated_saved(x[0], w), lambda: A.gated_saved(x, w[0]), lambda: A.gated_saved(x, w[0, 0]),
+                 lambda: A.gated_forward(x, w[0, 0], w), lambda: A.gated_forward(x, w[0], w[0]), lambda: A.gated_forward(x, w, w[0, 0]),
+                 lambda: A.gated_backward(torch.zeros(4, 16), x, w[0, 0], w, saved)):
+        with pytest.raises(ValueError):
+            call()
+    assert not boundary.calls
