@@ -31,8 +31,8 @@ class Dropout:
         self._ref = C.byref(self._spec)
 
     def _on(self, device: int):
-        """The spec for a call on `device`, which reads `step`."""
-        if self.step is not None and self.step.get_device() != device:
+        """The spec, with a step, for a call on `device`, which reads it."""
+        if self.step.get_device() != device:
             raise ValueError(f"Dropout: step is on {self.step.device}, the operands on device {device}")
         return self._ref
 
@@ -42,22 +42,10 @@ def _check(rc: int):
         raise AntdtError(rc, lib.antdt_last_error(None).decode())
 
 
-def _stream(device: int) -> int:
-    """Handle of torch's current stream of the operands' device."""
-    return _raw_stream(device) if _raw_stream is not None else torch.cuda.current_stream(device).cuda_stream
-
-
+# Handle of torch's current stream of a device.  Its default stream has the same handle on every device, and kernels on it
+# go to the current one: a call whose operands are on another makes that the current one first.
+_stream = _raw_stream or (lambda device: torch.cuda.current_stream(device).cuda_stream)
 _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
-
-
-def _enqueue(device: int, call, *args):
-    """call(*args, stream) with the operands' device current: torch's default stream has the same handle on every device,
-    and kernels on it go to the current one."""
-    if _current_device() == device:
-        _check(call(*args, _stream(device)))
-    else:
-        with torch.cuda.device(device):
-            _check(call(*args, _stream(device)))
 
 
 def _rows(t: torch.Tensor, name: str, rows: int, cols: int, dtype: torch.dtype, device: int) -> int:
@@ -126,6 +114,9 @@ def dropout(x: torch.Tensor, drop: Dropout, residual: Optional[torch.Tensor] = N
             out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """residual + dropout(x), or dropout(x).  `out` may be x or residual.  The gradient of x is dropout(gradient, drop)."""
     rows, cols, ldx, dev = _matrix(x, "x")
+    if dev != _current_device():
+        with torch.cuda.device(dev):
+            return dropout(x, drop, residual, out)
     dt = x.dtype
     if out is None:
         out = _new((rows, cols), dt, x)
@@ -133,8 +124,9 @@ def dropout(x: torch.Tensor, drop: Dropout, residual: Optional[torch.Tensor] = N
     if residual is not None:
         ldr, rp = _rows(residual, "residual", rows, cols, dt, dev), residual.data_ptr()
     ldo = _rows(out, "out", rows, cols, dt, dev)
-    _enqueue(dev, lib.antdt_dropout, x.data_ptr(), ldx, rp, ldr, rows, cols, _DTYPES[dt], drop._on(dev),
-             out.data_ptr(), ldo)
+    spec = drop._ref if drop.step is None else drop._on(dev)
+    _check(lib.antdt_dropout(x.data_ptr(), ldx, rp, ldr, rows, cols, _DTYPES[dt], spec, out.data_ptr(), ldo,
+                             _stream(dev)))
     return out
 
 
@@ -142,6 +134,9 @@ def token_lookup(table: torch.Tensor, tokens: torch.Tensor, scale: float = 1.0, 
                  out: Optional[torch.Tensor] = None, out_dtype: Optional[torch.dtype] = None) -> torch.Tensor:
     """scale * dropout(table[tokens]); tokens outside the table are padding and give zeros."""
     V, D, ldt, dev = _matrix(table, "table")
+    if dev != _current_device():
+        with torch.cuda.device(dev):
+            return token_lookup(table, tokens, scale, dropout, out, out_dtype)
     N = tokens.numel()
     tp = _vector(tokens, "tokens", N, torch.int32, dev)
     if out is None:
@@ -150,8 +145,9 @@ def token_lookup(table: torch.Tensor, tokens: torch.Tensor, scale: float = 1.0, 
     if odt not in _DTYPES:
         raise ValueError(f"out: {odt}")
     ldo = _rows(out, "out", N, D, odt, dev)
-    _enqueue(dev, lib.antdt_token_lookup, table.data_ptr(), ldt, V, D, _DTYPES[table.dtype], tp, N, scale,
-             None if dropout is None else dropout._on(dev), out.data_ptr(), ldo, _DTYPES[odt])
+    spec = None if dropout is None else dropout._ref if dropout.step is None else dropout._on(dev)
+    _check(lib.antdt_token_lookup(table.data_ptr(), ldt, V, D, _DTYPES[table.dtype], tp, N, scale, spec, out.data_ptr(),
+                                  ldo, _DTYPES[odt], _stream(dev)))
     return out
 
 
@@ -161,6 +157,9 @@ def token_gradient(dy: torch.Tensor, tokens: torch.Tensor, rows: int, scale: flo
     """Gradient (fp32 [rows, D]) of the table of token_lookup from that of its output.  With `accumulate` the sums are
     added to `out`, whose other rows are not touched."""
     N, D, ldd, dev = _matrix(dy, "dy")
+    if dev != _current_device():
+        with torch.cuda.device(dev):
+            return token_gradient(dy, tokens, rows, scale, dropout, out, accumulate, workspace)
     tp = _vector(tokens, "tokens", N, torch.int32, dev)
     if out is None:
         if accumulate:
@@ -168,9 +167,9 @@ def token_gradient(dy: torch.Tensor, tokens: torch.Tensor, rows: int, scale: flo
         out = _new((rows, D), torch.float32, dy)
     ldg = _rows(out, "out", rows, D, torch.float32, dev)
     held, ws, n = _workspace(workspace, _bytes("antdt_token_gradient_bytes", N, rows, D), dy)
-    _enqueue(dev, lib.antdt_token_gradient, dy.data_ptr(), ldd, _DTYPES[dy.dtype], tp, N, scale,
-             None if dropout is None else dropout._on(dev), out.data_ptr(), ldg, rows, D, 1 if accumulate else 0, ws,
-             n)
+    spec = None if dropout is None else dropout._ref if dropout.step is None else dropout._on(dev)
+    _check(lib.antdt_token_gradient(dy.data_ptr(), ldd, _DTYPES[dy.dtype], tp, N, scale, spec, out.data_ptr(), ldg,
+                                    rows, D, 1 if accumulate else 0, ws, n, _stream(dev)))
     return out
 
 
@@ -210,14 +209,18 @@ def gated_forward(x: torch.Tensor, wg: torch.Tensor, wu: torch.Tensor, act: str 
     if act not in ACTS:
         raise ValueError(f"act: one of {', '.join(ACTS)}")
     N, K, ldx, dev = _matrix(x, "x")
+    if dev != _current_device():
+        with torch.cuda.device(dev):
+            return gated_forward(x, wg, wu, act, out, saved, workspace)
     dt = x.dtype
     H, ldw = _weights(wg, wu, K, dt, dev)
     if out is None:
         out = _new((N, H), dt, x)
     ldh = _rows(out, "out", N, H, dt, dev)
     held, ws, n = _workspace(workspace, _bytes("antdt_gated_forward_bytes", N, K, H, _DTYPES[dt]), x)
-    _enqueue(dev, lib.antdt_gated_forward, x.data_ptr(), ldx, wg.data_ptr(), wu.data_ptr(), ldw, N, K, H, _DTYPES[dt],
-             ACTS[act], out.data_ptr(), ldh, None if saved is None else _saved(saved, N, H, dt, dev), ws, n)
+    _check(lib.antdt_gated_forward(x.data_ptr(), ldx, wg.data_ptr(), wu.data_ptr(), ldw, N, K, H, _DTYPES[dt],
+                                   ACTS[act], out.data_ptr(), ldh,
+                                   None if saved is None else _saved(saved, N, H, dt, dev), ws, n, _stream(dev)))
     return out
 
 
@@ -226,6 +229,9 @@ def gated_backward(dh: torch.Tensor, x: torch.Tensor, wg: torch.Tensor, wu: torc
                    dwu: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
     """(dx, dwg, dwu) of gated_forward from the gradient of its result."""
     N, K, ldx, dev = _matrix(x, "x")
+    if dev != _current_device():
+        with torch.cuda.device(dev):
+            return gated_backward(dh, x, wg, wu, saved, dx, dwg, dwu, workspace)
     dt = x.dtype
     H, ldw = _weights(wg, wu, K, dt, dev)
     ldd = _rows(dh, "dh", N, H, dt, dev)
@@ -236,9 +242,9 @@ def gated_backward(dh: torch.Tensor, x: torch.Tensor, wg: torch.Tensor, wu: torc
     if _rows(dwu, "dwu", K, H, dt, dev) != lddw:
         raise ValueError("dwg and dwu: one leading dimension")
     held, ws, n = _workspace(workspace, _bytes("antdt_gated_backward_bytes", N, K, H, _DTYPES[dt]), x)
-    _enqueue(dev, lib.antdt_gated_backward, dh.data_ptr(), ldd, x.data_ptr(), ldx, wg.data_ptr(), wu.data_ptr(), ldw,
-             N, K, H, _DTYPES[dt], _saved(saved, N, H, dt, dev), dx.data_ptr(), lddx, dwg.data_ptr(), dwu.data_ptr(),
-             lddw, ws, n)
+    _check(lib.antdt_gated_backward(dh.data_ptr(), ldd, x.data_ptr(), ldx, wg.data_ptr(), wu.data_ptr(), ldw, N, K, H,
+                                    _DTYPES[dt], _saved(saved, N, H, dt, dev), dx.data_ptr(), lddx, dwg.data_ptr(),
+                                    dwu.data_ptr(), lddw, ws, n, _stream(dev)))
     return dx, dwg, dwu
 
 
@@ -255,6 +261,9 @@ def token_logprobs(logits: torch.Tensor, tokens: Optional[torch.Tensor] = None, 
     """Log probabilities of `tokens` under softmax(logits), the rows' entropies and their `top` largest log
     probabilities with their columns."""
     N, V, ld, dev = _matrix(logits, "logits")
+    if dev != _current_device():
+        with torch.cuda.device(dev):
+            return token_logprobs(logits, tokens, top, workspace)
     n = _bytes("antdt_token_logprobs_bytes", N, V, top)
     f32, given, k = torch.float32, tokens is not None, top if top > 0 else 0
     tp = _vector(tokens, "tokens", N, torch.int32, dev) if given else None
@@ -274,8 +283,8 @@ def token_logprobs(logits: torch.Tensor, tokens: Optional[torch.Tensor] = None, 
         top_logp, top_index = top_logp.view(N, k), top_index.view(torch.int32).view(N, k)
     else:
         top_logp = top_index = None
-    _enqueue(dev, lib.antdt_token_logprobs, logits.data_ptr(), ld, N, V, _DTYPES[logits.dtype], tp,
-             lp if given else None, ep, sp, top, tl, ti, ws, n)
+    _check(lib.antdt_token_logprobs(logits.data_ptr(), ld, N, V, _DTYPES[logits.dtype], tp, lp if given else None, ep,
+                                    sp, top, tl, ti, ws, n, _stream(dev)))
     return LogProbs(logp, entropy, stats, top_logp, top_index)
 
 
@@ -284,14 +293,18 @@ def token_logprobs_gradient(logits: torch.Tensor, tokens: Optional[torch.Tensor]
                             out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Gradient of the logits from those of token_logprobs' logp and entropy.  `out` may be the logits themselves."""
     N, V, ld, dev = _matrix(logits, "logits")
+    if dev != _current_device():
+        with torch.cuda.device(dev):
+            return token_logprobs_gradient(logits, tokens, stats, d_logp, d_entropy, out)
     dt, f32 = logits.dtype, torch.float32
     if _rows(stats, "stats", N, 4, f32, dev) != 4:
         raise ValueError("stats: as token_logprobs left them")
     if out is None:
         out = _new((N, V), dt, logits)
     ldd = _rows(out, "out", N, V, dt, dev)
-    _enqueue(dev, lib.antdt_token_logprobs_gradient, logits.data_ptr(), ld, N, V, _DTYPES[dt],
-             None if tokens is None else _vector(tokens, "tokens", N, torch.int32, dev), stats.data_ptr(),
-             None if d_logp is None else _vector(d_logp, "d_logp", N, f32, dev),
-             None if d_entropy is None else _vector(d_entropy, "d_entropy", N, f32, dev), out.data_ptr(), ldd)
+    tp = None if tokens is None else _vector(tokens, "tokens", N, torch.int32, dev)
+    dl = None if d_logp is None else _vector(d_logp, "d_logp", N, f32, dev)
+    dh = None if d_entropy is None else _vector(d_entropy, "d_entropy", N, f32, dev)
+    _check(lib.antdt_token_logprobs_gradient(logits.data_ptr(), ld, N, V, _DTYPES[dt], tp, stats.data_ptr(), dl, dh,
+                                             out.data_ptr(), ldd, _stream(dev)))
     return out
