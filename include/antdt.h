@@ -410,8 +410,10 @@ int antdt_dense_aggregate_adam(float* p, float* m, float* v, const float* const*
  *  - matrices are row-major, `ld...` elements from one row to the next, at least the row's length; any alignment
  *    of the element type is accepted (16-byte aligned rows are read and written 16 bytes at a time) unless said
  *    otherwise.  Buffers must not overlap unless said otherwise.
- *  - dtype: ANTDT_F32 or ANTDT_BF16.  All arithmetic is fp32; results are rounded once, to nearest even.
+ *  - dtype: ANTDT_F32 or ANTDT_BF16.  All arithmetic is fp32; results are rounded once, to nearest even (antdt_gated_backward of bf16
+ *    rounds the operand of its products as well).
  *  - a token outside [0, V) is padding: it has no row and no gradient.
+ *  - sizes: rows, columns and leading dimensions below 2^40 unless a call says less.
  *  - empty shapes are legal and enqueue what is left to do (usually nothing); their buffers may be NULL.
  *  - `workspace`: DEVICE, 256-byte aligned, of at least the size that the matching ..._bytes call reports (0: may be
  *    NULL).  It holds nothing between calls and needs no clearing; calls that overlap need one each.
@@ -433,7 +435,7 @@ typedef struct antdt_dropout_spec {
 } antdt_dropout_spec;
 
 /* y = residual + dropout(x), or dropout(x) when residual is NULL.  x, residual, y: DEVICE [rows, cols] of `dtype`; y may be x or
- * residual (with the same ld).  The gradient with respect to x is antdt_dropout of that with respect to y, without a residual. */
+ * residual (with the same ld).  cols < 2^31 - 1.  The gradient with respect to x is antdt_dropout of that with respect to y, without a residual. */
 int antdt_dropout(const void* x, int64_t ldx, const void* residual, int64_t ldr, int64_t rows, int64_t cols,
                   int32_t dtype, const antdt_dropout_spec* drop, void* y, int64_t ldy, void* stream);
 
@@ -464,7 +466,9 @@ int antdt_gated_forward(const void* x, int64_t ldx, const void* wg, const void* 
                         int32_t dtype, int32_t act, void* h, int64_t ldh, void* saved, void* workspace, size_t workspace_bytes,
                         void* stream);
 /* Its gradients, from dh = that of h: dx [N, K] (or NULL), dwg and dwu [K, H] (lddw both; both or neither NULL), of `dtype`.  x, Wg, Wu
- * and saved as antdt_gated_forward was given and left them. */
+ * and saved as antdt_gated_forward was given and left them.  The gradients of x Wg and x Wu are formed in fp32; in a bf16 block they are
+ * then rounded to bf16, as the matrix cores' operands (of random inputs dx, dwg and dwu are off by 0.0023 of their norm, their own
+ * rounding alone would be 0.0017). */
 int antdt_gated_backward_bytes(int64_t N, int64_t K, int64_t H, int32_t dtype, size_t* bytes);
 int antdt_gated_backward(const void* dh, int64_t lddh, const void* x, int64_t ldx, const void* wg, const void* wu, int64_t ldw,
                          int64_t N, int64_t K, int64_t H, int32_t dtype, const void* saved, void* dx, int64_t lddx, void* dwg,
@@ -475,11 +479,11 @@ int antdt_gated_backward(const void* dh, int64_t lddh, const void* x, int64_t ld
  *   logp        fp32 [N]         log p[tokens[n]]; 0 for padding.  NULL, as tokens, when not wanted
  *   entropy     fp32 [N]         -sum p log p (terms of p = 0 are 0).  May be NULL
  *   stats       fp32 [N, 4]      for antdt_token_logprobs_gradient: largest logit, log of the sum of exp(logit - largest), entropy, 0.
- *                                May be NULL
+ *                                16-byte aligned, here and there.  May be NULL
  *   top_logp    fp32 [N, top]    the `top` largest log probabilities, descending, and
  *   top_index   int32 [N, top]   their columns, equal logits by the lower column; 0 <= top <= min(V, ANTDT_MAX_TOP)
  * A row without an allowed column (all -infinity): logp and top_logp -infinity, entropy 0.  A row with a NaN or +infinity: NaN, its
- * NaN counted largest in top_index.  1 <= V < 2^31.
+ * NaN counted largest in top_index.  1 <= V < 2^31 - 1, N < 2^29 - 1.
  */
 #define ANTDT_MAX_TOP 64
 int antdt_token_logprobs_bytes(int64_t N, int64_t V, int32_t top, size_t* bytes);

@@ -2,7 +2,8 @@
 
 Every call works on torch's current stream.  Results go to `out` (or the other named outputs) where
 given, else to new tensors; a workspace that is not given comes from torch's allocator.  Nothing here is registered
-with autograd: a backward pass is a call of its own.
+with autograd: a backward pass is a call of its own, results do not require a gradient whatever the operands do, and what
+is written through `out` (and the other named outputs) does not count as an in-place change of that tensor.
 """
 from __future__ import annotations
 
@@ -227,7 +228,8 @@ def gated_forward(x: torch.Tensor, wg: torch.Tensor, wu: torch.Tensor, act: str 
 def gated_backward(dh: torch.Tensor, x: torch.Tensor, wg: torch.Tensor, wu: torch.Tensor, saved: torch.Tensor,
                    dx: Optional[torch.Tensor] = None, dwg: Optional[torch.Tensor] = None,
                    dwu: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
-    """(dx, dwg, dwu) of gated_forward from the gradient of its result."""
+    """(dx, dwg, dwu) of gated_forward from the gradient of its result.  In bf16 the gradients of both projections, operands of
+    the products, are rounded to bf16 too."""
     N, K, ldx, dev = _matrix(x, "x")
     if dev != _current_device():
         with torch.cuda.device(dev):
