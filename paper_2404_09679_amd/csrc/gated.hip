@@ -401,7 +401,7 @@ __global__ __launch_bounds__(FEW_THREADS) void gated_few_kernel(GatedArgs a) {
   }
 }
 
-// dz = [dh R | dh P], [N, 2H].  Bound by memory: 8192 x 5632 bf16 102 us (6.3 TB/s).  A launch of its own, because a product would form every element
+// dz = [dh R | dh P], [N, 2H].  Bound by memory: 8192 x 5632 bf16 100 us (6.5 TB/s).  A launch of its own, because a product would form every element
 // again for each of its 8 or 22 tiles along the other side.
 struct DzArgs {
   const void* dh;
@@ -430,7 +430,7 @@ __global__ __launch_bounds__(256) void gated_dz_kernel(DzArgs a) {
   }
 }
 
-// The backward products of 8192 tokens of 2048-5632: 583-600 us in one launch (1.26-1.3 PFLOP/s; matrix cores busy 74 % of the cycles).
+// The backward products of 8192 tokens of 2048-5632: 572-600 us in one launch (1.26-1.32 PFLOP/s; matrix cores busy 77 % of the cycles).
 // dx = dz [Wg | Wu]^T, a contraction over the columns of one and then of the other.
 struct DxArgs {
   const void* dz;
