@@ -11,6 +11,7 @@
 
 #include "ops.h"
 #include "product.h"
+#include "sort.h"
 
 namespace antdt {
 namespace {
@@ -48,11 +49,6 @@ __device__ __forceinline__ void activation(int act, float g, float& p, float& r)
   }
 }
 
-__device__ __forceinline__ void wave_order() {
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-}
-
 // How the tiles of a product are handed out: the first `whole` to a block each, the contraction of the others in `parts`, whose sums go to
 // memory in the order of the accumulators and are added up, in order, by a second launch.
 struct Split {
@@ -87,7 +83,7 @@ __device__ __forceinline__ void store_rows(float* st, const f32x16 (&x)[TN], T* 
 #pragma unroll
     for (int v = 0; v < 4; ++v)
       *reinterpret_cast<float4*>(st + fr * SP + j * 32 + 8 * v + 4 * fg) = make_float4(x[j][4 * v], x[j][4 * v + 1], x[j][4 * v + 2], x[j][4 * v + 3]);
-  wave_order();
+  wave_lds_order();
   constexpr int CPR = WN / PER, RPI = 64 / CPR;
   const int rr = lane / CPR, cc = (lane % CPR) * PER;
 #pragma unroll
@@ -111,7 +107,7 @@ __device__ __forceinline__ void store_rows(float* st, const f32x16 (&x)[TN], T* 
       }
     }
   }
-  wave_order();
+  wave_lds_order();
 }
 
 template <typename A>

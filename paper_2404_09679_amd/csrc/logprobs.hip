@@ -6,6 +6,7 @@
 #include <type_traits>
 
 #include "ops.h"
+#include "sort.h"
 
 namespace antdt {
 namespace {
@@ -235,13 +236,7 @@ __device__ __forceinline__ void digit_at_rank(LpLds& lds, const uint32_t* hist, 
     c[q] = hist[ascending ? at : 255 - at];
     mine += c[q];
   }
-  uint32_t up = mine;   // of this lane's digits and those before
-  up += dpp<0x111, 0xF>(0, up);
-  up += dpp<0x112, 0xF>(0, up);
-  up += dpp<0x114, 0xF>(0, up);
-  up += dpp<0x118, 0xF>(0, up);
-  up += dpp<0x142, 0xA>(0, up);
-  up += dpp<0x143, 0xC>(0, up);
+  const uint32_t up = wave_prefix(mine);   // of this lane's digits and those before
   uint32_t run = up - mine;
   if (run < want && up >= want) {   // (one lane; none if there are fewer keys)
 #pragma unroll

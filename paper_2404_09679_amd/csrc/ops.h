@@ -118,19 +118,19 @@ __device__ __forceinline__ void load8(const T* p, int n, float (&v)[8]) {
     }
   }
 }
-template <int Q, bool STREAM = false, typename T>
+template <int Q, typename T>
 __device__ __forceinline__ void store8(T* p, int n, const float (&v)[8]) {
   if constexpr (Q == 1) {
 #pragma unroll
     for (int e = 0; e < 8; ++e)
       if (e < n) p[e] = from_f32<T>(v[e]);
   } else if constexpr (sizeof(T) == 4) {
-    store16<STREAM>(p, bits4(v[0], v[1], v[2], v[3]));
-    if (Q == 8 || n > 4) store16<STREAM>(p + 4, bits4(v[4], v[5], v[6], v[7]));
+    store16<false>(p, bits4(v[0], v[1], v[2], v[3]));
+    if (Q == 8 || n > 4) store16<false>(p + 4, bits4(v[4], v[5], v[6], v[7]));
   } else {
     const uint4 a = make_uint4(f2bf2(v[0], v[1]), f2bf2(v[2], v[3]), f2bf2(v[4], v[5]), f2bf2(v[6], v[7]));
     if constexpr (Q == 8) {
-      store16<STREAM>(p, a);
+      store16<false>(p, a);
     } else {
       *reinterpret_cast<uint2*>(p) = make_uint2(a.x, a.y);
       if (n > 4) *reinterpret_cast<uint2*>(p + 4) = make_uint2(a.z, a.w);
