@@ -498,6 +498,87 @@ int antdt_token_logprobs_gradient(const void* logits, int64_t ld, int64_t N, int
                                   void* stream);
 
 /*
+ * Attention over a user's history.  The conventions of the operators on sequences of tokens hold, and:
+ *  - heads are [rows, heads, D] or [batch, rows, heads, D] with D neighbouring columns and any strides otherwise (`ld...`: elements from one
+ *    row to the next, `ld..._head` from one head to the next, `ld..._batch`; of what there is one of the stride means nothing).  The elements of
+ *    a result must not share memory; an operand's stride may be 0, which repeats it.
+ *  - heads <= q_heads, q_heads a multiple of heads: head h of the queries belongs to head h / (q_heads / heads) of keys and values.
+ *  - lengths: DEVICE int32 [B], of a sequence's rows; what lies outside 0 .. the size is taken as the nearer end.  Rows behind a length
+ *    are never read into a result, whatever they hold, and are zeros in one.
+ *  - attention: D a multiple of 8, at most ANTDT_MAX_ATTENTION_DIM, heads that start at multiples of 16 bytes (ANTDT_UNSUPPORTED otherwise).  Scores, the
+ *    softmax and sums are fp32.  Of bf16 heads the probabilities, and in the backward pass the scores' gradients, are rounded to bf16 as the matrix cores'
+ *    operands.  A query without keys, or all of whose scores are -infinity, has zeros and passes no gradient.
+ */
+#define ANTDT_MAX_HEAD_DIM 256
+#define ANTDT_MAX_ATTENTION_DIM 128
+
+/*
+ * Rotary positions.  Pair i < dim / 2 of a head's first `dim` columns (2 i and 2 i + 1 when interleaved, else i and i + dim / 2) at position p is
+ * turned by a = p * turns[i] 2^-64 turns: (u, v) -> magnitude * (u cos a - v sin a, v cos a + u sin a).  The other columns are as they were.
+ * Whole turns are dropped in whole numbers, so that an angle is as exact at position 2^31 as at 1.
+ */
+typedef struct antdt_rotary_spec {
+  int32_t dim;            /* even, 2 .. D */
+  int32_t interleaved;
+  float magnitude;
+  const uint64_t* turns;  /* DEVICE [dim / 2], see antdt_rotary_turns */
+} antdt_rotary_spec;
+/* turns (HOST [dim / 2]) of the frequencies f_i = base^(-2 i / dim) / (2 pi) turns a position, slowed for a context `factor` times as long as the
+ * `original` one: f_i (g + (1 - g) / factor), where g goes from 0 for pairs of `low` turns in the original context to 1 for `high` turns; high = 0: all
+ * pairs alike (g = 0).  base, factor >= 1 (1: none); 0 <= low < high, original > 0. */
+int antdt_rotary_turns(int32_t dim, double base, double factor, double original, double low, double high, uint64_t* turns);
+/* y = x turned by its rows' positions (DEVICE int32 [N]), or, with inverse != 0, the gradient of x from that of y: turned back (and times the magnitude).
+ * x, y: DEVICE [N, H, D] of `dtype`, 0 <= D <= ANTDT_MAX_HEAD_DIM, H <= 65536, N < 2^31 - 1; y may be x (with the same strides). */
+int antdt_rotary(const void* x, int64_t ldx, int64_t ldx_head, int64_t N, int64_t H, int64_t D, int32_t dtype, const int32_t* positions,
+                 const antdt_rotary_spec* rotary, int32_t inverse, void* y, int64_t ldy, int64_t ldy_head, void* stream);
+
+/*
+ * A paged cache: k_cache and v_cache, DEVICE [pages, page_size, heads, D] (the same strides both), and table, DEVICE int32 [B, table_cols]: tokens
+ * i page_size .. of sequence b are the rows of page table[b, i].  A page outside 0 .. pages - 1 is none: what belongs there is not kept, and
+ * not there to be read.  pages, page_size, table_cols < 2^31 - 1.
+ *
+ * Appends k and v (DEVICE [N, heads, D]) of new tokens, k turned by their positions when `rotary` (HOST) is given.  Sequence b's new tokens are
+ * n = offsets[b] .. offsets[b + 1] - 1 (DEVICE int32 [B + 1], ascending), or, offsets NULL, n = b.  lengths (DEVICE int32 [B]) count them in: the last
+ * one's position is lengths[b] - 1.  A token of a position below 0 (length 0: a place of the batch that is not in use), in no sequence, or beyond the
+ * table's pages is not appended.  q, q_out: DEVICE [N, q_heads, D], the same tokens' queries, turned likewise to q_out (which may be q with the same
+ * strides), zeros for tokens without a position; q_heads may be 0.  Sequences share no page that is appended to.  D, heads as antdt_rotary.
+ */
+int antdt_cache_append(const void* q, int64_t ldq, int64_t ldq_head, void* q_out, int64_t ldqo, int64_t ldqo_head, const void* k, int64_t ldk,
+                       int64_t ldk_head, const void* v, int64_t ldv, int64_t ldv_head, int64_t N, int64_t q_heads, int64_t heads, int64_t D, int32_t dtype,
+                       const antdt_rotary_spec* rotary, void* k_cache, void* v_cache, int64_t ld_page, int64_t ld_row, int64_t ld_head, int64_t pages,
+                       int64_t page_size, const int32_t* table, int64_t ld_table, int64_t B, int64_t table_cols, const int32_t* lengths,
+                       const int32_t* offsets, void* stream);
+/* Attention of one new token of each sequence (q: DEVICE [B, q_heads, D]) over the lengths[b] tokens that the cache holds of it:
+ * out[b] = softmax(scale q k^T) v, of `dtype` [B, q_heads, D].  scale >= 1e-30.  B q_heads < 2^24. */
+int antdt_cache_attention_bytes(int64_t B, int64_t q_heads, int64_t heads, int64_t D, int32_t dtype, size_t* bytes);
+int antdt_cache_attention(const void* q, int64_t ldq, int64_t ldq_head, const void* k_cache, const void* v_cache, int64_t ld_page, int64_t ld_row,
+                          int64_t ld_head, int64_t pages, int64_t page_size, const int32_t* table, int64_t ld_table, int64_t B, int64_t table_cols,
+                          const int32_t* lengths, int64_t q_heads, int64_t heads, int64_t D, int32_t dtype, float scale, void* out, int64_t ldo,
+                          int64_t ldo_head, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Attention of S queries (candidates, a decoder's tokens) over T keys and values of another length (an encoded history), for every batch entry:
+ * out = softmax(scale q k^T) v.  q, out: DEVICE [B, S, q_heads, D], k, v: DEVICE [B, T, heads, D], of `dtype`.  q_lengths, k_lengths: rows that an
+ * entry has (NULL: all).  stats: DEVICE fp32 [B, q_heads, S], or NULL: log2 of the sum of 2^(scale log2(e) q k^T) for the backward pass, +infinity
+ * for a query without keys.  scale >= 1e-30.  B q_heads max(S, T) / 128 (rounded up) < 2^24, S, T < 2^31 - 1.
+ */
+int antdt_cross_attention_bytes(int64_t B, int64_t S, int64_t T, int64_t q_heads, int64_t heads, int64_t D, int32_t dtype, size_t* bytes);
+int antdt_cross_attention(const void* q, int64_t ldq_batch, int64_t ldq, int64_t ldq_head, const void* k, int64_t ldk_batch, int64_t ldk, int64_t ldk_head,
+                          const void* v, int64_t ldv_batch, int64_t ldv, int64_t ldv_head, int64_t B, int64_t S, int64_t T, int64_t q_heads, int64_t heads,
+                          int64_t D, int32_t dtype, const int32_t* q_lengths, const int32_t* k_lengths, float scale, void* out, int64_t ldo_batch,
+                          int64_t ldo, int64_t ldo_head, float* stats, void* workspace, size_t workspace_bytes, void* stream);
+/* Its gradients, from dout = that of out: dq [B, S, q_heads, D] (or NULL), dk and dv [B, T, heads, D] (both or neither NULL), of `dtype`; a repeated
+ * operand's gradient is that of each repetition.  q, k, v, out, stats and lengths as antdt_cross_attention was given and left them. */
+int antdt_cross_attention_backward_bytes(int64_t B, int64_t S, int64_t T, int64_t q_heads, int64_t heads, int64_t D, int32_t dtype, size_t* bytes);
+int antdt_cross_attention_backward(const void* dout, int64_t lddo_batch, int64_t lddo, int64_t lddo_head, const void* q, int64_t ldq_batch, int64_t ldq,
+                                   int64_t ldq_head, const void* k, int64_t ldk_batch, int64_t ldk, int64_t ldk_head, const void* v, int64_t ldv_batch,
+                                   int64_t ldv, int64_t ldv_head, const void* out, int64_t ldo_batch, int64_t ldo, int64_t ldo_head, const float* stats,
+                                   int64_t B, int64_t S, int64_t T, int64_t q_heads, int64_t heads, int64_t D, int32_t dtype, const int32_t* q_lengths,
+                                   const int32_t* k_lengths, float scale, void* dq, int64_t lddq_batch, int64_t lddq, int64_t lddq_head, void* dk,
+                                   int64_t lddk_batch, int64_t lddk, int64_t lddk_head, void* dv, int64_t lddv_batch, int64_t lddv, int64_t lddv_head,
+                                   void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * Plain streaming copy dst[i] = src[i], i < n (measurement aid, not part of the iteration): the
  * bandwidth this kernel reaches on a large buffer is the practical ceiling that the memory-bound
  * kernels of the iteration are compared with, and its known traffic (4n bytes read, 4n written)

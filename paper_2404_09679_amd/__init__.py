@@ -20,6 +20,16 @@ from .binding import (  # noqa: F401
     plan_accumulation,
     stream_copy,
 )
+from .attention import (  # noqa: F401
+    Rotary,
+    cache_append,
+    cache_attention,
+    cross_attention,
+    cross_attention_backward,
+    cross_attention_stats,
+    rotary,
+    rotary_gradient,
+)
 from .tokens import (  # noqa: F401
     Dropout,
     LogProbs,

@@ -30,6 +30,8 @@ EXPORTS = [
     "antdt_dropout", "antdt_token_lookup", "antdt_token_gradient_bytes", "antdt_token_gradient",
     "antdt_gated_saved_bytes", "antdt_gated_forward_bytes", "antdt_gated_forward", "antdt_gated_backward_bytes",
     "antdt_gated_backward", "antdt_token_logprobs_bytes", "antdt_token_logprobs", "antdt_token_logprobs_gradient",
+    "antdt_rotary_turns", "antdt_rotary", "antdt_cache_append", "antdt_cache_attention_bytes", "antdt_cache_attention",
+    "antdt_cross_attention_bytes", "antdt_cross_attention", "antdt_cross_attention_backward_bytes", "antdt_cross_attention_backward",
 ]
 
 
@@ -62,6 +64,10 @@ class SimConfig(C.Structure):
 
 class DropoutSpec(C.Structure):
     _fields_ = [("p", C.c_float), ("call", C.c_uint32), ("seed", C.c_uint64), ("step", C.c_void_p)]
+
+
+class RotarySpec(C.Structure):
+    _fields_ = [("dim", C.c_int32), ("interleaved", C.c_int32), ("magnitude", C.c_float), ("turns", C.c_void_p)]
 
 
 class SimResult(C.Structure):
@@ -137,6 +143,17 @@ def _load():
     lib.antdt_token_logprobs_bytes.argtypes = [i64, i64, i32, size]
     lib.antdt_token_logprobs.argtypes = [vp, i64, i64, i64, i32, vp, vp, vp, vp, i32, vp, vp, vp, C.c_size_t, vp]
     lib.antdt_token_logprobs_gradient.argtypes = [vp, i64, i64, i64, i32, vp, vp, vp, vp, vp, i64, vp]
+    rot, heads = C.POINTER(RotarySpec), [vp, i64, i64, i64]
+    lib.antdt_rotary_turns.argtypes = [i32, C.c_double, C.c_double, C.c_double, C.c_double, C.c_double, C.POINTER(C.c_uint64)]
+    lib.antdt_rotary.argtypes = [vp, i64, i64, i64, i64, i64, i32, vp, rot, i32, vp, i64, i64, vp]
+    lib.antdt_cache_append.argtypes = [vp, i64, i64] * 4 + [i64, i64, i64, i64, i32, rot, vp, vp, i64, i64, i64, i64, i64, vp, i64, i64,
+                                                            i64, vp, vp, vp]
+    lib.antdt_cache_attention_bytes.argtypes = [i64, i64, i64, i64, i32, size]
+    lib.antdt_cache_attention.argtypes = [vp, i64, i64, vp, vp, i64, i64, i64, i64, i64, vp, i64, i64, i64, vp, i64, i64, i64, i32, f32,
+                                          vp, i64, i64, vp, C.c_size_t, vp]
+    lib.antdt_cross_attention_bytes.argtypes = lib.antdt_cross_attention_backward_bytes.argtypes = [i64] * 6 + [i32, size]
+    lib.antdt_cross_attention.argtypes = heads * 3 + [i64] * 6 + [i32, vp, vp, f32] + heads + [vp, vp, C.c_size_t, vp]
+    lib.antdt_cross_attention_backward.argtypes = heads * 5 + [vp] + [i64] * 6 + [i32, vp, vp, f32] + heads * 3 + [vp, C.c_size_t, vp]
     return lib
 
 

@@ -59,8 +59,6 @@ struct Split {
   __host__ __device__ int blocks() const { return whole + rest() * (halves ? 2 : parts); }
 };
 
-// Place of block i of n in the order of the work: an XCD (block i runs on XCD i mod 8) has a share of consecutive places.
-__device__ __forceinline__ int xcd_order(int i, int n) { return (i & 7) * (n >> 3) + min(i & 7, n & 7) + (i >> 3); }
 // Tile `t`: in stripes of 8 along the shorter side, so that the 32 tiles an XCD works on at a time are 8 x 4 and read 12 panels of the operands
 // between them (one stripe of all 32 rows: 33 panels, which the other caches have to deliver; 8192 x 2 x 5632 x 2048).
 __device__ __forceinline__ void tile_at(int t, int tiles_m, int tiles_n, int& tm, int& tn) {
@@ -70,44 +68,6 @@ __device__ __forceinline__ void tile_at(int t, int tiles_m, int tiles_n, int& tm
   const int j = in / w, i = 8 * g + (in - j * w);
   tm = m_minor ? i : j;
   tn = m_minor ? j : i;
-}
-
-// 32 rows of a wavefront's tile to memory, staged in LDS as fp32 so that a row's columns leave 16 bytes at a time.  x[j][e]: as an
-// accumulator's elements.  `rows`, `cols`: that exist from there on; VEC: whole 16-byte groups may be written.
-template <typename T, int TN, bool VEC>
-__device__ __forceinline__ void store_rows(float* st, const f32x16 (&x)[TN], T* out, int64_t ld, int rows, int cols, int lane) {
-  constexpr int WN = 32 * TN, SP = WN + 4, PER = 16 / sizeof(T);   // columns of a lane's store
-  const int fr = lane & 31, fg = lane >> 5;
-#pragma unroll
-  for (int j = 0; j < TN; ++j)
-#pragma unroll
-    for (int v = 0; v < 4; ++v)
-      *reinterpret_cast<float4*>(st + fr * SP + j * 32 + 8 * v + 4 * fg) = make_float4(x[j][4 * v], x[j][4 * v + 1], x[j][4 * v + 2], x[j][4 * v + 3]);
-  wave_lds_order();
-  constexpr int CPR = WN / PER, RPI = 64 / CPR;
-  const int rr = lane / CPR, cc = (lane % CPR) * PER;
-#pragma unroll
-  for (int r0 = 0; r0 < 32; r0 += RPI) {
-    const int r = r0 + rr;
-    const float* s = st + r * SP + cc;
-    T* o = out + (int64_t)r * ld + cc;
-    if (r < rows && cc < cols) {
-      if (VEC) {   // (a whole group exists)
-        const float4 a = *reinterpret_cast<const float4*>(s);
-        if constexpr (sizeof(T) == 4) {
-          store16<false>(o, bits4(a.x, a.y, a.z, a.w));
-        } else {
-          const float4 b = *reinterpret_cast<const float4*>(s + 4);
-          store16<false>(o, make_uint4(f2bf2(a.x, a.y), f2bf2(a.z, a.w), f2bf2(b.x, b.y), f2bf2(b.z, b.w)));
-        }
-      } else {
-#pragma unroll
-        for (int e = 0; e < PER; ++e)
-          if (cc + e < cols) o[e] = from_f32<T>(s[e]);
-      }
-    }
-  }
-  wave_lds_order();
 }
 
 template <typename A>
