@@ -59,28 +59,43 @@ struct HeadTile {
   }
   static __device__ __forceinline__ int slot(int r, int c) { return r * PITCH + (c ^ swizzle(r)); }
 
-  // Row r0 + lane % 32, contraction slots (columns) STEP i ..
-  static __device__ __forceinline__ Fragment along(const char* tile, int r0, int i, int lane) {
-    return *reinterpret_cast<const Fragment*>(tile + slot(r0 + (lane & 31), 2 * i + (lane >> 5)) * 16);
+  // A lane's reads differ from one another by constants, added to the row and exclusive-ored to the slot (the permutation of rows 16 apart is the same),
+  // so that one address serves them all: along_at, down_at of a tile (opaque, lest a register is kept for each).
+  static __device__ __forceinline__ uint32_t at(uint32_t x) {
+    asm volatile("" : "+v"(x));
+    return x;
   }
-  // Column c0 + lane % 32, contraction slots (rows r0 ..) STEP i .. in the order of pack().
-  static __device__ __forceinline__ Fragment down(const char* tile, int r0, int i, int c0, int lane) {
+  static __device__ __forceinline__ uint32_t along_at(uint32_t tile, int lane) { return at(tile + slot(lane & 31, lane >> 5) * 16); }
+  static __device__ __forceinline__ uint32_t down_at(uint32_t tile, int lane) {
+    if constexpr (sizeof(T) == 2) {
+      const int j = lane & 15;
+      return at(tile + slot(4 * (lane >> 5) + (j >> 2), ((lane >> 4) & 1) * 2 + ((j & 3) >> 1)) * 16 + (j & 1) * 8);
+    } else {
+      return at(tile + slot(4 * (lane >> 5), (lane & 31) >> 2) * 16 + (lane & 3) * 4);
+    }
+  }
+  // Row r0 + lane % 32 (r0 a multiple of 32), contraction slots (columns) STEP i ..
+  static __device__ __forceinline__ Fragment along(uint32_t at, int r0, int i) {
+    typedef __attribute__((address_space(3))) Fragment lds_fragment;
+    return *(const lds_fragment*)(uintptr_t)((at ^ (32 * i)) + r0 * ROW);
+  }
+  // Column 32 d + lane % 32, contraction slots (rows r0 ..) STEP i .. in the order of pack().
+  static __device__ __forceinline__ Fragment down(uint32_t at, int r0, int i, int d) {
     if constexpr (sizeof(T) == 2) {
       // (16 lanes read a block of four rows x 16 columns: lane j supplies the address of row j / 4, columns 4 (j % 4) .. + 3 and receives column j)
       typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-      const int j = lane & 15, r = r0 + 16 * i + 4 * (lane >> 5) + (j >> 2), c = (c0 >> 3) + ((lane >> 4) & 1) * 2 + ((j & 3) >> 1);
       union {
         s16x4 s[2];
         Fragment v;
       } u;
-      u.s[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(tile + slot(r, c) * 16 + (j & 1) * 8));
-      u.s[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(tile + slot(r + 8, c) * 16 + (j & 1) * 8));
+      u.s[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(uintptr_t)((at ^ (64 * d)) + (r0 + 16 * i) * ROW));
+      u.s[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(uintptr_t)((at ^ (64 * d) ^ 32) + (r0 + 16 * i + 8) * ROW));
       return u.v;
     } else {
-      const int r = r0 + 8 * i + 4 * (lane >> 5), c = c0 + (lane & 31);
+      typedef __attribute__((address_space(3))) float lds_float;
       Fragment f;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) f[e] = *reinterpret_cast<const float*>(tile + slot(r + e, c >> 2) * 16 + (c & 3) * 4);
+      for (int e = 0; e < 4; ++e) f[e] = *(const lds_float*)(uintptr_t)((at ^ (128 * d) ^ (swizzle(8 * (i & 1) + e) * 16)) + (r0 + 8 * i + e) * ROW);
       return f;
     }
   }

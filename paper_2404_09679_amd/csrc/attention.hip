@@ -19,15 +19,57 @@ struct CrossArgs {
   float* delta;        // d, the same shape
   int64_t S, T;
   int32_t q_heads, heads, group, D;
-  int32_t tiles;       // of a head
+  int32_t tiles, units;   // of a head; heads of all batch entries' keys
   float scale, scale2;   // scale2: scale log2 e
 };
 
-// Own loads have arrived, own reads of LDS are done; then everybody's.
+// Own loads but the last N have arrived, own reads of LDS are done; then everybody's.
+template <int N>
 __device__ __forceinline__ void arrive() {
-  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N) : "memory");
   __builtin_amdgcn_sched_barrier(0);
   block_barrier();
+}
+// Tiles through a ring of STAGES buffers in LDS, LOADS of a wavefront each: while one is worked on, the next STAGES - 1 are under way.
+template <int STAGES, int LOADS, int BYTES>
+struct Ring {
+  uint32_t fill = 0, read = 0;   // bytes from the ring's start: the next buffer to fill, the one to read
+  int64_t left;                  // tiles not asked for yet
+  int64_t behind = 0;            // tiles asked for and not worked on
+  __device__ __forceinline__ explicit Ring(int64_t tiles) : left(tiles) {}
+  template <typename F>
+  __device__ __forceinline__ void ask(F issue) {
+    if (left == 0) return;
+    issue(fill);
+    fill = fill == (STAGES - 1) * BYTES ? 0 : fill + BYTES;
+    --left;
+    ++behind;
+  }
+  template <typename F>
+  __device__ __forceinline__ void start(F issue) {
+#pragma unroll
+    for (int i = 0; i < STAGES - 1; ++i) ask(issue);
+  }
+  // The next tile is in LDS, and the buffer of the one before is asked for again.
+  template <typename F>
+  __device__ __forceinline__ void next(F issue) {
+    if (behind == STAGES - 1) arrive<(STAGES - 2) * LOADS>();
+    else arrive<0>();
+    --behind;
+    ask(issue);
+  }
+  __device__ __forceinline__ void done() { read = read == (STAGES - 1) * BYTES ? 0 : read + BYTES; }
+};
+
+// Block i of `units` x n: which unit, and which of its blocks.  Blocks of a unit (a head of one batch entry's keys, and who reads it) share an XCD (block
+// i runs on XCD i mod 8), whose L2 then has the rows they all read; neighbouring units are on different ones, so that a batch entry of long
+// sequences is everybody's work.  What is left of less than 8 units is spread over all.
+__device__ __forceinline__ void place_of(int i, int units, int n, int& unit, int& block) {
+  const int whole = (units & ~7) * n;
+  const int x = i < whole ? i & 7 : 0, j = i < whole ? i >> 3 : i - whole;
+  const int u = j / n;
+  block = j - u * n;
+  unit = i < whole ? 8 * u + x : (units & ~7) + u;
 }
 
 constexpr int BLOCK_ROWS = 128;   // queries or keys of a block, 32 to a wavefront
@@ -62,42 +104,46 @@ __device__ __forceinline__ void clear_rows(const Rows& to, int64_t r0, int64_t r
 
 // ------------------------------------------------------------- forward
 // A block has 128 queries of a head, 32 to a wavefront; tiles of BT keys and values go through LDS, the next one's loads under way.
-template <typename T, int DP, int BT>
-struct Forward {
+template <typename T, int DP, int BT, int STAGES_>
+struct KeyTiles {
   typedef HeadTile<T, DP> Tile;
   typedef TileLoad<T, DP, BT, 256> Load;
-  static constexpr int STAGE = 2 * Load::BYTES;
-  static constexpr int LDS = 2 * STAGE > 4 * Staging<DP>::BYTES ? 2 * STAGE : 4 * Staging<DP>::BYTES;
+  static constexpr int STAGES = STAGES_, STAGE = 2 * Load::BYTES, RING = STAGES * STAGE;
+  static constexpr int LDS = RING > 4 * Staging<DP>::BYTES ? RING : 4 * Staging<DP>::BYTES;
+  typedef ::antdt::Ring<STAGES, 2 * Load::PIECES, STAGE> Ring;
 };
-template <typename T, int DP, int BT>
+template <typename T, int DP, int BT, int STAGES>
 __global__ __launch_bounds__(256, 2) void cross_forward_kernel(CrossArgs a) {
-  typedef Forward<T, DP, BT> F;
+  typedef KeyTiles<T, DP, BT, STAGES> F;
   typedef typename F::Tile Tile;
   typedef Core<T> C;
   extern __shared__ __attribute__((aligned(1024))) char lds[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
-  const int place = xcd_order(blockIdx.x, gridDim.x), tile = place % a.tiles, bh = place / a.tiles;
-  const int h = bh % a.q_heads;
-  const int64_t b = bh / a.q_heads;
+  int unit, block;
+  place_of(blockIdx.x, a.units, a.group * a.tiles, unit, block);
+  const int tile = block % a.tiles, h = unit % a.heads * a.group + block / a.tiles;
+  const int64_t b = unit / a.heads, bh = b * a.q_heads + h;
   const int64_t q_len = length_of(a.q_lengths, b, a.S), k_len = length_of(a.k_lengths, b, a.T);
   const int64_t first = (int64_t)tile * BLOCK_ROWS, last = min(first + BLOCK_ROWS, a.S), r0 = first + wave * 32;
   const Rows out = a.out.rows(b, h);
-  float* stats = a.stats ? a.stats + ((int64_t)bh * a.S) : nullptr;
+  float* stats = a.stats ? a.stats + (bh * a.S) : nullptr;
   const int64_t end = k_len > 0 ? min(max(q_len, first), last) : first;   // rows with keys
   clear_rows<T>(out, end, last, a.D);
   if (stats)
     for (int64_t r = end + threadIdx.x; r < last; r += 256) stats[r] = INFINITY;
   if (end == first) return;
   if (a.D < DP) {
-    clear_lds(lds, 2 * F::STAGE, 256);
+    clear_lds(lds, F::RING, 256);
     __syncthreads();
   }
   const typename F::Load load(threadIdx.x, a.D);
   const Rows k = a.k.rows(b, h / a.group), v = a.v.rows(b, h / a.group);
   const uint32_t lds0 = lds_address(lds) + wave * 1024;
-  auto issue = [&](int64_t t, int stage) {
-    load(k, t, k_len, lds0 + stage * F::STAGE);
-    load(v, t, k_len, lds0 + stage * F::STAGE + F::Load::BYTES);
+  int64_t asked = 0;
+  auto issue = [&](uint32_t to) {
+    load(k, asked, k_len, lds0 + to);
+    load(v, asked, k_len, lds0 + to + F::Load::BYTES);
+    asked += BT;
   };
   typename C::Fragment q[DP / C::STEP];
   load_rows<T, DP>(a.q.rows(b, h), r0, q_len, a.D, lane, q);
@@ -105,19 +151,18 @@ __global__ __launch_bounds__(256, 2) void cross_forward_kernel(CrossArgs a) {
 #pragma unroll
   for (int d = 0; d < DP / 32; ++d) o[d] = zeros();
   float m = -INFINITY, l = 0.0f;   // of row lane % 32; l: of this lane's keys
-  issue(0, 0);
-  int stage = 0;
-  for (int64_t t = 0; t < k_len; t += BT, stage ^= 1) {
-    arrive();
-    if (t + BT < k_len) issue(t + BT, stage ^ 1);
-    const char* tk = lds + stage * F::STAGE;
-    const char* tv = tk + F::Load::BYTES;
+  typename F::Ring ring((k_len + BT - 1) / BT);
+  ring.start(issue);
+  for (int64_t t = 0; t < k_len; t += BT, ring.done()) {
+    ring.next(issue);
+    const uint32_t tile0 = lds_address(lds) + ring.read;
+    const uint32_t tk = Tile::along_at(tile0, lane), tv = Tile::down_at(tile0 + F::Load::BYTES, lane);
     f32x16 s[BT / 32];
 #pragma unroll
     for (int j = 0; j < BT / 32; ++j) {
       s[j] = zeros();
 #pragma unroll
-      for (int i = 0; i < DP / C::STEP; ++i) C::multiply(Tile::along(tk, 32 * j, i, lane), q[i], s[j]);
+      for (int i = 0; i < DP / C::STEP; ++i) C::multiply(Tile::along(tk, 32 * j, i), q[i], s[j]);
     }
     if (t + BT > k_len) {
 #pragma unroll
@@ -156,10 +201,10 @@ __global__ __launch_bounds__(256, 2) void cross_forward_kernel(CrossArgs a) {
       for (int i = 0; i < 32 / C::STEP; ++i) {
         const typename C::Fragment p = C::pack(s[j], i);
 #pragma unroll
-        for (int d = 0; d < DP / 32; ++d) C::multiply(Tile::down(tv, 32 * j, i, 32 * d, lane), p, o[d]);
+        for (int d = 0; d < DP / 32; ++d) C::multiply(Tile::down(tv, 32 * j, i, d), p, o[d]);
       }
   }
-  arrive();   // (the buffers are free)
+  arrive<0>();   // (the buffers are free)
   l += other_half(l);
   write_rows<T, DP>(lds + wave * Staging<DP>::BYTES, o, l == 0.0f ? 0.0f : 1.0f / l, out, r0, end, a.D, lane);
   const int64_t r = r0 + (lane & 31);
@@ -170,16 +215,17 @@ __global__ __launch_bounds__(256, 2) void cross_forward_kernel(CrossArgs a) {
 // As the forward pass; a lane has the sums L and d of its row.  Also leaves d for the gradients of keys and values.  d comes from out as it was
 // kept; where one tile has all the keys it is the sum of p dP instead (the same number): of few keys dP - d nearly vanishes, and what out lost to its
 // rounding would show (2 keys, bf16: dQ off by 0.005 of its norm, so by 0.0025, the operands' rounding).
-template <typename T, int DP, int BT>
+template <typename T, int DP, int BT, int STAGES>
 __global__ __launch_bounds__(256, sizeof(T) == 4 && DP == 128 ? 1 : 2) void cross_dq_kernel(CrossArgs a) {
-  typedef Forward<T, DP, BT> F;
+  typedef KeyTiles<T, DP, BT, STAGES> F;
   typedef typename F::Tile Tile;
   typedef Core<T> C;
   extern __shared__ __attribute__((aligned(1024))) char lds[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
-  const int place = xcd_order(blockIdx.x, gridDim.x), tile = place % a.tiles, bh = place / a.tiles;
-  const int h = bh % a.q_heads;
-  const int64_t b = bh / a.q_heads;
+  int unit, block;
+  place_of(blockIdx.x, a.units, a.group * a.tiles, unit, block);
+  const int tile = block % a.tiles, h = unit % a.heads * a.group + block / a.tiles;
+  const int64_t b = unit / a.heads, bh = b * a.q_heads + h;
   const int64_t q_len = length_of(a.q_lengths, b, a.S), k_len = length_of(a.k_lengths, b, a.T);
   const int64_t first = (int64_t)tile * BLOCK_ROWS, last = min(first + BLOCK_ROWS, a.S), r0 = first + wave * 32;
   const int64_t end = k_len > 0 ? min(max(q_len, first), last) : first;
@@ -197,41 +243,42 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP == 128 ? 1 : 2) void cros
     for (int e = 0; e < C::PER; ++e) delta = fmaf((float)q[i][e], (float)g[i][e], delta);
   delta += other_half(delta);
   const int64_t r = r0 + (lane & 31);
-  const float sum = r < end ? a.stats[(int64_t)bh * a.S + r] : INFINITY;
+  const float sum = r < end ? a.stats[bh * a.S + r] : INFINITY;
   const bool one_tile = k_len <= BT;
   if (!one_tile) {
-    if (r < end && lane < 32) a.delta[(int64_t)bh * a.S + r] = delta;
+    if (r < end && lane < 32) a.delta[bh * a.S + r] = delta;
     if (!wanted) return;
   }
   load_rows<T, DP>(a.q.rows(b, h), r0, q_len, a.D, lane, q);
   if (a.D < DP) {
-    clear_lds(lds, 2 * F::STAGE, 256);
+    clear_lds(lds, F::RING, 256);
     __syncthreads();
   }
   const typename F::Load load(threadIdx.x, a.D);
   const Rows k = a.k.rows(b, h / a.group), v = a.v.rows(b, h / a.group);
   const uint32_t lds0 = lds_address(lds) + wave * 1024;
-  auto issue = [&](int64_t t, int stage) {
-    load(k, t, k_len, lds0 + stage * F::STAGE);
-    load(v, t, k_len, lds0 + stage * F::STAGE + F::Load::BYTES);
+  int64_t asked = 0;
+  auto issue = [&](uint32_t to) {
+    load(k, asked, k_len, lds0 + to);
+    load(v, asked, k_len, lds0 + to + F::Load::BYTES);
+    asked += BT;
   };
   f32x16 o[DP / 32];
 #pragma unroll
   for (int d = 0; d < DP / 32; ++d) o[d] = zeros();
-  issue(0, 0);
-  int stage = 0;
-  for (int64_t t = 0; t < k_len; t += BT, stage ^= 1) {
-    arrive();
-    if (t + BT < k_len) issue(t + BT, stage ^ 1);
-    const char* tk = lds + stage * F::STAGE;
-    const char* tv = tk + F::Load::BYTES;
+  typename F::Ring ring((k_len + BT - 1) / BT);
+  ring.start(issue);
+  for (int64_t t = 0; t < k_len; t += BT, ring.done()) {
+    ring.next(issue);
+    const uint32_t tile0 = lds_address(lds) + ring.read;
+    const uint32_t tk = Tile::along_at(tile0, lane), tv = Tile::along_at(tile0 + F::Load::BYTES, lane), kt = Tile::down_at(tile0, lane);
     // p and dP of keys 32 j .. of the tile
     auto scores = [&](int j, f32x16& s, f32x16& dp) {
       s = dp = zeros();
 #pragma unroll
-      for (int i = 0; i < DP / C::STEP; ++i) C::multiply(Tile::along(tk, 32 * j, i, lane), q[i], s);
+      for (int i = 0; i < DP / C::STEP; ++i) C::multiply(Tile::along(tk, 32 * j, i), q[i], s);
 #pragma unroll
-      for (int i = 0; i < DP / C::STEP; ++i) C::multiply(Tile::along(tv, 32 * j, i, lane), g[i], dp);
+      for (int i = 0; i < DP / C::STEP; ++i) C::multiply(Tile::along(tv, 32 * j, i), g[i], dp);
 #pragma unroll
       for (int e = 0; e < 16; ++e) s[e] = exp2_(fmaf(s[e], a.scale2, -sum));
       if (t + BT > k_len) {
@@ -249,7 +296,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP == 128 ? 1 : 2) void cros
         for (int e = 0; e < 16; ++e) delta = fmaf(s[e], dp[e], delta);
       }
       delta += other_half(delta);
-      if (r < end && lane < 32) a.delta[(int64_t)bh * a.S + r] = delta;
+      if (r < end && lane < 32) a.delta[bh * a.S + r] = delta;
       if (!wanted) return;   // (nothing is under way)
     }
 #pragma unroll
@@ -262,109 +309,155 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DP == 128 ? 1 : 2) void cros
       for (int i = 0; i < 32 / C::STEP; ++i) {
         const typename C::Fragment ds = C::pack(s, i);
 #pragma unroll
-        for (int d = 0; d < DP / 32; ++d) C::multiply(Tile::down(tk, 32 * j, i, 32 * d, lane), ds, o[d]);
+        for (int d = 0; d < DP / 32; ++d) C::multiply(Tile::down(kt, 32 * j, i, d), ds, o[d]);
       }
     }
   }
-  arrive();
+  arrive<0>();
   write_rows<T, DP>(lds + wave * Staging<DP>::BYTES, o, a.scale, dq, r0, end, a.D, lane);
 }
 
 // ------------------------------------------------------------- gradients of keys and values
 // A block has 128 keys of a head, 32 to a wavefront, and goes through tiles of BR queries and their outputs' gradients, of every head that shares
 // the keys.
-template <typename T, int DP, int BR>
-struct Shared {
+template <typename T, int DP, int BR, int STAGES_, int KEYS, bool HELD>
+struct QueryTiles {
   typedef HeadTile<T, DP> Tile;
   typedef TileLoad<T, DP, BR, 256> Load;
-  static constexpr int STATS = 2 * BR * 4, STAGE = 2 * Load::BYTES;
-  static constexpr int RING = 2 * (STAGE + STATS), LDS = RING > 4 * Staging<DP>::BYTES ? RING : 4 * Staging<DP>::BYTES;
+  static constexpr int STATS = 2 * BR * 4;   // L and d of the rows, for each wavefront: (L, d) of 32 rows behind each other
+  typedef TileLoad<T, DP, KEYS, 256> Values;
+  static constexpr int STAGES = STAGES_, STAGE = 2 * Load::BYTES + 4 * STATS, RING = STAGES * STAGE + (HELD ? 0 : Values::BYTES);
+  static constexpr int LDS = RING > 4 * Staging<DP>::BYTES ? RING : 4 * Staging<DP>::BYTES;
+  typedef ::antdt::Ring<STAGES, 2 * Load::PIECES + BR / 32, STAGE> Ring;
 };
-template <typename T, int DP, int BR>
-__global__ __launch_bounds__(256, sizeof(T) == 4 && DP == 128 ? 1 : 2) void cross_dkv_kernel(CrossArgs a) {
-  typedef Shared<T, DP, BR> F;
+template <typename T, int DP, int BR, int STAGES, int NT, bool HELD, int PER_CU>
+__global__ __launch_bounds__(256, PER_CU) void cross_dkv_kernel(CrossArgs a) {
+  typedef QueryTiles<T, DP, BR, STAGES, 128 * NT, HELD> F;
   typedef typename F::Tile Tile;
   typedef Core<T> C;
+  constexpr int KEYS = 128 * NT;
   extern __shared__ __attribute__((aligned(1024))) char lds[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
-  const int place = xcd_order(blockIdx.x, gridDim.x), tile = place % a.tiles, bh = place / a.tiles;
-  const int h = bh % a.heads;
-  const int64_t b = bh / a.heads;
+  int unit, tile;
+  place_of(blockIdx.x, a.units, a.tiles, unit, tile);
+  const int h = unit % a.heads;
+  const int64_t b = unit / a.heads;
   const int64_t q_len = length_of(a.q_lengths, b, a.S), k_len = length_of(a.k_lengths, b, a.T);
-  const int64_t first = (int64_t)tile * BLOCK_ROWS, last = min(first + BLOCK_ROWS, a.T), t0 = first + wave * 32;
+  const int64_t first = (int64_t)tile * KEYS, last = min(first + KEYS, a.T), t0 = first + wave * (32 * NT);
   const int64_t end = q_len > 0 ? min(max(k_len, first), last) : first;
   const Rows dk = a.dk.rows(b, h), dv = a.dv.rows(b, h);
   clear_rows<T>(dk, end, last, a.D);
   clear_rows<T>(dv, end, last, a.D);
   if (end == first) return;
   if (a.D < DP) {
-    clear_lds(lds, 2 * F::STAGE, 256);
+    clear_lds(lds, F::RING, 256);
     __syncthreads();
   }
   const typename F::Load load(threadIdx.x, a.D);
-  const uint32_t lds0 = lds_address(lds) + wave * 1024, stats0 = lds_address(lds) + 2 * F::STAGE;
-  auto issue = [&](int64_t g, int64_t r, int stage) {
-    const int64_t hq = (int64_t)h * a.group + g;
-    load(a.q.rows(b, hq), r, q_len, lds0 + stage * F::STAGE);
-    load(a.dout.rows(b, hq), r, q_len, lds0 + stage * F::STAGE + F::Load::BYTES);
-    if (wave < 2 && lane < BR) {   // L, then d
-      const float* from = (wave == 0 ? a.stats : a.delta) + (b * a.q_heads + hq) * a.S;
-      load_lds4(from + min(r + lane, q_len - 1), stats0 + stage * F::STATS + wave * (BR * 4));
+  const uint32_t lds0 = lds_address(lds) + wave * 1024;
+  int64_t asked_g = 0, asked = 0;
+  const float* const sums_of = half ? a.delta : a.stats;
+  auto issue = [&](uint32_t to) {
+    const int64_t hq = (int64_t)h * a.group + asked_g;
+    load(a.q.rows(b, hq), asked, q_len, lds0 + to);
+    load(a.dout.rows(b, hq), asked, q_len, lds0 + to + F::Load::BYTES);
+#pragma unroll
+    for (int j = 0; j < BR / 32; ++j)
+      load_lds4(sums_of + (b * a.q_heads + hq) * a.S + min(asked + 32 * j + (lane & 31), q_len - 1),
+                lds_address(lds) + to + 2 * F::Load::BYTES + wave * F::STATS + j * 256);
+    asked += BR;
+    if (asked >= q_len) {
+      asked = 0;
+      ++asked_g;
     }
   };
-  typename C::Fragment k[DP / C::STEP], v[DP / C::STEP];
-  load_rows<T, DP>(a.k.rows(b, h), t0, k_len, a.D, lane, k);
-  load_rows<T, DP>(a.v.rows(b, h), t0, k_len, a.D, lane, v);
-  f32x16 ok[DP / 32], ov[DP / 32];
+  typename C::Fragment k[NT][DP / C::STEP], v[HELD ? NT : 1][HELD ? DP / C::STEP : 1];
+  f32x16 ok[NT][DP / 32], ov[NT][DP / 32];
 #pragma unroll
-  for (int d = 0; d < DP / 32; ++d) ok[d] = ov[d] = zeros();
-  issue(0, 0, 0);
-  int stage = 0;
-  for (int64_t g = 0, r = 0; g < a.group; stage ^= 1) {
-    arrive();
-    int64_t g1 = g, r1 = r + BR;
-    if (r1 >= q_len) {
-      r1 = 0;
-      ++g1;
-    }
-    if (g1 < a.group) issue(g1, r1, stage ^ 1);
-    const char* tq = lds + stage * F::STAGE;
-    const char* tg = tq + F::Load::BYTES;
-    const float* sums = reinterpret_cast<const float*>(lds + 2 * F::STAGE + stage * F::STATS);
+  for (int n = 0; n < NT; ++n) {
+    load_rows<T, DP>(a.k.rows(b, h), t0 + 32 * n, k_len, a.D, lane, k[n]);
+    if constexpr (HELD) load_rows<T, DP>(a.v.rows(b, h), t0 + 32 * n, k_len, a.D, lane, v[n]);
 #pragma unroll
+    for (int d = 0; d < DP / 32; ++d) ok[n][d] = ov[n][d] = zeros();
+  }
+  if constexpr (!HELD) {
+    const typename F::Values values(threadIdx.x, a.D);
+    values(a.v.rows(b, h), first, k_len, lds0 + STAGES * F::STAGE);
+  }
+  typename F::Ring ring((q_len + BR - 1) / BR * a.group);
+  ring.start(issue);
+  for (int64_t g = 0, r = 0; g < a.group; ring.done()) {
+    ring.next(issue);
+    const uint32_t tile0 = lds_address(lds) + ring.read;
+    const float* sums = reinterpret_cast<const float*>(lds + ring.read + 2 * F::Load::BYTES + wave * F::STATS);
+    const uint32_t tq = Tile::along_at(tile0, lane), tg = Tile::along_at(tile0 + F::Load::BYTES, lane);
+    const uint32_t vt = HELD ? 0 : Tile::along_at(lds_address(lds) + STAGES * F::STAGE + wave * (32 * NT * Tile::ROW), lane);
+    const uint32_t qt = Tile::down_at(tile0, lane), gt = Tile::down_at(tile0 + F::Load::BYTES, lane);
+#pragma unroll 1
     for (int j = 0; j < BR / 32; ++j) {
-      f32x16 s = zeros(), dp = zeros();
+      f32x16 s[NT], dp[NT];
 #pragma unroll
-      for (int i = 0; i < DP / C::STEP; ++i) C::multiply(Tile::along(tq, 32 * j, i, lane), k[i], s);
+      for (int n = 0; n < NT; ++n) s[n] = dp[n] = zeros();
 #pragma unroll
-      for (int i = 0; i < DP / C::STEP; ++i) C::multiply(Tile::along(tg, 32 * j, i, lane), v[i], dp);
+      for (int i = 0; i < DP / C::STEP; ++i) {
+        const typename C::Fragment x = Tile::along(tq, 32 * j, i);
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const int row = 32 * j + 8 * (e >> 2) + 4 * half + (e & 3);
-        s[e] = exp2_(fmaf(s[e], a.scale2, -sums[row]));
-        dp[e] = s[e] * (dp[e] - sums[BR + row]);
+        for (int n = 0; n < NT; ++n) C::multiply(x, k[n][i], s[n]);
       }
+#pragma unroll
+      for (int i = 0; i < DP / C::STEP; ++i) {
+        const typename C::Fragment x = Tile::along(tg, 32 * j, i);
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          if constexpr (HELD) C::multiply(x, v[n][i], dp[n]);
+          else C::multiply(x, Tile::along(vt, 32 * n, i), dp[n]);
+        }
+      }
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int row = 64 * j + 8 * (e >> 2) + 4 * half + (e & 3);
+          s[n][e] = exp2_(fmaf(s[n][e], a.scale2, -sums[row]));
+          dp[n][e] = s[n][e] * (dp[n][e] - sums[32 + row]);
+        }
       if (r + BR > q_len) {
 #pragma unroll
-        for (int e = 0; e < 16; ++e)
-          if (r + 32 * j + 8 * (e >> 2) + 4 * half + (e & 3) >= q_len) s[e] = dp[e] = 0.0f;
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            if (r + 32 * j + 8 * (e >> 2) + 4 * half + (e & 3) >= q_len) s[n][e] = dp[n][e] = 0.0f;
       }
 #pragma unroll
       for (int i = 0; i < 32 / C::STEP; ++i) {
-        const typename C::Fragment p = C::pack(s, i), ds = C::pack(dp, i);
+        typename C::Fragment p[NT], ds[NT];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          p[n] = C::pack(s[n], i);
+          ds[n] = C::pack(dp[n], i);
+        }
 #pragma unroll
         for (int d = 0; d < DP / 32; ++d) {
-          C::multiply(Tile::down(tg, 32 * j, i, 32 * d, lane), p, ov[d]);
-          C::multiply(Tile::down(tq, 32 * j, i, 32 * d, lane), ds, ok[d]);
+          const typename C::Fragment x = Tile::down(gt, 32 * j, i, d), y = Tile::down(qt, 32 * j, i, d);
+#pragma unroll
+          for (int n = 0; n < NT; ++n) C::multiply(x, p[n], ov[n][d]);
+#pragma unroll
+          for (int n = 0; n < NT; ++n) C::multiply(y, ds[n], ok[n][d]);
         }
       }
     }
-    g = g1;
-    r = r1;
+    r += BR;
+    if (r >= q_len) {
+      r = 0;
+      ++g;
+    }
   }
-  arrive();
-  write_rows<T, DP>(lds + wave * Staging<DP>::BYTES, ok, a.scale, dk, t0, end, a.D, lane);
-  write_rows<T, DP>(lds + wave * Staging<DP>::BYTES, ov, 1.0f, dv, t0, end, a.D, lane);
+  arrive<0>();
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    write_rows<T, DP>(lds + wave * Staging<DP>::BYTES, ok[n], a.scale, dk, t0 + 32 * n, end, a.D, lane);
+    write_rows<T, DP>(lds + wave * Staging<DP>::BYTES, ov[n], 1.0f, dv, t0 + 32 * n, end, a.D, lane);
+  }
 }
 
 // ------------------------------------------------------------- launches
@@ -375,24 +468,36 @@ hipError_t launch(K kernel, int lds, std::atomic<uint64_t>& allowed, int64_t blo
   hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), lds, s, a);
   return hipGetLastError();
 }
+// Tiles: rows, and buffers of the ring.
+template <typename T, int DP>
+struct Tiles {
+  static constexpr bool LARGE = DP * sizeof(T) >= 256;
+  static constexpr int KEYS = DP * sizeof(T) == 512 ? 32 : 64, KEY_STAGES = 2;
+  static constexpr int QUERIES = LARGE ? 32 : 64, QUERY_STAGES = 2;
+  static constexpr bool HELD = !(sizeof(T) == 2 && DP == 128);
+  static constexpr int KEY_TILES = 1, PER_CU = DP * sizeof(T) == 512 ? 1 : 2;
+};
 template <typename T, int DP>
 hipError_t launch_forward(const CrossArgs& a, int64_t blocks, hipStream_t s) {
   static std::atomic<uint64_t> allowed{0};
-  constexpr int BT = sizeof(T) == 4 && DP == 128 ? 32 : 64;
-  return launch(cross_forward_kernel<T, DP, BT>, Forward<T, DP, BT>::LDS, allowed, blocks, a, s);
+  typedef Tiles<T, DP> Z;
+  return launch(cross_forward_kernel<T, DP, Z::KEYS, Z::KEY_STAGES>, KeyTiles<T, DP, Z::KEYS, Z::KEY_STAGES>::LDS, allowed, blocks, a, s);
 }
 template <typename T, int DP>
 hipError_t launch_dq(const CrossArgs& a, int64_t blocks, hipStream_t s) {
   static std::atomic<uint64_t> allowed{0};
-  constexpr int BT = sizeof(T) == 4 && DP == 128 ? 32 : 64;
-  return launch(cross_dq_kernel<T, DP, BT>, Forward<T, DP, BT>::LDS, allowed, blocks, a, s);
+  typedef Tiles<T, DP> Z;
+  return launch(cross_dq_kernel<T, DP, Z::KEYS, Z::KEY_STAGES>, KeyTiles<T, DP, Z::KEYS, Z::KEY_STAGES>::LDS, allowed, blocks, a, s);
 }
 template <typename T, int DP>
-hipError_t launch_dkv(const CrossArgs& a, int64_t blocks, hipStream_t s) {
+hipError_t launch_dkv(CrossArgs a, int64_t heads, hipStream_t s) {
   static std::atomic<uint64_t> allowed{0};
-  constexpr int BR = sizeof(T) == 4 && DP == 128 ? 32 : 64;
-  return launch(cross_dkv_kernel<T, DP, BR>, Shared<T, DP, BR>::LDS, allowed, blocks, a, s);
+  typedef Tiles<T, DP> Z;
+  a.tiles = (int)div_up(a.T, 128 * Z::KEY_TILES);
+  return launch(cross_dkv_kernel<T, DP, Z::QUERIES, Z::QUERY_STAGES, Z::KEY_TILES, Z::HELD, Z::PER_CU>,
+                QueryTiles<T, DP, Z::QUERIES, Z::QUERY_STAGES, 128 * Z::KEY_TILES, Z::HELD>::LDS, allowed, heads * a.tiles, a, s);
 }
+
 struct Shape {
   int64_t B, S, T, q_heads, heads, D;
   int32_t dtype;
@@ -455,7 +560,7 @@ int antdt_cross_attention(const void* q, int64_t ldq_batch, int64_t ldq, int64_t
     return op_hip(call, launch_stream(f, dtype, workspace, s));
   }
   a.q_lengths = q_lengths; a.k_lengths = k_lengths; a.stats = stats; a.S = S; a.T = T;
-  a.q_heads = (int)q_heads; a.heads = (int)heads; a.group = (int)(q_heads / heads); a.D = (int)D;
+  a.q_heads = (int)q_heads; a.heads = (int)heads; a.group = (int)(q_heads / heads); a.D = (int)D; a.units = (int)(B * heads);
   a.tiles = (int)div_up(S, BLOCK_ROWS);
   return op_hip(call, by_size(dtype, (int)D, [&](auto t, auto dp) { return launch_forward<decltype(t), decltype(dp)::value>(a, B * q_heads * a.tiles, s); }));
 }
@@ -498,16 +603,13 @@ int antdt_cross_attention_backward(const void* dout, int64_t lddo_batch, int64_t
   if (!keys && !queries) return ANTDT_OK;
   OP_TRY(op_workspace(call, workspace, workspace_bytes, need));
   a.q_lengths = q_lengths; a.k_lengths = k_lengths; a.stats = const_cast<float*>(stats); a.delta = reinterpret_cast<float*>(workspace); a.S = S; a.T = T;
-  a.q_heads = (int)q_heads; a.heads = (int)heads; a.group = (int)(q_heads / heads); a.D = (int)D;
+  a.q_heads = (int)q_heads; a.heads = (int)heads; a.group = (int)(q_heads / heads); a.D = (int)D; a.units = (int)(B * heads);
   const hipStream_t s = (hipStream_t)stream;
   if (queries) {
     a.tiles = (int)div_up(S, BLOCK_ROWS);
     OP_TRY(op_hip(call, by_size(dtype, (int)D, [&](auto t, auto dp) { return launch_dq<decltype(t), decltype(dp)::value>(a, B * q_heads * a.tiles, s); })));
   }
-  if (keys) {
-    a.tiles = (int)div_up(T, BLOCK_ROWS);
-    OP_TRY(op_hip(call, by_size(dtype, (int)D, [&](auto t, auto dp) { return launch_dkv<decltype(t), decltype(dp)::value>(a, B * heads * a.tiles, s); })));
-  }
+  if (keys) OP_TRY(op_hip(call, by_size(dtype, (int)D, [&](auto t, auto dp) { return launch_dkv<decltype(t), decltype(dp)::value>(a, B * heads, s); })));
   return ANTDT_OK;
 }
 

@@ -30,7 +30,7 @@ struct Stream {
   typedef HeadTile<T, DP> Tile;
   static constexpr int BYTES = 32 * Tile::ROW, PIECES = BYTES / 1024;
   static constexpr int STAGES = BYTES >= 16384 ? 1 : BYTES >= 8192 ? 2 : 4;
-  static constexpr int ENTRIES = 2 * STAGES + 1, WAVE = 2 * STAGES * BYTES + ENTRIES * 256, LDS = WAVES * WAVE;
+  static constexpr int ENTRIES = 2 * STAGES + 1, WAVE = (2 * STAGES * BYTES + ENTRIES * 256 + 1023) / 1024 * 1024, LDS = WAVES * WAVE;
 };
 
 template <typename T, int DP, bool PAGED>
@@ -183,10 +183,10 @@ __global__ __launch_bounds__(64 * WAVES, 1) void stream_kernel(StreamArgs a) {
         }
         some = (uint32_t)__ballot(x);
       }
-      const char* tk = mine + slot_of(i);
+      const uint32_t tk = Tile::along_at(ring + slot_of(i), lane);
       f32x16 s = zeros();
 #pragma unroll
-      for (int j = 0; j < DP / C::STEP; ++j) C::multiply(Tile::along(tk, 0, j, lane), q[j], s);
+      for (int j = 0; j < DP / C::STEP; ++j) C::multiply(Tile::along(tk, 0, j), q[j], s);
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
       __builtin_amdgcn_sched_barrier(0);
       keys(i + S);
@@ -216,12 +216,12 @@ __global__ __launch_bounds__(64 * WAVES, 1) void stream_kernel(StreamArgs a) {
       }
       wait_loads<S * (N + E) + (S - 1) * N>();
       __builtin_amdgcn_sched_barrier(0);
-      const char* tv = mine + S * F::BYTES + slot_of(i);
+      const uint32_t tv = Tile::down_at(ring + S * F::BYTES + slot_of(i), lane);
 #pragma unroll
       for (int j = 0; j < 32 / C::STEP; ++j) {
         const typename C::Fragment p = C::pack(s, j);
 #pragma unroll
-        for (int d = 0; d < DP / 32; ++d) C::multiply(Tile::down(tv, 0, j, 32 * d, lane), p, o[d]);
+        for (int d = 0; d < DP / 32; ++d) C::multiply(Tile::down(tv, 0, j, d), p, o[d]);
       }
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
       __builtin_amdgcn_sched_barrier(0);
