@@ -7,6 +7,7 @@
 //   m = max m_i,  l = sum l_i 2^(m_i - m),  out = sum o_i 2^(m_i - m) / l.
 // Bound by memory: a key head's queries share what is read of it.
 #include "attend.h"
+#include "sort.h"
 
 namespace antdt {
 namespace {
@@ -15,84 +16,82 @@ constexpr int WAVES = 4;                // of a block
 constexpr int BLOCKS = 256;             // one to a compute unit
 constexpr int LEAST = 4;                // tiles of a wavefront, before the next one gets some
 
-// Work in tiles: [0, total) in `waves` pieces.
-struct Pieces {
-  int64_t total, waves;
-  __device__ __forceinline__ Pieces(int64_t n, int most) : total(n), waves(max((int64_t)1, min((int64_t)most, (n + LEAST - 1) / LEAST))) {}
-  __device__ __forceinline__ int64_t first(int64_t w) const { return w >= waves ? total : w * total / waves; }
-  __device__ __forceinline__ int64_t owner(int64_t tile) const { return ((tile + 1) * waves - 1) / total; }
+// Work in tiles, [0, total), to the wavefronts: the first `more` have one more than the others.
+struct Shares {
+  int64_t total, waves, each, more;
+  __device__ __forceinline__ Shares(int64_t n, int most) : total(n), waves(max((int64_t)1, min((int64_t)most, (n + LEAST - 1) / LEAST))), each(n / waves), more(n - each * waves) {}
+  __device__ __forceinline__ int64_t first(int64_t w) const { return min(w * each + min(w, more), total); }
+  __device__ __forceinline__ int64_t owner(int64_t tile) const {
+    const int64_t large = more * (each + 1), behind = tile - large;   // (one division for both kinds)
+    return (behind < 0 ? tile : behind) / (behind < 0 ? each + 1 : each) + (behind < 0 ? 0 : more);
+  }
 };
 
 __device__ __forceinline__ int64_t tiles_of(const StreamArgs& a, int64_t b) { return (length_of(a.k_lengths, b, a.T) + 31) >> 5; }
+// x of lane `from`, known to the compiler to be the wavefront's.
+__device__ __forceinline__ int64_t of_lane(int64_t x, int from) {
+  return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)((uint64_t)x >> 32), from) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)x, from));
+}
+
+// What a row that there is not is read from.
+static __device__ __attribute__((aligned(16))) uint32_t zero_row[128];
 
 template <typename T, int DP>
 struct Stream {
   typedef HeadTile<T, DP> Tile;
-  static constexpr int BYTES = 32 * Tile::ROW, PIECES = BYTES / 1024;
+  static constexpr int BYTES = 32 * Tile::ROW, PIECES = BYTES / 1024, PIECE_ROWS = 64 / Tile::PITCH;
   static constexpr int STAGES = BYTES >= 16384 ? 1 : BYTES >= 8192 ? 2 : 4;
-  static constexpr int ENTRIES = 2 * STAGES + 1, WAVE = (2 * STAGES * BYTES + ENTRIES * 256 + 1023) / 1024 * 1024, LDS = WAVES * WAVE;
+  // A wavefront's LDS: the rings of keys and of values, where a tile's rows are, the pages of the next tiles' rows.
+  static constexpr int VALUES = STAGES * BYTES, WHERE = 2 * VALUES, PAGES = WHERE + 512, AHEAD = 2 * STAGES + 1;
+  static constexpr int WAVE = (PAGES + AHEAD * 256 + 1023) / 1024 * 1024, LDS = WAVES * WAVE;
 };
 
-template <typename T, int DP, bool PAGED>
+// DP columns of a row in LDS, of which the first COLS take part.  The loops that only move data stay rolled up: a launch this short waits for its code
+// as well as for its data (of 34 KB, 20 us before the first tile was done; these 10 to 16 KB: see the table of times).
+template <typename T, int DP, int COLS, bool PAGED>
 __global__ __launch_bounds__(64 * WAVES, 1) void stream_kernel(StreamArgs a) {
   typedef Stream<T, DP> F;
   typedef typename F::Tile Tile;
   typedef Core<T> C;
-  constexpr int N = F::PIECES, S = F::STAGES;
+  constexpr int N = F::PIECES, S = F::STAGES, STEPS = COLS / C::STEP, GROUPS = COLS / 32;
   extern __shared__ __attribute__((aligned(1024))) char lds[];
-  __shared__ int64_t upto[64 * WAVES + 1];   // tiles of the sequences before a thread's
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5;
-  const int64_t per = (a.B + 64 * WAVES - 1) / (64 * WAVES);   // sequences of a thread
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
+  const int w = blockIdx.x * WAVES + wave;
+  const int64_t per = (a.B + 63) >> 6;   // sequences of a lane
+  int64_t before, total;                 // tiles of the sequences before a lane's (of one head and one 32 of queries); of all
   {
     int64_t n = 0;
-    const int64_t b0 = min(tid * per, a.B), b1 = min(b0 + per, a.B);
+    const int64_t b0 = min(lane * per, a.B), b1 = min(b0 + per, a.B);
     for (int64_t b = b0; b < b1; ++b) n += tiles_of(a, b);
-    upto[tid + 1] = n;
-    if (tid == 0) upto[0] = 0;
-    __syncthreads();
-    for (int step = 1; step < 64 * WAVES; step <<= 1) {
-      const int64_t x = tid + 1 > step ? upto[tid + 1 - step] : 0;
-      __syncthreads();
-      upto[tid + 1] += x;
-      __syncthreads();
+    int64_t upto = n;
+    for (int step = 1; step < 64; step <<= 1) {
+      const int64_t x = __shfl_up((long long)upto, step, 64);
+      if (lane >= step) upto += x;
     }
-    if (blockIdx.x == 0) {
-      int64_t at = upto[tid];
+    before = upto - n;
+    total = of_lane(upto, 63);
+    if (w == 0) {
+      int64_t x = before;
       for (int64_t b = b0; b < b1; ++b) {
-        a.before[b] = at;
-        at += tiles_of(a, b);
+        a.before[b] = x;
+        x += tiles_of(a, b);
       }
-      if (tid == 0) a.before[a.B] = upto[64 * WAVES];
+      if (lane == 63) a.before[a.B] = total;
     }
   }
-  const int64_t w = (int64_t)blockIdx.x * WAVES + wave;
   const int64_t times = (int64_t)a.heads * a.row_tiles;
-  const Pieces pieces(upto[64 * WAVES] * times, a.waves);
-  int64_t at = pieces.first(w);
-  const int64_t stop = pieces.first(w + 1);
+  const Shares shares(total * times, a.waves);
+  int64_t at = shares.first(w);
+  const int64_t stop = shares.first(w + 1);
   if (at >= stop) return;
-  // the sequence that `at` lies in
-  int64_t b = 0, start = 0;   // start: its first tile
-  {
-    int lo = 0, hi = 64 * WAVES;
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (upto[mid] * times <= at) lo = mid;
-      else hi = mid;
-    }
-    b = lo * per;
-    start = upto[lo] * times;
-  }
-  int64_t n = tiles_of(a, b);
-  while (start + n * times <= at) {
-    start += n * times;
-    n = tiles_of(a, ++b);
-  }
+  const int in = __popcll(__ballot(before * times <= at)) - 1;   // the lane whose sequences `at` lies in
+  int64_t b = in * per, start = of_lane(before, in) * times, n = tiles_of(a, b);   // start: b's first tile
   char* mine = lds + wave * F::WAVE;
-  const uint32_t ring = __builtin_amdgcn_readfirstlane(lds_address(mine)), entries = ring + 2 * S * F::BYTES;
+  const uint32_t ring = __builtin_amdgcn_readfirstlane(lds_address(mine));
   const int width = a.D * (int)sizeof(T);
-  if (a.D < DP)
-    for (int i = lane * 16; i < 2 * S * F::BYTES; i += 1024) *reinterpret_cast<uint4*>(mine + i) = make_uint4(0, 0, 0, 0);
+  if (a.D < DP) {
+    for (int i = lane * 16; i < F::WHERE; i += 1024) *reinterpret_cast<uint4*>(mine + i) = make_uint4(0, 0, 0, 0);
+  }
 
   while (at < stop) {
     while (start + n * times <= at) {   // (sequences of no keys too)
@@ -101,162 +100,152 @@ __global__ __launch_bounds__(64 * WAVES, 1) void stream_kernel(StreamArgs a) {
     }
     const int64_t k_len = length_of(a.k_lengths, b, a.T), q_len = length_of(a.q_lengths, b, a.S);
     const int64_t segment = (at - start) / n, begin = start + segment * n;   // a head and its 32 queries
-    const int h = (int)(segment / a.row_tiles), rt = (int)(segment % a.row_tiles);
+    const int h = (int)(segment / a.row_tiles), rt = (int)(segment - (int64_t)h * a.row_tiles);
     const int64_t i0 = at - begin, i1 = min(stop - begin, n);
     const bool came = i0 > 0, goes = i1 < n;
 
-    const int64_t row = (int64_t)rt * 32 + (lane & 31), query = row / a.group;
+    const uint32_t row = rt * 32 + (lane & 31), query = row / (uint32_t)a.group;
     const int64_t hq = (int64_t)h * a.group + (row - query * a.group);
     const bool there = query < q_len;   // (rows behind the last head's: query >= S)
-    typename C::Fragment q[DP / C::STEP];
+    typename C::Fragment q[STEPS];
     {
       const char* p = reinterpret_cast<const char*>(a.q.p) + b * a.q.s.b + query * a.q.s.l + hq * a.q.s.h;
 #pragma unroll
-      for (int i = 0; i < DP / C::STEP; ++i) {
+      for (int i = 0; i < STEPS; ++i) {
         const int c = (2 * i + half) * 16;
         uint4 x = make_uint4(0, 0, 0, 0);
         if (there && c < width) x = load16<false>(p + c);
         q[i] = __builtin_bit_cast(typename C::Fragment, x);
       }
     }
-    const char* kp = reinterpret_cast<const char*>(a.k.p) + (PAGED ? 0 : b * a.k.s.b) + h * a.k.s.h;
-    const char* vp = reinterpret_cast<const char*>(a.v.p) + (PAGED ? 0 : b * a.v.s.b) + h * a.v.s.h;
+    // Lanes below 32 look after the rows of the keys, the others after those of the values.
+    const HeadsArg& kv = half ? a.v : a.k;
+    const char* rows = reinterpret_cast<const char*>(kv.p) + (PAGED ? 0 : b * kv.s.b) + h * kv.s.h;
     const int32_t* table = PAGED ? a.table + b * a.ldt : nullptr;
-    // Tile i's pages, one for each of its rows, to LDS.
+    auto first_of = [&](uint32_t t) { return (uint32_t)((uint64_t)t * a.page_magic >> a.page_shift); };
+    // The pages of tile i's rows, to LDS.
     auto pages = [&](int64_t i) {
-      const uint32_t t = (uint32_t)min(32 * i + (lane & 31), k_len - 1);
-      load_lds4(table + (uint32_t)((uint64_t)t * a.page_magic >> a.page_shift), entries + (uint32_t)(i - i0) % F::ENTRIES * 256);
+      load_lds4(table + first_of((uint32_t)min(32 * i + (lane & 31), k_len - 1)), ring + F::PAGES + (uint32_t)(i - i0) % F::AHEAD * 256);
     };
-    auto entry = [&](int64_t i, int r) {
-      return *reinterpret_cast<const int*>(mine + 2 * S * F::BYTES + (uint32_t)(i - i0) % F::ENTRIES * 256 + r * 4);
+    // Where tile i's rows are, to LDS; which of them there are.
+    auto places = [&](int64_t i) {
+      const int64_t t = 32 * i + (lane & 31);
+      bool x = i < i1 && t < k_len;
+      int64_t off;
+      if (PAGED) {
+        const int e = *reinterpret_cast<const int*>(mine + F::PAGES + (uint32_t)(i - i0) % F::AHEAD * 256 + lane * 4);
+        x = x && e >= 0 && e < a.pages;
+        off = e * a.k.s.b + ((uint32_t)t - first_of((uint32_t)t) * (uint32_t)a.page) * a.k.s.l;
+      } else {
+        off = t * kv.s.l;
+      }
+      *reinterpret_cast<const char**>(mine + F::WHERE + lane * 8) = x ? rows + off : reinterpret_cast<const char*>(zero_row);
+      wave_lds_order();
+      return (uint32_t)__ballot(x);
     };
-    // Tile i of keys or values; a row that there is not, or whose page is none of the cache's, is zeros.
-    auto tile = [&](const char* x, int64_t ld, int64_t i, uint32_t to) {
-#pragma unroll
+    auto move = [&](int which, uint32_t to) {
+#pragma unroll 2
       for (int p = 0; p < N; ++p) {
-        const int slot = p * 64 + lane, r = slot / Tile::PITCH, c = ((slot % Tile::PITCH) ^ Tile::swizzle(r)) * 16;
-        const int64_t t = 32 * i + r;
-        const char* src = reinterpret_cast<const char*>(mfma_zero16);
-        if (i < i1 && t < k_len) {
-          if (PAGED) {
-            const int e = entry(i, r);
-            const uint32_t first = (uint32_t)((uint64_t)(uint32_t)t * a.page_magic >> a.page_shift);
-            if (e >= 0 && e < a.pages) src = x + e * a.k.s.b + ((uint32_t)t - first * (uint32_t)a.page) * ld + c;
-          } else {
-            src = x + t * ld + c;
-          }
-        }
+        const int r = p * F::PIECE_ROWS + lane / Tile::PITCH, c = ((lane % Tile::PITCH) ^ Tile::swizzle(r)) * 16;
+        const char* src = *reinterpret_cast<const char* const*>(mine + F::WHERE + which * 256 + r * 8) + c;
         if (c < width) load_lds16(src, to + p * 1024);
       }
     };
-    auto slot_of = [&](int64_t i) { return (uint32_t)(i - i0) % S * F::BYTES; };
-    auto keys = [&](int64_t i) {
-      if (PAGED) pages(i + S);
-      tile(kp, a.k.s.l, i, ring + slot_of(i));
-    };
-    auto values = [&](int64_t i) { tile(vp, a.v.s.l, i, ring + S * F::BYTES + slot_of(i)); };
-
-    f32x16 o[DP / 32];
+    f32x16 o[GROUPS], s;
 #pragma unroll
-    for (int d = 0; d < DP / 32; ++d) o[d] = zeros();
+    for (int d = 0; d < GROUPS; ++d) o[d] = zeros();
     float m = -INFINITY, l = 0.0f;
+    uint32_t some[S] = {};   // keys of the next tiles that there are
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");   // (the ring is free)
     if (PAGED) {
+#pragma unroll 1
       for (int j = 0; j < S; ++j) pages(i0 + j);
       wait_loads<0>();
     }
-    for (int j = 0; j < S; ++j) {
-      keys(i0 + j);
-      values(i0 + j);
-    }
-    // Behind a tile of keys: S of values and S - 1 of keys with their pages; behind one of values the other way round.
+    // Behind a tile of keys S of values and S - 1 of keys with their pages are under way, behind one of values the other way round; behind the last
+    // tile rows of zeros are, so that the counts hold.
     constexpr int E = PAGED ? 1 : 0;
-    for (int64_t i = i0; i < i1; ++i) {
-      wait_loads<S * N + (S - 1) * (N + E)>();
-      __builtin_amdgcn_sched_barrier(0);
-      uint32_t some = ~0u;   // keys of the tile that are there
-      {
-        bool x = 32 * i + (lane & 31) < k_len;
-        if (PAGED) {
-          const int e = entry(i, lane & 31);
-          x = x && e >= 0 && e < a.pages;
+#pragma unroll 1
+    for (int64_t i = i0 - S; i < i1; ++i) {
+      const bool work = i >= i0;
+      const uint32_t slot = (uint32_t)(i + S - i0) % S * F::BYTES;
+      if (work) {
+        wait_loads<S * N + (S - 1) * (N + E)>();
+        __builtin_amdgcn_sched_barrier(0);
+        const uint32_t tk = Tile::along_at(ring + slot, lane);
+        s = zeros();
+#pragma unroll
+        for (int j = 0; j < STEPS; ++j) C::multiply(Tile::along(tk, 0, j), q[j], s);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      const uint32_t now_some = some[0];
+#pragma unroll
+      for (int j = 0; j + 1 < S; ++j) some[j] = some[j + 1];
+      if (PAGED) pages(i + 2 * S);
+      some[S - 1] = places(i + S);
+      move(0, ring + slot);
+      if (work) {
+        if (now_some != ~0u) {
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            if (!(now_some >> (8 * (e >> 2) + 4 * half + (e & 3)) & 1)) s[e] = -INFINITY;
         }
-        some = (uint32_t)__ballot(x);
+        float top = s[0];
+#pragma unroll
+        for (int e = 1; e < 16; ++e) top = fmaxf(top, s[e]);
+        top = fmaxf(top, other_half(top));
+        if (__any(top > m && (top - m) * a.scale2 > 8.0f)) {   // (else sums stay under the older maximum)
+          const float now = fmaxf(m, top), f = m == -INFINITY ? 0.0f : exp2_((m - now) * a.scale2);
+          m = now;
+          l *= f;
+#pragma unroll
+          for (int d = 0; d < GROUPS; ++d)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) o[d][e] *= f;
+        }
+        const float mc = m == -INFINITY ? 0.0f : m * a.scale2;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          s[e] = exp2_(fmaf(s[e], a.scale2, -mc));
+          l += s[e];
+        }
+        wait_loads<S * (N + E) + (S - 1) * N>();
+        __builtin_amdgcn_sched_barrier(0);
+        const uint32_t tv = Tile::down_at(ring + F::VALUES + slot, lane);
+#pragma unroll
+        for (int j = 0; j < 32 / C::STEP; ++j) {
+          const typename C::Fragment p = C::pack(s, j);
+#pragma unroll
+          for (int d = 0; d < GROUPS; ++d) C::multiply(Tile::down(tv, 0, j, d), p, o[d]);
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
       }
-      const uint32_t tk = Tile::along_at(ring + slot_of(i), lane);
-      f32x16 s = zeros();
-#pragma unroll
-      for (int j = 0; j < DP / C::STEP; ++j) C::multiply(Tile::along(tk, 0, j), q[j], s);
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-      __builtin_amdgcn_sched_barrier(0);
-      keys(i + S);
-      if (some != ~0u) {
-#pragma unroll
-        for (int e = 0; e < 16; ++e)
-          if (!(some >> (8 * (e >> 2) + 4 * half + (e & 3)) & 1)) s[e] = -INFINITY;
-      }
-      float top = s[0];
-#pragma unroll
-      for (int e = 1; e < 16; ++e) top = fmaxf(top, s[e]);
-      top = fmaxf(top, other_half(top));
-      if (__any(top > m && (top - m) * a.scale2 > 8.0f)) {   // (else sums stay under the older maximum)
-        const float now = fmaxf(m, top), f = m == -INFINITY ? 0.0f : exp2_((m - now) * a.scale2);
-        m = now;
-        l *= f;
-#pragma unroll
-        for (int d = 0; d < DP / 32; ++d)
-#pragma unroll
-          for (int e = 0; e < 16; ++e) o[d][e] *= f;
-      }
-      const float mc = m == -INFINITY ? 0.0f : m * a.scale2;
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        s[e] = exp2_(fmaf(s[e], a.scale2, -mc));
-        l += s[e];
-      }
-      wait_loads<S * (N + E) + (S - 1) * N>();
-      __builtin_amdgcn_sched_barrier(0);
-      const uint32_t tv = Tile::down_at(ring + S * F::BYTES + slot_of(i), lane);
-#pragma unroll
-      for (int j = 0; j < 32 / C::STEP; ++j) {
-        const typename C::Fragment p = C::pack(s, j);
-#pragma unroll
-        for (int d = 0; d < DP / 32; ++d) C::multiply(Tile::down(tv, 0, j, d), p, o[d]);
-      }
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-      __builtin_amdgcn_sched_barrier(0);
-      values(i + S);
+      move(1, ring + F::VALUES + slot);
     }
     l += other_half(l);
     const float top2 = m == -INFINITY ? 0.0f : m * a.scale2;
-    if (came || goes) {
-      const int64_t slot = (w * 2 + (came ? 0 : 1)) * a.rows + (lane & 31);
-      if ((lane & 31) < a.rows) {
-        if (half == 0) *reinterpret_cast<float2*>(a.top_sum + 2 * slot) = make_float2(l == 0.0f ? -INFINITY : top2, l);
-        float* to = a.partial + slot * DP + 4 * half;
+    const bool part = came || goes;
+    const int64_t slot = ((int64_t)w * 2 + (came ? 0 : 1)) * a.rows + (lane & 31);
+    const bool stored = part ? (lane & 31) < a.rows : query < a.S;
+    if (part && stored && half == 0) *reinterpret_cast<float2*>(a.top_sum + 2 * slot) = make_float2(l == 0.0f ? -INFINITY : top2, l);
+    if (!part && stored && half == 0 && a.stats) a.stats[(b * a.q_heads + hq) * a.S + query] = l == 0.0f || !there ? INFINITY : top2 + log2_(l);
+    const float f = part ? 1.0f : l == 0.0f ? 0.0f : 1.0f / l;
+    float* to_part = a.partial + slot * DP;
+    T* to = reinterpret_cast<T*>(reinterpret_cast<char*>(const_cast<void*>(a.out.p)) + b * a.out.s.b + query * a.out.s.l + hq * a.out.s.h);
 #pragma unroll
-        for (int d = 0; d < DP / 32; ++d)
+    for (int d = 0; d < GROUPS; ++d)
 #pragma unroll
-          for (int v = 0; v < 4; ++v)
-            *reinterpret_cast<float4*>(to + 32 * d + 8 * v) = make_float4(o[d][4 * v], o[d][4 * v + 1], o[d][4 * v + 2], o[d][4 * v + 3]);
+      for (int v = 0; v < 4; ++v) {
+        const int c = 32 * d + 8 * v + 4 * half;
+        float4 x = make_float4(o[d][4 * v] * f, o[d][4 * v + 1] * f, o[d][4 * v + 2] * f, o[d][4 * v + 3] * f);
+        if (!there) x = make_float4(0, 0, 0, 0);
+        if (!stored || c >= a.D) continue;
+        if (part) *reinterpret_cast<float4*>(to_part + c) = x;
+        else if constexpr (sizeof(T) == 4) *reinterpret_cast<float4*>(to + c) = x;
+        else *reinterpret_cast<uint2*>(to + c) = make_uint2(f2bf2(x.x, x.y), f2bf2(x.z, x.w));
       }
-    } else if (query < a.S) {
-      const float f = l == 0.0f || !there ? 0.0f : 1.0f / l;
-      char* to = reinterpret_cast<char*>(const_cast<void*>(a.out.p)) + b * a.out.s.b + query * a.out.s.l + hq * a.out.s.h;
-#pragma unroll
-      for (int d = 0; d < DP / 32; ++d)
-#pragma unroll
-        for (int v = 0; v < 4; ++v) {
-          const int c = 32 * d + 8 * v + 4 * half;
-          float x[4];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) x[e] = there ? o[d][4 * v + e] * f : 0.0f;
-          if (c >= a.D) continue;
-          if constexpr (sizeof(T) == 4) *reinterpret_cast<float4*>(to + c * 4) = make_float4(x[0], x[1], x[2], x[3]);
-          else *reinterpret_cast<uint2*>(to + c * 2) = make_uint2(f2bf2(x[0], x[1]), f2bf2(x[2], x[3]));
-        }
-      if (a.stats && half == 0) a.stats[(b * a.q_heads + hq) * a.S + query] = l == 0.0f || !there ? INFINITY : top2 + log2_(l);
-    }
     at = begin + i1;
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // (nothing is under way to LDS when the block ends)
@@ -268,25 +257,25 @@ __global__ __launch_bounds__(256) void stream_join_kernel(StreamArgs a) {
   constexpr int LANES = DP / 4, GROUPS = 256 / LANES;
   __shared__ float4 sums[GROUPS][LANES];
   __shared__ float parts[GROUPS];
-  const int64_t id = blockIdx.x, query = id % a.S, bh = id / a.S, hq = bh % a.q_heads, b = bh / a.q_heads;
-  const int64_t h = hq / a.group, row = query * a.group + hq - h * a.group;
+  const uint32_t id = blockIdx.x, bh = id / (uint32_t)a.S, query = id - bh * (uint32_t)a.S;   // (below 2^24)
+  const uint32_t b = bh / (uint32_t)a.q_heads, hq = bh - b * (uint32_t)a.q_heads, h = hq / (uint32_t)a.group, row = query * a.group + hq - h * a.group;
   const int64_t n = a.before[b + 1] - a.before[b], times = (int64_t)a.heads * a.row_tiles;
   const bool there = n > 0 && query < length_of(a.q_lengths, b, a.S);
   const int lane = threadIdx.x % LANES, group = threadIdx.x / LANES;
   float4 sum = make_float4(0, 0, 0, 0);
   float l = 0.0f, top = -INFINITY;
   if (there) {
-    const Pieces pieces(a.before[a.B] * times, a.waves);
+    const Shares shares(a.before[a.B] * times, a.waves);
     const int64_t begin = a.before[b] * times + (h * a.row_tiles + row / 32) * n;
-    const int64_t w0 = pieces.owner(begin), w1 = pieces.owner(begin + n - 1);
+    const int w0 = (int)shares.owner(begin), w1 = (int)shares.owner(begin + n - 1);
     if (w0 == w1) return;   // (written by that wavefront)
-    auto slot = [&](int64_t w) { return (w * 2 + (w == w0 ? 1 : 0)) * a.rows + row % 32; };
-    for (int64_t w = w0 + threadIdx.x % 64; w <= w1; w += 64) top = fmaxf(top, a.top_sum[2 * slot(w)]);
+    auto slot = [&](int w) { return (int64_t)(w * 2 + (w == w0 ? 1 : 0)) * a.rows + (row & 31); };
+    for (int w = w0 + (threadIdx.x & 63); w <= w1; w += 64) top = fmaxf(top, a.top_sum[2 * slot(w)]);
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
     const float base = top == -INFINITY ? 0.0f : top;
 #pragma unroll 4
-    for (int64_t w = w0 + group; w <= w1; w += GROUPS) {
+    for (int w = w0 + group; w <= w1; w += GROUPS) {
       const float2 ml = *reinterpret_cast<const float2*>(a.top_sum + 2 * slot(w));
       const float4 x = *reinterpret_cast<const float4*>(a.partial + slot(w) * DP + 4 * lane);
       const float f = exp2_(ml.x - base);
@@ -312,7 +301,7 @@ __global__ __launch_bounds__(256) void stream_join_kernel(StreamArgs a) {
     if constexpr (sizeof(T) == 4) *reinterpret_cast<float4*>(to + 16 * lane) = make_float4(sum.x * f, sum.y * f, sum.z * f, sum.w * f);
     else *reinterpret_cast<uint2*>(to + 8 * lane) = make_uint2(f2bf2(sum.x * f, sum.y * f), f2bf2(sum.z * f, sum.w * f));
   }
-  if (a.stats && lane == 0) a.stats[bh * a.S + query] = l == 0.0f ? INFINITY : top + log2_(l);
+  if (a.stats && lane == 0) a.stats[(int64_t)bh * a.S + query] = l == 0.0f ? INFINITY : top + log2_(l);
 }
 
 struct StreamPlan {
@@ -332,13 +321,13 @@ StreamPlan stream_plan(int64_t B, int64_t S, int64_t q_heads, int64_t heads, int
   return p;
 }
 
-template <typename T, int DP, bool PAGED>
+template <typename T, int DP, int COLS, bool PAGED>
 hipError_t launch(const StreamArgs& a, hipStream_t s) {
   static std::atomic<uint64_t> allowed{0};
   typedef Stream<T, DP> F;
-  const hipError_t e = allow_lds(stream_kernel<T, DP, PAGED>, F::LDS, (64 * WAVES + 1) * 8, allowed);
+  const hipError_t e = allow_lds(stream_kernel<T, DP, COLS, PAGED>, F::LDS, 0, allowed);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((stream_kernel<T, DP, PAGED>), dim3(BLOCKS), dim3(64 * WAVES), F::LDS, s, a);
+  hipLaunchKernelGGL((stream_kernel<T, DP, COLS, PAGED>), dim3(BLOCKS), dim3(64 * WAVES), F::LDS, s, a);
   hipLaunchKernelGGL((stream_join_kernel<T, DP>), dim3((unsigned)(a.B * a.S * a.q_heads)), dim3(256), 0, s, a);
   return hipGetLastError();
 }
@@ -356,7 +345,9 @@ hipError_t launch_stream(StreamArgs a, int32_t dtype, void* workspace, hipStream
   a.partial = reinterpret_cast<float*>(ws + p.partial);
   return by_size(dtype, a.D, [&](auto t, auto dp) {
     typedef decltype(t) T;
-    return a.table ? launch<T, decltype(dp)::value, true>(a, s) : launch<T, decltype(dp)::value, false>(a, s);
+    constexpr int DP = decltype(dp)::value;
+    if (DP == 128 && a.D <= 96) return a.table ? launch<T, 128, 96, true>(a, s) : launch<T, 128, 96, false>(a, s);
+    return a.table ? launch<T, DP, DP, true>(a, s) : launch<T, DP, DP, false>(a, s);
   });
 }
 
