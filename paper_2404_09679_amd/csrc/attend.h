@@ -184,13 +184,14 @@ struct StreamArgs {
   int32_t page, page_shift;    // t / page = t page_magic >> page_shift, t < 2^31
   uint32_t page_magic;
   int32_t q_heads, heads, group, D;
-  int32_t row_tiles, rows;     // 32s of a key head's queries (row r: query r / group of head r mod group); rows of a partial result
+  int32_t row_tile, row_tiles, rows;   // a key head's queries (row r: query r / group of head r mod group) in 16s or 32s; rows of a partial result
   int32_t waves;               // of the launch
   float scale2;
-  int64_t* before;             // [B + 1] tiles of the sequences before, of a single head and tile of rows
+  uint32_t* before;            // [B + 1] tiles of 32 keys of the sequences before, of a single head and tile of rows
   float* top_sum;              // [waves, 2, rows, 2] maximum and sum of the partial results, and
   float* partial;              // [waves, 2, rows, DP]
 };
+bool stream_fits(int64_t B, int64_t S, int64_t T, int64_t q_heads, int64_t heads);   // fewer than 2^31 tiles
 size_t stream_bytes(int64_t B, int64_t S, int64_t q_heads, int64_t heads, int64_t D);
 // The rest of a's fields from its sizes and a workspace of that many bytes; the launches.
 hipError_t launch_stream(StreamArgs a, int32_t dtype, void* workspace, hipStream_t s);

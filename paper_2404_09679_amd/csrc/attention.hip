@@ -513,7 +513,7 @@ int cross_sizes(const char* call, const Shape& z) {
   return ANTDT_OK;
 }
 // Few queries for each head of the keys: by an equal share of the keys to each wavefront.
-bool cross_streams(const Shape& z) { return z.S * (z.q_heads / z.heads) <= 32; }
+bool cross_streams(const Shape& z) { return z.S * (z.q_heads / z.heads) <= 32 && stream_fits(z.B, z.S, z.T, z.q_heads, z.heads); }
 int cross_lengths(const char* call, const int32_t* q_lengths, const int32_t* k_lengths) {
   if ((reinterpret_cast<uintptr_t>(q_lengths) | reinterpret_cast<uintptr_t>(k_lengths)) & 3) return op_fail(ANTDT_INVALID_ARG, "%s: lengths are misaligned", call);
   return ANTDT_OK;

@@ -18,60 +18,139 @@ constexpr int LEAST = 4;                // tiles of a wavefront, before the next
 
 // Work in tiles, [0, total), to the wavefronts: the first `more` have one more than the others.
 struct Shares {
-  int64_t total, waves, each, more;
-  __device__ __forceinline__ Shares(int64_t n, int most) : total(n), waves(max((int64_t)1, min((int64_t)most, (n + LEAST - 1) / LEAST))), each(n / waves), more(n - each * waves) {}
-  __device__ __forceinline__ int64_t first(int64_t w) const { return min(w * each + min(w, more), total); }
-  __device__ __forceinline__ int64_t owner(int64_t tile) const {
-    const int64_t large = more * (each + 1), behind = tile - large;   // (one division for both kinds)
-    return (behind < 0 ? tile : behind) / (behind < 0 ? each + 1 : each) + (behind < 0 ? 0 : more);
+  uint32_t total, waves, each, more;
+  __device__ __forceinline__ Shares(uint32_t n, uint32_t most) : total(n), waves(max(1u, min(most, (n + LEAST - 1) / LEAST))), each(n / waves), more(n - each * waves) {}
+  __device__ __forceinline__ uint32_t first(uint32_t w) const { return min(w * each + min(w, more), total); }
+  __device__ __forceinline__ uint32_t owner(uint32_t tile) const {
+    const uint32_t large = more * (each + 1);
+    return tile < large ? tile / (each + 1) : more + (tile - large) / each;
   }
 };
 
-__device__ __forceinline__ int64_t tiles_of(const StreamArgs& a, int64_t b) { return (length_of(a.k_lengths, b, a.T) + 31) >> 5; }
-// x of lane `from`, known to the compiler to be the wavefront's.
-__device__ __forceinline__ int64_t of_lane(int64_t x, int from) {
-  return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)((uint64_t)x >> 32), from) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)x, from));
-}
+__device__ __forceinline__ uint32_t tiles_of(const StreamArgs& a, int64_t b) { return (uint32_t)((length_of(a.k_lengths, b, a.T) + 31) >> 5); }
 
 // What a row that there is not is read from.
 static __device__ __attribute__((aligned(16))) uint32_t zero_row[128];
 
-template <typename T, int DP>
+// Products of R queries at a time, 32 or 16 (v_mfma_f32_16x16x32_bf16, v_mfma_f32_16x16x4_f32): as Core and HeadTile, with 64 / R lanes to a query
+// instead of two.  Lane l has query l % R and, of 32 keys or columns, 4 GROUPS (e / 4) + 4 (l / R) + e % 4, e < R / 2.
+template <typename T, int R>
+struct Few;
+template <typename T>
+struct Few<T, 32> {
+  static constexpr int STEP = Core<T>::STEP;
+  typedef f32x16 Acc;
+  static __device__ __forceinline__ void multiply(const typename Core<T>::Fragment& a, const typename Core<T>::Fragment& b, Acc& c) { Core<T>::multiply(a, b, c); }
+};
+template <>
+struct Few<bf16_t, 16> {
+  static constexpr int STEP = 32;
+  typedef f32x4v Acc;
+  static __device__ __forceinline__ void multiply(const bf16x8& a, const bf16x8& b, Acc& c) { c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+};
+template <>
+struct Few<float, 16> {
+  static constexpr int STEP = 16;
+  typedef f32x4v Acc;
+  static __device__ __forceinline__ void multiply(const f32x4v& a, const f32x4v& b, Acc& c) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], b[e], c, 0, 0, 0);
+  }
+};
+
+template <typename T, int DP, int R>
 struct Stream {
   typedef HeadTile<T, DP> Tile;
+  typedef typename Core<T>::Fragment Fragment;
   static constexpr int BYTES = 32 * Tile::ROW, PIECES = BYTES / 1024, PIECE_ROWS = 64 / Tile::PITCH;
   static constexpr int STAGES = BYTES >= 16384 ? 1 : BYTES >= 8192 ? 2 : 4;
   // A wavefront's LDS: the rings of keys and of values, where a tile's rows are, the pages of the next tiles' rows.
   static constexpr int VALUES = STAGES * BYTES, WHERE = 2 * VALUES, PAGES = WHERE + 512, AHEAD = 2 * STAGES + 1;
   static constexpr int WAVE = (PAGES + AHEAD * 256 + 1023) / 1024 * 1024, LDS = WAVES * WAVE;
+
+  // A lane's addresses for both ways of reading a tile, see HeadTile.
+  static __device__ __forceinline__ uint32_t along_at(uint32_t tile, int lane) { return Tile::at(tile + Tile::slot(lane % R, lane / R) * 16); }
+  static __device__ __forceinline__ uint32_t down_at(uint32_t tile, int lane) {
+    if constexpr (R == 32) return Tile::down_at(tile, lane);
+    if constexpr (sizeof(T) == 2) {
+      const int j = lane & 15;
+      return Tile::at(tile + Tile::slot(4 * (lane >> 4) + (j >> 2), (j & 3) >> 1) * 16 + (j & 1) * 8);
+    } else {
+      return Tile::at(tile + Tile::slot(4 * (lane >> 4), (lane & 15) >> 2) * 16 + (lane & 3) * 4);
+    }
+  }
+  // Key r0 + lane % R (r0: 0, or 16 of R = 16), columns STEP i ..
+  static __device__ __forceinline__ Fragment along(uint32_t at, int r0, int i) {
+    typedef __attribute__((address_space(3))) Fragment lds_fragment;
+    return *(const lds_fragment*)(uintptr_t)((at ^ (1024 / R * i)) + r0 * Tile::ROW);
+  }
+  // Column R d + lane % R, contraction slots (keys) i of pack().
+  static __device__ __forceinline__ Fragment down(uint32_t at, int i, int d) {
+    if constexpr (R == 32) return Tile::down(at, 0, i, d);
+    if constexpr (sizeof(T) == 2) {
+      typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+      union {
+        s16x4 s[2];
+        Fragment v;
+      } u;
+#pragma unroll
+      for (int s = 0; s < 2; ++s) u.s[s] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(uintptr_t)((at ^ (32 * d)) + 16 * s * Tile::ROW));
+      return u.v;
+    } else {
+      typedef __attribute__((address_space(3))) float lds_float;
+      Fragment f;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) f[e] = *(const lds_float*)(uintptr_t)((at ^ (64 * d) ^ (Tile::swizzle(e) * 16)) + (16 * i + e) * Tile::ROW);
+      return f;
+    }
+  }
+  template <typename A>
+  static __device__ __forceinline__ Fragment pack(const A& x, int i) {
+    if constexpr (sizeof(T) == 2) {
+      union {
+        uint32_t w[4];
+        Fragment f;
+      } u;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) u.w[e] = f2bf2(x[8 * i + 2 * e], x[8 * i + 2 * e + 1]);
+      return u.f;
+    } else {
+      return Fragment{x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]};
+    }
+  }
 };
 
+// Over the lanes of a query.
+template <int R, typename F>
+__device__ __forceinline__ float over_lanes(float x, F f) {
+  x = f(x, __shfl_xor(x, 32, 64));
+  if (R == 16) x = f(x, __shfl_xor(x, 16, 64));
+  return x;
+}
+
 // DP columns of a row in LDS, of which the first COLS take part.  The loops that only move data stay rolled up: a launch this short waits for its code
-// as well as for its data (of 34 KB, 20 us before the first tile was done; these 10 to 16 KB: see the table of times).
-template <typename T, int DP, int COLS, bool PAGED>
+// as well as for its data (of 34 KB, 20 us before the first tile was done).
+template <typename T, int DP, int COLS, int R, bool PAGED>
 __global__ __launch_bounds__(64 * WAVES, 1) void stream_kernel(StreamArgs a) {
-  typedef Stream<T, DP> F;
+  typedef Stream<T, DP, R> F;
   typedef typename F::Tile Tile;
-  typedef Core<T> C;
-  constexpr int N = F::PIECES, S = F::STAGES, STEPS = COLS / C::STEP, GROUPS = COLS / 32;
+  typedef Few<T, R> C;
+  typedef typename F::Fragment Fragment;
+  constexpr int N = F::PIECES, S = F::STAGES, STEPS = COLS / C::STEP, DT = COLS / R, GROUPS = 64 / R, EL = R / 2, PER = R * R / 64;
   extern __shared__ __attribute__((aligned(1024))) char lds[];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
-  const int w = blockIdx.x * WAVES + wave;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), group = lane / R;
+  const uint32_t w = blockIdx.x * WAVES + wave;
   const int64_t per = (a.B + 63) >> 6;   // sequences of a lane
-  int64_t before, total;                 // tiles of the sequences before a lane's (of one head and one 32 of queries); of all
+  uint32_t before, total;                // tiles of the sequences before a lane's (of one head and one R of queries); of all
   {
-    int64_t n = 0;
+    uint32_t n = 0;
     const int64_t b0 = min(lane * per, a.B), b1 = min(b0 + per, a.B);
     for (int64_t b = b0; b < b1; ++b) n += tiles_of(a, b);
-    int64_t upto = n;
-    for (int step = 1; step < 64; step <<= 1) {
-      const int64_t x = __shfl_up((long long)upto, step, 64);
-      if (lane >= step) upto += x;
-    }
+    const uint32_t upto = wave_prefix(n);
     before = upto - n;
-    total = of_lane(upto, 63);
-    if (w == 0) {
-      int64_t x = before;
+    total = __builtin_amdgcn_readlane(upto, 63);
+    if (w == 0) {   // for the second launch
+      uint32_t x = before;
       for (int64_t b = b0; b < b1; ++b) {
         a.before[b] = x;
         x += tiles_of(a, b);
@@ -79,13 +158,14 @@ __global__ __launch_bounds__(64 * WAVES, 1) void stream_kernel(StreamArgs a) {
       if (lane == 63) a.before[a.B] = total;
     }
   }
-  const int64_t times = (int64_t)a.heads * a.row_tiles;
+  const uint32_t times = a.heads * a.row_tiles;
   const Shares shares(total * times, a.waves);
-  int64_t at = shares.first(w);
-  const int64_t stop = shares.first(w + 1);
+  uint32_t at = shares.first(w);
+  const uint32_t stop = shares.first(w + 1);
   if (at >= stop) return;
   const int in = __popcll(__ballot(before * times <= at)) - 1;   // the lane whose sequences `at` lies in
-  int64_t b = in * per, start = of_lane(before, in) * times, n = tiles_of(a, b);   // start: b's first tile
+  int64_t b = in * per;
+  uint32_t start = __builtin_amdgcn_readlane(before, in) * times, n = tiles_of(a, b);   // start: b's first tile
   char* mine = lds + wave * F::WAVE;
   const uint32_t ring = __builtin_amdgcn_readfirstlane(lds_address(mine));
   const int width = a.D * (int)sizeof(T);
@@ -99,41 +179,46 @@ __global__ __launch_bounds__(64 * WAVES, 1) void stream_kernel(StreamArgs a) {
       n = tiles_of(a, ++b);
     }
     const int64_t k_len = length_of(a.k_lengths, b, a.T), q_len = length_of(a.q_lengths, b, a.S);
-    const int64_t segment = (at - start) / n, begin = start + segment * n;   // a head and its 32 queries
-    const int h = (int)(segment / a.row_tiles), rt = (int)(segment - (int64_t)h * a.row_tiles);
-    const int64_t i0 = at - begin, i1 = min(stop - begin, n);
+    const uint32_t segment = (at - start) / n, begin = start + segment * n;   // a head and its R queries
+    const uint32_t h = segment / (uint32_t)a.row_tiles, rt = segment - h * a.row_tiles;
+    const uint32_t i0 = at - begin, i1 = min(stop - begin, n);
     const bool came = i0 > 0, goes = i1 < n;
 
-    const uint32_t row = rt * 32 + (lane & 31), query = row / (uint32_t)a.group;
+    const int32_t* table = PAGED ? a.table + b * a.ldt : nullptr;
+    auto first_of = [&](uint32_t t) { return (uint32_t)((uint64_t)t * a.page_magic >> a.page_shift); };
+    // The pages of tile i's rows, to LDS.
+    auto pages = [&](uint32_t i) {
+      load_lds4(table + first_of((uint32_t)min((int64_t)32 * i + (lane & 31), k_len - 1)), ring + F::PAGES + (i - i0) % F::AHEAD * 256);
+    };
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");   // (the rings are free)
+    if (PAGED) {
+#pragma unroll 1
+      for (int j = 0; j < S; ++j) pages(i0 + j);
+    }
+    const uint32_t row = rt * R + lane % R, query = row / (uint32_t)a.group;
     const int64_t hq = (int64_t)h * a.group + (row - query * a.group);
     const bool there = query < q_len;   // (rows behind the last head's: query >= S)
-    typename C::Fragment q[STEPS];
+    Fragment q[STEPS];
     {
       const char* p = reinterpret_cast<const char*>(a.q.p) + b * a.q.s.b + query * a.q.s.l + hq * a.q.s.h;
 #pragma unroll
       for (int i = 0; i < STEPS; ++i) {
-        const int c = (2 * i + half) * 16;
+        const int c = (GROUPS * i + group) * 16;
         uint4 x = make_uint4(0, 0, 0, 0);
         if (there && c < width) x = load16<false>(p + c);
-        q[i] = __builtin_bit_cast(typename C::Fragment, x);
+        q[i] = __builtin_bit_cast(Fragment, x);
       }
     }
     // Lanes below 32 look after the rows of the keys, the others after those of the values.
-    const HeadsArg& kv = half ? a.v : a.k;
+    const HeadsArg& kv = lane >= 32 ? a.v : a.k;
     const char* rows = reinterpret_cast<const char*>(kv.p) + (PAGED ? 0 : b * kv.s.b) + h * kv.s.h;
-    const int32_t* table = PAGED ? a.table + b * a.ldt : nullptr;
-    auto first_of = [&](uint32_t t) { return (uint32_t)((uint64_t)t * a.page_magic >> a.page_shift); };
-    // The pages of tile i's rows, to LDS.
-    auto pages = [&](int64_t i) {
-      load_lds4(table + first_of((uint32_t)min(32 * i + (lane & 31), k_len - 1)), ring + F::PAGES + (uint32_t)(i - i0) % F::AHEAD * 256);
-    };
     // Where tile i's rows are, to LDS; which of them there are.
-    auto places = [&](int64_t i) {
-      const int64_t t = 32 * i + (lane & 31);
-      bool x = i < i1 && t < k_len;
+    auto places = [&](uint32_t i) {
+      const int64_t t = (int64_t)32 * i + (lane & 31);
+      bool x = t < k_len;
       int64_t off;
       if (PAGED) {
-        const int e = *reinterpret_cast<const int*>(mine + F::PAGES + (uint32_t)(i - i0) % F::AHEAD * 256 + lane * 4);
+        const int e = *reinterpret_cast<const int*>(mine + F::PAGES + (i - i0) % F::AHEAD * 256 + lane * 4);
         x = x && e >= 0 && e < a.pages;
         off = e * a.k.s.b + ((uint32_t)t - first_of((uint32_t)t) * (uint32_t)a.page) * a.k.s.l;
       } else {
@@ -144,101 +229,120 @@ __global__ __launch_bounds__(64 * WAVES, 1) void stream_kernel(StreamArgs a) {
       return (uint32_t)__ballot(x);
     };
     auto move = [&](int which, uint32_t to) {
-#pragma unroll 2
-      for (int p = 0; p < N; ++p) {
-        const int r = p * F::PIECE_ROWS + lane / Tile::PITCH, c = ((lane % Tile::PITCH) ^ Tile::swizzle(r)) * 16;
-        const char* src = *reinterpret_cast<const char* const*>(mine + F::WHERE + which * 256 + r * 8) + c;
-        if (c < width) load_lds16(src, to + p * 1024);
+      constexpr int U = N < 4 ? N : 4;
+#pragma unroll 1
+      for (int p = 0; p < N; p += U) {
+        const char* src[U];
+        int c[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const int r = (p + u) * F::PIECE_ROWS + lane / Tile::PITCH;
+          c[u] = ((lane % Tile::PITCH) ^ Tile::swizzle(r)) * 16;
+          src[u] = *reinterpret_cast<const char* const*>(mine + F::WHERE + which * 256 + r * 8);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+          if (c[u] < width) load_lds16(src[u] + c[u], to + (p + u) * 1024);
       }
     };
-    f32x16 o[GROUPS], s;
+    typename C::Acc o[DT];
+    float s[EL];
 #pragma unroll
-    for (int d = 0; d < GROUPS; ++d) o[d] = zeros();
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int e = 0; e < PER; ++e) o[d][e] = 0.0f;
     float m = -INFINITY, l = 0.0f;
     uint32_t some[S] = {};   // keys of the next tiles that there are
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");   // (the ring is free)
-    if (PAGED) {
-#pragma unroll 1
-      for (int j = 0; j < S; ++j) pages(i0 + j);
-      wait_loads<0>();
-    }
-    // Behind a tile of keys S of values and S - 1 of keys with their pages are under way, behind one of values the other way round; behind the last
-    // tile rows of zeros are, so that the counts hold.
+    if (PAGED) wait_loads<0>();
+    // Behind a tile of keys S of values and S - 1 of keys with their pages are under way, behind one of values the other way round (fewer towards
+    // the end, where everything is waited for).
     constexpr int E = PAGED ? 1 : 0;
+    uint32_t slot = 0;
 #pragma unroll 1
-    for (int64_t i = i0 - S; i < i1; ++i) {
-      const bool work = i >= i0;
-      const uint32_t slot = (uint32_t)(i + S - i0) % S * F::BYTES;
+    for (int64_t i = (int64_t)i0 - S; i < i1; ++i) {
+      const bool work = i >= i0, more = i + S < i1;
       if (work) {
-        wait_loads<S * N + (S - 1) * (N + E)>();
+        if (more) wait_loads<S * N + (S - 1) * (N + E)>();
+        else wait_loads<0>();
         __builtin_amdgcn_sched_barrier(0);
-        const uint32_t tk = Tile::along_at(ring + slot, lane);
-        s = zeros();
+        const uint32_t tk = F::along_at(ring + slot, lane);
 #pragma unroll
-        for (int j = 0; j < STEPS; ++j) C::multiply(Tile::along(tk, 0, j), q[j], s);
+        for (int t = 0; t < 32 / R; ++t) {
+          typename C::Acc x;
+#pragma unroll
+          for (int e = 0; e < PER; ++e) x[e] = 0.0f;
+#pragma unroll
+          for (int j = 0; j < STEPS; ++j) C::multiply(F::along(tk, R * t, j), q[j], x);
+#pragma unroll
+          for (int e = 0; e < PER; ++e) s[PER * t + e] = x[e];
+        }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_sched_barrier(0);
       }
       const uint32_t now_some = some[0];
 #pragma unroll
       for (int j = 0; j + 1 < S; ++j) some[j] = some[j + 1];
-      if (PAGED) pages(i + 2 * S);
-      some[S - 1] = places(i + S);
-      move(0, ring + slot);
+      if (more) {
+        if (PAGED) pages((uint32_t)(i + 2 * S));
+        some[S - 1] = places((uint32_t)(i + S));
+        move(0, ring + slot);
+      }
       if (work) {
         if (now_some != ~0u) {
 #pragma unroll
-          for (int e = 0; e < 16; ++e)
-            if (!(now_some >> (8 * (e >> 2) + 4 * half + (e & 3)) & 1)) s[e] = -INFINITY;
+          for (int e = 0; e < EL; ++e)
+            if (!(now_some >> (4 * GROUPS * (e >> 2) + 4 * group + (e & 3)) & 1)) s[e] = -INFINITY;
         }
         float top = s[0];
 #pragma unroll
-        for (int e = 1; e < 16; ++e) top = fmaxf(top, s[e]);
-        top = fmaxf(top, other_half(top));
+        for (int e = 1; e < EL; ++e) top = fmaxf(top, s[e]);
+        top = over_lanes<R>(top, [](float x, float y) { return fmaxf(x, y); });
         if (__any(top > m && (top - m) * a.scale2 > 8.0f)) {   // (else sums stay under the older maximum)
           const float now = fmaxf(m, top), f = m == -INFINITY ? 0.0f : exp2_((m - now) * a.scale2);
           m = now;
           l *= f;
 #pragma unroll
-          for (int d = 0; d < GROUPS; ++d)
+          for (int d = 0; d < DT; ++d)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) o[d][e] *= f;
+            for (int e = 0; e < PER; ++e) o[d][e] *= f;
         }
         const float mc = m == -INFINITY ? 0.0f : m * a.scale2;
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
+        for (int e = 0; e < EL; ++e) {
           s[e] = exp2_(fmaf(s[e], a.scale2, -mc));
           l += s[e];
         }
-        wait_loads<S * (N + E) + (S - 1) * N>();
+        if (more) wait_loads<S * (N + E) + (S - 1) * N>();
+        else wait_loads<0>();
         __builtin_amdgcn_sched_barrier(0);
-        const uint32_t tv = Tile::down_at(ring + F::VALUES + slot, lane);
+        const uint32_t tv = F::down_at(ring + F::VALUES + slot, lane);
 #pragma unroll
-        for (int j = 0; j < 32 / C::STEP; ++j) {
-          const typename C::Fragment p = C::pack(s, j);
+        for (int j = 0; j < EL / (sizeof(T) == 2 ? 8 : 4); ++j) {
+          const Fragment p = F::pack(s, j);
 #pragma unroll
-          for (int d = 0; d < GROUPS; ++d) C::multiply(Tile::down(tv, 0, j, d), p, o[d]);
+          for (int d = 0; d < DT; ++d) C::multiply(F::down(tv, j, d), p, o[d]);
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_sched_barrier(0);
       }
-      move(1, ring + F::VALUES + slot);
+      if (more) move(1, ring + F::VALUES + slot);
+      slot = slot == (S - 1) * F::BYTES ? 0 : slot + F::BYTES;
     }
-    l += other_half(l);
+    l = over_lanes<R>(l, [](float x, float y) { return x + y; });
     const float top2 = m == -INFINITY ? 0.0f : m * a.scale2;
     const bool part = came || goes;
-    const int64_t slot = ((int64_t)w * 2 + (came ? 0 : 1)) * a.rows + (lane & 31);
-    const bool stored = part ? (lane & 31) < a.rows : query < a.S;
-    if (part && stored && half == 0) *reinterpret_cast<float2*>(a.top_sum + 2 * slot) = make_float2(l == 0.0f ? -INFINITY : top2, l);
-    if (!part && stored && half == 0 && a.stats) a.stats[(b * a.q_heads + hq) * a.S + query] = l == 0.0f || !there ? INFINITY : top2 + log2_(l);
+    const int64_t at_part = ((int64_t)w * 2 + (came ? 0 : 1)) * a.rows + lane % R;
+    const bool stored = part ? lane % R < a.rows : query < a.S;
+    if (part && stored && group == 0) *reinterpret_cast<float2*>(a.top_sum + 2 * at_part) = make_float2(l == 0.0f ? -INFINITY : top2, l);
+    if (!part && stored && group == 0 && a.stats) a.stats[(b * a.q_heads + hq) * a.S + query] = l == 0.0f || !there ? INFINITY : top2 + log2_(l);
     const float f = part ? 1.0f : l == 0.0f ? 0.0f : 1.0f / l;
-    float* to_part = a.partial + slot * DP;
+    float* to_part = a.partial + at_part * DP;
     T* to = reinterpret_cast<T*>(reinterpret_cast<char*>(const_cast<void*>(a.out.p)) + b * a.out.s.b + query * a.out.s.l + hq * a.out.s.h);
 #pragma unroll
-    for (int d = 0; d < GROUPS; ++d)
+    for (int d = 0; d < DT; ++d)
 #pragma unroll
-      for (int v = 0; v < 4; ++v) {
-        const int c = 32 * d + 8 * v + 4 * half;
+      for (int v = 0; v < PER / 4; ++v) {
+        const int c = R * d + 4 * GROUPS * v + 4 * group;
         float4 x = make_float4(o[d][4 * v] * f, o[d][4 * v + 1] * f, o[d][4 * v + 2] * f, o[d][4 * v + 3] * f);
         if (!there) x = make_float4(0, 0, 0, 0);
         if (!stored || c >= a.D) continue;
@@ -248,7 +352,6 @@ __global__ __launch_bounds__(64 * WAVES, 1) void stream_kernel(StreamArgs a) {
       }
     at = begin + i1;
   }
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // (nothing is under way to LDS when the block ends)
 }
 
 // One query of one head to a block: its parts, 256 / (DP / 4) of them at a time, added up in the order of the wavefronts.
@@ -259,17 +362,17 @@ __global__ __launch_bounds__(256) void stream_join_kernel(StreamArgs a) {
   __shared__ float parts[GROUPS];
   const uint32_t id = blockIdx.x, bh = id / (uint32_t)a.S, query = id - bh * (uint32_t)a.S;   // (below 2^24)
   const uint32_t b = bh / (uint32_t)a.q_heads, hq = bh - b * (uint32_t)a.q_heads, h = hq / (uint32_t)a.group, row = query * a.group + hq - h * a.group;
-  const int64_t n = a.before[b + 1] - a.before[b], times = (int64_t)a.heads * a.row_tiles;
+  const uint32_t n = a.before[b + 1] - a.before[b], times = a.heads * a.row_tiles;
   const bool there = n > 0 && query < length_of(a.q_lengths, b, a.S);
   const int lane = threadIdx.x % LANES, group = threadIdx.x / LANES;
   float4 sum = make_float4(0, 0, 0, 0);
   float l = 0.0f, top = -INFINITY;
   if (there) {
     const Shares shares(a.before[a.B] * times, a.waves);
-    const int64_t begin = a.before[b] * times + (h * a.row_tiles + row / 32) * n;
+    const uint32_t begin = a.before[b] * times + (h * a.row_tiles + row / a.row_tile) * n;
     const int w0 = (int)shares.owner(begin), w1 = (int)shares.owner(begin + n - 1);
     if (w0 == w1) return;   // (written by that wavefront)
-    auto slot = [&](int w) { return (int64_t)(w * 2 + (w == w0 ? 1 : 0)) * a.rows + (row & 31); };
+    auto slot = [&](int w) { return (int64_t)(w * 2 + (w == w0 ? 1 : 0)) * a.rows + row % a.row_tile; };
     for (int w = w0 + (threadIdx.x & 63); w <= w1; w += 64) top = fmaxf(top, a.top_sum[2 * slot(w)]);
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
@@ -306,48 +409,59 @@ __global__ __launch_bounds__(256) void stream_join_kernel(StreamArgs a) {
 
 struct StreamPlan {
   int64_t before, top_sum, partial, bytes;
-  int32_t rows, row_tiles;
+  int32_t row_tile, rows, row_tiles;
 };
 StreamPlan stream_plan(int64_t B, int64_t S, int64_t q_heads, int64_t heads, int64_t D) {
   StreamPlan p;
   const int64_t all = S * (q_heads / heads), dp = D <= 32 ? 32 : D <= 64 ? 64 : 128;
-  p.row_tiles = (int)div_up(all, 32);
-  p.rows = (int)std::min<int64_t>(all, 32);
+  p.row_tile = all <= 16 ? 16 : 32;
+  p.row_tiles = (int)div_up(all, p.row_tile);
+  p.rows = (int)std::min<int64_t>(all, p.row_tile);
   auto room = [](int64_t n) { return div_up(n, 256) * 256; };
   p.before = 0;
-  p.top_sum = room((B + 1) * 8);
+  p.top_sum = room((B + 1) * 4);
   p.partial = p.top_sum + room((int64_t)BLOCKS * WAVES * 2 * p.rows * 8);
   p.bytes = p.partial + (int64_t)BLOCKS * WAVES * 2 * p.rows * dp * 4;
   return p;
 }
 
-template <typename T, int DP, int COLS, bool PAGED>
+template <typename T, int DP, int COLS, int R, bool PAGED>
 hipError_t launch(const StreamArgs& a, hipStream_t s) {
   static std::atomic<uint64_t> allowed{0};
-  typedef Stream<T, DP> F;
-  const hipError_t e = allow_lds(stream_kernel<T, DP, COLS, PAGED>, F::LDS, 0, allowed);
+  typedef Stream<T, DP, R> F;
+  const hipError_t e = allow_lds(stream_kernel<T, DP, COLS, R, PAGED>, F::LDS, 0, allowed);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((stream_kernel<T, DP, COLS, PAGED>), dim3(BLOCKS), dim3(64 * WAVES), F::LDS, s, a);
+  hipLaunchKernelGGL((stream_kernel<T, DP, COLS, R, PAGED>), dim3(BLOCKS), dim3(64 * WAVES), F::LDS, s, a);
   hipLaunchKernelGGL((stream_join_kernel<T, DP>), dim3((unsigned)(a.B * a.S * a.q_heads)), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 
 }  // namespace
 
+bool stream_fits(int64_t B, int64_t S, int64_t T, int64_t q_heads, int64_t heads) {
+  return (__int128)B * heads * div_up(S * (q_heads / heads), 16) * div_up(T, 32) < 1ll << 31;
+}
 size_t stream_bytes(int64_t B, int64_t S, int64_t q_heads, int64_t heads, int64_t D) { return (size_t)stream_plan(B, S, q_heads, heads, D).bytes; }
 
 hipError_t launch_stream(StreamArgs a, int32_t dtype, void* workspace, hipStream_t s) {
   const StreamPlan p = stream_plan(a.B, a.S, a.q_heads, a.heads, a.D);
   char* ws = reinterpret_cast<char*>(workspace);
-  a.row_tiles = p.row_tiles; a.rows = p.rows; a.waves = BLOCKS * WAVES;
-  a.before = reinterpret_cast<int64_t*>(ws + p.before);
+  a.row_tile = p.row_tile; a.row_tiles = p.row_tiles; a.rows = p.rows; a.waves = BLOCKS * WAVES;
+  a.before = reinterpret_cast<uint32_t*>(ws + p.before);
   a.top_sum = reinterpret_cast<float*>(ws + p.top_sum);
   a.partial = reinterpret_cast<float*>(ws + p.partial);
   return by_size(dtype, a.D, [&](auto t, auto dp) {
     typedef decltype(t) T;
     constexpr int DP = decltype(dp)::value;
-    if (DP == 128 && a.D <= 96) return a.table ? launch<T, 128, 96, true>(a, s) : launch<T, 128, 96, false>(a, s);
-    return a.table ? launch<T, DP, DP, true>(a, s) : launch<T, DP, DP, false>(a, s);
+    auto go = [&](auto cols, auto r) {
+      constexpr int COLS = decltype(cols)::value, R = decltype(r)::value;
+      return a.table ? launch<T, DP, COLS, R, true>(a, s) : launch<T, DP, COLS, R, false>(a, s);
+    };
+    auto rows = [&](auto cols) { return a.row_tile == 16 ? go(cols, std::integral_constant<int, 16>()) : go(cols, std::integral_constant<int, 32>()); };
+    if constexpr (DP == 128) {
+      if (a.D <= 96) return rows(std::integral_constant<int, 96>());
+    }
+    return rows(std::integral_constant<int, DP>());
   });
 }
 
@@ -394,6 +508,7 @@ int antdt_cache_attention(const void* q, int64_t ldq, int64_t ldq_head, const vo
   a.table = table_cols > 0 ? table : &none;   // (without columns no length is above 0, and nothing reads it)
   a.ldt = ld_table; a.pages = pages; a.k_lengths = lengths; a.B = B; a.S = 1;
   a.T = std::min<int64_t>(table_cols * page_size, (1ll << 31) - 1);
+  if (!stream_fits(B, 1, a.T, q_heads, heads)) return op_fail(ANTDT_UNSUPPORTED, "%s: B heads table_cols page_size / 32: 2^31 or more", call);
   a.page = (int)page_size;
   int shift = 0;
   while ((1ll << shift) < page_size) ++shift;
