@@ -14,12 +14,11 @@ namespace {
 
 constexpr int WAVES = 4;                // of a block
 constexpr int BLOCKS = 256;             // one to a compute unit
-constexpr int LEAST = 4;                // tiles of a wavefront, before the next one gets some
 
 // Work in tiles, [0, total), to the wavefronts: the first `more` have one more than the others.
 struct Shares {
   uint32_t total, waves, each, more;
-  __device__ __forceinline__ Shares(uint32_t n, uint32_t most) : total(n), waves(max(1u, min(most, (n + LEAST - 1) / LEAST))), each(n / waves), more(n - each * waves) {}
+  __device__ __forceinline__ Shares(uint32_t n, uint32_t most) : total(n), waves(max(1u, min(most, n))), each(n / waves), more(n - each * waves) {}
   __device__ __forceinline__ uint32_t first(uint32_t w) const { return min(w * each + min(w, more), total); }
   __device__ __forceinline__ uint32_t owner(uint32_t tile) const {
     const uint32_t large = more * (each + 1);
