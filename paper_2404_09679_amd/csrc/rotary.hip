@@ -13,6 +13,17 @@ namespace {
 constexpr int WAVES = 4, MOST_TOKENS = 16, MOST_PAIRS = 512;   // of a wavefront, at a time
 constexpr int BATCH = 2;                                       // chunks that a lane has under way
 
+// x / d of x < 2^31 without a division: x m >> 31 + s, where 2^s is d or the next larger power of two and m = 2^(31 + s) / d, rounded up.
+struct Divisor {
+  uint32_t d, m, s;
+  static Divisor of(uint32_t d) {
+    uint32_t s = 0;
+    while ((1u << s) < d) ++s;
+    return Divisor{d, (uint32_t)(((1ull << (31 + s)) + d - 1) / d), s};
+  }
+  __device__ __forceinline__ uint32_t operator()(uint32_t x) const { return (uint32_t)((uint64_t)x * m >> 31 >> s); }
+};
+
 // Some heads of every token: queries, keys or values.  A chunk is 16 columns of a head: 8 pairs, or columns that are copied.
 struct HeadsPart {
   const void* x;
@@ -20,7 +31,8 @@ struct HeadsPart {
   int64_t xl, xh;        // strides of the token and the head
   int64_t yp, yl, yh;    // of the page, the row in it (without pages: of the token) and the head
   int32_t first;         // chunk of a token that is the part's first
-  int32_t chunks, turned;   // chunks of a head, and how many of them are turned
+  Divisor chunks;        // of a head
+  int32_t turned;        // how many of them are turned
   int32_t paged;
 };
 struct RotaryArgs {
@@ -32,7 +44,9 @@ struct RotaryArgs {
   const int32_t* table;
   int64_t N, B, ldt, room, pages;   // room: tokens that a row of the table has pages for
   int32_t page, parts, half, interleaved, D;
-  int32_t per_token, tokens, slices, span;   // chunks of a token, tokens of a wavefront; wavefronts of a token, chunks of one
+  int32_t pitch;                    // of a token's cosines in LDS: pairs, rounded up to a multiple of 8
+  int32_t tokens, slices, span;     // tokens of a wavefront; wavefronts of a token, chunks of one
+  Divisor per_token, pairs;         // chunks and pairs of a token
   float magnitude, sign;
 };
 
@@ -77,31 +91,65 @@ __device__ __forceinline__ int place(const RotaryArgs& a, int64_t n, int& page, 
   return (int)at;
 }
 
-template <typename T, int Q>
-struct Chunk {
-  const HeadsPart* part;
-  const T* x;
-  T* y;
-  float v[2][8];
-  int at[2], n[2];        // columns of its two halves
-  int token, pair;        // place in the wavefront's tokens; first pair, -1: copied
-  bool clear;
-};
-
-// Every wavefront has some tokens, or a part of one: their cosines and sines go to LDS once, for all heads.  Bound by memory; a token alone by its
-// chain of loads (place in the sequence, page, row).
-template <typename T, int Q, bool CACHE>
+// Every wavefront has some tokens, or a part of one.  Its first columns are asked for before the positions are; cosines and sines go to LDS once, for
+// all heads.  Bound by memory; a token alone by its chain of loads (place in the sequence, page).
+template <typename T, int Q, bool INTERLEAVED, bool CACHE>
 __global__ __launch_bounds__(64 * WAVES) void rotary_kernel(RotaryArgs a) {
-  __shared__ float cosines[WAVES][MOST_PAIRS], sines[WAVES][MOST_PAIRS];
+  __shared__ __attribute__((aligned(16))) float cosines[WAVES][MOST_PAIRS], sines[WAVES][MOST_PAIRS];
   __shared__ int where[WAVES][3][MOST_TOKENS];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t groups = (a.N + a.tokens - 1) / a.tokens;
   float* cs = cosines[wave];
   float* sn = sines[wave];
   int(&at)[3][MOST_TOKENS] = where[wave];
+  // f of a part, by selects: a lane's own part would be read from the arguments' memory.
+  auto of_part = [&](int which, auto f) {
+    if constexpr (!CACHE) return f(a.part[0]);
+    else return which == 0 ? f(a.part[0]) : which == 1 ? f(a.part[1]) : f(a.part[2]);
+  };
   for (int64_t w = (int64_t)blockIdx.x * WAVES + wave; w < groups * a.slices; w += (int64_t)gridDim.x * WAVES) {
-    const int64_t group = w / a.slices, n0 = group * a.tokens;
+    const int64_t group = a.slices == 1 ? w : w / a.slices, n0 = group * a.tokens;
     const int tokens = (int)min((int64_t)a.tokens, a.N - n0);
+    const int begin = (int)(w - group * a.slices) * a.span, end = min(begin + a.span, tokens * (int)a.per_token.d);
+    // A lane's chunks: 16 columns of a head in two halves of n0, n1 columns.
+    float v[BATCH][2][8];
+    int part[BATCH], token[BATCH], head[BATCH], pair[BATCH], at0[BATCH], at1[BATCH], n_0[BATCH], n_1[BATCH];
+    auto load = [&](int i0) {
+#pragma unroll
+      for (int q = 0; q < BATCH; ++q) {
+        const int i = i0 + 64 * q;
+        const bool some = i < end;
+        const int j = a.per_token(some ? i : 0), c = (some ? i : 0) - j * (int)a.per_token.d;
+        const int which = !CACHE ? 0 : a.parts > 2 && c >= a.part[2].first ? 2 : a.parts > 1 && c >= a.part[1].first ? 1 : 0;
+        const int in = c - of_part(which, [](const HeadsPart& p) { return p.first; });
+        const Divisor chunks = {of_part(which, [](const HeadsPart& p) { return p.chunks.d; }), of_part(which, [](const HeadsPart& p) { return p.chunks.m; }),
+                                of_part(which, [](const HeadsPart& p) { return p.chunks.s; })};
+        const int turned = of_part(which, [](const HeadsPart& p) { return p.turned; });
+        const int h = chunks(in), e = in - h * (int)chunks.d;
+        part[q] = which; token[q] = j; head[q] = h;
+        int m0, m1;
+        if (e < turned) {
+          pair[q] = 8 * e;
+          at0[q] = INTERLEAVED ? 16 * e : 8 * e;
+          at1[q] = INTERLEAVED ? 16 * e + 8 : a.half + 8 * e;
+          m0 = INTERLEAVED ? 2 * a.half - 16 * e : a.half - 8 * e;
+          m1 = INTERLEAVED ? m0 - 8 : m0;
+        } else {
+          pair[q] = -1;
+          at0[q] = (turned ? 2 * a.half : 0) + 16 * (e - turned);
+          at1[q] = at0[q] + 8;
+          m0 = a.D - at0[q];
+          m1 = m0 - 8;
+        }
+        n_0[q] = some ? min(8, m0) : 0;
+        n_1[q] = some ? max(0, min(8, m1)) : 0;
+        const T* x = reinterpret_cast<const T*>(of_part(which, [](const HeadsPart& p) { return p.x; })) + (n0 + j) * of_part(which, [](const HeadsPart& p) { return p.xl; }) +
+                     h * of_part(which, [](const HeadsPart& p) { return p.xh; });
+        if (n_0[q] > 0) load8<Q>(x + at0[q], n_0[q], v[q][0]);
+        if (n_1[q] > 0) load8<Q>(x + at1[q], n_1[q], v[q][1]);
+      }
+    };
+    load(begin + lane);
     if (lane < tokens) {
       int page = 0, row = 0, p;
       if (CACHE) p = place(a, n0 + lane, page, row);
@@ -112,102 +160,65 @@ __global__ __launch_bounds__(64 * WAVES) void rotary_kernel(RotaryArgs a) {
     }
     wave_lds_order();
     for (int i = lane; i < tokens * a.half; i += 64) {
-      const int j = i / a.half;
+      const int j = a.pairs(i), k = i - j * a.half;
       float c, s;
-      turn((uint64_t)(int64_t)at[0][j] * a.turns[i - j * a.half], c, s);
-      cs[i] = c * a.magnitude;
-      sn[i] = s * a.magnitude * a.sign;
+      turn((uint64_t)(int64_t)at[0][j] * a.turns[k], c, s);
+      cs[j * a.pitch + k] = c * a.magnitude;
+      sn[j * a.pitch + k] = s * a.magnitude * a.sign;
     }
     wave_lds_order();
-    const int begin = (int)(w - group * a.slices) * a.span, end = min(begin + a.span, tokens * a.per_token);
-    for (int i0 = begin + lane; i0 < end; i0 += 64 * BATCH) {
-      Chunk<T, Q> ch[BATCH];
+    for (int i0 = begin;;) {
 #pragma unroll
       for (int q = 0; q < BATCH; ++q) {
-        const int i = i0 + 64 * q;
-        Chunk<T, Q>& k = ch[q];
-        k.n[0] = k.n[1] = 0;
-        if (i >= end) continue;
-        const int j = i / a.per_token, c = i - j * a.per_token;
-        const int which = a.parts > 2 && c >= a.part[2].first ? 2 : a.parts > 1 && c >= a.part[1].first ? 1 : 0;
-        const HeadsPart& p = a.part[which];
-        const int h = (c - p.first) / p.chunks, e = c - p.first - h * p.chunks;
-        k.token = j;
-        k.clear = CACHE && !p.paged && at[0][j] < 0;
-        if (CACHE && p.paged && at[2][j] < 0) continue;
-        k.x = reinterpret_cast<const T*>(p.x) + (n0 + j) * p.xl + h * p.xh;
-        k.y = reinterpret_cast<T*>(p.y) + h * p.yh + (CACHE && p.paged ? at[1][j] * p.yp + at[2][j] * p.yl : (n0 + j) * p.yl);
-        if (e < p.turned) {
-          k.pair = 8 * e;
-          k.at[0] = a.interleaved ? 16 * e : 8 * e;
-          k.at[1] = a.interleaved ? 16 * e + 8 : a.half + 8 * e;
-          const int left = a.interleaved ? 2 * a.half - 16 * e : a.half - 8 * e;
-          k.n[0] = min(8, left);
-          k.n[1] = a.interleaved ? max(0, min(8, left - 8)) : k.n[0];
-        } else {
-          k.pair = -1;
-          k.at[0] = (p.turned ? 2 * a.half : 0) + 16 * (e - p.turned);
-          k.at[1] = k.at[0] + 8;
-          k.n[0] = min(8, a.D - k.at[0]);
-          k.n[1] = max(0, min(8, a.D - k.at[1]));
-        }
+        if (n_0[q] <= 0) continue;
+        const bool paged = CACHE && of_part(part[q], [](const HeadsPart& p) { return p.paged; }) != 0;
+        if (paged && at[2][token[q]] < 0) continue;
+        if (pair[q] >= 0) {
+          float c[8], s[8];
+          load8<4>(cs + token[q] * a.pitch + pair[q], 8, c);   // (behind the last pair whatever lies there, for columns that are not stored)
+          load8<4>(sn + token[q] * a.pitch + pair[q], 8, s);
 #pragma unroll
-        for (int s = 0; s < 2; ++s)
-          if (k.n[s] > 0) load8<Q>(k.x + k.at[s], k.n[s], k.v[s]);
-      }
-#pragma unroll
-      for (int q = 0; q < BATCH; ++q) {
-        Chunk<T, Q>& k = ch[q];
-        if (k.n[0] <= 0) continue;
-        if (k.pair >= 0) {
-          const float* c = cs + k.token * a.half + k.pair;
-          const float* s = sn + k.token * a.half + k.pair;
-          const int last = a.half - 1 - k.pair;
-          float y[2][8];
-          if (a.interleaved) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              const int f = min(e, last);
-              const float u = k.v[e >> 2][2 * (e & 3)], v = k.v[e >> 2][2 * (e & 3) + 1];
-              y[e >> 2][2 * (e & 3)] = fmaf(-v, s[f], u * c[f]);
-              y[e >> 2][2 * (e & 3) + 1] = fmaf(u, s[f], v * c[f]);
-            }
-          } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              const int f = min(e, last);
-              const float u = k.v[0][e], v = k.v[1][e];
-              y[0][e] = fmaf(-v, s[f], u * c[f]);   // (said so: every layout's kernel rounds alike)
-              y[1][e] = fmaf(u, s[f], v * c[f]);
-            }
+          for (int e = 0; e < 8; ++e) {
+            float& x = INTERLEAVED ? v[q][e >> 2][2 * (e & 3)] : v[q][0][e];
+            float& y = INTERLEAVED ? v[q][e >> 2][2 * (e & 3) + 1] : v[q][1][e];
+            const float x0 = x;
+            x = fmaf(-y, s[e], x0 * c[e]);   // (said so: every layout's kernel rounds alike)
+            y = fmaf(x0, s[e], y * c[e]);
           }
-#pragma unroll
-          for (int e = 0; e < 16; ++e) k.v[e >> 3][e & 7] = y[e >> 3][e & 7];
         }
-        if (k.clear) {
+        if (CACHE && !paged && at[0][token[q]] < 0) {
 #pragma unroll
-          for (int e = 0; e < 16; ++e) k.v[e >> 3][e & 7] = 0.0f;
+          for (int e = 0; e < 16; ++e) v[q][e >> 3][e & 7] = 0.0f;
         }
-#pragma unroll
-        for (int s = 0; s < 2; ++s)
-          if (k.n[s] > 0) store8<Q>(k.y + k.at[s], k.n[s], k.v[s]);
+        const int64_t yl = of_part(part[q], [](const HeadsPart& p) { return p.yl; }), yh = of_part(part[q], [](const HeadsPart& p) { return p.yh; });
+        T* y = reinterpret_cast<T*>(of_part(part[q], [](const HeadsPart& p) { return p.y; })) + head[q] * yh;
+        if (paged) y += at[1][token[q]] * of_part(part[q], [](const HeadsPart& p) { return p.yp; }) + at[2][token[q]] * yl;
+        else y += (n0 + token[q]) * yl;
+        store8<Q>(y + at0[q], n_0[q], v[q][0]);
+        if (n_1[q] > 0) store8<Q>(y + at1[q], n_1[q], v[q][1]);
       }
+      i0 += 64 * BATCH;
+      if (i0 >= end) break;
+      load(i0 + lane);
     }
     wave_lds_order();   // (the next tokens' go to the same places)
   }
 }
 
 // Wavefronts: several small tokens to one, or several to a large token.
-void share(RotaryArgs& a) {
-  a.tokens = std::max(1, std::min(64 / a.per_token, MOST_TOKENS));
-  if (a.half) a.tokens = std::max(1, std::min(a.tokens, MOST_PAIRS / a.half));
+void share(RotaryArgs& a, int per_token) {
+  a.per_token = Divisor::of(per_token);
+  a.pairs = Divisor::of(std::max(a.half, 1));
+  a.pitch = (a.half + 7) & ~7;
+  a.tokens = std::max(1, std::min(64 / per_token, MOST_TOKENS));
+  if (a.half) a.tokens = std::max(1, std::min(a.tokens, MOST_PAIRS / a.pitch));
   a.slices = 1;
-  a.span = a.tokens * a.per_token;
-  if (a.per_token > 64) {
+  a.span = a.tokens * per_token;
+  if (per_token > 64) {
     int turns = 4;
-    while (turns > 1 && a.N * div_up(a.per_token, 64 * turns) < 8192) turns >>= 1;
+    while (turns > 1 && a.N * div_up(per_token, 64 * turns) < 8192) turns >>= 1;
     a.span = 64 * turns;
-    a.slices = (int)div_up(a.per_token, a.span);
+    a.slices = (int)div_up(per_token, a.span);
   }
 }
 
@@ -215,9 +226,14 @@ template <typename T, bool CACHE>
 hipError_t launch_rotary(const RotaryArgs& a, int quantum, hipStream_t s) {
   const int64_t waves = div_up(a.N, a.tokens) * a.slices;
   const dim3 grid((unsigned)std::min<int64_t>(div_up(waves, WAVES), 1 << 20)), block(64 * WAVES);
-  if (quantum == 8) hipLaunchKernelGGL((rotary_kernel<T, 8, CACHE>), grid, block, 0, s, a);
-  else if (quantum == 4) hipLaunchKernelGGL((rotary_kernel<T, 4, CACHE>), grid, block, 0, s, a);
-  else hipLaunchKernelGGL((rotary_kernel<T, 1, CACHE>), grid, block, 0, s, a);
+  auto go = [&](auto q) {
+    constexpr int Q = decltype(q)::value;
+    if (a.interleaved) hipLaunchKernelGGL((rotary_kernel<T, Q, true, CACHE>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((rotary_kernel<T, Q, false, CACHE>), grid, block, 0, s, a);
+  };
+  if (quantum == 8) go(std::integral_constant<int, 8>());
+  else if (quantum == 4) go(std::integral_constant<int, 4>());
+  else go(std::integral_constant<int, 1>());
   return hipGetLastError();
 }
 
@@ -236,16 +252,17 @@ int rotary_spec(const char* call, const antdt_rotary_spec* r, int64_t D, RotaryA
   if (!isfinite(r->magnitude)) return op_fail(ANTDT_INVALID_ARG, "%s: rotary: magnitude is not finite", call);
   if (!r->turns || (reinterpret_cast<uintptr_t>(r->turns) & 7)) return op_fail(ANTDT_INVALID_ARG, "%s: rotary: turns is null or misaligned", call);
   a.turns = r->turns; a.half = r->dim / 2; a.interleaved = r->interleaved; a.magnitude = r->magnitude;
-  quantum = a.half % 8 == 0 ? 8 : a.half % 4 == 0 ? 4 : 1;   // (a chunk's halves start at multiples of `half`, or of 8)
+  const int wide = a.interleaved ? r->dim : a.half;   // (a chunk's halves start at multiples of it, or of 8)
+  quantum = wide % 8 == 0 ? 8 : wide % 4 == 0 ? 4 : 1;
   return ANTDT_OK;
 }
-// Chunks of the parts, in the order of a token.
-void chunks(RotaryArgs& a, int part, int64_t heads, bool turned, bool copied) {
+// Chunks of the parts, in the order of a token; `per_token` those of the parts so far.
+void chunks(RotaryArgs& a, int part, int64_t heads, bool turned, bool copied, int& per_token) {
   HeadsPart& p = a.part[part];
-  p.first = a.per_token;
+  p.first = per_token;
   p.turned = turned ? (int)div_up(a.half, 8) : 0;
-  p.chunks = p.turned + (copied ? (int)div_up(a.D - (turned ? 2 * a.half : 0), 16) : 0);
-  a.per_token += p.chunks * (int)heads;
+  p.chunks = Divisor::of(p.turned + (copied ? (int)div_up(a.D - (turned ? 2 * a.half : 0), 16) : 0));
+  per_token += p.chunks.d * (int)heads;
   a.parts = part + 1;
 }
 
@@ -290,10 +307,11 @@ int antdt_rotary(const void* x, int64_t ldx, int64_t ldx_head, int64_t N, int64_
   OP_TRY(op_heads(call, "y", y, 1, N, H, D, sy, size, true));
   OP_TRY(op_matrix(call, "positions", positions, N, 1, 1, 4));
   a.N = N; a.D = (int)D; a.positions = positions; a.sign = inverse ? -1.0f : 1.0f;
-  a.part[0] = HeadsPart{x, y, sx.l, sx.h, 0, sy.l, sy.h, 0, 0, 0, 0};
+  a.part[0] = HeadsPart{x, y, sx.l, sx.h, 0, sy.l, sy.h, 0, Divisor(), 0, 0};
   const bool copied = rotary->dim < D && !same_heads(x, sx, y, sy);
-  chunks(a, 0, H, true, copied);
-  share(a);
+  int per_token = 0;
+  chunks(a, 0, H, true, copied, per_token);
+  share(a, per_token);
   q = std::min(q, std::min(head_quantum(copied ? D : 2 * a.half, size, x, sx), head_quantum(copied ? D : 2 * a.half, size, y, sy)));
   const hipStream_t s = (hipStream_t)stream;
   return op_hip(call, dtype == ANTDT_F32 ? launch_rotary<float, false>(a, q, s) : launch_rotary<bf16_t, false>(a, q, s));
@@ -331,21 +349,21 @@ int antdt_cache_append(const void* q, int64_t ldq, int64_t ldq_head, void* q_out
   a.N = N; a.B = B; a.D = (int)D; a.sign = 1.0f;
   a.lengths = lengths; a.offsets = offsets; a.table = table; a.ldt = ld_table;
   a.page = (int)page_size; a.pages = pages; a.room = table_cols * page_size;
-  int part = 0;
+  int part = 0, per_token = 0;
   if (q_heads > 0) {
-    a.part[part] = HeadsPart{q, q_out, sq.l, sq.h, 0, so.l, so.h, 0, 0, 0, 0};
-    chunks(a, part++, q_heads, rotary != nullptr, !rotary || rotary->dim < D);
+    a.part[part] = HeadsPart{q, q_out, sq.l, sq.h, 0, so.l, so.h, 0, Divisor(), 0, 0};
+    chunks(a, part++, q_heads, rotary != nullptr, !rotary || rotary->dim < D, per_token);
     quantum = std::min(quantum, std::min(head_quantum(D, size, q, sq), head_quantum(D, size, q_out, so)));
   }
   if (heads > 0) {
-    a.part[part] = HeadsPart{k, k_cache, sk.l, sk.h, sc.b, sc.l, sc.h, 0, 0, 0, 1};
-    chunks(a, part++, heads, rotary != nullptr, !rotary || rotary->dim < D);
-    a.part[part] = HeadsPart{v, v_cache, sv.l, sv.h, sc.b, sc.l, sc.h, 0, 0, 0, 1};
-    chunks(a, part++, heads, false, true);
+    a.part[part] = HeadsPart{k, k_cache, sk.l, sk.h, sc.b, sc.l, sc.h, 0, Divisor(), 0, 1};
+    chunks(a, part++, heads, rotary != nullptr, !rotary || rotary->dim < D, per_token);
+    a.part[part] = HeadsPart{v, v_cache, sv.l, sv.h, sc.b, sc.l, sc.h, 0, Divisor(), 0, 1};
+    chunks(a, part++, heads, false, true, per_token);
     quantum = std::min(std::min(quantum, head_quantum(D, size, k_cache, sc)), std::min(head_quantum(D, size, k, sk), head_quantum(D, size, v, sv)));
     quantum = std::min(quantum, head_quantum(D, size, v_cache, sc));
   }
-  share(a);
+  share(a, per_token);
   const hipStream_t s = (hipStream_t)stream;
   return op_hip(call, dtype == ANTDT_F32 ? launch_rotary<float, true>(a, quantum, s) : launch_rotary<bf16_t, true>(a, quantum, s));
 }
