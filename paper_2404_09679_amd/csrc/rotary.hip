@@ -11,7 +11,6 @@ namespace antdt {
 namespace {
 
 constexpr int WAVES = 4, MOST_TOKENS = 16, MOST_PAIRS = 512;   // of a wavefront, at a time
-constexpr int BATCH = 2;                                       // chunks that a lane has under way
 
 // x / d of x < 2^31 without a division: x m >> 31 + s, where 2^s is d or the next larger power of two and m = 2^(31 + s) / d, rounded up.
 struct Divisor {
@@ -43,10 +42,10 @@ struct RotaryArgs {
   const int32_t* offsets;
   const int32_t* table;
   int64_t N, B, ldt, room, pages;   // room: tokens that a row of the table has pages for
-  int32_t page, parts, half, interleaved, D;
+  int32_t parts, half, interleaved, D;
   int32_t pitch;                    // of a token's cosines in LDS: pairs, rounded up to a multiple of 8
   int32_t tokens, slices, span;     // tokens of a wavefront; wavefronts of a token, chunks of one
-  Divisor per_token, pairs;         // chunks and pairs of a token
+  Divisor per_token, pairs, pages_of;   // chunks and pairs of a token, tokens of a page
   float magnitude, sign;
 };
 
@@ -65,28 +64,45 @@ __device__ __forceinline__ void turn(uint64_t t, float& c, float& s) {
   if (quarter >= 2) s = -s;
 }
 
-// Position of token n in its sequence (-1: in none), and where in the cache it belongs (row -1: nowhere).
-__device__ __forceinline__ int place(const RotaryArgs& a, int64_t n, int& page, int& row) {
-  int64_t b = n, first = n, behind = n + 1;
+// Position of each lane's token n in its sequence (-1: in none), and where in the cache it belongs (row -1: nowhere).  Called by the whole wavefront:
+// the sequence is found among 64 of the offsets, one in each lane, and then (of 64 sequences and more) between two of them in memory.  Of fewer
+// sequences the lanes hold the lengths too, so that nothing but the page waits for another load.
+__device__ __forceinline__ int place(const RotaryArgs& a, int64_t n, int lane, int& page, int& row) {
+  int64_t b = n, first = n, behind = n + 1, length;
   page = 0; row = -1;
   if (a.offsets) {
-    int64_t lo = 0, hi = a.B;   // the last sequence that starts at n or before
-    while (hi - lo > 1) {
-      const int64_t mid = (lo + hi) >> 1;
-      if (a.offsets[mid] <= n) lo = mid;
-      else hi = mid;
+    const int64_t step = (a.B + 63) >> 6;
+    const bool all = a.B < 64;
+    const int mine = a.offsets[min(lane * step, a.B)], of_mine = all ? a.lengths[min((int64_t)lane, a.B - 1)] : 0;
+    int at = 0;   // the last lane whose sequence starts at n or before
+#pragma unroll
+    for (int s = 32; s > 0; s >>= 1)
+      if (__shfl(mine, at + s, 64) <= n) at += s;
+    b = min(at * step, a.B - 1);
+    if (all) {
+      first = __shfl(mine, (int)b, 64);
+      behind = __shfl(mine, (int)b + 1, 64);
+      length = __shfl(of_mine, (int)b, 64);
+    } else {
+      int64_t end = min(b + step, a.B);
+      while (end - b > 1) {
+        const int64_t mid = (b + end) >> 1;
+        if (a.offsets[mid] <= n) b = mid;
+        else end = mid;
+      }
+      first = a.offsets[b];
+      behind = a.offsets[b + 1];
+      length = a.lengths[b];
     }
-    b = lo;
-    first = a.offsets[b];
-    behind = a.offsets[b + 1];
-    if (n < first || n >= behind) return -1;
+  } else {
+    length = a.lengths[b];
   }
-  const int64_t at = a.lengths[b] - (behind - n);
-  if (at < 0) return -1;
+  const int64_t at = length - (behind - n);
+  if (n < first || n >= behind || at < 0) return -1;
   if (at < a.room) {
-    const int64_t i = at / a.page;
+    const uint32_t i = a.pages_of((uint32_t)at);
     page = a.table[b * a.ldt + i];
-    if (page >= 0 && page < a.pages) row = (int)(at - i * a.page);
+    if (page >= 0 && page < a.pages) row = (int)(at - (int64_t)i * a.pages_of.d);
   }
   return (int)at;
 }
@@ -108,98 +124,98 @@ __global__ __launch_bounds__(64 * WAVES) void rotary_kernel(RotaryArgs a) {
     else return which == 0 ? f(a.part[0]) : which == 1 ? f(a.part[1]) : f(a.part[2]);
   };
   for (int64_t w = (int64_t)blockIdx.x * WAVES + wave; w < groups * a.slices; w += (int64_t)gridDim.x * WAVES) {
-    const int64_t group = a.slices == 1 ? w : w / a.slices, n0 = group * a.tokens;
-    const int tokens = (int)min((int64_t)a.tokens, a.N - n0);
+    const int64_t group = a.slices == 1 ? w : w / a.slices, t0 = group * a.tokens;
+    const int tokens = (int)min((int64_t)a.tokens, a.N - t0);
     const int begin = (int)(w - group * a.slices) * a.span, end = min(begin + a.span, tokens * (int)a.per_token.d);
-    // A lane's chunks: 16 columns of a head in two halves of n0, n1 columns.
-    float v[BATCH][2][8];
-    int part[BATCH], token[BATCH], head[BATCH], pair[BATCH], at0[BATCH], at1[BATCH], n_0[BATCH], n_1[BATCH];
-    auto load = [&](int i0) {
-#pragma unroll
-      for (int q = 0; q < BATCH; ++q) {
-        const int i = i0 + 64 * q;
-        const bool some = i < end;
-        const int j = a.per_token(some ? i : 0), c = (some ? i : 0) - j * (int)a.per_token.d;
-        const int which = !CACHE ? 0 : a.parts > 2 && c >= a.part[2].first ? 2 : a.parts > 1 && c >= a.part[1].first ? 1 : 0;
-        const int in = c - of_part(which, [](const HeadsPart& p) { return p.first; });
-        const Divisor chunks = {of_part(which, [](const HeadsPart& p) { return p.chunks.d; }), of_part(which, [](const HeadsPart& p) { return p.chunks.m; }),
-                                of_part(which, [](const HeadsPart& p) { return p.chunks.s; })};
-        const int turned = of_part(which, [](const HeadsPart& p) { return p.turned; });
-        const int h = chunks(in), e = in - h * (int)chunks.d;
-        part[q] = which; token[q] = j; head[q] = h;
-        int m0, m1;
-        if (e < turned) {
-          pair[q] = 8 * e;
-          at0[q] = INTERLEAVED ? 16 * e : 8 * e;
-          at1[q] = INTERLEAVED ? 16 * e + 8 : a.half + 8 * e;
-          m0 = INTERLEAVED ? 2 * a.half - 16 * e : a.half - 8 * e;
-          m1 = INTERLEAVED ? m0 - 8 : m0;
-        } else {
-          pair[q] = -1;
-          at0[q] = (turned ? 2 * a.half : 0) + 16 * (e - turned);
-          at1[q] = at0[q] + 8;
-          m0 = a.D - at0[q];
-          m1 = m0 - 8;
-        }
-        n_0[q] = some ? min(8, m0) : 0;
-        n_1[q] = some ? max(0, min(8, m1)) : 0;
-        const T* x = reinterpret_cast<const T*>(of_part(which, [](const HeadsPart& p) { return p.x; })) + (n0 + j) * of_part(which, [](const HeadsPart& p) { return p.xl; }) +
-                     h * of_part(which, [](const HeadsPart& p) { return p.xh; });
-        if (n_0[q] > 0) load8<Q>(x + at0[q], n_0[q], v[q][0]);
-        if (n_1[q] > 0) load8<Q>(x + at1[q], n_1[q], v[q][1]);
+    // A lane's chunk: 16 columns of a head, two halves of n0 and n1.
+    float v[2][8];
+    int part, token, head, pair, at0, at1, n0, n1;
+    auto load = [&](int i) {
+      const bool some = i < end;
+      i = some ? i : 0;
+      token = a.per_token(i);
+      const int c = i - token * (int)a.per_token.d;
+      part = !CACHE ? 0 : a.parts > 2 && c >= a.part[2].first ? 2 : a.parts > 1 && c >= a.part[1].first ? 1 : 0;
+      const int in = c - of_part(part, [](const HeadsPart& p) { return p.first; });
+      const Divisor chunks = {of_part(part, [](const HeadsPart& p) { return p.chunks.d; }), of_part(part, [](const HeadsPart& p) { return p.chunks.m; }),
+                              of_part(part, [](const HeadsPart& p) { return p.chunks.s; })};
+      const int turned = of_part(part, [](const HeadsPart& p) { return p.turned; });
+      head = chunks(in);
+      const int e = in - head * (int)chunks.d;
+      int left0, left1;
+      if (e < turned) {
+        pair = 8 * e;
+        at0 = INTERLEAVED ? 16 * e : 8 * e;
+        at1 = INTERLEAVED ? 16 * e + 8 : a.half + 8 * e;
+        left0 = INTERLEAVED ? 2 * a.half - 16 * e : a.half - 8 * e;
+        left1 = INTERLEAVED ? left0 - 8 : left0;
+      } else {
+        pair = -1;
+        at0 = (turned ? 2 * a.half : 0) + 16 * (e - turned);
+        at1 = at0 + 8;
+        left0 = a.D - at0;
+        left1 = left0 - 8;
       }
+      n0 = some ? min(8, left0) : 0;
+      n1 = some ? max(0, min(8, left1)) : 0;
+      const T* x = reinterpret_cast<const T*>(of_part(part, [](const HeadsPart& p) { return p.x; })) + (t0 + token) * of_part(part, [](const HeadsPart& p) { return p.xl; }) +
+                   head * of_part(part, [](const HeadsPart& p) { return p.xh; });
+      if (n0 > 0) load8<Q>(x + at0, n0, v[0]);
+      if (n1 > 0) load8<Q>(x + at1, n1, v[1]);
     };
-    load(begin + lane);
-    if (lane < tokens) {
-      int page = 0, row = 0, p;
-      if (CACHE) p = place(a, n0 + lane, page, row);
-      else p = a.positions[n0 + lane];
-      at[0][lane] = p;
-      at[1][lane] = page;
-      at[2][lane] = row;
+    load(begin + lane);   // (two under way a lane: 115 us for 95)
+    const int pairs = tokens * a.half;
+    uint64_t f = lane < pairs ? a.turns[lane - a.pairs(lane) * a.half] : 0;
+    {
+      int page = 0, row = 0, p = 0;
+      if (CACHE) p = place(a, t0 + min(lane, tokens - 1), lane, page, row);
+      else if (lane < tokens) p = a.positions[t0 + lane];
+      if (lane < tokens) {
+        at[0][lane] = p;
+        at[1][lane] = page;
+        at[2][lane] = row;
+      }
     }
     wave_lds_order();
-    for (int i = lane; i < tokens * a.half; i += 64) {
+    for (int i = lane; i < pairs; i += 64) {
       const int j = a.pairs(i), k = i - j * a.half;
+      if (i != lane) f = a.turns[k];
       float c, s;
-      turn((uint64_t)(int64_t)at[0][j] * a.turns[k], c, s);
+      turn((uint64_t)(int64_t)at[0][j] * f, c, s);
       cs[j * a.pitch + k] = c * a.magnitude;
       sn[j * a.pitch + k] = s * a.magnitude * a.sign;
     }
     wave_lds_order();
-    for (int i0 = begin;;) {
-#pragma unroll
-      for (int q = 0; q < BATCH; ++q) {
-        if (n_0[q] <= 0) continue;
-        const bool paged = CACHE && of_part(part[q], [](const HeadsPart& p) { return p.paged; }) != 0;
-        if (paged && at[2][token[q]] < 0) continue;
-        if (pair[q] >= 0) {
+    for (int i = begin;;) {
+      const bool paged = CACHE && of_part(part, [](const HeadsPart& p) { return p.paged; }) != 0;
+      if (n0 > 0 && !(paged && at[2][token] < 0)) {
+        if (pair >= 0) {
           float c[8], s[8];
-          load8<4>(cs + token[q] * a.pitch + pair[q], 8, c);   // (behind the last pair whatever lies there, for columns that are not stored)
-          load8<4>(sn + token[q] * a.pitch + pair[q], 8, s);
+          load8<4>(cs + token * a.pitch + pair, 8, c);   // (behind the last pair whatever lies there, for columns that are not stored)
+          load8<4>(sn + token * a.pitch + pair, 8, s);
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
-            float& x = INTERLEAVED ? v[q][e >> 2][2 * (e & 3)] : v[q][0][e];
-            float& y = INTERLEAVED ? v[q][e >> 2][2 * (e & 3) + 1] : v[q][1][e];
+            float& x = INTERLEAVED ? v[e >> 2][2 * (e & 3)] : v[0][e];
+            float& y = INTERLEAVED ? v[e >> 2][2 * (e & 3) + 1] : v[1][e];
             const float x0 = x;
             x = fmaf(-y, s[e], x0 * c[e]);   // (said so: every layout's kernel rounds alike)
             y = fmaf(x0, s[e], y * c[e]);
           }
         }
-        if (CACHE && !paged && at[0][token[q]] < 0) {
+        if (CACHE && !paged && at[0][token] < 0) {
 #pragma unroll
-          for (int e = 0; e < 16; ++e) v[q][e >> 3][e & 7] = 0.0f;
+          for (int e = 0; e < 16; ++e) v[e >> 3][e & 7] = 0.0f;
         }
-        const int64_t yl = of_part(part[q], [](const HeadsPart& p) { return p.yl; }), yh = of_part(part[q], [](const HeadsPart& p) { return p.yh; });
-        T* y = reinterpret_cast<T*>(of_part(part[q], [](const HeadsPart& p) { return p.y; })) + head[q] * yh;
-        if (paged) y += at[1][token[q]] * of_part(part[q], [](const HeadsPart& p) { return p.yp; }) + at[2][token[q]] * yl;
-        else y += (n0 + token[q]) * yl;
-        store8<Q>(y + at0[q], n_0[q], v[q][0]);
-        if (n_1[q] > 0) store8<Q>(y + at1[q], n_1[q], v[q][1]);
+        const int64_t yl = of_part(part, [](const HeadsPart& p) { return p.yl; }), yh = of_part(part, [](const HeadsPart& p) { return p.yh; });
+        T* y = reinterpret_cast<T*>(of_part(part, [](const HeadsPart& p) { return p.y; })) + head * yh;
+        if (paged) y += at[1][token] * of_part(part, [](const HeadsPart& p) { return p.yp; }) + at[2][token] * yl;
+        else y += (t0 + token) * yl;
+        store8<Q>(y + at0, n0, v[0]);
+        if (n1 > 0) store8<Q>(y + at1, n1, v[1]);
       }
-      i0 += 64 * BATCH;
-      if (i0 >= end) break;
-      load(i0 + lane);
+      i += 64;
+      if (i >= end) break;
+      load(i + lane);
     }
     wave_lds_order();   // (the next tokens' go to the same places)
   }
@@ -348,7 +364,7 @@ int antdt_cache_append(const void* q, int64_t ldq, int64_t ldq_head, void* q_out
   if (offsets) OP_TRY(op_matrix(call, "offsets", offsets, B + 1, 1, 1, 4));
   a.N = N; a.B = B; a.D = (int)D; a.sign = 1.0f;
   a.lengths = lengths; a.offsets = offsets; a.table = table; a.ldt = ld_table;
-  a.page = (int)page_size; a.pages = pages; a.room = table_cols * page_size;
+  a.pages_of = Divisor::of((uint32_t)page_size); a.pages = pages; a.room = table_cols * page_size;
   int part = 0, per_token = 0;
   if (q_heads > 0) {
     a.part[part] = HeadsPart{q, q_out, sq.l, sq.h, 0, so.l, so.h, 0, Divisor(), 0, 0};
