@@ -240,7 +240,10 @@ def test_cache_far_into_its_memory():
 CROSS = [  # B, S, T, q heads, heads, D, lengths: all, "ragged"
     (1, 1, 1, 1, 1, 8, ""), (2, 1, 5, 2, 2, 32, "ragged"), (3, 1, 700, 4, 2, 64, "ragged"), (2, 5, 33, 3, 1, 40, ""), (1, 33, 65, 2, 2, 16, "ragged"),
     (2, 127, 64, 2, 1, 128, ""), (3, 129, 200, 4, 2, 72, "ragged"), (2, 200, 31, 2, 2, 64, "ragged"), (1, 300, 333, 8, 2, 32, ""), (6, 40, 130, 6, 2, 56, "ragged"),
-    (1, 16, 2000, 2, 1, 128, ""), (2, 260, 513, 2, 2, 104, "ragged"), (1, 50, 1, 1, 1, 24, ""), (4, 3, 4, 70, 10, 8, "ragged")]
+    (1, 16, 2000, 2, 1, 128, ""), (2, 260, 513, 2, 2, 104, "ragged"), (1, 50, 1, 1, 1, 24, ""), (4, 3, 4, 70, 10, 8, "ragged"),
+    # few results with many terms each, and so many results that nothing is shared out
+    (1, 40, 1100, 2, 1, 64, ""), (2, 70, 900, 1, 1, 88, "ragged"), (1, 33, 1500, 2, 2, 128, "ragged"), (1, 1000, 40, 4, 1, 64, ""), (2, 700, 20, 2, 1, 128, "ragged"),
+    (3, 600, 33, 2, 1, 16, "ragged"), (9, 130, 140, 32, 32, 24, "ragged"), (9, 140, 130, 32, 32, 64, ""), (5, 131, 200, 64, 64, 88, "ragged"), (9, 129, 131, 32, 32, 128, "ragged")]
 
 
 def cross_inputs(rng, B, S, T, HQ, H, D, kind, dtype, std=1.0):
