@@ -13,7 +13,7 @@ namespace antdt {
 namespace {
 
 constexpr int WAVES = 4;                // of a block
-constexpr int BLOCKS = 256;             // one to a compute unit
+constexpr int BLOCKS = 512;             // of the largest launch
 
 // Work in tiles, [0, total), to the wavefronts: the first `more` have one more than the others.
 struct Shares {
@@ -27,6 +27,11 @@ struct Shares {
 };
 
 __device__ __forceinline__ uint32_t tiles_of(const StreamArgs& a, int64_t b) { return (uint32_t)((length_of(a.k_lengths, b, a.T) + 31) >> 5); }
+
+// As load_lds16, not kept in the caches beyond this use.
+__device__ __forceinline__ void load_lds16_once(const void* src, uint32_t lds) {
+  asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %1, off nt" ::"{m0}"(lds), "v"(src) : "memory");
+}
 
 // What a row that there is not is read from.
 static __device__ __attribute__((aligned(16))) uint32_t zero_row[128];
@@ -62,7 +67,8 @@ struct Stream {
   typedef HeadTile<T, DP> Tile;
   typedef typename Core<T>::Fragment Fragment;
   static constexpr int BYTES = 32 * Tile::ROW, PIECES = BYTES / 1024, PIECE_ROWS = 64 / Tile::PITCH;
-  static constexpr int STAGES = BYTES >= 16384 ? 1 : BYTES >= 8192 ? 2 : 4;
+  static constexpr int STAGES = BYTES >= 8192 ? 1 : BYTES >= 4096 ? 2 : 4;
+  static constexpr int PER_CU = BYTES >= 16384 ? 1 : 2;   // blocks of a compute unit
   // A wavefront's LDS: the rings of keys and of values, where a tile's rows are, the pages of the next tiles' rows.
   static constexpr int VALUES = STAGES * BYTES, WHERE = 2 * VALUES, PAGES = WHERE + 512, AHEAD = 2 * STAGES + 1;
   static constexpr int WAVE = (PAGES + AHEAD * 256 + 1023) / 1024 * 1024, LDS = WAVES * WAVE;
@@ -130,7 +136,7 @@ __device__ __forceinline__ float over_lanes(float x, F f) {
 // DP columns of a row in LDS, of which the first COLS take part.  The loops that only move data stay rolled up: a launch this short waits for its code
 // as well as for its data (of 34 KB, 20 us before the first tile was done).
 template <typename T, int DP, int COLS, int R, bool PAGED>
-__global__ __launch_bounds__(64 * WAVES, 1) void stream_kernel(StreamArgs a) {
+__global__ __launch_bounds__(64 * WAVES, (Stream<T, DP, R>::PER_CU)) void stream_kernel(StreamArgs a) {
   typedef Stream<T, DP, R> F;
   typedef typename F::Tile Tile;
   typedef Few<T, R> C;
@@ -159,6 +165,8 @@ __global__ __launch_bounds__(64 * WAVES, 1) void stream_kernel(StreamArgs a) {
   }
   const uint32_t times = a.heads * a.row_tiles;
   const Shares shares(total * times, a.waves);
+  // Keys and values that the last-level cache (256 MB) has no room for are not kept by the others (537 MB 102 us, so 90; but 178 MB 35 and 36).
+  const bool once = a.row_tiles == 1 && (int64_t)shares.total * 2 * F::BYTES > 256 << 20;
   uint32_t at = shares.first(w);
   const uint32_t stop = shares.first(w + 1);
   if (at >= stop) return;
@@ -241,7 +249,10 @@ __global__ __launch_bounds__(64 * WAVES, 1) void stream_kernel(StreamArgs a) {
         }
 #pragma unroll
         for (int u = 0; u < U; ++u)
-          if (c[u] < width) load_lds16(src[u] + c[u], to + (p + u) * 1024);
+          if (c[u] < width) {
+            if (once) load_lds16_once(src[u] + c[u], to + (p + u) * 1024);
+            else load_lds16(src[u] + c[u], to + (p + u) * 1024);
+          }
       }
     };
     typename C::Acc o[DT];
@@ -353,10 +364,10 @@ __global__ __launch_bounds__(64 * WAVES, 1) void stream_kernel(StreamArgs a) {
   }
 }
 
-// One query of one head to a block: its parts, 256 / (DP / 4) of them at a time, added up in the order of the wavefronts.
-template <typename T, int DP>
-__global__ __launch_bounds__(256) void stream_join_kernel(StreamArgs a) {
-  constexpr int LANES = DP / 4, GROUPS = 256 / LANES;
+// One query of one head to a block: its parts, THREADS / (DP / 4) of them at a time, each thread's in the order of the wavefronts.
+template <typename T, int DP, int THREADS>
+__global__ __launch_bounds__(THREADS) void stream_join_kernel(StreamArgs a) {
+  constexpr int LANES = DP / 4, GROUPS = THREADS / LANES;
   __shared__ float4 sums[GROUPS][LANES];
   __shared__ float parts[GROUPS];
   const uint32_t id = blockIdx.x, bh = id / (uint32_t)a.S, query = id - bh * (uint32_t)a.S;   // (below 2^24)
@@ -425,13 +436,17 @@ StreamPlan stream_plan(int64_t B, int64_t S, int64_t q_heads, int64_t heads, int
 }
 
 template <typename T, int DP, int COLS, int R, bool PAGED>
-hipError_t launch(const StreamArgs& a, hipStream_t s) {
+hipError_t launch(StreamArgs a, hipStream_t s) {
   static std::atomic<uint64_t> allowed{0};
   typedef Stream<T, DP, R> F;
+  a.waves = 256 * F::PER_CU * WAVES;
   const hipError_t e = allow_lds(stream_kernel<T, DP, COLS, R, PAGED>, F::LDS, 0, allowed);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((stream_kernel<T, DP, COLS, R, PAGED>), dim3(BLOCKS), dim3(64 * WAVES), F::LDS, s, a);
-  hipLaunchKernelGGL((stream_join_kernel<T, DP>), dim3((unsigned)(a.B * a.S * a.q_heads)), dim3(256), 0, s, a);
+  hipLaunchKernelGGL((stream_kernel<T, DP, COLS, R, PAGED>), dim3(a.waves / WAVES), dim3(64 * WAVES), F::LDS, s, a);
+  // (few sequences and heads: many parts each.  One user's 131072 tokens, 8 heads, us of 128 / 512 threads: 11.1 / 6.4; 64 users, 4 heads 5.1 / 6.1)
+  const dim3 rows((unsigned)(a.B * a.S * a.q_heads));
+  if (a.B * a.heads * a.row_tiles <= 64) hipLaunchKernelGGL((stream_join_kernel<T, DP, 512>), rows, dim3(512), 0, s, a);
+  else hipLaunchKernelGGL((stream_join_kernel<T, DP, 128>), rows, dim3(128), 0, s, a);
   return hipGetLastError();
 }
 
@@ -445,7 +460,7 @@ size_t stream_bytes(int64_t B, int64_t S, int64_t q_heads, int64_t heads, int64_
 hipError_t launch_stream(StreamArgs a, int32_t dtype, void* workspace, hipStream_t s) {
   const StreamPlan p = stream_plan(a.B, a.S, a.q_heads, a.heads, a.D);
   char* ws = reinterpret_cast<char*>(workspace);
-  a.row_tile = p.row_tile; a.row_tiles = p.row_tiles; a.rows = p.rows; a.waves = BLOCKS * WAVES;
+  a.row_tile = p.row_tile; a.row_tiles = p.row_tiles; a.rows = p.rows;
   a.before = reinterpret_cast<uint32_t*>(ws + p.before);
   a.top_sum = reinterpret_cast<float*>(ws + p.top_sum);
   a.partial = reinterpret_cast<float*>(ws + p.partial);
