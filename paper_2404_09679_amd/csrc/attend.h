@@ -154,14 +154,48 @@ __device__ __forceinline__ void load_rows(const Rows& x, int64_t r0, int64_t end
   }
 }
 
+// use(i, read(i)) for i < N in order, with AHEAD fragments under way from LDS: left to itself the compiler asks for each one right before its product,
+// which then waits for LDS and not for the matrix core.  first: the first ones may be asked for earlier, by start().
+template <typename Fragment, int N, int AHEAD>
+struct Fragments {
+  Fragment f[AHEAD];
+  template <typename R>
+  __device__ __forceinline__ void start(R read) {
+#pragma unroll
+    for (int i = 0; i < AHEAD && i < N; ++i) f[i] = read(i);
+    __builtin_amdgcn_sched_barrier(ARITHMETIC);
+  }
+  template <typename R, typename U>
+  __device__ __forceinline__ void run(R read, U use) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      use(i, f[i % AHEAD]);
+      __builtin_amdgcn_sched_barrier(ARITHMETIC);
+      if (i + AHEAD < N) f[i % AHEAD] = read(i + AHEAD);
+      __builtin_amdgcn_sched_barrier(ARITHMETIC);
+    }
+  }
+  static constexpr int ARITHMETIC = 6;   // what may move: vector and scalar instructions
+};
+
 __device__ __forceinline__ f32x16 zeros() {
   f32x16 x;
 #pragma unroll
   for (int e = 0; e < 16; ++e) x[e] = 0.0f;
   return x;
 }
-// What the other half of the wavefront holds for the same column.
-__device__ __forceinline__ float other_half(float x) { return __shfl_xor(x, 32, 64); }
+// f of what both halves of the wavefront hold for the same column (v_permlane32_swap: no way through LDS).
+template <typename F>
+__device__ __forceinline__ float over_halves(float x, F f) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return f(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float max_of_halves(float x) {
+  return over_halves(x, [](float a, float b) { return fmaxf(a, b); });
+}
+__device__ __forceinline__ float sum_of_halves(float x) {
+  return over_halves(x, [](float a, float b) { return a + b; });
+}
 
 // 2^x and log2 by one instruction each (off by a unit in the last place).
 __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }

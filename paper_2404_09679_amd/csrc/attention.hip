@@ -64,6 +64,12 @@ struct Ring {
   __device__ __forceinline__ void done() { read = read == (STAGES - 1) * BYTES ? 0 : read + BYTES; }
 };
 
+// x where there are more than `row` rows left, else `other`.  Said to be unforeseeable, lest the choices are made for every tile and not for the last.
+__device__ __forceinline__ float where_left(int row, int left, float x, float other) {
+  x = row < left ? x : other;
+  asm volatile("" : "+v"(x));
+  return x;
+}
 // Block i of `units` x n: which unit, and which of its blocks.  Blocks of a unit (a head of one batch entry's keys, and who reads it) share an XCD (block
 // i runs on XCD i mod 8), whose L2 then has the rows they all read; neighbouring units are on different ones, so that a batch entry of long
 // sequences is everybody's work.  What is left of less than 8 units is spread over all.
@@ -78,13 +84,14 @@ __device__ __forceinline__ void place_of(int i, int units, int n, int& unit, int
 // How a kernel goes about its work.  DP columns of a row in LDS, the first COLS of which take part; TILE rows to a stage of the ring, STAGES of them.
 // A block's wavefronts have 32 rows of results each and share the tiles; SPLIT: they share 32 rows, every one has a part of the tiles, in a ring of its
 // own, and their sums are added up at the end (four times the blocks, each a quarter as long).
-template <typename T_, int DP_, int COLS_, int TILE_, int STAGES_, int WAVES_, bool SPLIT_, int PER_CU_>
+template <typename T_, int DP_, int COLS_, int TILE_, int STAGES_, int WAVES_, bool SPLIT_, int PER_CU_, int AHEAD_>
 struct Way {
   typedef T_ T;
   static constexpr int DP = DP_, COLS = COLS_, TILE = TILE_, STAGES = STAGES_, WAVES = WAVES_, PER_CU = PER_CU_, THREADS = 64 * WAVES;
   static constexpr bool SPLIT = SPLIT_;
   static constexpr int ROWS = SPLIT ? 32 : 32 * WAVES;       // of a block
-  static constexpr int STEPS = COLS / Core<T>::STEP, DT = COLS / 32;
+  static constexpr int STEPS = COLS / Core<T>::STEP, DT = COLS / 32, PACKS = 32 / Core<T>::STEP;
+  static constexpr int AHEAD = AHEAD_;
   typedef HeadTile<T, DP> Tile;
   typedef TileLoad<T, DP, TILE, SPLIT ? 64 : THREADS> Load;
   // Sums on their way to memory: a wavefront's, some columns at a time, or all of the block's
@@ -227,24 +234,28 @@ __global__ __launch_bounds__(W::THREADS, W::PER_CU) void cross_forward_kernel(Cr
     const uint32_t tk = Tile::along_at(tile0, lane), tv = Tile::down_at(tile0 + W::Load::BYTES, lane);
     f32x16 s[BT / 32];
 #pragma unroll
-    for (int j = 0; j < BT / 32; ++j) {
-      s[j] = zeros();
-#pragma unroll
-      for (int i = 0; i < W::STEPS; ++i) C::multiply(Tile::along(tk, 32 * j, i), q[i], s[j]);
-    }
+    for (int j = 0; j < BT / 32; ++j) s[j] = zeros();
+    auto key = [&](int i) { return Tile::along(tk, i / W::STEPS * 32, i % W::STEPS); };
+    Fragments<typename C::Fragment, BT / 32 * W::STEPS, W::AHEAD> keys;
+    keys.start(key);
+    keys.run(key, [&](int i, const typename C::Fragment& x) { C::multiply(x, q[i % W::STEPS], s[i / W::STEPS]); });
+    auto value = [&](int i) { return Tile::down(tv, i / (W::DT * W::PACKS) * 32, i / W::DT % W::PACKS, i % W::DT); };
+    Fragments<typename C::Fragment, BT / 32 * W::PACKS * W::DT, W::AHEAD> values;
+    values.start(value);   // (there when the probabilities are)
     if (t + BT > k_len) {
+      const int left = (int)(k_len - t) - 4 * half;
 #pragma unroll
       for (int j = 0; j < BT / 32; ++j)
 #pragma unroll
         for (int e = 0; e < 16; ++e)
-          if (t + 32 * j + 8 * (e >> 2) + 4 * half + (e & 3) >= k_len) s[j][e] = -INFINITY;
+          s[j][e] = where_left(32 * j + 8 * (e >> 2) + (e & 3), left, s[j][e], -INFINITY);
     }
     float top = -INFINITY;
 #pragma unroll
     for (int j = 0; j < BT / 32; ++j)
 #pragma unroll
       for (int e = 0; e < 16; ++e) top = fmaxf(top, s[j][e]);
-    top = fmaxf(top, other_half(top));
+    top = max_of_halves(top);
     // The sums are scaled anew only where a maximum grew by more than 2^8: until then p may exceed 1.
     if (__any(top > m && (top - m) * a.scale2 > 8.0f)) {
       const float now = fmaxf(m, top), f = m == -INFINITY ? 0.0f : exp2_((m - now) * a.scale2);
@@ -263,17 +274,14 @@ __global__ __launch_bounds__(W::THREADS, W::PER_CU) void cross_forward_kernel(Cr
         s[j][e] = exp2_(fmaf(s[j][e], a.scale2, -mc));
         l += s[j][e];
       }
-#pragma unroll
-    for (int j = 0; j < BT / 32; ++j)
-#pragma unroll
-      for (int i = 0; i < 32 / C::STEP; ++i) {
-        const typename C::Fragment p = C::pack(s[j], i);
-#pragma unroll
-        for (int d = 0; d < W::DT; ++d) C::multiply(Tile::down(tv, 32 * j, i, d), p, o[d]);
-      }
+    typename C::Fragment p;
+    values.run(value, [&](int i, const typename C::Fragment& x) {
+      if (i % W::DT == 0) p = C::pack(s[i / (W::DT * W::PACKS)], i / W::DT % W::PACKS);
+      C::multiply(x, p, o[i % W::DT]);
+    });
   }
   arrive<0, true>();   // (the buffers are free)
-  l += other_half(l);
+  l = sum_of_halves(l);
   const float top2 = m == -INFINITY ? 0.0f : m * a.scale2;
   if constexpr (W::SPLIT) {
     float* sums = reinterpret_cast<float*>(lds);
@@ -334,7 +342,7 @@ __global__ __launch_bounds__(W::THREADS, W::PER_CU) void cross_dq_kernel(CrossAr
   for (int i = 0; i < W::STEPS; ++i)
 #pragma unroll
     for (int e = 0; e < C::PER; ++e) delta = fmaf((float)q[i][e], (float)g[i][e], delta);
-  delta += other_half(delta);
+  delta = sum_of_halves(delta);
   const int64_t r = r0 + (lane & 31);
   const float sum = r < end ? a.stats[bh * a.S + r] : INFINITY;
   const bool one_tile = k_len <= BT, writes_d = r < end && lane < 32 && part == 0 && (!W::SPLIT || wave == 0);
@@ -371,16 +379,22 @@ __global__ __launch_bounds__(W::THREADS, W::PER_CU) void cross_dq_kernel(CrossAr
     // p and dP of keys 32 j .. of the tile
     auto scores = [&](int j, f32x16& s, f32x16& dp) {
       s = dp = zeros();
-#pragma unroll
-      for (int i = 0; i < W::STEPS; ++i) C::multiply(Tile::along(tk, 32 * j, i), q[i], s);
-#pragma unroll
-      for (int i = 0; i < W::STEPS; ++i) C::multiply(Tile::along(tv, 32 * j, i), g[i], dp);
+      auto row = [&](int i) { return Tile::along(i < W::STEPS ? tk : tv, 32 * j, i % W::STEPS); };
+      Fragments<typename C::Fragment, 2 * W::STEPS, W::AHEAD> rows;
+      rows.start(row);
+      rows.run(row, [&](int i, const typename C::Fragment& x) {
+        if (i < W::STEPS) C::multiply(x, q[i], s);
+        else C::multiply(x, g[i % W::STEPS], dp);
+      });
 #pragma unroll
       for (int e = 0; e < 16; ++e) s[e] = exp2_(fmaf(s[e], a.scale2, -sum));
       if (t + BT > k_len) {
+        const int left = (int)(k_len - t) - 32 * j - 4 * half;
 #pragma unroll
-        for (int e = 0; e < 16; ++e)
-          if (t + 32 * j + 8 * (e >> 2) + 4 * half + (e & 3) >= k_len) s[e] = dp[e] = 0.0f;
+        for (int e = 0; e < 16; ++e) {
+          s[e] = where_left(8 * (e >> 2) + (e & 3), left, s[e], 0.0f);
+          dp[e] = where_left(8 * (e >> 2) + (e & 3), left, dp[e], 0.0f);
+        }
       }
     };
     if (one_tile) {   // (a block's, or, SPLIT, the first wavefront's, in the last part)
@@ -391,7 +405,7 @@ __global__ __launch_bounds__(W::THREADS, W::PER_CU) void cross_dq_kernel(CrossAr
 #pragma unroll
         for (int e = 0; e < 16; ++e) delta = fmaf(s[e], dp[e], delta);
       }
-      delta += other_half(delta);
+      delta = sum_of_halves(delta);
       if (r < end && lane < 32) a.delta[bh * a.S + r] = delta;
       if (!wanted) break;   // (nothing is under way)
     }
@@ -399,14 +413,16 @@ __global__ __launch_bounds__(W::THREADS, W::PER_CU) void cross_dq_kernel(CrossAr
     for (int j = 0; j < BT / 32; ++j) {
       f32x16 s, dp;
       scores(j, s, dp);
+      auto column = [&](int i) { return Tile::down(kt, 32 * j, i / W::DT, i % W::DT); };
+      Fragments<typename C::Fragment, W::PACKS * W::DT, W::AHEAD> columns;
+      columns.start(column);
 #pragma unroll
       for (int e = 0; e < 16; ++e) s[e] *= dp[e] - delta;
-#pragma unroll
-      for (int i = 0; i < 32 / C::STEP; ++i) {
-        const typename C::Fragment ds = C::pack(s, i);
-#pragma unroll
-        for (int d = 0; d < W::DT; ++d) C::multiply(Tile::down(kt, 32 * j, i, d), ds, o[d]);
-      }
+      typename C::Fragment ds;
+      columns.run(column, [&](int i, const typename C::Fragment& x) {
+        if (i % W::DT == 0) ds = C::pack(s, i / W::DT);
+        C::multiply(x, ds, o[i % W::DT]);
+      });
     }
   }
   arrive<0, true>();
@@ -507,13 +523,20 @@ __global__ __launch_bounds__(W::THREADS, W::PER_CU) void cross_dkv_kernel(CrossA
 #pragma unroll UNROLL
     for (int j = 0; j < BR / 32; ++j) {
       f32x16 s = zeros(), dp = zeros();
-#pragma unroll
-      for (int n = 0; n < W::STEPS; ++n) C::multiply(Tile::along(tq, 32 * j, n), k[n], s);
-#pragma unroll
-      for (int n = 0; n < W::STEPS; ++n) {
-        if constexpr (HELD) C::multiply(Tile::along(tg, 32 * j, n), v[n], dp);
-        else C::multiply(Tile::along(tg, 32 * j, n), Tile::along(vt, 0, n), dp);
-      }
+      auto row = [&](int i) { return Tile::along(i < W::STEPS ? tq : tg, 32 * j, i % W::STEPS); };
+      Fragments<typename C::Fragment, 2 * W::STEPS, W::AHEAD> rows;
+      rows.start(row);
+      rows.run(row, [&](int i, const typename C::Fragment& x) {
+        if (i < W::STEPS) {
+          C::multiply(x, k[i], s);
+        } else {
+          if constexpr (HELD) C::multiply(x, v[i % W::STEPS], dp);
+          else C::multiply(x, Tile::along(vt, 0, i % W::STEPS), dp);
+        }
+      });
+      auto column = [&](int i) { return Tile::down(i & 1 ? qt : gt, 32 * j, i / (2 * W::DT), i / 2 % W::DT); };
+      Fragments<typename C::Fragment, 2 * W::PACKS * W::DT, W::AHEAD> columns;
+      columns.start(column);
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
         const int row = 64 * j + 8 * (e >> 2) + 4 * half + (e & 3);
@@ -521,19 +544,22 @@ __global__ __launch_bounds__(W::THREADS, W::PER_CU) void cross_dkv_kernel(CrossA
         dp[e] = s[e] * (dp[e] - sums[32 + row]);
       }
       if (now.r + BR > q_len) {
+        const int left = (int)(q_len - now.r) - 32 * j - 4 * half;
 #pragma unroll
-        for (int e = 0; e < 16; ++e)
-          if (now.r + 32 * j + 8 * (e >> 2) + 4 * half + (e & 3) >= q_len) s[e] = dp[e] = 0.0f;
-      }
-#pragma unroll
-      for (int n = 0; n < 32 / C::STEP; ++n) {
-        const typename C::Fragment p = C::pack(s, n), ds = C::pack(dp, n);
-#pragma unroll
-        for (int d = 0; d < W::DT; ++d) {
-          C::multiply(Tile::down(gt, 32 * j, n, d), p, ov[d]);
-          C::multiply(Tile::down(qt, 32 * j, n, d), ds, ok[d]);
+        for (int e = 0; e < 16; ++e) {
+          s[e] = where_left(8 * (e >> 2) + (e & 3), left, s[e], 0.0f);
+          dp[e] = where_left(8 * (e >> 2) + (e & 3), left, dp[e], 0.0f);
         }
       }
+      typename C::Fragment p, ds;
+      columns.run(column, [&](int i, const typename C::Fragment& x) {
+        if (i % (2 * W::DT) == 0) {
+          p = C::pack(s, i / (2 * W::DT));
+          ds = C::pack(dp, i / (2 * W::DT));
+        }
+        if (i & 1) C::multiply(x, ds, ok[i / 2 % W::DT]);
+        else C::multiply(x, p, ov[i / 2 % W::DT]);
+      });
     }
   }
   arrive<0, true>();
@@ -574,11 +600,11 @@ __global__ __launch_bounds__(256) void cross_join_kernel(JoinArgs a) {
 template <typename T, int DP>
 struct Ways {
   static constexpr int ROW = DP * sizeof(T);   // bytes
-  template <int COLS> using Keys = Way<T, DP, COLS, ROW == 512 ? 32 : 64, 2, 4, false, 2>;
-  template <int COLS> using KeysDq = Way<T, DP, COLS, ROW == 512 ? 32 : 64, 2, 4, false, ROW == 512 ? 1 : 2>;
-  template <int COLS> using Queries = Way<T, DP, COLS, ROW >= 256 ? 32 : 64, 2, 4, false, ROW == 512 ? 1 : 2>;
-  template <int COLS> using SplitKeys = Way<T, DP, COLS, 32, 2, ROW == 512 ? 2 : 4, true, ROW >= 256 ? 1 : 2>;
-  template <int COLS> using SplitQueries = Way<T, DP, COLS, 32, 2, 2, true, ROW >= 256 ? 1 : 2>;
+  template <int COLS> using Keys = Way<T, DP, COLS, ROW == 512 ? 32 : 64, 2, 4, false, 2, 4>;
+  template <int COLS> using KeysDq = Way<T, DP, COLS, ROW == 512 ? 32 : 64, 2, 4, false, ROW == 512 ? 1 : 2, 4>;
+  template <int COLS> using Queries = Way<T, DP, COLS, ROW >= 256 ? 32 : 64, 2, 4, false, ROW == 512 ? 1 : 2, 4>;
+  template <int COLS> using SplitKeys = Way<T, DP, COLS, 32, 2, ROW == 512 ? 2 : 4, true, ROW >= 256 ? 1 : 2, 4>;
+  template <int COLS> using SplitQueries = Way<T, DP, COLS, 32, 2, 2, true, ROW >= 256 ? 1 : 2, 4>;
   static constexpr bool HELD = !(sizeof(T) == 2 && DP == 128);
 };
 struct Plan {

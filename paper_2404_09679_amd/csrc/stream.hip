@@ -128,7 +128,7 @@ struct Stream {
 // Over the lanes of a query.
 template <int R, typename F>
 __device__ __forceinline__ float over_lanes(float x, F f) {
-  x = f(x, __shfl_xor(x, 32, 64));
+  x = over_halves(x, f);
   if (R == 16) x = f(x, __shfl_xor(x, 16, 64));
   return x;
 }
