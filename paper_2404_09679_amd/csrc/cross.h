@@ -1,0 +1,281 @@
+// Attention of queries over keys and values of another length, and its backward pass.
+//
+// With scores z = scale q k^T over the keys that there are, p = softmax(z), out = p v.  Forward: one pass over the keys with the running maximum m and
+// sum l of a row's softmax; a sum of values under an older maximum is scaled by 2^(old - new).  Kept for the backward pass: L = log2 of the sum of
+// 2^(z log2 e), so that p = 2^(z log2 e - L) again.  With g the gradient of out and d = sum of g out over a row's columns:
+//   dP = g v^T,  dZ = p (dP - d),  dQ = scale dZ k,  dK = scale dZ^T q,  dV = p^T g,
+// dQ in blocks of queries and dK, dV in blocks of keys: each forms p and dP anew (14 products for the 10 there are), and every sum has one order.
+// Of bf16 heads p and dZ are rounded to bf16 as the matrix cores' operands.
+#pragma once
+
+#include "attend.h"
+
+namespace antdt {
+
+// How rows of results are shared out: `tiles` blocks of rows to a head, each by `parts` blocks, whose sums go through
+// partial [parts, heads, rows, D] (of keys and values [parts, 2, ...]).
+struct Share {
+  int32_t tiles, parts, blocks;
+  float* partial;
+};
+struct CrossArgs {
+  HeadsArg q, k, v, out, dout, dq, dk, dv;
+  const int32_t* q_lengths;
+  const int32_t* k_lengths;
+  float* stats;        // L [B, q_heads, S], +infinity for a row without keys: its p come out 0
+  float* delta;        // d, the same shape
+  int64_t S, T;
+  int32_t q_heads, heads, group, D;
+  int32_t units;       // heads of all batch entries' keys
+  float scale, scale2;   // scale2: scale log2 e
+  Share queries, keys;   // blocks of queries, and (backward) of keys
+};
+
+// Own loads but the last N have arrived and own reads of LDS are done; BLOCK: then everybody's.
+template <int N, bool BLOCK>
+__device__ __forceinline__ void arrive() {
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N) : "memory");
+  __builtin_amdgcn_sched_barrier(0);
+  if (BLOCK) block_barrier();
+}
+// Tiles through a ring of STAGES buffers in LDS, LOADS of a wavefront each: while one is worked on, the next STAGES - 1 are under way.  The ring is the
+// block's, or (not BLOCK) a wavefront's own.
+template <int STAGES, int LOADS, int BYTES, bool BLOCK>
+struct Ring {
+  uint32_t fill = 0, read = 0;   // bytes from the ring's start: the next buffer to fill, the one to read
+  int64_t left;                  // tiles not asked for yet
+  int32_t behind = 0;            // tiles asked for and not worked on
+  __device__ __forceinline__ explicit Ring(int64_t tiles) : left(tiles) {}
+  template <typename F>
+  __device__ __forceinline__ void ask(F issue) {
+    if (left <= 0) return;
+    issue(fill);
+    fill = fill == (STAGES - 1) * BYTES ? 0 : fill + BYTES;
+    --left;
+    ++behind;
+  }
+  template <typename F>
+  __device__ __forceinline__ void start(F issue) {
+#pragma unroll
+    for (int i = 0; i < STAGES - 1; ++i) ask(issue);
+  }
+  // The next tile is in LDS, and the buffer of the one before is asked for again.
+  template <typename F>
+  __device__ __forceinline__ void next(F issue) {
+    if (behind == STAGES - 1) arrive<(STAGES - 2) * LOADS, BLOCK>();
+    else arrive<0, BLOCK>();
+    --behind;
+    ask(issue);
+  }
+  __device__ __forceinline__ void done() { read = read == (STAGES - 1) * BYTES ? 0 : read + BYTES; }
+};
+
+// x where there are more than `row` rows left, else `other`.  Said to be unforeseeable, lest the choices are made for every tile and not for the last.
+__device__ __forceinline__ float where_left(int row, int left, float x, float other) {
+  x = row < left ? x : other;
+  asm volatile("" : "+v"(x));
+  return x;
+}
+// Block i of `units` x n: which unit, and which of its blocks.  Blocks of a unit (a head of one batch entry's keys, and who reads it) share an XCD (block
+// i runs on XCD i mod 8), whose L2 then has the rows they all read; neighbouring units are on different ones, so that a batch entry of long
+// sequences is everybody's work.  What is left of less than 8 units is spread over all.
+__device__ __forceinline__ void place_of(int i, int units, int n, int& unit, int& block) {
+  const int whole = (units & ~7) * n;
+  const int x = i < whole ? i & 7 : 0, j = i < whole ? i >> 3 : i - whole;
+  const int u = j / n;
+  block = j - u * n;
+  unit = i < whole ? 8 * u + x : (units & ~7) + u;
+}
+
+// How a kernel goes about its work.  DP columns of a row in LDS, the first COLS of which take part; TILE rows to a stage of the ring, STAGES of them.
+// A block's wavefronts have 32 rows of results each and share the tiles; SPLIT: they share 32 rows, every one has a part of the tiles, in a ring of its
+// own, and their sums are added up at the end (four times the blocks, each a quarter as long).
+template <typename T_, int DP_, int COLS_, int TILE_, int STAGES_, int WAVES_, bool SPLIT_, int PER_CU_, int AHEAD_>
+struct Way {
+  typedef T_ T;
+  static constexpr int DP = DP_, COLS = COLS_, TILE = TILE_, STAGES = STAGES_, WAVES = WAVES_, PER_CU = PER_CU_, THREADS = 64 * WAVES;
+  static constexpr bool SPLIT = SPLIT_;
+  static constexpr int ROWS = SPLIT ? 32 : 32 * WAVES;       // of a block
+  static constexpr int STEPS = COLS / Core<T>::STEP, DT = COLS / 32, PACKS = 32 / Core<T>::STEP;
+  static constexpr int AHEAD = AHEAD_;
+  typedef HeadTile<T, DP> Tile;
+  typedef TileLoad<T, DP, TILE, SPLIT ? 64 : THREADS> Load;
+  // Sums on their way to memory: a wavefront's, some columns at a time, or all of the block's
+  static constexpr int TN = COLS % 64 ? 1 : 2, STAGING = 32 * (32 * TN + 4) * 4;
+  static constexpr int PITCH = COLS + 4, MERGE = SPLIT ? WAVES * 32 * (PITCH + 2) * 4 : WAVES * STAGING;
+  static constexpr int lds(int ring) { return ring > MERGE ? ring : MERGE; }
+};
+// A lane's row and columns of 32 x COLS sums: row lane % 32, columns 32 d + 8 (e / 4) + 4 (lane / 32) + e % 4.
+template <typename W>
+using Sums = f32x16[W::DT];
+
+template <typename W>
+__device__ __forceinline__ void clear_sums(Sums<W>& x) {
+#pragma unroll
+  for (int d = 0; d < W::DT; ++d) x[d] = zeros();
+}
+// f x, rows r0 .. of `to` that lie before `end`.  (A wavefront's own rows.)
+template <typename W, typename TO>
+__device__ __forceinline__ void write_rows(char* staging, const Sums<W>& x, float f, const Rows& to, int64_t r0, int64_t end, int D, int lane) {
+  const int left = (int)max(min(end - r0, (int64_t)32), (int64_t)0);
+  TO* p = reinterpret_cast<TO*>(const_cast<char*>(to.p + r0 * to.ld));
+#pragma unroll
+  for (int i = 0; i < W::DT; i += W::TN) {
+    f32x16 y[W::TN];
+#pragma unroll
+    for (int j = 0; j < W::TN; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) y[j][e] = x[i + j][e] * f;
+    store_rows<TO, W::TN, true>(reinterpret_cast<float*>(staging), y, p + 32 * i, to.ld / (int64_t)sizeof(TO), left, D - 32 * i, lane);
+  }
+}
+// The wavefronts' sums of the same 32 rows to LDS, with a maximum and a sum of each row; then, wavefront by wavefront, added up with factors f(w).
+template <typename W>
+__device__ __forceinline__ void put_sums(float* lds, const Sums<W>& x, float m, float l, int wave, int lane) {
+  float* to = lds + (wave * 32 + (lane & 31)) * W::PITCH + 4 * (lane >> 5);
+#pragma unroll
+  for (int d = 0; d < W::DT; ++d)
+#pragma unroll
+    for (int v = 0; v < 4; ++v) *reinterpret_cast<float4*>(to + 32 * d + 8 * v) = make_float4(x[d][4 * v], x[d][4 * v + 1], x[d][4 * v + 2], x[d][4 * v + 3]);
+  if (lane < 32) *reinterpret_cast<float2*>(lds + W::WAVES * 32 * W::PITCH + (wave * 32 + lane) * 2) = make_float2(m, l);
+}
+template <typename W, typename TO>
+__device__ __forceinline__ void write_merged(const float* lds, const float (&f)[W::WAVES], const Rows& to, int64_t r0, int64_t end, int D) {
+  constexpr int LANES = W::THREADS / 32;   // of a row
+  const int row = threadIdx.x / LANES;
+  if (r0 + row >= end) return;
+  TO* p = reinterpret_cast<TO*>(const_cast<char*>(to.p + (r0 + row) * to.ld));
+  for (int c = threadIdx.x % LANES * 4; c < D; c += LANES * 4) {
+    float x[4] = {};
+#pragma unroll
+    for (int w = 0; w < W::WAVES; ++w) {
+      const float4 y = *reinterpret_cast<const float4*>(lds + (w * 32 + row) * W::PITCH + c);
+      x[0] = fmaf(y.x, f[w], x[0]); x[1] = fmaf(y.y, f[w], x[1]); x[2] = fmaf(y.z, f[w], x[2]); x[3] = fmaf(y.w, f[w], x[3]);
+    }
+    if constexpr (sizeof(TO) == 4) *reinterpret_cast<float4*>(p + c) = make_float4(x[0], x[1], x[2], x[3]);
+    else *reinterpret_cast<uint2*>(p + c) = make_uint2(f2bf2(x[0], x[1]), f2bf2(x[2], x[3]));
+  }
+}
+// Zeros to rows [r0, r1) of a head, by a block of that many threads.
+template <typename T>
+__device__ __forceinline__ void clear_rows(const Rows& to, int64_t r0, int64_t r1, int D, int threads) {
+  const int per = D / Core<T>::PER;
+  for (int64_t i = threadIdx.x; i < (r1 - r0) * per; i += threads)
+    store16<false>(const_cast<char*>(to.p + (r0 + i / per) * to.ld + i % per * 16), make_uint4(0, 0, 0, 0));
+}
+// Sums to their results, or to a part's sums in the workspace.
+template <typename W>
+__device__ __forceinline__ void write_result(char* lds, const Sums<W>& x, float f, const Rows& to, float* part, int64_t r0, int64_t end, int D, int wave, int lane) {
+  const Rows parts = {reinterpret_cast<const char*>(part), (int64_t)D * 4};
+  if constexpr (W::SPLIT) {
+    float* sums = reinterpret_cast<float*>(lds);
+    put_sums<W>(sums, x, 0.0f, 0.0f, wave, lane);
+    __syncthreads();
+    float g[W::WAVES];
+#pragma unroll
+    for (int w = 0; w < W::WAVES; ++w) g[w] = f;
+    if (part) write_merged<W, float>(sums, g, parts, r0, end, D);
+    else write_merged<W, typename W::T>(sums, g, to, r0, end, D);
+    __syncthreads();
+  } else {
+    if (part) write_rows<W, float>(lds + wave * W::STAGING, x, f, parts, r0, end, D, lane);
+    else write_rows<W, typename W::T>(lds + wave * W::STAGING, x, f, to, r0, end, D, lane);
+  }
+}
+
+// Tiles of keys and values go through LDS.
+template <typename W>
+struct KeyTiles {
+  static constexpr int STAGE = 2 * W::Load::BYTES, RING = W::STAGES * STAGE, ALL = W::SPLIT ? W::WAVES * RING : RING, LDS = W::lds(ALL);
+  typedef antdt::Ring<W::STAGES, 2 * W::Load::PIECES, STAGE, !W::SPLIT> Ring;
+};
+// ------------------------------------------------------------- which way
+template <typename T, int DP>
+struct Ways {
+  static constexpr int ROW = DP * sizeof(T);   // bytes
+  template <int COLS> using Keys = Way<T, DP, COLS, ROW == 512 ? 32 : 64, 2, 4, false, 2, 4>;
+  template <int COLS> using KeysDq = Way<T, DP, COLS, ROW == 512 ? 32 : 64, 2, 4, false, ROW == 512 ? 1 : 2, 4>;
+  template <int COLS> using Queries = Way<T, DP, COLS, ROW >= 256 ? 32 : 64, 2, 4, false, ROW == 512 ? 1 : 2, 4>;
+  template <int COLS> using SplitKeys = Way<T, DP, COLS, 32, 2, ROW == 512 ? 2 : 4, true, ROW >= 256 ? 1 : 2, 4>;
+  template <int COLS> using SplitQueries = Way<T, DP, COLS, 32, 2, ROW == 512 ? 2 : 4, true, ROW >= 256 ? 1 : 2, 4>;
+  static constexpr bool HELD = !(sizeof(T) == 2 && DP == 128);
+};
+// go(Ways<T, DP>, COLS)
+template <typename F>
+hipError_t by_columns(int32_t dtype, int D, F go) {
+  return by_size(dtype, D, [&](auto t, auto dp) {
+    constexpr int DP = decltype(dp)::value;
+    typedef Ways<decltype(t), DP> Z;
+    if constexpr (DP == 128) {
+      if (D <= 96) return go(Z(), std::integral_constant<int, 96>());
+    }
+    return go(Z(), dp);
+  });
+}
+
+struct Plan {
+  bool split;
+  int32_t tiles, parts;
+  int64_t blocks;
+  Share share(float* partial) const { return Share{tiles, parts, (int32_t)blocks, partial}; }
+};
+struct Shape {
+  int64_t B, S, T, q_heads, heads, D;
+  int32_t dtype;
+};
+// Microseconds that a wavefront takes for 32 queries and 32 keys in the forward pass, alone on its SIMD (measured; of a multiple of 32 columns).
+inline double tile_us(const Shape& z) {
+  const int columns = (int)div_up(z.D, 32) - 1;
+  constexpr double BF16[] = {0.6, 0.9, 1.3, 1.6}, F32[] = {1.7, 3.1, 4.3, 5.5};
+  return z.dtype == ANTDT_F32 ? F32[columns] : BF16[columns];
+}
+// Results' rows in blocks of 128, or of 32 whose `waves` wavefronts share the other side's rows (`tiles` of 32), or these again in parts.
+//  - Blocks of 32 as long as all of them run at once: `most` of them.  bf16, 1024 queries and keys, 64 columns, us of blocks of 128 / 32: 16 heads 22 / 15,
+//    32 heads 23.5 / 28; gradient of the queries 27 / 19, 28 / 32; 128 columns, gradient of the keys: 16 heads 57 / 44, 32 heads 62 / 90.
+//  - Parts where their shorter way outweighs the launch that adds them up, about 6 us.
+inline Plan cross_plan(int64_t heads, int64_t rows, int64_t tiles, int64_t most, int waves, double us, bool parted) {
+  Plan p = {false, (int32_t)div_up(rows, 128), 1, 0};
+  p.blocks = heads * p.tiles;
+  const int64_t split = heads * div_up(rows, 32);
+  if (split == 0 || split > most || tiles < 2) return p;
+  p.split = true;
+  p.tiles = (int32_t)div_up(rows, 32);
+  p.blocks = split;
+  const int64_t parts = std::min<int64_t>(256 / split, tiles / (2 * waves));
+  if (parted && parts > 1 && us * tiles / waves * (1.0 - 1.0 / parts) > 6.0) {
+    p.parts = (int32_t)parts;
+    p.blocks *= parts;
+  }
+  return p;
+}
+inline int64_t delta_bytes(const Shape& z) { return div_up(z.B * z.S * z.q_heads * 4, 256) * 256; }
+inline bool wide(const Shape& z) { return z.dtype == ANTDT_BF16 && z.D > 64; }          // (a block of 32 fills a compute unit's LDS)
+inline int key_waves(const Shape& z) { return z.dtype == ANTDT_F32 && z.D > 64 ? 2 : 4; }
+inline Plan forward_plan(const Shape& z) { return cross_plan(z.B * z.q_heads, z.S, div_up(z.T, 32), wide(z) ? 256 : 512, key_waves(z), tile_us(z), false); }
+inline Plan dq_plan(const Shape& z) { return cross_plan(z.B * z.q_heads, z.S, div_up(z.T, 32), wide(z) ? 256 : 512, key_waves(z), 1.3 * tile_us(z), true); }
+inline Plan dkv_plan(const Shape& z) { return cross_plan(z.B * z.heads, z.T, div_up(z.S, 32) * (z.q_heads / z.heads), wide(z) ? 256 : 512, key_waves(z), 2.0 * tile_us(z), true); }
+// Whether the forward pass goes by an equal share of all keys to each wavefront (stream.hip) instead, by the time that both would take: that costs a
+// second launch, about 9 us, and the tiles of 32 keys and 16 or 32 queries of a key's heads take 1.4 times as long.  us by blocks / shares, 8 heads of
+// 64 bf16 columns: 1 query, 500 keys 8 / 16, 2000 19 / 15, 8000 61 / 16; 4 x 128 queries, 2000 keys 20 / 31, 8000 75 / 64; fp32, 1 query, 500 keys 16 / 14.
+inline bool cross_streams(const Shape& z) {
+  if (z.B == 0 || z.S == 0 || !stream_fits(z.B, z.S, z.T, z.q_heads, z.heads)) return false;
+  const int64_t tiles = div_up(z.T, 32), rows = z.S * (z.q_heads / z.heads), row_tiles = rows <= 16 ? 1 : div_up(rows, 32);
+  const Plan p = forward_plan(z);
+  const double blocks = p.split ? (double)div_up(tiles, key_waves(z)) : std::max(1.0, p.blocks / 512.0) * tiles * 1.1;
+  return 9.0 + 1.4 * tile_us(z) * z.B * z.heads * row_tiles * tiles / 1024 < tile_us(z) * blocks;
+}
+inline int cross_sizes(const char* call, const Shape& z) {
+  OP_TRY(op_head_sizes(call, z.q_heads, z.heads, z.D, z.dtype));
+  constexpr int64_t MOST = (1ll << 31) - 1;
+  if (z.B < 0 || z.B >= MOST) return op_fail(ANTDT_INVALID_ARG, "%s: B out of range", call);
+  if (z.S < 0 || z.S >= MOST) return op_fail(ANTDT_INVALID_ARG, "%s: S out of range", call);
+  if (z.T < 0 || z.T >= MOST) return op_fail(ANTDT_INVALID_ARG, "%s: T out of range", call);
+  const int64_t longest = div_up(std::max(z.S, z.T), 128);
+  if ((__int128)z.B * z.q_heads * longest >= 1 << 24) return op_fail(ANTDT_UNSUPPORTED, "%s: B q_heads and the longer of S and T in 128s: 2^24 or more blocks", call);
+  return ANTDT_OK;
+}
+inline int cross_lengths(const char* call, const int32_t* q_lengths, const int32_t* k_lengths) {
+  if ((reinterpret_cast<uintptr_t>(q_lengths) | reinterpret_cast<uintptr_t>(k_lengths)) & 3) return op_fail(ANTDT_INVALID_ARG, "%s: lengths are misaligned", call);
+  return ANTDT_OK;
+}
+}  // namespace antdt
