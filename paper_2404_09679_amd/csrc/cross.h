@@ -193,12 +193,12 @@ struct KeyTiles {
 template <typename T, int DP>
 struct Ways {
   static constexpr int ROW = DP * sizeof(T);   // bytes
+  static constexpr bool HELD = !(sizeof(T) == 2 && DP == 128);   // (see QueryTiles; nor are there registers for fragments ahead)
   template <int COLS> using Keys = Way<T, DP, COLS, ROW == 512 ? 32 : 64, 2, 4, false, 2, 4>;
   template <int COLS> using KeysDq = Way<T, DP, COLS, ROW == 512 ? 32 : 64, 2, 4, false, ROW == 512 ? 1 : 2, 4>;
-  template <int COLS> using Queries = Way<T, DP, COLS, ROW >= 256 ? 32 : 64, 2, 4, false, ROW == 512 ? 1 : 2, 4>;
+  template <int COLS> using Queries = Way<T, DP, COLS, ROW >= 256 ? 32 : 64, 2, 4, false, ROW == 512 ? 1 : 2, HELD ? 4 : 1>;
   template <int COLS> using SplitKeys = Way<T, DP, COLS, 32, 2, ROW == 512 ? 2 : 4, true, ROW >= 256 ? 1 : 2, 4>;
   template <int COLS> using SplitQueries = Way<T, DP, COLS, 32, 2, ROW == 512 ? 2 : 4, true, ROW >= 256 ? 1 : 2, 4>;
-  static constexpr bool HELD = !(sizeof(T) == 2 && DP == 128);
 };
 // go(Ways<T, DP>, COLS)
 template <typename F>
