@@ -507,7 +507,8 @@ int antdt_token_logprobs_gradient(const void* logits, int64_t ld, int64_t N, int
  *    are never read into a result, whatever they hold, and are zeros in one.
  *  - attention: D a multiple of 8, at most ANTDT_MAX_ATTENTION_DIM, heads that start at multiples of 16 bytes (ANTDT_UNSUPPORTED otherwise).  Scores, the
  *    softmax and sums are fp32.  Of bf16 heads the probabilities, and in the backward pass the scores' gradients, are rounded to bf16 as the matrix cores'
- *    operands.  A query without keys, or all of whose scores are -infinity, has zeros and passes no gradient.
+ *    operands.  A query without keys, or all of whose scores are -infinity, has zeros and passes no gradient; one
+ *    with a score of NaN, +infinity or beyond fp32's range has NaN.
  */
 #define ANTDT_MAX_HEAD_DIM 256
 #define ANTDT_MAX_ATTENTION_DIM 128

@@ -35,25 +35,18 @@ class Rotary:
 
 def _first(t: torch.Tensor, name: str, dims: int) -> Tuple[torch.dtype, int]:
     """(dtype, device) of a call's first heads."""
-    if len(t.shape) != dims or t.dtype not in _DTYPES:
-        raise ValueError(f"{name}: {dims} dimensions of float32 or bfloat16, not {tuple(t.shape)} of {t.dtype}")
     device = t.get_device()
-    if device < 0:
-        raise ValueError(f"{name}: not on the device")
+    if len(t.shape) != dims or t.dtype not in _DTYPES or device < 0:
+        raise ValueError(f"{name}: {dims} dimensions of float32 or bfloat16 on the device, not {tuple(t.shape)} of {t.dtype} on {t.device}")
     return t.dtype, device
 
 
 def _heads(t: torch.Tensor, name: str, shape: Tuple[int, ...], dtype: torch.dtype, device: int) -> Tuple[int, ...]:
     """Strides of a heads argument but its columns', after the checks that the C boundary cannot make."""
-    if t.shape != shape:
-        raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {tuple(shape)}")
-    if t.dtype is not dtype:
-        raise ValueError(f"{name}: {t.dtype}, expected {dtype}")
-    if t.get_device() != device:
-        raise ValueError(f"{name}: on {t.device}, expected device {device}")
     s = t.stride()
-    if s[-1] != 1 and shape[-1] > 1:
-        raise ValueError(f"{name}: columns of a head must be neighbours")
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != device or (s[-1] != 1 and shape[-1] > 1):
+        raise ValueError(f"{name}: heads of neighbouring columns, {tuple(shape)} of {dtype} on device {device}, not {tuple(t.shape)} "
+                         f"(strides {s}) of {t.dtype} on {t.device}")
     return s[:-1]
 
 

@@ -106,7 +106,7 @@ __global__ __launch_bounds__(W::THREADS, W::PER_CU) void cross_forward_kernel(Cr
   const float top2 = m == -INFINITY ? 0.0f : m * a.scale2;
   if constexpr (W::SPLIT) {
     float* sums = reinterpret_cast<float*>(lds);
-    put_sums<W>(sums, o, l == 0.0f ? -INFINITY : top2, l, wave, lane);
+    put_sums<W>(sums, o, m == -INFINITY ? -INFINITY : top2, l, wave, lane);
     __syncthreads();
     const int row = threadIdx.x / (W::THREADS / 32);
     const float2* ml = reinterpret_cast<const float2*>(sums + W::WAVES * 32 * W::PITCH) + row;
@@ -121,13 +121,13 @@ __global__ __launch_bounds__(W::THREADS, W::PER_CU) void cross_forward_kernel(Cr
       l += ml[32 * w].y * f[w];
     }
 #pragma unroll
-    for (int w = 0; w < W::WAVES; ++w) f[w] *= l == 0.0f ? 0.0f : 1.0f / l;
+    for (int w = 0; w < W::WAVES; ++w) f[w] *= most == -INFINITY ? 0.0f : 1.0f / l;
     write_merged<W, T>(sums, f, out, first, end, a.D);
-    if (stats && threadIdx.x % (W::THREADS / 32) == 0 && first + row < end) stats[first + row] = l == 0.0f ? INFINITY : base + log2_(l);
+    if (stats && threadIdx.x % (W::THREADS / 32) == 0 && first + row < end) stats[first + row] = most == -INFINITY ? INFINITY : base + log2_(l);
   } else {
-    write_rows<W, T>(lds + wave * W::STAGING, o, l == 0.0f ? 0.0f : 1.0f / l, out, r0, end, a.D, lane);
+    write_rows<W, T>(lds + wave * W::STAGING, o, m == -INFINITY ? 0.0f : 1.0f / l, out, r0, end, a.D, lane);
     const int64_t r = r0 + (lane & 31);
-    if (stats && lane < 32 && r < end) stats[r] = l == 0.0f ? INFINITY : top2 + log2_(l);
+    if (stats && lane < 32 && r < end) stats[r] = m == -INFINITY ? INFINITY : top2 + log2_(l);
   }
 }
 

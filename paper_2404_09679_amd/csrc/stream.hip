@@ -343,9 +343,9 @@ __global__ __launch_bounds__(64 * WAVES, (Stream<T, DP, R>::PER_CU)) void stream
     const bool part = came || goes;
     const int64_t at_part = ((int64_t)w * 2 + (came ? 0 : 1)) * a.rows + lane % R;
     const bool stored = part ? lane % R < a.rows : query < a.S;
-    if (part && stored && group == 0) *reinterpret_cast<float2*>(a.top_sum + 2 * at_part) = make_float2(l == 0.0f ? -INFINITY : top2, l);
-    if (!part && stored && group == 0 && a.stats) a.stats[(b * a.q_heads + hq) * a.S + query] = l == 0.0f || !there ? INFINITY : top2 + log2_(l);
-    const float f = part ? 1.0f : l == 0.0f ? 0.0f : 1.0f / l;
+    if (part && stored && group == 0) *reinterpret_cast<float2*>(a.top_sum + 2 * at_part) = make_float2(m == -INFINITY ? -INFINITY : top2, l);
+    if (!part && stored && group == 0 && a.stats) a.stats[(b * a.q_heads + hq) * a.S + query] = m == -INFINITY || !there ? INFINITY : top2 + log2_(l);
+    const float f = part ? 1.0f : m == -INFINITY ? 0.0f : 1.0f / l;   // (scores beyond fp32: l is 0 or infinite, and NaN comes out)
     float* to_part = a.partial + at_part * DP;
     T* to = reinterpret_cast<T*>(reinterpret_cast<char*>(const_cast<void*>(a.out.p)) + b * a.out.s.b + query * a.out.s.l + hq * a.out.s.h);
 #pragma unroll
@@ -369,7 +369,7 @@ template <typename T, int DP, int THREADS>
 __global__ __launch_bounds__(THREADS) void stream_join_kernel(StreamArgs a) {
   constexpr int LANES = DP / 4, GROUPS = THREADS / LANES;
   __shared__ float4 sums[GROUPS][LANES];
-  __shared__ float parts[GROUPS];
+  __shared__ float2 parts[GROUPS];   // maximum and sum
   const uint32_t id = blockIdx.x, bh = id / (uint32_t)a.S, query = id - bh * (uint32_t)a.S;   // (below 2^24)
   const uint32_t b = bh / (uint32_t)a.q_heads, hq = bh - b * (uint32_t)a.q_heads, h = hq / (uint32_t)a.group, row = query * a.group + hq - h * a.group;
   const uint32_t n = a.before[b + 1] - a.before[b], times = a.heads * a.row_tiles;
@@ -383,38 +383,39 @@ __global__ __launch_bounds__(THREADS) void stream_join_kernel(StreamArgs a) {
     const int w0 = (int)shares.owner(begin), w1 = (int)shares.owner(begin + n - 1);
     if (w0 == w1) return;   // (written by that wavefront)
     auto slot = [&](int w) { return (int64_t)(w * 2 + (w == w0 ? 1 : 0)) * a.rows + row % a.row_tile; };
-    for (int w = w0 + (threadIdx.x & 63); w <= w1; w += 64) top = fmaxf(top, a.top_sum[2 * slot(w)]);
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
-    const float base = top == -INFINITY ? 0.0f : top;
 #pragma unroll 4
-    for (int w = w0 + group; w <= w1; w += GROUPS) {
+    for (int w = w0 + group; w <= w1; w += GROUPS) {   // (one pass: nothing waits for the maximum of all)
       const float2 ml = *reinterpret_cast<const float2*>(a.top_sum + 2 * slot(w));
       const float4 x = *reinterpret_cast<const float4*>(a.partial + slot(w) * DP + 4 * lane);
-      const float f = exp2_(ml.x - base);
-      // (a part without keys that are there: nothing, whatever its sums hold)
-      l += ml.y * f;
-      sum.x += x.x * f; sum.y += x.y * f; sum.z += x.z * f; sum.w += x.w * f;
+      const float now = fmaxf(top, ml.x), base = now == -INFINITY ? 0.0f : now, f = exp2_(top - base), g = exp2_(ml.x - base);
+      top = now;
+      l = l * f + ml.y * g;
+      sum.x = sum.x * f + x.x * g; sum.y = sum.y * f + x.y * g; sum.z = sum.z * f + x.z * g; sum.w = sum.w * f + x.w * g;
     }
   }
   sums[group][lane] = sum;
-  if (lane == 0) parts[group] = l;
+  if (lane == 0) parts[group] = make_float2(top, l);
   __syncthreads();
   if (group > 0) return;
   l = 0.0f;
   sum = make_float4(0, 0, 0, 0);
 #pragma unroll
+  for (int g = 0; g < GROUPS; ++g) top = fmaxf(top, parts[g].x);
+  const float base = top == -INFINITY ? 0.0f : top;
+#pragma unroll
   for (int g = 0; g < GROUPS; ++g) {
-    l += parts[g];
-    sum.x += sums[g][lane].x; sum.y += sums[g][lane].y; sum.z += sums[g][lane].z; sum.w += sums[g][lane].w;
+    const float f = exp2_(parts[g].x - base);
+    const float4 x = sums[g][lane];
+    l += parts[g].y * f;
+    sum.x += x.x * f; sum.y += x.y * f; sum.z += x.z * f; sum.w += x.w * f;
   }
-  const float f = l == 0.0f ? 0.0f : 1.0f / l;
+  const float f = top == -INFINITY ? 0.0f : 1.0f / l;
   if (4 * lane < a.D) {
     char* to = reinterpret_cast<char*>(const_cast<void*>(a.out.p)) + b * a.out.s.b + query * a.out.s.l + hq * a.out.s.h;
     if constexpr (sizeof(T) == 4) *reinterpret_cast<float4*>(to + 16 * lane) = make_float4(sum.x * f, sum.y * f, sum.z * f, sum.w * f);
     else *reinterpret_cast<uint2*>(to + 8 * lane) = make_uint2(f2bf2(sum.x * f, sum.y * f), f2bf2(sum.z * f, sum.w * f));
   }
-  if (a.stats && lane == 0) a.stats[(int64_t)bh * a.S + query] = l == 0.0f ? INFINITY : top + log2_(l);
+  if (a.stats && lane == 0) a.stats[(int64_t)bh * a.S + query] = top == -INFINITY ? INFINITY : top + log2_(l);
 }
 
 struct StreamPlan {

@@ -146,6 +146,21 @@ def test_cross_attention_refusals(dtype):
     assert fwd(S=0, q=None, out=None) == OK and bwd(dq=None, dk=None, dv=None) == OK
 
 
+def test_sizes_of_workspaces():
+    """Whatever the sizes, also none at all."""
+    rng, n = np.random.default_rng(1), C.c_size_t()
+    for _ in range(4000):
+        B, S, T_ = (int(10 ** rng.uniform(0, 4)) * int(rng.random() > 0.1) for _ in range(3))
+        H, D, dtype = int(rng.integers(1, 9)), 8 * int(rng.integers(1, 17)), int(rng.integers(0, 2))
+        HQ = H * int(rng.integers(1, 9))
+        for f in (lib.antdt_cross_attention_bytes, lib.antdt_cross_attention_backward_bytes):
+            rc = f(B, S, T_, HQ, H, D, dtype, C.byref(n))
+            assert rc == OK or (rc == UNSUPPORTED and B * HQ * (max(S, T_) / 128 + 1) >= 1 << 24), (B, S, T_, HQ, H, D, message())
+            # d of the rows, or two parts of 32 rows of 128 columns, a maximum and a sum for each of 2048 wavefronts, and a word for each sequence
+            assert rc or n.value <= 4 * B * S * HQ + 2048 * 2 * 32 * (128 * 4 + 8) + 4 * B + 512
+    assert lib.antdt_cross_attention_bytes(0, 0, 0, 1, 1, 8, 0, C.byref(n)) == OK and n.value == 0
+
+
 def test_formulas_against_differences():
     rng = np.random.default_rng(3)
     q, k, v, g = rng.normal(size=(4, 6)), rng.normal(size=(9, 6)), rng.normal(size=(9, 6)), rng.normal(size=(4, 6))
