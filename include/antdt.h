@@ -503,12 +503,14 @@ int antdt_token_logprobs_gradient(const void* logits, int64_t ld, int64_t N, int
  *    row to the next, `ld..._head` from one head to the next, `ld..._batch`; of what there is one of the stride means nothing).  The elements of
  *    a result must not share memory; an operand's stride may be 0, which repeats it.
  *  - heads <= q_heads, q_heads a multiple of heads: head h of the queries belongs to head h / (q_heads / heads) of keys and values.
+ *  - results share no memory with operands unless a call says so.
  *  - lengths: DEVICE int32 [B], of a sequence's rows; what lies outside 0 .. the size is taken as the nearer end.  Rows behind a length
  *    are never read into a result, whatever they hold, and are zeros in one.
  *  - attention: D a multiple of 8, at most ANTDT_MAX_ATTENTION_DIM, heads that start at multiples of 16 bytes (ANTDT_UNSUPPORTED otherwise).  Scores, the
  *    softmax and sums are fp32.  Of bf16 heads the probabilities, and in the backward pass the scores' gradients, are rounded to bf16 as the matrix cores'
- *    operands.  A query without keys, or all of whose scores are -infinity, has zeros and passes no gradient; one
- *    with a score of NaN, +infinity or beyond fp32's range has NaN.
+ *    operands.  scale is 1e-30 or more (finite times log2(e)).  A query without keys has zeros and passes no gradient.  So has one all of whose scores
+ *    are -infinity (but infinite operands times its scores' gradients, which are zeros, are NaN); one with a score of NaN, +infinity or beyond fp32's range
+ *    has NaN.
  */
 #define ANTDT_MAX_HEAD_DIM 256
 #define ANTDT_MAX_ATTENTION_DIM 128
@@ -536,7 +538,7 @@ int antdt_rotary(const void* x, int64_t ldx, int64_t ldx_head, int64_t N, int64_
 /*
  * A paged cache: k_cache and v_cache, DEVICE [pages, page_size, heads, D] (the same strides both), and table, DEVICE int32 [B, table_cols]: tokens
  * i page_size .. of sequence b are the rows of page table[b, i].  A page outside 0 .. pages - 1 is none: what belongs there is not kept, and
- * not there to be read.  pages, page_size, table_cols < 2^31 - 1.
+ * not there to be read.  pages, page_size, table_cols < 2^31.
  *
  * Appends k and v (DEVICE [N, heads, D]) of new tokens, k turned by their positions when `rotary` (HOST) is given.  Sequence b's new tokens are
  * n = offsets[b] .. offsets[b + 1] - 1 (DEVICE int32 [B + 1], ascending), or, offsets NULL, n = b.  lengths (DEVICE int32 [B]) count them in: the last
@@ -550,7 +552,7 @@ int antdt_cache_append(const void* q, int64_t ldq, int64_t ldq_head, void* q_out
                        int64_t page_size, const int32_t* table, int64_t ld_table, int64_t B, int64_t table_cols, const int32_t* lengths,
                        const int32_t* offsets, void* stream);
 /* Attention of one new token of each sequence (q: DEVICE [B, q_heads, D]) over the lengths[b] tokens that the cache holds of it:
- * out[b] = softmax(scale q k^T) v, of `dtype` [B, q_heads, D].  scale >= 1e-30.  B q_heads < 2^24. */
+ * out[b] = softmax(scale q k^T) v, of `dtype` [B, q_heads, D].  B q_heads < 2^24 and B heads table_cols page_size / 32 < 2^31 (ANTDT_UNSUPPORTED otherwise). */
 int antdt_cache_attention_bytes(int64_t B, int64_t q_heads, int64_t heads, int64_t D, int32_t dtype, size_t* bytes);
 int antdt_cache_attention(const void* q, int64_t ldq, int64_t ldq_head, const void* k_cache, const void* v_cache, int64_t ld_page, int64_t ld_row,
                           int64_t ld_head, int64_t pages, int64_t page_size, const int32_t* table, int64_t ld_table, int64_t B, int64_t table_cols,
@@ -561,7 +563,7 @@ int antdt_cache_attention(const void* q, int64_t ldq, int64_t ldq_head, const vo
  * Attention of S queries (candidates, a decoder's tokens) over T keys and values of another length (an encoded history), for every batch entry:
  * out = softmax(scale q k^T) v.  q, out: DEVICE [B, S, q_heads, D], k, v: DEVICE [B, T, heads, D], of `dtype`.  q_lengths, k_lengths: rows that an
  * entry has (NULL: all).  stats: DEVICE fp32 [B, q_heads, S], or NULL: log2 of the sum of 2^(scale log2(e) q k^T) for the backward pass, +infinity
- * for a query without keys.  scale >= 1e-30.  B q_heads max(S, T) / 128 (rounded up) < 2^24, S, T < 2^31 - 1.
+ * for a query without keys.  B q_heads max(S, T) / 128 (rounded up) < 2^24 (ANTDT_UNSUPPORTED otherwise), B, S, T < 2^31 - 1.
  */
 int antdt_cross_attention_bytes(int64_t B, int64_t S, int64_t T, int64_t q_heads, int64_t heads, int64_t D, int32_t dtype, size_t* bytes);
 int antdt_cross_attention(const void* q, int64_t ldq_batch, int64_t ldq, int64_t ldq_head, const void* k, int64_t ldk_batch, int64_t ldk, int64_t ldk_head,

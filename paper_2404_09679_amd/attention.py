@@ -58,6 +58,10 @@ def _lengths(t: Optional[torch.Tensor], name: str, n: int, device: int) -> Optio
     return None if t is None else _vector(t, name, n, torch.int32, device)
 
 
+def _scale(scale: Optional[float], D: int) -> float:
+    return max(D, 1) ** -0.5 if scale is None else scale
+
+
 def _turned(x: torch.Tensor, positions: torch.Tensor, rotary: Rotary, inverse: int, out: Optional[torch.Tensor]) -> torch.Tensor:
     dt, dev = _first(x, "x", 3)
     if dev != _current_device():
@@ -154,7 +158,7 @@ def cache_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tenso
     held, ws, n = _workspace(workspace, _bytes("antdt_cache_attention_bytes", B, HQ, H, D, _DTYPES[dt]), q)
     _check(lib.antdt_cache_attention(q.data_ptr(), *ldq, k_cache.data_ptr(), v_cache.data_ptr(), *ldc, pages, page, table.data_ptr(), ldt, B, W,
                                      _vector(lengths, "lengths", B, torch.int32, dev), HQ, H, D, _DTYPES[dt],
-                                     D ** -0.5 if scale is None else scale, out.data_ptr(), *ldo, ws, n, _stream(dev)))
+                                     _scale(scale, D), out.data_ptr(), *ldo, ws, n, _stream(dev)))
     return out
 
 
@@ -196,7 +200,7 @@ def cross_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_lengths
     held, ws, n = _workspace(workspace, _bytes("antdt_cross_attention_bytes", B, S, T, HQ, H, D, _DTYPES[dt]), q)
     _check(lib.antdt_cross_attention(q.data_ptr(), *ldq, k.data_ptr(), *ldk, v.data_ptr(), *ldv, B, S, T, HQ, H, D, _DTYPES[dt],
                                      _lengths(q_lengths, "q_lengths", B, dev), _lengths(k_lengths, "k_lengths", B, dev),
-                                     D ** -0.5 if scale is None else scale, out.data_ptr(), *ldo,
+                                     _scale(scale, D), out.data_ptr(), *ldo,
                                      None if stats is None else _stats(stats, B, S, HQ, dev), ws, n, _stream(dev)))
     return out
 
@@ -221,6 +225,6 @@ def cross_attention_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tenso
     _check(lib.antdt_cross_attention_backward(dout.data_ptr(), *ldg, q.data_ptr(), *ldq, k.data_ptr(), *ldk, v.data_ptr(), *ldv, out.data_ptr(),
                                               *ldo, _stats(stats, B, S, HQ, dev), B, S, T, HQ, H, D, _DTYPES[dt],
                                               _lengths(q_lengths, "q_lengths", B, dev), _lengths(k_lengths, "k_lengths", B, dev),
-                                              D ** -0.5 if scale is None else scale, dq.data_ptr(), *lddq, dk.data_ptr(), *lddk, dv.data_ptr(),
+                                              _scale(scale, D), dq.data_ptr(), *lddq, dk.data_ptr(), *lddk, dv.data_ptr(),
                                               *lddv, ws, n, _stream(dev)))
     return dq, dk, dv

@@ -255,7 +255,7 @@ inline int op_wide_heads(const char* call, const char* name, const void* p, int6
   return ANTDT_OK;
 }
 inline int op_scale(const char* call, float scale) {
-  return scale >= 1e-30f && isfinite(scale) ? ANTDT_OK : op_fail(ANTDT_INVALID_ARG, "%s: scale is below 1e-30 or not finite", call);
+  return scale >= 1e-30f && isfinite(scale * LOG2E) ? ANTDT_OK : op_fail(ANTDT_INVALID_ARG, "%s: scale is below 1e-30 or not finite", call);
 }
 inline int op_head_sizes(const char* call, int64_t q_heads, int64_t heads, int64_t D, int32_t dtype) {
   if (!op_dtype(dtype)) return op_fail(ANTDT_INVALID_ARG, "%s: dtype", call);

@@ -70,6 +70,7 @@ __device__ __forceinline__ void turn(uint64_t t, float& c, float& s) {
 __device__ __forceinline__ int place(const RotaryArgs& a, int64_t n, int lane, int& page, int& row) {
   int64_t b = n, first = n, behind = n + 1, length;
   page = 0; row = -1;
+  if (a.B == 0) return -1;
   if (a.offsets) {
     const int64_t step = (a.B + 63) >> 6;
     const bool all = a.B < 64;
@@ -348,7 +349,7 @@ int antdt_cache_append(const void* q, int64_t ldq, int64_t ldq_head, void* q_out
   if (pages < 0 || pages >= (1ll << 31)) return op_fail(ANTDT_INVALID_ARG, "%s: pages out of range", call);
   RotaryArgs a = {};
   int quantum = 8;
-  if (N == 0 || B == 0 || D == 0 || (heads == 0 && q_heads == 0)) return ANTDT_OK;
+  if (N == 0 || D == 0 || (heads == 0 && q_heads == 0)) return ANTDT_OK;
   if (rotary) OP_TRY(rotary_spec(call, rotary, D, a, quantum));
   const int64_t size = op_size(dtype);
   HeadStrides sq = {0, ldq, ldq_head}, so = {0, ldqo, ldqo_head}, sk = {0, ldk, ldk_head}, sv = {0, ldv, ldv_head};

@@ -5,7 +5,9 @@
 // its tiles to LDS, several ahead, and keeps the running maximum, sum and output of a softmax over its part of a sequence.  Where a sequence lies
 // in one piece, that is the result; else the pieces' are joined by a second launch:
 //   m = max m_i,  l = sum l_i 2^(m_i - m),  out = sum o_i 2^(m_i - m) / l.
-// Bound by memory: a key head's queries share what is read of it.
+// Bound by memory, a key head's queries share what is read of it: one user's 131072 tokens (8 heads of 128 bf16 columns, 537 MB) 90 us (6.0 TB/s) and 5.5 to
+// join; 64 users of 16 to 8192 tokens (178 MB) 35 and 5.  Where there is little to read, by the chain of a wavefront's loads (lengths, page, rows) and
+// by its code's: one tile takes 10 us.
 #include "attend.h"
 #include "sort.h"
 
@@ -488,7 +490,7 @@ extern "C" {
 
 static int cache_attention_sizes(const char* call, int64_t B, int64_t q_heads, int64_t heads, int64_t D, int32_t dtype) {
   OP_TRY(op_head_sizes(call, q_heads, heads, D, dtype));
-  if (B < 0 || B * q_heads >= 1 << 24) return op_fail(ANTDT_UNSUPPORTED, "%s: B q_heads: 2^24 or more", call);
+  if (B < 0 || B >= 1 << 24 || B * q_heads >= 1 << 24) return op_fail(ANTDT_UNSUPPORTED, "%s: B q_heads: 2^24 or more", call);
   return ANTDT_OK;
 }
 

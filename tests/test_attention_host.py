@@ -269,3 +269,33 @@ def test_refusals_of_tensors(boundary, monkeypatch):
     monkeypatch.setattr(torch.Tensor, "get_device", lambda s: 1 if s.dtype == torch.int64 else 0)
     with pytest.raises(ValueError, match="Rotary"):
         A.rotary(x, i4, rot)
+
+
+def test_the_largest_scale():
+    def call(scale):
+        return lib.antdt_cross_attention(PTR, 0, 64, 64, PTR, 0, 64, 64, PTR, 0, 64, 64, 1, 0, 4, 1, 1, 64, 0, None, None, scale, PTR, 0, 64, 64, None, None, 0, None)
+
+    assert call(2.3e38) == OK and call(2.4e38) == INVALID and "scale" in message()      # (times log2(e): 3.32e38 and 3.46e38, of 3.40e38)
+
+
+def test_sizes_whose_product_passes_64_bits():
+    n = C.c_size_t()
+    for B in (1 << 50, 1 << 60, (1 << 63) - 1):
+        assert lib.antdt_cache_attention_bytes(B, 1 << 14, 1, 64, 1, C.byref(n)) == UNSUPPORTED
+        assert lib.antdt_cross_attention_bytes(B, 1, 1, 1 << 14, 1, 64, 1, C.byref(n)) == INVALID
+
+
+def test_tokens_of_no_sequence_have_their_operands_checked():
+    """Offsets of no sequences: every token is in none, and its query's place is written all the same."""
+    def call(q, qo):
+        return lib.antdt_cache_append(q, 32, 8, qo, 32, 8, PTR, 16, 8, PTR, 16, 8, 3, 4, 2, 8, 0, None, 3 * PTR, 4 * PTR, 256, 16, 8, 5, 16, None, 7, 0, 7, None,
+                                      PTR, None)
+
+    assert call(None, 2 * PTR) == INVALID and call(PTR, None) == INVALID and "q_out" in message()
+
+
+def test_heads_without_columns():
+    """Refused by the call, not by the default scale."""
+    for name in ("antdt_cache_attention_bytes", "antdt_cross_attention_bytes"):
+        assert getattr(lib, name)(1, *((1, 1) if "cross" in name else ()), 1, 1, 0, 0, C.byref(C.c_size_t())) == UNSUPPORTED
+    assert T._scale(None, 0) == 1.0 and T._scale(None, 64) == 0.125 and T._scale(0.5, 64) == 0.5

@@ -155,3 +155,14 @@ def test_two_calls_at_once():
     torch.cuda.synchronize()
     for a, b in zip(want, got):
         assert all(torch.equal(x, y) for x, y in zip(a, b))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_tokens_of_no_sequence_at_all(dtype):
+    rng = np.random.default_rng(5)
+    kc, vc = (torch.full((2, 4, 1, 32), 5.0, device=DEV, dtype=DT[dtype]) for _ in range(2))
+    k, q = normal(rng, 3, 1, 32, dtype=dtype), normal(rng, 3, 2, 32, dtype=dtype)
+    for rot in (None, A.Rotary(32, device=DEV)):
+        q_out = torch.full_like(q, 7.0)
+        A.cache_append(k, k, kc, vc, torch.zeros(0, 2, dtype=torch.int32, device=DEV), torch.zeros(0, dtype=torch.int32, device=DEV), ints([0]), rot, q, q_out)
+        assert not q_out.any() and bool((kc == 5).all()) and bool((vc == 5).all())
