@@ -6,7 +6,7 @@ namespace {
 
 // ------------------------------------------------------------- d
 // From out as it was kept; of few keys, which fit in LDS, the sum of p dP instead (the same number): dP - d nearly vanishes there, and what out lost to
-// its rounding would show (2 keys, bf16: dQ off by 0.005 of its norm, so by 0.0025, the operands' rounding).  Bound by memory.
+// its rounding would show (2 keys, bf16: dQ off by 0.005 of its norm, so by 0.0025, the operands' rounding).  Bound by memory: 134 MB 27 us.
 template <typename T, int DP, int COLS>
 struct FewKeys {
   static constexpr int KEYS = 64, STEPS = COLS / Core<T>::STEP;
@@ -292,8 +292,11 @@ __device__ __forceinline__ void dkv_block(const CrossArgs& a, int index, char* l
   write_result<W>(lds, ov, 1.0f, dv, sums ? sums + all : nullptr, t0, end, a.D, wave, lane);
 }
 
-// Both in one launch: blocks of keys first, which take longer, so that blocks of queries fill the chip while the last of them run (8 x 2048 x 4096, 16
-// and 4 heads of 128 bf16 columns: TWO us in two launches, ONE so).  Waves behind a kind's own leave at once.
+// Both in one launch: blocks of keys first, which take longer, so that blocks of queries fill the chip while the last of them run (8 ragged histories of
+// 2048 queries and 4096 keys, 16 and 4 heads of 128 bf16 columns: 640 + 980 us in two launches, 1460 so; 13 of 77 and 777, 6 and 2 heads of 64: 13 + 16,
+// so 18).  Wavefronts behind a kind's own leave at once.
+// Bound by the matrix cores, whose operands LDS and the vector units have to keep up with: 14 products of 18 that the large case computes in all run at
+// 914 TFLOP/s there (a library product of 8192 cubed: 1131).
 template <typename WQ, typename WK, bool HELD>
 __global__ __launch_bounds__(256, (WQ::PER_CU < WK::PER_CU ? WQ::PER_CU : WK::PER_CU)) void cross_backward_kernel(CrossArgs a) {
   extern __shared__ __attribute__((aligned(1024))) char lds[];
