@@ -17,10 +17,10 @@ __global__ __launch_bounds__(W::THREADS, W::PER_CU) void cross_forward_kernel(Cr
   extern __shared__ __attribute__((aligned(1024))) char lds[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
   int unit, block;
-  place_of(blockIdx.x, a.units, a.group * a.queries.tiles, unit, block);
+  place_of(a, blockIdx.x, a.group * a.queries.tiles, unit, block);
   const int tile = block % a.queries.tiles, h = unit % a.heads * a.group + block / a.queries.tiles;
-  const int64_t b = unit / a.heads, bh = b * a.q_heads + h;
-  const int64_t q_len = length_of(a.q_lengths, b, a.S), k_len = length_of(a.k_lengths, b, a.T);
+  const Entry of = entry_of(a, unit / a.heads, a.k_lengths, a.T, a.q_lengths, a.S, lane);
+  const int64_t b = of.b, bh = b * a.q_heads + h, q_len = of.own, k_len = of.through;
   const int64_t first = (int64_t)tile * W::ROWS, last = min(first + W::ROWS, a.S), r0 = first + (W::SPLIT ? 0 : wave * 32);
   const Rows out = a.out.rows(b, h);
   float* stats = a.stats ? a.stats + bh * a.S : nullptr;
@@ -134,11 +134,12 @@ __global__ __launch_bounds__(W::THREADS, W::PER_CU) void cross_forward_kernel(Cr
 }
 
 template <typename W>
-hipError_t launch_forward(CrossArgs a, const Plan& pl, hipStream_t s) {
+hipError_t launch_forward(CrossArgs a, const Shape& z, const Plan& pl, hipStream_t s) {
   static std::atomic<uint64_t> allowed{0};
   const hipError_t e = allow_lds(cross_forward_kernel<W>, KeyTiles<W>::LDS, 0, allowed);
   if (e != hipSuccess) return e;
   a.queries = pl.share(nullptr);
+  a.longest_first = longest_first(z, pl.blocks, 256 * W::PER_CU);
   hipLaunchKernelGGL(cross_forward_kernel<W>, dim3((unsigned)pl.blocks), dim3(W::THREADS), KeyTiles<W>::LDS, s, a);
   return hipGetLastError();
 }
@@ -185,12 +186,12 @@ int antdt_cross_attention(const void* q, int64_t ldq_batch, int64_t ldq, int64_t
     return op_hip(call, launch_stream(f, dtype, workspace, s));
   }
   a.q_lengths = q_lengths; a.k_lengths = k_lengths; a.stats = stats; a.S = S; a.T = T;
-  a.q_heads = (int)q_heads; a.heads = (int)heads; a.group = (int)(q_heads / heads); a.D = (int)D; a.units = (int)(B * heads);
+  a.q_heads = (int)q_heads; a.heads = (int)heads; a.group = (int)(q_heads / heads); a.D = (int)D; a.units = (int)(B * heads); a.B = (int)B;
   const Plan pl = forward_plan(z);
-  return op_hip(call, by_columns(dtype, (int)D, [&](auto z, auto cols) {
-    typedef decltype(z) Z;
+  return op_hip(call, by_columns(dtype, (int)D, [&](auto way, auto cols) {
+    typedef decltype(way) Z;
     constexpr int COLS = decltype(cols)::value;
-    return pl.split ? launch_forward<typename Z::template SplitKeys<COLS>>(a, pl, s) : launch_forward<typename Z::template Keys<COLS>>(a, pl, s);
+    return pl.split ? launch_forward<typename Z::template SplitKeys<COLS>>(a, z, pl, s) : launch_forward<typename Z::template Keys<COLS>>(a, z, pl, s);
   }));
 }
 

@@ -76,10 +76,10 @@ __device__ __forceinline__ void dq_block(const CrossArgs& a, int index, char* ld
   if (wave >= W::WAVES) return;
   const Share& share = a.queries;
   int unit, block;
-  place_of(index, a.units, a.group * share.tiles * share.parts, unit, block);
+  place_of(a, index, a.group * share.tiles * share.parts, unit, block);
   const int part = block % share.parts, tile = block / share.parts % share.tiles, h = unit % a.heads * a.group + block / share.parts / share.tiles;
-  const int64_t b = unit / a.heads, bh = b * a.q_heads + h;
-  const int64_t q_len = length_of(a.q_lengths, b, a.S), k_len = length_of(a.k_lengths, b, a.T);
+  const Entry of = entry_of(a, unit / a.heads, a.k_lengths, a.T, a.q_lengths, a.S, lane);
+  const int64_t b = of.b, bh = b * a.q_heads + h, q_len = of.own, k_len = of.through;
   const int64_t first = (int64_t)tile * W::ROWS, last = min(first + W::ROWS, a.S), r0 = first + (W::SPLIT ? 0 : wave * 32);
   const int64_t end = k_len > 0 ? min(max(q_len, first), last) : first;
   const Rows dq = a.dq.rows(b, h);
@@ -178,10 +178,10 @@ __device__ __forceinline__ void dkv_block(const CrossArgs& a, int index, char* l
   if (wave >= W::WAVES) return;
   const Share& share = a.keys;
   int unit, block;
-  place_of(index, a.units, share.tiles * share.parts, unit, block);
+  place_of(a, index, share.tiles * share.parts, unit, block);
   const int part = block % share.parts, tile = block / share.parts, h = unit % a.heads;
-  const int64_t b = unit / a.heads;
-  const int64_t q_len = length_of(a.q_lengths, b, a.S), k_len = length_of(a.k_lengths, b, a.T);
+  const Entry of = entry_of(a, unit / a.heads, a.q_lengths, a.S, a.k_lengths, a.T, lane);
+  const int64_t b = of.b, q_len = of.through, k_len = of.own;
   const int64_t first = (int64_t)tile * W::ROWS, last = min(first + W::ROWS, a.T), t0 = first + (W::SPLIT ? 0 : wave * 32);
   const int64_t end = q_len > 0 ? min(max(k_len, first), last) : first;
   const Rows dk = a.dk.rows(b, h), dv = a.dv.rows(b, h);
@@ -287,7 +287,7 @@ __device__ __forceinline__ void dkv_block(const CrossArgs& a, int index, char* l
   }
   arrive<0, true>();
   const int64_t all = (int64_t)a.units * a.T * a.D;
-  float* sums = share.parts == 1 ? nullptr : share.partial + 2 * part * all + (int64_t)unit * a.T * a.D;
+  float* sums = share.parts == 1 ? nullptr : share.partial + 2 * part * all + (b * a.heads + h) * a.T * a.D;
   write_result<W>(lds, ok, a.scale, dk, sums, t0, end, a.D, wave, lane);
   write_result<W>(lds, ov, 1.0f, dv, sums ? sums + all : nullptr, t0, end, a.D, wave, lane);
 }
@@ -345,11 +345,12 @@ hipError_t launch_d(const CrossArgs& a, int64_t blocks, hipStream_t s) {
   return hipGetLastError();
 }
 template <typename WQ, typename WK, bool HELD>
-hipError_t launch_backward(const CrossArgs& a, hipStream_t s) {
+hipError_t launch_backward(CrossArgs a, const Shape& z, hipStream_t s) {
   static std::atomic<uint64_t> allowed{0};
   constexpr int LDS = KeyTiles<WQ>::LDS > QueryTiles<WK, HELD>::LDS ? KeyTiles<WQ>::LDS : QueryTiles<WK, HELD>::LDS;
   const hipError_t e = allow_lds(cross_backward_kernel<WQ, WK, HELD>, LDS, 0, allowed);
   if (e != hipSuccess) return e;
+  a.longest_first = longest_first(z, a.keys.blocks + a.queries.blocks, 256 * std::min(WQ::PER_CU, WK::PER_CU));
   hipLaunchKernelGGL((cross_backward_kernel<WQ, WK, HELD>), dim3((unsigned)(div_up(a.keys.blocks, 8) * 8 + a.queries.blocks)), dim3(256), LDS, s, a);
   return hipGetLastError();
 }
@@ -404,7 +405,7 @@ int antdt_cross_attention_backward(const void* dout, int64_t lddo_batch, int64_t
   if (!keys && !queries) return ANTDT_OK;
   OP_TRY(op_workspace(call, workspace, workspace_bytes, need));
   a.q_lengths = q_lengths; a.k_lengths = k_lengths; a.stats = const_cast<float*>(stats); a.delta = reinterpret_cast<float*>(workspace); a.S = S; a.T = T;
-  a.q_heads = (int)q_heads; a.heads = (int)heads; a.group = (int)(q_heads / heads); a.D = (int)D; a.units = (int)(B * heads);
+  a.q_heads = (int)q_heads; a.heads = (int)heads; a.group = (int)(q_heads / heads); a.D = (int)D; a.units = (int)(B * heads); a.B = (int)B;
   const hipStream_t s = (hipStream_t)stream;
   float* partial = reinterpret_cast<float*>(reinterpret_cast<char*>(workspace) + delta_bytes(z));
   const Plan of_q = dq_plan(z), of_k = dkv_plan(z);
@@ -422,8 +423,8 @@ int antdt_cross_attention_backward(const void* dout, int64_t lddo_batch, int64_t
       const hipError_t e = launch_d<typename Q::T, Q::DP, COLS>(a, B * q_heads * div_up(S, 128), s);
       if (e != hipSuccess) return e;
     }
-    if (of_q.split) return of_k.split ? launch_backward<SQ, SK, true>(a, s) : launch_backward<SQ, K, Z::HELD>(a, s);
-    return of_k.split ? launch_backward<Q, SK, true>(a, s) : launch_backward<Q, K, Z::HELD>(a, s);
+    if (of_q.split) return of_k.split ? launch_backward<SQ, SK, true>(a, z, s) : launch_backward<SQ, K, Z::HELD>(a, z, s);
+    return of_k.split ? launch_backward<Q, SK, true>(a, z, s) : launch_backward<Q, K, Z::HELD>(a, z, s);
   })));
   // The parts' sums to the results.
   auto join = [&](const Share& sh, const HeadsArg& x, const HeadsArg& y, int results, int64_t H, int64_t L, int64_t other, const int32_t* lengths, const int32_t* others) {

@@ -27,6 +27,8 @@ struct CrossArgs {
   int64_t S, T;
   int32_t q_heads, heads, group, D;
   int32_t units;       // heads of all batch entries' keys
+  int32_t B;
+  int32_t longest_first;   // whether batch entries are gone through by length, see entry_of
   float scale, scale2;   // scale2: scale log2 e
   Share queries, keys;   // blocks of queries, and (backward) of keys
 };
@@ -78,13 +80,33 @@ __device__ __forceinline__ float where_left(int row, int left, float x, float ot
 }
 // Block i of `units` x n: which unit, and which of its blocks.  Blocks of a unit (a head of one batch entry's keys, and who reads it) share an XCD (block
 // i runs on XCD i mod 8), whose L2 then has the rows they all read; neighbouring units are on different ones, so that a batch entry of long
-// sequences is everybody's work.  What is left of less than 8 units is spread over all.
-__device__ __forceinline__ void place_of(int i, int units, int n, int& unit, int& block) {
-  const int whole = (units & ~7) * n;
+// sequences is everybody's work.  What is left of less than 8 units is spread over all.  Longest first, the longer ones of 8 go to one half of the XCDs
+// and to the other in turn.
+__device__ __forceinline__ void place_of(const CrossArgs& a, int i, int n, int& unit, int& block) {
+  const int units = a.units, whole = (units & ~7) * n;
   const int x = i < whole ? i & 7 : 0, j = i < whole ? i >> 3 : i - whole;
   const int u = j / n;
   block = j - u * n;
-  unit = i < whole ? 8 * u + x : (units & ~7) + u;
+  unit = i < whole ? 8 * u + (a.longest_first ? x ^ (4 * (u & 1)) : x) : (units & ~7) + u;
+}
+
+// A batch entry with the rows it has of both sides: `through`, which a block of it goes through, and `own`, which are shared out over blocks.
+struct Entry {
+  int64_t b, through, own;
+};
+// Entry in place i when the longest come first, so that the last blocks are short ones: of each 16 entries, one in each lane, by counting.
+// Forward / backward in us, of 128 bf16 columns, in the order given and so: 32 entries of 1 to 1024 queries and keys, 8 heads 72 / 191, 63 / 182; 8 of 1366
+// to 2048 queries and 2560 to 4096 keys, 16 and 4 heads, in four orders 430-480 / 1311-1463, 434-443 / 1317-1400.
+__device__ __forceinline__ Entry entry_of(const CrossArgs& a, int64_t i, const int32_t* through, int64_t most, const int32_t* own, int64_t most_own, int lane) {
+  if (!a.longest_first || !through) return Entry{i, length_of(through, i, most), length_of(own, i, most_own)};
+  const int64_t first = i & ~15ll, mine = min(first + (lane & 15), (int64_t)a.B - 1);
+  const int x = (int)length_of(through, mine, most), y = (int)length_of(own, mine, most_own);
+  const uint32_t key = (uint32_t)(first + lane < a.B ? min(x, (1 << 27) - 1) : 0) << 4 | (15 - (lane & 15));   // (no two alike, and behind the last entry less)
+  int before = 0;
+#pragma unroll
+  for (int j = 0; j < 16; ++j) before += (uint32_t)__builtin_amdgcn_readlane(key, j) > key ? 1 : 0;
+  const int at = __ffsll((unsigned long long)__ballot(before == (int)(i - first))) - 1;
+  return Entry{first + at, __builtin_amdgcn_readlane(x, at), __builtin_amdgcn_readlane(y, at)};
 }
 
 // How a kernel goes about its work.  DP columns of a row in LDS, the first COLS of which take part; TILE rows to a stage of the ring, STAGES of them.
@@ -254,6 +276,12 @@ inline int key_waves(const Shape& z) { return z.dtype == ANTDT_F32 && z.D > 64 ?
 inline Plan forward_plan(const Shape& z) { return cross_plan(z.B * z.q_heads, z.S, div_up(z.T, 32), wide(z) ? 256 : 512, key_waves(z), tile_us(z), false); }
 inline Plan dq_plan(const Shape& z) { return cross_plan(z.B * z.q_heads, z.S, div_up(z.T, 32), wide(z) ? 256 : 512, key_waves(z), 1.3 * tile_us(z), true); }
 inline Plan dkv_plan(const Shape& z) { return cross_plan(z.B * z.heads, z.T, div_up(z.S, 32) * (z.q_heads / z.heads), wide(z) ? 256 : 512, key_waves(z), 2.0 * tile_us(z), true); }
+// Whether entries are gone through by length: costs a block about a microsecond and shortens the end by some of the longest block's time
+// (200 entries of 1 to 300, 8 and 2 heads of 64: 41 / 105 us, by length 43 / 116).
+inline bool longest_first(const Shape& z, int64_t blocks, int at_once) {
+  const double rounds = (double)blocks / at_once;
+  return z.B > 1 && rounds > 1.0 && tile_us(z) * div_up(std::max(z.S, z.T), 32) > 4.0 * rounds;
+}
 // Whether the forward pass goes by an equal share of all keys to each wavefront (stream.hip) instead, by the time that both would take: that costs a
 // second launch, about 9 us, and the tiles of 32 keys and 16 or 32 queries of a key's heads take 1.4 times as long.  us by blocks / shares, 8 heads of
 // 64 bf16 columns: 1 query, 500 keys 8 / 16, 2000 19 / 15, 8000 61 / 16; 4 x 128 queries, 2000 keys 20 / 31, 8000 75 / 64; fp32, 1 query, 500 keys 16 / 14.

@@ -166,3 +166,22 @@ def test_tokens_of_no_sequence_at_all(dtype):
         q_out = torch.full_like(q, 7.0)
         A.cache_append(k, k, kc, vc, torch.zeros(0, 2, dtype=torch.int32, device=DEV), torch.zeros(0, dtype=torch.int32, device=DEV), ints([0]), rot, q, q_out)
         assert not q_out.any() and bool((kc == 5).all()) and bool((vc == 5).all())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("B,S,T,HQ,H,D", [(37, 400, 512, 4, 2, 32), (16, 500, 700, 12, 6, 64), (50, 640, 384, 4, 1, 8)])
+def test_entries_in_another_order(B, S, T, HQ, H, D, dtype):
+    """More blocks than run at once, long and short entries: each has its results wherever in the batch it stands."""
+    rng = np.random.default_rng(B)
+    q, k, v, g, ql, kl = cross_inputs(rng, B, S, T, HQ, H, D, "ragged", dtype)
+    kl[5] = kl[6] = kl[7]
+    ql[9] = ql[8]
+    for b in (5, 6, 8, 9):
+        k[b].nan_to_num_(1.0), v[b].nan_to_num_(1.0), q[b].nan_to_num_(1.0), g[b].nan_to_num_(1.0)
+    got = cross(q, k, v, g, ints(ql), ints(kl))
+    check_cross([x[:12] for x in got], q[:12], k[:12], v[:12], g[:12], ql[:12], kl[:12], D ** -0.5, dtype, "")
+    order = rng.permutation(B)
+    other = cross(*(x[torch.as_tensor(order, device=DEV)] for x in (q, k, v, g)), ints(np.array(ql)[order]), ints(np.array(kl)[order]))
+    assert all(torch.equal(x[torch.as_tensor(order, device=DEV)], y) for x, y in zip(got, other))
+    full = [normal(rng, *x.shape, dtype=dtype) for x in (q, k, v, g)]
+    assert all(torch.equal(x, y) for x, y in zip(cross(*full, None, ints([T] * B)), cross(*full, ints([S] * B), None)))
