@@ -6,7 +6,7 @@
 // in one piece, that is the result; else the pieces' are joined by a second launch:
 //   m = max m_i,  l = sum l_i 2^(m_i - m),  out = sum o_i 2^(m_i - m) / l.
 // Bound by memory, a key head's queries share what is read of it: one user's 131072 tokens (8 heads of 128 bf16 columns, 537 MB) 90 us (6.0 TB/s) and 5.5 to
-// join; 64 users of 16 to 8192 tokens (178 MB) 35 and 5.  Where there is little to read, by the chain of a wavefront's loads (lengths, page, rows) and
+// join; 64 users of 16 to 8192 tokens (178 MB) 39 and 5.  Where there is little to read, by the chain of a wavefront's loads (lengths, page, rows) and
 // by its code's: one tile takes 10 us.
 #include "attend.h"
 #include "sort.h"
@@ -167,8 +167,10 @@ __global__ __launch_bounds__(64 * WAVES, (Stream<T, DP, R>::PER_CU)) void stream
   }
   const uint32_t times = a.heads * a.row_tiles;
   const Shares shares(total * times, a.waves);
-  // Keys and values that the last-level cache (256 MB) has no room for are not kept by the others (537 MB 102 us, so 90; but 178 MB 35 and 36).
-  const bool once = a.row_tiles == 1 && (int64_t)shares.total * 2 * F::BYTES > 256 << 20;
+  // Keys and values that take more than a quarter of the last-level cache (256 MB) and are read once are not kept there: a step of answering reads those of
+  // other layers before it comes back.  us, kept / not: eight caches in turn of 16 MB 8.9 / 9.0, 33 MB 12.6 / 14.0, 262 MB 54 / 47; three of 178 MB 43 / 39
+  // (one alone 35 / 36); 537 MB 102 / 92.
+  const bool once = a.row_tiles == 1 && (int64_t)shares.total * 2 * F::BYTES > 64 << 20;
   uint32_t at = shares.first(w);
   const uint32_t stop = shares.first(w + 1);
   if (at >= stop) return;
