@@ -6,7 +6,7 @@ namespace {
 
 // A block has queries of a head; tiles of keys and values go through LDS, the next one's loads under way.  A wavefront's 32 queries take a pass over the
 // vector units (maximum, exponential, sum) for each over the matrix core, about as long; two wavefronts on a SIMD have them at the same time.  8 ragged
-// histories of 2048 queries and 4096 keys, 16 and 4 heads of 128 bf16 columns: 381 GFLOP in 490 us, a sixth of it the last blocks' of uneven users.
+// histories of 2048 queries and 4096 keys, 16 and 4 heads of 128 bf16 columns: 381 GFLOP in 440 us, an eighth of it the last blocks, when not all compute units have one.
 template <typename W>
 __global__ __launch_bounds__(W::THREADS, W::PER_CU) void cross_forward_kernel(CrossArgs a) {
   typedef typename W::T T;
@@ -19,8 +19,8 @@ __global__ __launch_bounds__(W::THREADS, W::PER_CU) void cross_forward_kernel(Cr
   int unit, block;
   place_of(a, blockIdx.x, a.group * a.queries.tiles, unit, block);
   const int tile = block % a.queries.tiles, h = unit % a.heads * a.group + block / a.queries.tiles;
-  const Entry of = entry_of(a, unit / a.heads, a.k_lengths, a.T, a.q_lengths, a.S, lane);
-  const int64_t b = of.b, bh = b * a.q_heads + h, q_len = of.own, k_len = of.through;
+  const Entry of = entry_of(a, unit / a.heads, lane);
+  const int64_t b = of.b, bh = b * a.q_heads + h, q_len = of.q_len, k_len = of.k_len;
   const int64_t first = (int64_t)tile * W::ROWS, last = min(first + W::ROWS, a.S), r0 = first + (W::SPLIT ? 0 : wave * 32);
   const Rows out = a.out.rows(b, h);
   float* stats = a.stats ? a.stats + bh * a.S : nullptr;
@@ -139,7 +139,7 @@ hipError_t launch_forward(CrossArgs a, const Shape& z, const Plan& pl, hipStream
   const hipError_t e = allow_lds(cross_forward_kernel<W>, KeyTiles<W>::LDS, 0, allowed);
   if (e != hipSuccess) return e;
   a.queries = pl.share(nullptr);
-  a.longest_first = longest_first(z, pl.blocks, 256 * W::PER_CU);
+  a.longest_first = longest_first(z, a.k_lengths || a.q_lengths, pl.blocks, 256 * W::PER_CU);
   hipLaunchKernelGGL(cross_forward_kernel<W>, dim3((unsigned)pl.blocks), dim3(W::THREADS), KeyTiles<W>::LDS, s, a);
   return hipGetLastError();
 }

@@ -78,8 +78,8 @@ __device__ __forceinline__ void dq_block(const CrossArgs& a, int index, char* ld
   int unit, block;
   place_of(a, index, a.group * share.tiles * share.parts, unit, block);
   const int part = block % share.parts, tile = block / share.parts % share.tiles, h = unit % a.heads * a.group + block / share.parts / share.tiles;
-  const Entry of = entry_of(a, unit / a.heads, a.k_lengths, a.T, a.q_lengths, a.S, lane);
-  const int64_t b = of.b, bh = b * a.q_heads + h, q_len = of.own, k_len = of.through;
+  const Entry of = entry_of(a, unit / a.heads, lane);
+  const int64_t b = of.b, bh = b * a.q_heads + h, q_len = of.q_len, k_len = of.k_len;
   const int64_t first = (int64_t)tile * W::ROWS, last = min(first + W::ROWS, a.S), r0 = first + (W::SPLIT ? 0 : wave * 32);
   const int64_t end = k_len > 0 ? min(max(q_len, first), last) : first;
   const Rows dq = a.dq.rows(b, h);
@@ -180,8 +180,8 @@ __device__ __forceinline__ void dkv_block(const CrossArgs& a, int index, char* l
   int unit, block;
   place_of(a, index, share.tiles * share.parts, unit, block);
   const int part = block % share.parts, tile = block / share.parts, h = unit % a.heads;
-  const Entry of = entry_of(a, unit / a.heads, a.q_lengths, a.S, a.k_lengths, a.T, lane);
-  const int64_t b = of.b, q_len = of.through, k_len = of.own;
+  const Entry of = entry_of(a, unit / a.heads, lane);
+  const int64_t b = of.b, q_len = of.q_len, k_len = of.k_len;
   const int64_t first = (int64_t)tile * W::ROWS, last = min(first + W::ROWS, a.T), t0 = first + (W::SPLIT ? 0 : wave * 32);
   const int64_t end = q_len > 0 ? min(max(k_len, first), last) : first;
   const Rows dk = a.dk.rows(b, h), dv = a.dv.rows(b, h);
@@ -293,10 +293,10 @@ __device__ __forceinline__ void dkv_block(const CrossArgs& a, int index, char* l
 }
 
 // Both in one launch: blocks of keys first, which take longer, so that blocks of queries fill the chip while the last of them run (8 ragged histories of
-// 2048 queries and 4096 keys, 16 and 4 heads of 128 bf16 columns: 640 + 980 us in two launches, 1460 so; 13 of 77 and 777, 6 and 2 heads of 64: 13 + 16,
+// 2048 queries and 4096 keys, 16 and 4 heads of 128 bf16 columns: 640 + 980 us in two launches, 1340 so; 13 of 77 and 777, 6 and 2 heads of 64: 13 + 16,
 // so 18).  Wavefronts behind a kind's own leave at once.
 // Bound by the matrix cores, whose operands LDS and the vector units have to keep up with: 14 products of 18 that the large case computes in all run at
-// 914 TFLOP/s there (a library product of 8192 cubed: 1131).
+// 1000 TFLOP/s there (a library product of 8192 cubed: 1131).
 template <typename WQ, typename WK, bool HELD>
 __global__ __launch_bounds__(256, (WQ::PER_CU < WK::PER_CU ? WQ::PER_CU : WK::PER_CU)) void cross_backward_kernel(CrossArgs a) {
   extern __shared__ __attribute__((aligned(1024))) char lds[];
@@ -350,7 +350,7 @@ hipError_t launch_backward(CrossArgs a, const Shape& z, hipStream_t s) {
   constexpr int LDS = KeyTiles<WQ>::LDS > QueryTiles<WK, HELD>::LDS ? KeyTiles<WQ>::LDS : QueryTiles<WK, HELD>::LDS;
   const hipError_t e = allow_lds(cross_backward_kernel<WQ, WK, HELD>, LDS, 0, allowed);
   if (e != hipSuccess) return e;
-  a.longest_first = longest_first(z, a.keys.blocks + a.queries.blocks, 256 * std::min(WQ::PER_CU, WK::PER_CU));
+  a.longest_first = longest_first(z, a.k_lengths || a.q_lengths, a.keys.blocks + a.queries.blocks, 256 * std::min(WQ::PER_CU, WK::PER_CU));
   hipLaunchKernelGGL((cross_backward_kernel<WQ, WK, HELD>), dim3((unsigned)(div_up(a.keys.blocks, 8) * 8 + a.queries.blocks)), dim3(256), LDS, s, a);
   return hipGetLastError();
 }

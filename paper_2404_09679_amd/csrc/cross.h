@@ -90,23 +90,27 @@ __device__ __forceinline__ void place_of(const CrossArgs& a, int i, int n, int& 
   unit = i < whole ? 8 * u + (a.longest_first ? x ^ (4 * (u & 1)) : x) : (units & ~7) + u;
 }
 
-// A batch entry with the rows it has of both sides: `through`, which a block of it goes through, and `own`, which are shared out over blocks.
+// A batch entry and the rows it has.
 struct Entry {
-  int64_t b, through, own;
+  int64_t b, q_len, k_len;
 };
-// Entry in place i when the longest come first, so that the last blocks are short ones: of each 16 entries, one in each lane, by counting.
+// Entry in place i when those of most keys come first (of as many those of most queries), so that the last blocks are short ones: of each 16 entries, one in
+// each lane, by counting.
 // Forward / backward in us, of 128 bf16 columns, in the order given and so: 32 entries of 1 to 1024 queries and keys, 8 heads 72 / 191, 63 / 182; 8 of 1366
-// to 2048 queries and 2560 to 4096 keys, 16 and 4 heads, in four orders 430-480 / 1311-1463, 434-443 / 1317-1400.
-__device__ __forceinline__ Entry entry_of(const CrossArgs& a, int64_t i, const int32_t* through, int64_t most, const int32_t* own, int64_t most_own, int lane) {
-  if (!a.longest_first || !through) return Entry{i, length_of(through, i, most), length_of(own, i, most_own)};
+// to 2048 queries and 2560 to 4096 keys, 16 and 4 heads, in four orders 430-480 / 1311-1463, 435-439 / 1333-1341.
+__device__ __forceinline__ Entry entry_of(const CrossArgs& a, int64_t i, int lane) {
+  if (!a.longest_first) return Entry{i, length_of(a.q_lengths, i, a.S), length_of(a.k_lengths, i, a.T)};
   const int64_t first = i & ~15ll, mine = min(first + (lane & 15), (int64_t)a.B - 1);
-  const int x = (int)length_of(through, mine, most), y = (int)length_of(own, mine, most_own);
-  const uint32_t key = (uint32_t)(first + lane < a.B ? min(x, (1 << 27) - 1) : 0) << 4 | (15 - (lane & 15));   // (no two alike, and behind the last entry less)
+  const int q = (int)length_of(a.q_lengths, mine, a.S), k = (int)length_of(a.k_lengths, mine, a.T);
+  const bool there = first + lane < a.B;
+  const uint32_t high = there ? k : 0, low = (there ? min(q, (1 << 27) - 1) : 0) << 4 | (15 - (lane & 15));   // (no two alike, and behind the last entry less)
+  const uint64_t key = (uint64_t)high << 32 | low;
   int before = 0;
 #pragma unroll
-  for (int j = 0; j < 16; ++j) before += (uint32_t)__builtin_amdgcn_readlane(key, j) > key ? 1 : 0;
+  for (int j = 0; j < 16; ++j)
+    before += ((uint64_t)(uint32_t)__builtin_amdgcn_readlane(high, j) << 32 | (uint32_t)__builtin_amdgcn_readlane(low, j)) > key ? 1 : 0;
   const int at = __ffsll((unsigned long long)__ballot(before == (int)(i - first))) - 1;
-  return Entry{first + at, __builtin_amdgcn_readlane(x, at), __builtin_amdgcn_readlane(y, at)};
+  return Entry{first + at, __builtin_amdgcn_readlane(q, at), __builtin_amdgcn_readlane(k, at)};
 }
 
 // How a kernel goes about its work.  DP columns of a row in LDS, the first COLS of which take part; TILE rows to a stage of the ring, STAGES of them.
@@ -278,9 +282,9 @@ inline Plan dq_plan(const Shape& z) { return cross_plan(z.B * z.q_heads, z.S, di
 inline Plan dkv_plan(const Shape& z) { return cross_plan(z.B * z.heads, z.T, div_up(z.S, 32) * (z.q_heads / z.heads), wide(z) ? 256 : 512, key_waves(z), 2.0 * tile_us(z), true); }
 // Whether entries are gone through by length: costs a block about a microsecond and shortens the end by some of the longest block's time
 // (200 entries of 1 to 300, 8 and 2 heads of 64: 41 / 105 us, by length 43 / 116).
-inline bool longest_first(const Shape& z, int64_t blocks, int at_once) {
+inline bool longest_first(const Shape& z, bool ragged, int64_t blocks, int at_once) {
   const double rounds = (double)blocks / at_once;
-  return z.B > 1 && rounds > 1.0 && tile_us(z) * div_up(std::max(z.S, z.T), 32) > 4.0 * rounds;
+  return ragged && z.B > 1 && rounds > 1.0 && tile_us(z) * div_up(std::max(z.S, z.T), 32) > 4.0 * rounds;
 }
 // Whether the forward pass goes by an equal share of all keys to each wavefront (stream.hip) instead, by the time that both would take: that costs a
 // second launch, about 9 us, and the tiles of 32 keys and 16 or 32 queries of a key's heads take 1.4 times as long.  us by blocks / shares, 8 heads of
