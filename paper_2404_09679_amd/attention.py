@@ -33,16 +33,17 @@ class Rotary:
         return self._ref
 
 
-def _first(t: torch.Tensor, name: str, dims: int) -> Tuple[torch.dtype, int]:
-    """(dtype, device) of a call's first heads."""
-    device = t.get_device()
-    if len(t.shape) != dims or t.dtype not in _DTYPES or device < 0:
-        raise ValueError(f"{name}: {dims} dimensions of float32 or bfloat16 on the device, not {tuple(t.shape)} of {t.dtype} on {t.device}")
-    return t.dtype, device
+def _first(t: torch.Tensor, name: str, dims: int):
+    """(shape, strides but the columns', dtype, device) of a call's first heads."""
+    shape, s, device = t.shape, t.stride(), t.get_device()
+    if len(shape) != dims or t.dtype not in _DTYPES or device < 0 or (s[-1] != 1 and shape[-1] > 1):
+        raise ValueError(f"{name}: {dims} dimensions of float32 or bfloat16 on the device, columns neighbours, not {tuple(shape)} (strides {s}) "
+                         f"of {t.dtype} on {t.device}")
+    return shape, s[:-1], t.dtype, device
 
 
 def _heads(t: torch.Tensor, name: str, shape: Tuple[int, ...], dtype: torch.dtype, device: int) -> Tuple[int, ...]:
-    """Strides of a heads argument but its columns', after the checks that the C boundary cannot make."""
+    """Strides of another heads argument but its columns', after the checks that the C boundary cannot make."""
     s = t.stride()
     if t.shape != shape or t.dtype is not dtype or t.get_device() != device or (s[-1] != 1 and shape[-1] > 1):
         raise ValueError(f"{name}: heads of neighbouring columns, {tuple(shape)} of {dtype} on device {device}, not {tuple(t.shape)} "
@@ -51,7 +52,7 @@ def _heads(t: torch.Tensor, name: str, shape: Tuple[int, ...], dtype: torch.dtyp
 
 
 def _new(shape: Tuple[int, ...], like: torch.Tensor, dtype: Optional[torch.dtype] = None) -> torch.Tensor:
-    return torch.empty(shape, dtype=dtype or like.dtype, device=like.device)
+    return like.new_empty(shape, dtype=dtype)
 
 
 def _lengths(t: Optional[torch.Tensor], name: str, n: int, device: int) -> Optional[int]:
@@ -63,15 +64,14 @@ def _scale(scale: Optional[float], D: int) -> float:
 
 
 def _turned(x: torch.Tensor, positions: torch.Tensor, rotary: Rotary, inverse: int, out: Optional[torch.Tensor]) -> torch.Tensor:
-    dt, dev = _first(x, "x", 3)
+    shape, ldx, dt, dev = _first(x, "x", 3)
     if dev != _current_device():
         with torch.cuda.device(dev):
             return _turned(x, positions, rotary, inverse, out)
-    N, H, D = x.shape
-    ldx = _heads(x, "x", x.shape, dt, dev)
+    N, H, D = shape
     if out is None:
-        out = _new((N, H, D), x)
-    ldy = _heads(out, "out", x.shape, dt, dev)
+        out = _new(shape, x)
+    ldy = _heads(out, "out", shape, dt, dev)
     _check(lib.antdt_rotary(x.data_ptr(), *ldx, N, H, D, _DTYPES[dt], _vector(positions, "positions", N, torch.int32, dev), rotary._on(dev),
                             inverse, out.data_ptr(), *ldy, _stream(dev)))
     return out
@@ -89,20 +89,21 @@ def rotary_gradient(dy: torch.Tensor, positions: torch.Tensor, rotary: Rotary, o
 
 def _cache(k_cache: torch.Tensor, v_cache: torch.Tensor, dtype: torch.dtype, device: int):
     """(shape, strides) of the two caches."""
-    if len(k_cache.shape) != 4:
-        raise ValueError(f"k_cache: [pages, page size, heads, D], not {tuple(k_cache.shape)}")
-    s = _heads(k_cache, "k_cache", k_cache.shape, dtype, device)
-    if _heads(v_cache, "v_cache", k_cache.shape, dtype, device) != s:
+    shape, s, dt, dev = _first(k_cache, "k_cache", 4)
+    if dt is not dtype or dev != device:
+        raise ValueError(f"k_cache: {dt} on device {dev}, the tokens {dtype} on device {device}")
+    if _heads(v_cache, "v_cache", shape, dtype, device) != s:
         raise ValueError("k_cache and v_cache: one layout")
-    return k_cache.shape, s
+    return shape, s
 
 
 def _table(table: torch.Tensor, device: int) -> Tuple[int, int, int]:
     """(sequences, columns, leading dimension) of a cache's table."""
-    if len(table.shape) != 2 or table.dtype is not torch.int32 or table.get_device() != device or (table.shape[1] > 1 and table.stride(1) != 1):
+    shape, s = table.shape, table.stride()
+    if len(shape) != 2 or table.dtype is not torch.int32 or table.get_device() != device or (s[1] != 1 and shape[1] > 1):
         raise ValueError(f"table: int32 [sequences, pages of one], neighbours in a row, on device {device}")
-    B, W = table.shape
-    return B, W, table.stride(0) if B > 1 else W
+    B, W = shape
+    return B, W, s[0] if B > 1 else W
 
 
 def cache_append(k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, table: torch.Tensor, lengths: torch.Tensor,
@@ -111,12 +112,12 @@ def cache_append(k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_cach
     """New tokens' k and v [N, heads, D] to the caches [pages, page size, heads, D], k turned by its positions.  Tokens offsets[b] .. offsets[b + 1] - 1 (or
     token b) are the last ones of sequence b, whose lengths[b] counts them in and whose pages are table[b].  Returns the queries `q` [N, q heads, D] of the
     same tokens turned likewise (to `q_out`, which may be q), None without."""
-    dt, dev = _first(k, "k", 3)
+    shape, ldk, dt, dev = _first(k, "k", 3)
     if dev != _current_device():
         with torch.cuda.device(dev):
             return cache_append(k, v, k_cache, v_cache, table, lengths, offsets, rotary, q, q_out)
-    N, H, D = k.shape
-    ldk, ldv = _heads(k, "k", k.shape, dt, dev), _heads(v, "v", k.shape, dt, dev)
+    N, H, D = shape
+    ldv = _heads(v, "v", shape, dt, dev)
     (pages, page, CH, CD), ldc = _cache(k_cache, v_cache, dt, dev)
     if (CH, CD) != (H, D):
         raise ValueError(f"k_cache: heads {CH} x {CD}, k has {H} x {D}")
@@ -142,19 +143,18 @@ def cache_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tenso
                     scale: Optional[float] = None, out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
     """softmax(scale q k^T) v of one token of each sequence, q [B, q heads, D], over the lengths[b] tokens that the caches hold of it
     (see cache_append).  scale: D^-1/2 unless given."""
-    dt, dev = _first(q, "q", 3)
+    shape, ldq, dt, dev = _first(q, "q", 3)
     if dev != _current_device():
         with torch.cuda.device(dev):
             return cache_attention(q, k_cache, v_cache, table, lengths, scale, out, workspace)
-    B, HQ, D = q.shape
-    ldq = _heads(q, "q", q.shape, dt, dev)
+    B, HQ, D = shape
     (pages, page, H, CD), ldc = _cache(k_cache, v_cache, dt, dev)
     TB, W, ldt = _table(table, dev)
     if CD != D or TB != B:
         raise ValueError(f"q: {B} sequences of heads of {D}, the cache has {TB} of {CD}")
     if out is None:
-        out = _new((B, HQ, D), q)
-    ldo = _heads(out, "out", q.shape, dt, dev)
+        out = _new(shape, q)
+    ldo = _heads(out, "out", shape, dt, dev)
     held, ws, n = _workspace(workspace, _bytes("antdt_cache_attention_bytes", B, HQ, H, D, _DTYPES[dt]), q)
     _check(lib.antdt_cache_attention(q.data_ptr(), *ldq, k_cache.data_ptr(), v_cache.data_ptr(), *ldc, pages, page, table.data_ptr(), ldt, B, W,
                                      _vector(lengths, "lengths", B, torch.int32, dev), HQ, H, D, _DTYPES[dt],
@@ -175,13 +175,13 @@ def _stats(stats: torch.Tensor, B: int, S: int, H: int, device: int) -> int:
     return stats.data_ptr()
 
 
-def _shapes(q: torch.Tensor, k: torch.Tensor):
-    """(dtype, device, B, S, q heads, D, T, heads)."""
-    dt, dev = _first(q, "q", 4)
-    B, S, HQ, D = q.shape
-    if len(k.shape) != 4 or k.shape[0] != B or k.shape[3] != D:
-        raise ValueError(f"k: shape {tuple(k.shape)}, expected ({B}, keys, heads, {D})")
-    return dt, dev, B, S, HQ, D, k.shape[1], k.shape[2]
+def _sides(q: torch.Tensor, k: torch.Tensor):
+    """(shape of the queries and of the keys, their strides, dtype, device)."""
+    qs, ldq, dt, dev = _first(q, "q", 4)
+    ks = k.shape
+    if len(ks) != 4 or ks[0] != qs[0] or ks[3] != qs[3]:
+        raise ValueError(f"k: shape {tuple(ks)}, expected ({qs[0]}, keys, heads, {qs[3]})")
+    return qs, ks, ldq, _heads(k, "k", ks, dt, dev), dt, dev
 
 
 def cross_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_lengths: Optional[torch.Tensor] = None,
@@ -189,14 +189,15 @@ def cross_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_lengths
                     stats: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
     """softmax(scale q k^T) v of queries [B, S, q heads, D] over keys and values [B, T, heads, D].  q_lengths and k_lengths (int32 [B]): rows that an
     entry has; queries behind them have zeros.  scale: D^-1/2 unless given.  `stats` (see cross_attention_stats) is filled for cross_attention_backward."""
-    dt, dev, B, S, HQ, D, T, H = _shapes(q, k)
+    qs, ks, ldq, ldk, dt, dev = _sides(q, k)
     if dev != _current_device():
         with torch.cuda.device(dev):
             return cross_attention(q, k, v, q_lengths, k_lengths, scale, out, stats, workspace)
-    ldq, ldk, ldv = _heads(q, "q", q.shape, dt, dev), _heads(k, "k", k.shape, dt, dev), _heads(v, "v", k.shape, dt, dev)
+    (B, S, HQ, D), (_, T, H, _) = qs, ks
+    ldv = _heads(v, "v", ks, dt, dev)
     if out is None:
-        out = _new((B, S, HQ, D), q)
-    ldo = _heads(out, "out", q.shape, dt, dev)
+        out = _new(qs, q)
+    ldo = _heads(out, "out", qs, dt, dev)
     held, ws, n = _workspace(workspace, _bytes("antdt_cross_attention_bytes", B, S, T, HQ, H, D, _DTYPES[dt]), q)
     _check(lib.antdt_cross_attention(q.data_ptr(), *ldq, k.data_ptr(), *ldk, v.data_ptr(), *ldv, B, S, T, HQ, H, D, _DTYPES[dt],
                                      _lengths(q_lengths, "q_lengths", B, dev), _lengths(k_lengths, "k_lengths", B, dev),
@@ -211,16 +212,16 @@ def cross_attention_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tenso
                              workspace: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
     """(dq, dk, dv) of cross_attention from the gradient of its result; the other arguments as it was given and left them.  In bf16 the gradients
     of the scores, operands of the products, are rounded to bf16 too."""
-    dt, dev, B, S, HQ, D, T, H = _shapes(q, k)
+    qs, ks, ldq, ldk, dt, dev = _sides(q, k)
     if dev != _current_device():
         with torch.cuda.device(dev):
             return cross_attention_backward(dout, q, k, v, out, stats, q_lengths, k_lengths, scale, dq, dk, dv, workspace)
-    ldq, ldk, ldv = _heads(q, "q", q.shape, dt, dev), _heads(k, "k", k.shape, dt, dev), _heads(v, "v", k.shape, dt, dev)
-    ldo, ldg = _heads(out, "out", q.shape, dt, dev), _heads(dout, "dout", q.shape, dt, dev)
-    dq = _new((B, S, HQ, D), q) if dq is None else dq
-    dk = _new((B, T, H, D), q) if dk is None else dk
-    dv = _new((B, T, H, D), q) if dv is None else dv
-    lddq, lddk, lddv = _heads(dq, "dq", q.shape, dt, dev), _heads(dk, "dk", k.shape, dt, dev), _heads(dv, "dv", k.shape, dt, dev)
+    (B, S, HQ, D), (_, T, H, _) = qs, ks
+    ldv, ldo, ldg = _heads(v, "v", ks, dt, dev), _heads(out, "out", qs, dt, dev), _heads(dout, "dout", qs, dt, dev)
+    dq = _new(qs, q) if dq is None else dq
+    dk = _new(ks, q) if dk is None else dk
+    dv = _new(ks, q) if dv is None else dv
+    lddq, lddk, lddv = _heads(dq, "dq", qs, dt, dev), _heads(dk, "dk", ks, dt, dev), _heads(dv, "dv", ks, dt, dev)
     held, ws, n = _workspace(workspace, _bytes("antdt_cross_attention_backward_bytes", B, S, T, HQ, H, D, _DTYPES[dt]), q)
     _check(lib.antdt_cross_attention_backward(dout.data_ptr(), *ldg, q.data_ptr(), *ldq, k.data_ptr(), *ldk, v.data_ptr(), *ldv, out.data_ptr(),
                                               *ldo, _stats(stats, B, S, HQ, dev), B, S, T, HQ, H, D, _DTYPES[dt],
