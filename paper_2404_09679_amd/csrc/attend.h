@@ -52,7 +52,7 @@ struct HeadTile {
   static constexpr int STEP = Core<T>::STEP, PITCH = DP * (int)sizeof(T) / 16, ROW = DP * (int)sizeof(T);   // slots and bytes of a row
   // Along a row 16 lanes read one slot of 16 rows, down a column (bf16) 32 lanes four neighbouring slots of four rows: slots that have to differ modulo
   // 16 (256 bytes, all banks).
-  static __device__ __forceinline__ int swizzle(int r) {
+  static __host__ __device__ __forceinline__ constexpr int swizzle(int r) {
     if (PITCH >= 16) return sizeof(T) == 2 ? ((r & 3) << 2) | ((r >> 2) & 3) : r & 15;
     if (PITCH == 8) return sizeof(T) == 2 ? (((r >> 1) & 1) << 2) | ((r >> 2) & 3) : (r >> 1) & 7;
     return (r >> 2) & 3;
@@ -113,24 +113,40 @@ struct TileLoad {
   typedef HeadTile<T, DP> Tile;
   static constexpr int BYTES = ROWS * Tile::ROW, PIECES = BYTES / 16 / THREADS;
   static_assert(PIECES * THREADS * 16 == BYTES, "tile / thread count");
-  int r[PIECES], c[PIECES];   // row and byte of each piece
-  int width;                  // bytes of a row that exist
-  __device__ __forceinline__ TileLoad(int tid, int D) : width(D * (int)sizeof(T)) {
-#pragma unroll
-    for (int i = 0; i < PIECES; ++i) {
-      const int s = tid + i * THREADS;
-      r[i] = s / Tile::PITCH;
-      c[i] = ((s % Tile::PITCH) ^ Tile::swizzle(r[i])) * 16;
-    }
+  static constexpr int STRIDE = THREADS / Tile::PITCH;   // rows from one piece to the next
+  int row, column, width;   // of the first piece, column in bytes; bytes of a row that exist
+  __device__ __forceinline__ TileLoad(int tid, int D) : row(tid / Tile::PITCH), column((tid % Tile::PITCH ^ Tile::swizzle(row)) * 16), width(D * (int)sizeof(T)) {}
+  // (the permutation of a row is the exclusive or of those of its bits, and the first piece's row is below STRIDE)
+  static __host__ __device__ __forceinline__ constexpr int turn(int i) { return Tile::swizzle(i * STRIDE) * 16; }
+  static constexpr bool alike() {
+    for (int i = 1; i < PIECES; ++i)
+      if (turn(i)) return false;
+    return true;
   }
   // Rows t0 .. of `x` to LDS address `lds` (of the thread's wavefront); zeros from row `end` on.  What lies behind a row's end stays as it is: every
-  // row's columns take part in each load, so a wavefront always has as many under way as it has pieces.
+  // row's columns take part in each load, so a wavefront always has as many under way as it has pieces.  Of a tile within the rows, a lane's place in it
+  // is one number for all pieces, the rest is the wavefront's (forward, 128 bf16 columns, 8 x 2048 queries and keys, 16 heads: 298-318 us for 330-340).
   __device__ __forceinline__ void operator()(const Rows& x, int64_t t0, int64_t end, uint32_t lds) const {
     const char* base = x.p + t0 * x.ld;
+    if (t0 + ROWS <= end && x.ld < 1 << 24) {
+      const uint32_t to_row = (uint32_t)row * (uint32_t)x.ld;
+      if constexpr (alike()) {
+        if (column < width) {
 #pragma unroll
-    for (int i = 0; i < PIECES; ++i) {
-      const char* src = t0 + r[i] < end ? base + r[i] * x.ld + c[i] : reinterpret_cast<const char*>(mfma_zero16);
-      if (c[i] < width) load_lds16(src, lds + i * (THREADS * 16));
+          for (int i = 0; i < PIECES; ++i) load_lds16(base + i * STRIDE * x.ld, to_row + column, lds + i * (THREADS * 16));
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i)
+          if ((column ^ turn(i)) < width) load_lds16(base + i * STRIDE * x.ld, to_row + (column ^ turn(i)), lds + i * (THREADS * 16));
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < PIECES; ++i) {
+        const int r = row + i * STRIDE, c = column ^ turn(i);
+        const char* src = t0 + r < end ? base + r * x.ld + c : reinterpret_cast<const char*>(mfma_zero16);
+        if (c < width) load_lds16(src, lds + i * (THREADS * 16));
+      }
     }
   }
 };

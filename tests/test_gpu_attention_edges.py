@@ -185,3 +185,15 @@ def test_entries_in_another_order(B, S, T, HQ, H, D, dtype):
     assert all(torch.equal(x[torch.as_tensor(order, device=DEV)], y) for x, y in zip(got, other))
     full = [normal(rng, *x.shape, dtype=dtype) for x in (q, k, v, g)]
     assert all(torch.equal(x, y) for x, y in zip(cross(*full, None, ints([T] * B)), cross(*full, ints([S] * B), None)))
+
+
+@pytest.mark.parametrize("S,far", [(3, 2 ** 22 - 16), (70, 2 ** 22), (70, 2 ** 22 - 16)])
+def test_rows_far_apart(S, far):
+    """Rows of 2^24 bytes and a little less from one to the next: offsets within a tile in 32 bits and in 64."""
+    rng = np.random.default_rng(S)
+    q, k, v, g, ql, kl = cross_inputs(rng, 1, S, 69, 2, 1, 32, "", "f32")
+    want = cross(q, k, v, g, None, None)
+    room = torch.empty(71, far, device=DEV)
+    assert room.stride(0) == far
+    q2, k2, v2, g2 = (room[:x.shape[1], i * 256:i * 256 + x[0, 0].numel()].view(1, x.shape[1], *x.shape[2:]).copy_(x) for i, x in enumerate((q, k, v, g)))
+    assert all(torch.equal(x, y) for x, y in zip(cross(q2, k2, v2, g2, None, None), want))
