@@ -6,7 +6,8 @@ namespace {
 
 // A block has queries of a head; tiles of keys and values go through LDS, the next one's loads under way.  A wavefront's 32 queries take a pass over the
 // vector units (maximum, exponential, sum) for each over the matrix core, about as long; two wavefronts on a SIMD have them at the same time.  8 ragged
-// histories of 2048 queries and 4096 keys, 16 and 4 heads of 128 bf16 columns: 381 GFLOP in 400 us, an eighth of it the last blocks, when not all compute units have one.
+// histories of 2048 queries and 4096 keys, 16 and 4 heads of 128 bf16 columns: 381 GFLOP in 400-430 us (by the clock that
+// power leaves), an eighth of it the last blocks, when not all compute units have one.
 template <typename W>
 __global__ __launch_bounds__(W::THREADS, W::PER_CU) void cross_forward_kernel(CrossArgs a) {
   typedef typename W::T T;

@@ -297,9 +297,9 @@ __device__ __forceinline__ void dkv_block(const CrossArgs& a, int index, char* l
 
 // Both in one launch: blocks of keys first, which take longer, so that blocks of queries fill the chip while the last of them run (8 ragged histories of
 // 2048 queries and 4096 keys, 16 and 4 heads of 128 bf16 columns: 640 + 980 us in two launches, 1460 so; 13 of 77 and 777, 6 and 2 heads of 64: 13 + 16,
-// so 18; with what was saved since 1260 and 16.5).  Wavefronts behind a kind's own leave at once.
+// so 18; with what was saved since 1260-1320 and 16.5).  Wavefronts behind a kind's own leave at once.
 // Bound by the matrix cores, whose operands LDS and the vector units have to keep up with: 14 products of 18 that the large case computes in all run at
-// 1060 TFLOP/s there (a library product of 8192 cubed: 1131).
+// 1010-1060 TFLOP/s there (a library product of 8192 cubed: 1131).
 template <typename WQ, typename WK, bool HELD>
 __global__ __launch_bounds__(256, (WQ::PER_CU < WK::PER_CU ? WQ::PER_CU : WK::PER_CU)) void cross_backward_kernel(CrossArgs a) {
   extern __shared__ __attribute__((aligned(1024))) char lds[];
