@@ -252,12 +252,12 @@ struct Shape {
 // Microseconds that a wavefront takes for 32 queries and 32 keys in the forward pass, alone on its SIMD (measured; of a multiple of 32 columns).
 inline double tile_us(const Shape& z) {
   const int columns = (int)div_up(z.D, 32) - 1;
-  constexpr double BF16[] = {0.6, 0.9, 1.3, 1.6}, F32[] = {1.7, 3.1, 4.3, 5.5};
+  constexpr double BF16[] = {0.53, 0.71, 1.10, 1.22}, F32[] = {1.53, 2.88, 4.12, 4.90};
   return z.dtype == ANTDT_F32 ? F32[columns] : BF16[columns];
 }
 // Results' rows in blocks of 128, or of 32 whose `waves` wavefronts share the other side's rows (`tiles` of 32), or these again in parts.
-//  - Blocks of 32 as long as all of them run at once: `most` of them.  bf16, 1024 queries and keys, 64 columns, us of blocks of 128 / 32: 16 heads 22 / 15,
-//    32 heads 23.5 / 28; gradient of the queries 27 / 19, 28 / 32; 128 columns, gradient of the keys: 16 heads 57 / 44, 32 heads 62 / 90.
+//  - Blocks of 32 as long as all of them run at once: `most` of them.  bf16, 1024 queries and keys, 64 columns, us of blocks of 128 / 32: 16 heads 20 / 15,
+//    32 heads 22 / 26; gradient of the queries 24 / 16, 26 / 30; 128 columns, gradient of the keys: 16 heads 60 / 46, 32 heads 63 / 89.
 //  - Parts where their shorter way outweighs the launch that adds them up, about 6 us.
 inline Plan cross_plan(int64_t heads, int64_t rows, int64_t tiles, int64_t most, int waves, double us, bool parted) {
   Plan p = {false, (int32_t)div_up(rows, 128), 1, 0};
@@ -278,23 +278,25 @@ inline int64_t delta_bytes(const Shape& z) { return div_up(z.B * z.S * z.q_heads
 inline bool wide(const Shape& z) { return z.dtype == ANTDT_BF16 && z.D > 64; }          // (a block of 32 fills a compute unit's LDS)
 inline int key_waves(const Shape& z) { return z.dtype == ANTDT_F32 && z.D > 64 ? 2 : 4; }
 inline Plan forward_plan(const Shape& z) { return cross_plan(z.B * z.q_heads, z.S, div_up(z.T, 32), wide(z) ? 256 : 512, key_waves(z), tile_us(z), false); }
-inline Plan dq_plan(const Shape& z) { return cross_plan(z.B * z.q_heads, z.S, div_up(z.T, 32), wide(z) ? 256 : 512, key_waves(z), 1.3 * tile_us(z), true); }
-inline Plan dkv_plan(const Shape& z) { return cross_plan(z.B * z.heads, z.T, div_up(z.S, 32) * (z.q_heads / z.heads), wide(z) ? 256 : 512, key_waves(z), 2.0 * tile_us(z), true); }
+inline Plan dq_plan(const Shape& z) { return cross_plan(z.B * z.q_heads, z.S, div_up(z.T, 32), wide(z) ? 256 : 512, key_waves(z), 1.6 * tile_us(z), true); }
+inline Plan dkv_plan(const Shape& z) { return cross_plan(z.B * z.heads, z.T, div_up(z.S, 32) * (z.q_heads / z.heads), wide(z) ? 256 : 512, key_waves(z), 2.6 * tile_us(z), true); }
 // Whether entries are gone through by length: costs a block about a microsecond and shortens the end by some of the longest block's time
 // (200 entries of 1 to 300, 8 and 2 heads of 64: 41 / 105 us, by length 43 / 116).
 inline bool longest_first(const Shape& z, bool ragged, int64_t blocks, int at_once) {
   const double rounds = (double)blocks / at_once;
-  return ragged && z.B > 1 && rounds > 1.0 && tile_us(z) * div_up(std::max(z.S, z.T), 32) > 4.0 * rounds;
+  return ragged && z.B > 1 && rounds > 1.0 && tile_us(z) * div_up(std::max(z.S, z.T), 32) > 3.0 * rounds;
 }
 // Whether the forward pass goes by an equal share of all keys to each wavefront (stream.hip) instead, by the time that both would take: that costs a
-// second launch, about 9 us, and the tiles of 32 keys and 16 or 32 queries of a key's heads take 1.4 times as long.  us by blocks / shares, 8 heads of
-// 64 bf16 columns: 1 query, 500 keys 8 / 16, 2000 19 / 15, 8000 61 / 16; 4 x 128 queries, 2000 keys 20 / 31, 8000 75 / 64; fp32, 1 query, 500 keys 16 / 14.
+// second launch, and a tile's keys and values that nobody else reads.  us by blocks / shares of 500, 2000 and 8000 keys, 8 heads: 64 bf16 columns, 1 query 7 / 18,
+// 16 / 17, 49 / 21; 4 x 128 queries 8 / 21, 17 / 27, 61 / 55; 128 columns 10 / 17, 25 / 17, 84 / 22 and 12 / 25, 29 / 41, 96 / 97; 64 fp32 columns 16 / 18, 49 / 16,
+// 184 / 17 and 17 / 26, 55 / 46, 195 / 114.
 inline bool cross_streams(const Shape& z) {
   if (z.B == 0 || z.S == 0 || !stream_fits(z.B, z.S, z.T, z.q_heads, z.heads)) return false;
   const int64_t tiles = div_up(z.T, 32), rows = z.S * (z.q_heads / z.heads), row_tiles = rows <= 16 ? 1 : div_up(rows, 32);
   const Plan p = forward_plan(z);
-  const double blocks = p.split ? (double)div_up(tiles, key_waves(z)) : std::max(1.0, p.blocks / 512.0) * tiles * 1.1;
-  return 9.0 + 1.4 * tile_us(z) * z.B * z.heads * row_tiles * tiles / 1024 < tile_us(z) * blocks;
+  const double blocks = p.split ? div_up(tiles, key_waves(z)) * (p.blocks < 128 ? 1.0 : 1.25) : std::max(1.0, p.blocks / 512.0) * tiles;
+  const double shares = (z.dtype == ANTDT_F32 ? 1.3 : 2.0) * z.B * z.heads * row_tiles * tiles / 1024;
+  return 16.0 + tile_us(z) * shares < 4.5 + tile_us(z) * blocks;
 }
 inline int cross_sizes(const char* call, const Shape& z) {
   OP_TRY(op_head_sizes(call, z.q_heads, z.heads, z.D, z.dtype));
