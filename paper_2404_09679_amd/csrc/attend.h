@@ -123,6 +123,13 @@ struct TileLoad {
       if (turn(i)) return false;
     return true;
   }
+  // f(row of the tile, byte in it, byte of LDS) of each piece that exists.
+  template <typename F>
+  __device__ __forceinline__ void each(F f) const {
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i)
+      if ((column ^ turn(i)) < width) f(row + i * STRIDE, column ^ turn(i), i * (THREADS * 16));
+  }
   // Rows t0 .. of `x` to LDS address `lds` (of the thread's wavefront); zeros from row `end` on.  What lies behind a row's end stays as it is: every
   // row's columns take part in each load, so a wavefront always has as many under way as it has pieces.  Of a tile within the rows, a lane's place in it
   // is one number for all pieces, the rest is the wavefront's (forward, 128 bf16 columns, 8 x 2048 queries and keys, 16 heads: 298-318 us for 330-340).
@@ -231,8 +238,7 @@ struct StreamArgs {
   const int32_t* k_lengths;
   float* stats;                // [B, q_heads, S] or NULL, see cross_forward_kernel
   int64_t ldt, pages, B, S, T;
-  int32_t page, page_shift;    // t / page = t page_magic >> page_shift, t < 2^31
-  uint32_t page_magic;
+  Divisor page;                // tokens of a page
   int32_t q_heads, heads, group, D;
   int32_t row_tile, row_tiles, rows;   // a key head's queries (row r: query r / group of head r mod group) in 16s or 32s; rows of a partial result
   int32_t waves;               // of the launch

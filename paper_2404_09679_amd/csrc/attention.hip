@@ -8,7 +8,8 @@ namespace {
 // vector units (maximum, exponential, sum) for each over the matrix core, about as long; two wavefronts on a SIMD have them at the same time.  8 ragged
 // histories of 2048 queries and 4096 keys, 16 and 4 heads of 128 bf16 columns: 381 GFLOP in 400-430 us (by the clock that
 // power leaves), an eighth of it the last blocks, when not all compute units have one.
-template <typename W>
+// PAGED: keys and values are a cache's, the user's pages looked up before the first tile.
+template <typename W, bool PAGED>
 __global__ __launch_bounds__(W::THREADS, W::PER_CU) void cross_forward_kernel(CrossArgs a) {
   typedef typename W::T T;
   typedef typename W::Tile Tile;
@@ -35,14 +36,39 @@ __global__ __launch_bounds__(W::THREADS, W::PER_CU) void cross_forward_kernel(Cr
     __syncthreads();
   }
   const typename W::Load load(W::SPLIT ? lane : threadIdx.x, a.D);
-  const Rows k = a.k.rows(b, h / a.group), v = a.v.rows(b, h / a.group);
+  const Rows k = a.k.rows(PAGED ? 0 : b, h / a.group), v = a.v.rows(PAGED ? 0 : b, h / a.group);
+  int* const pages = reinterpret_cast<int*>(lds + F::LDS);
+  // Page of key t, below 0 where there is none.
+  auto page_of = [&](int64_t t, uint32_t& row) {
+    const uint32_t i = a.page((uint32_t)t);
+    row = (uint32_t)t - i * a.page.d;
+    return t < k_len ? pages[i] : -1;
+  };
+  if constexpr (PAGED) {
+    const int n = (int)a.page((uint32_t)k_len - 1) + 1;
+    for (int i = threadIdx.x; i < n; i += W::THREADS) {
+      const int e = a.table[b * a.ldt + i];
+      pages[i] = e < a.pages ? e : -1;
+    }
+    __syncthreads();
+  }
   const uint32_t ring0 = lds_address(lds) + (W::SPLIT ? wave * F::RING : 0), lds0 = ring0 + (W::SPLIT ? 0 : wave * 1024);
   constexpr int64_t STEP = (W::SPLIT ? W::WAVES : 1) * BT;
   const int64_t t0 = W::SPLIT ? wave * BT : 0;
   int64_t asked = t0;
   auto issue = [&](uint32_t to) {
-    load(k, asked, k_len, lds0 + to);
-    load(v, asked, k_len, lds0 + to + W::Load::BYTES);
+    if constexpr (PAGED) {
+      load.each([&](int row, int column, uint32_t at) {
+        uint32_t in;
+        const int e = page_of(asked + row, in);
+        const int64_t off = e * a.k.s.b + in * k.ld + column;
+        load_lds16(e < 0 ? reinterpret_cast<const char*>(mfma_zero16) : k.p + off, lds0 + to + at);
+        load_lds16(e < 0 ? reinterpret_cast<const char*>(mfma_zero16) : v.p + off, lds0 + to + W::Load::BYTES + at);
+      });
+    } else {
+      load(k, asked, k_len, lds0 + to);
+      load(v, asked, k_len, lds0 + to + W::Load::BYTES);
+    }
     asked += STEP;
   };
   typename C::Fragment q[W::STEPS];
@@ -66,7 +92,15 @@ __global__ __launch_bounds__(W::THREADS, W::PER_CU) void cross_forward_kernel(Cr
     auto value = [&](int i) { return Tile::down(tv, i / (W::DT * W::PACKS) * 32, i / W::DT % W::PACKS, i % W::DT); };
     Fragments<typename C::Fragment, BT / 32 * W::PACKS * W::DT, W::AHEAD> values;
     values.start(value);   // (there when the probabilities are)
-    if (t + BT > k_len) {
+    if constexpr (PAGED) {
+      uint32_t in;
+      const uint32_t some = (uint32_t)__ballot(page_of(t + (lane & 31), in) >= 0);   // keys of the tile that there are
+      if (some != ~0u) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (!(some >> (8 * (e >> 2) + 4 * half + (e & 3)) & 1)) s[0][e] = -INFINITY;
+      }
+    } else if (t + BT > k_len) {
       const int left = (int)(k_len - t) - 4 * half;
 #pragma unroll
       for (int j = 0; j < BT / 32; ++j)
@@ -134,18 +168,25 @@ __global__ __launch_bounds__(W::THREADS, W::PER_CU) void cross_forward_kernel(Cr
   }
 }
 
-template <typename W>
+template <typename W, bool PAGED = false>
 hipError_t launch_forward(CrossArgs a, const Shape& z, const Plan& pl, hipStream_t s) {
   static std::atomic<uint64_t> allowed{0};
-  const hipError_t e = allow_lds(cross_forward_kernel<W>, KeyTiles<W>::LDS, 0, allowed);
+  constexpr int LDS = KeyTiles<W>::LDS + (PAGED ? TABLE * 4 : 0);
+  const hipError_t e = allow_lds(cross_forward_kernel<W, PAGED>, LDS, 0, allowed);
   if (e != hipSuccess) return e;
   a.queries = pl.share(nullptr);
   a.longest_first = longest_first(z, a.k_lengths || a.q_lengths, pl.blocks, 256 * W::PER_CU);
-  hipLaunchKernelGGL(cross_forward_kernel<W>, dim3((unsigned)pl.blocks), dim3(W::THREADS), KeyTiles<W>::LDS, s, a);
+  hipLaunchKernelGGL((cross_forward_kernel<W, PAGED>), dim3((unsigned)pl.blocks), dim3(W::THREADS), LDS, s, a);
   return hipGetLastError();
 }
 
 }  // namespace
+
+hipError_t launch_cache_blocks(const CrossArgs& a, const Shape& z, hipStream_t s) {
+  return by_columns(z.dtype, (int)z.D, [&](auto way, auto cols) {
+    return launch_forward<typename decltype(way)::template SplitKeys<decltype(cols)::value>, true>(a, z, forward_plan(z), s);
+  });
+}
 }  // namespace antdt
 
 using namespace antdt;

@@ -31,6 +31,10 @@ struct CrossArgs {
   int32_t longest_first;   // whether batch entries are gone through by length, see entry_of
   float scale, scale2;   // scale2: scale log2 e
   Share queries, keys;   // blocks of queries, and (backward) of keys
+  // Of a cache, whose keys and values are [pages, page, heads, D]:
+  const int32_t* table;
+  int64_t ldt, pages;
+  Divisor page;
 };
 
 // Own loads but the last N have arrived and own reads of LDS are done; BLOCK: then everybody's.
@@ -286,18 +290,31 @@ inline bool longest_first(const Shape& z, bool ragged, int64_t blocks, int at_on
   const double rounds = (double)blocks / at_once;
   return ragged && z.B > 1 && rounds > 1.0 && tile_us(z) * div_up(std::max(z.S, z.T), 32) > 3.0 * rounds;
 }
-// Whether the forward pass goes by an equal share of all keys to each wavefront (stream.hip) instead, by the time that both would take: that costs a
-// second launch, and a tile's keys and values that nobody else reads.  us by blocks / shares of 500, 2000 and 8000 keys, 8 heads: 64 bf16 columns, 1 query 7 / 18,
-// 16 / 17, 49 / 21; 4 x 128 queries 8 / 21, 17 / 27, 61 / 55; 128 columns 10 / 17, 25 / 17, 84 / 22 and 12 / 25, 29 / 41, 96 / 97; 64 fp32 columns 16 / 18, 49 / 16,
-// 184 / 17 and 17 / 26, 55 / 46, 195 / 114.
-inline bool cross_streams(const Shape& z) {
+// Whether an equal share of all keys to each wavefront (stream.hip) takes less time than the forward pass's blocks: it has a second launch, `fixed` us in all, and
+// tiles that nobody else reads, each `share` times tile_us on one of 1024 SIMDs; a block's take `own` times that.
+inline bool by_shares(const Shape& z, double fixed, double share, double own) {
   if (z.B == 0 || z.S == 0 || !stream_fits(z.B, z.S, z.T, z.q_heads, z.heads)) return false;
   const int64_t tiles = div_up(z.T, 32), rows = z.S * (z.q_heads / z.heads), row_tiles = rows <= 16 ? 1 : div_up(rows, 32);
   const Plan p = forward_plan(z);
   const double blocks = p.split ? div_up(tiles, key_waves(z)) * (p.blocks < 128 ? 1.0 : 1.25) : std::max(1.0, p.blocks / 512.0) * tiles;
-  const double shares = (z.dtype == ANTDT_F32 ? 1.3 : 2.0) * z.B * z.heads * row_tiles * tiles / 1024;
-  return 16.0 + tile_us(z) * shares < 4.5 + tile_us(z) * blocks;
+  const double shares = (double)z.B * z.heads * row_tiles * tiles / 1024;
+  return fixed + tile_us(z) * share * shares < 4.5 + tile_us(z) * own * blocks;
 }
+// us by blocks / shares of 500, 2000 and 8000 keys, 8 heads: 64 bf16 columns, 1 query 7 / 18, 16 / 17, 49 / 21; 4 x 128 queries 8 / 21, 17 / 27, 61 / 55; 128
+// columns 10 / 17, 25 / 17, 84 / 22 and 12 / 25, 29 / 41, 96 / 97; 64 fp32 columns 16 / 18, 49 / 16, 184 / 17 and 17 / 26, 55 / 46, 195 / 114.
+inline bool cross_streams(const Shape& z) { return by_shares(z, 16.0, z.dtype == ANTDT_F32 ? 1.3 : 2.0, 1.0); }
+// The same for one token of each user over a cache of room for T: the tokens of a key's heads are one block's rows, which looks up the user's pages once.
+// us of 100, 500, 1000 and 2000 tokens in pages of 16: 16 users, 16 and 4 heads of 64 bf16 columns 5.5 / 16, 9 / 16, 13 / 17, 23 / 17; 64 users of 128
+// columns 8 / 15, 17 / 20, 28 / 29, 49 / 50; fp32, 64 users of 64 columns 8 / 17, 23 / 21, 40 / 30, 72 / 52.
+constexpr int TABLE = 2048;   // pages of a user, at most
+inline Shape cache_shape(int64_t B, int64_t T, int64_t q_heads, int64_t heads, int64_t D, int32_t dtype) {
+  return Shape{B, q_heads / heads, T, heads, heads, D, dtype};
+}
+inline bool cache_streams(const Shape& z, int64_t page) {
+  return !forward_plan(z).split || div_up(z.T, page) > TABLE || by_shares(z, 15.0, z.dtype == ANTDT_F32 ? 1.0 : 1.5, 1.5);
+}
+hipError_t launch_cache_blocks(const CrossArgs& a, const Shape& z, hipStream_t s);
+
 inline int cross_sizes(const char* call, const Shape& z) {
   OP_TRY(op_head_sizes(call, z.q_heads, z.heads, z.D, z.dtype));
   constexpr int64_t MOST = (1ll << 31) - 1;

@@ -9,6 +9,17 @@
 
 namespace antdt {
 
+// x / d of x < 2^31 without a division: x m >> 31 + s, where 2^s is d or the next larger power of two and m = 2^(31 + s) / d, rounded up.
+struct Divisor {
+  uint32_t d, m, s;
+  static Divisor of(uint32_t d) {
+    uint32_t s = 0;
+    while ((1u << s) < d) ++s;
+    return Divisor{d, (uint32_t)(((1ull << (31 + s)) + d - 1) / d), s};
+  }
+  __device__ __forceinline__ uint32_t operator()(uint32_t x) const { return (uint32_t)((uint64_t)x * m >> 31 >> s); }
+};
+
 // Elements from one batch, row and head to the next (0 where there is only one); a head's columns are neighbours.
 struct HeadStrides {
   int64_t b, l, h;

@@ -12,17 +12,6 @@ namespace {
 
 constexpr int WAVES = 4, MOST_TOKENS = 16, MOST_PAIRS = 512;   // of a wavefront, at a time
 
-// x / d of x < 2^31 without a division: x m >> 31 + s, where 2^s is d or the next larger power of two and m = 2^(31 + s) / d, rounded up.
-struct Divisor {
-  uint32_t d, m, s;
-  static Divisor of(uint32_t d) {
-    uint32_t s = 0;
-    while ((1u << s) < d) ++s;
-    return Divisor{d, (uint32_t)(((1ull << (31 + s)) + d - 1) / d), s};
-  }
-  __device__ __forceinline__ uint32_t operator()(uint32_t x) const { return (uint32_t)((uint64_t)x * m >> 31 >> s); }
-};
-
 // Some heads of every token: queries, keys or values.  A chunk is 16 columns of a head: 8 pairs, or columns that are copied.
 struct HeadsPart {
   const void* x;

@@ -8,7 +8,7 @@
 // Bound by memory, a key head's queries share what is read of it: one user's 131072 tokens (8 heads of 128 bf16 columns, 537 MB) 90 us (6.0 TB/s) and 5.5 to
 // join; 64 users of 16 to 8192 tokens (178 MB) 39 and 5.  Where there is little to read, by the chain of a wavefront's loads (lengths, page, rows) and
 // by its code's: one tile takes 10 us.
-#include "attend.h"
+#include "cross.h"
 #include "sort.h"
 
 namespace antdt {
@@ -196,7 +196,7 @@ __global__ __launch_bounds__(64 * WAVES, (Stream<T, DP, R>::PER_CU)) void stream
     const bool came = i0 > 0, goes = i1 < n;
 
     const int32_t* table = PAGED ? a.table + b * a.ldt : nullptr;
-    auto first_of = [&](uint32_t t) { return (uint32_t)((uint64_t)t * a.page_magic >> a.page_shift); };
+    auto first_of = [&](uint32_t t) { return a.page(t); };
     // The pages of tile i's rows, to LDS.
     auto pages = [&](uint32_t i) {
       load_lds4(table + first_of((uint32_t)min((int64_t)32 * i + (lane & 31), k_len - 1)), ring + F::PAGES + (i - i0) % F::AHEAD * 256);
@@ -231,7 +231,7 @@ __global__ __launch_bounds__(64 * WAVES, (Stream<T, DP, R>::PER_CU)) void stream
       if (PAGED) {
         const int e = *reinterpret_cast<const int*>(mine + F::PAGES + (i - i0) % F::AHEAD * 256 + lane * 4);
         x = x && e >= 0 && e < a.pages;
-        off = e * a.k.s.b + ((uint32_t)t - first_of((uint32_t)t) * (uint32_t)a.page) * a.k.s.l;
+        off = e * a.k.s.b + ((uint32_t)t - first_of((uint32_t)t) * a.page.d) * a.k.s.l;
       } else {
         off = t * kv.s.l;
       }
@@ -523,16 +523,22 @@ int antdt_cache_attention(const void* q, int64_t ldq, int64_t ldq_head, const vo
   OP_TRY(op_matrix(call, "lengths", lengths, B, 1, 1, 4));
   if (B == 0) return ANTDT_OK;
   OP_TRY(op_workspace(call, workspace, workspace_bytes, stream_bytes(B, 1, q_heads, heads, D)));
+  const Shape z = cache_shape(B, std::min<int64_t>(table_cols * page_size, (1ll << 31) - 1), q_heads, heads, D, dtype);
+  if (!cache_streams(z, page_size)) {
+    CrossArgs f = {};
+    f.q = {a.q.p, {a.q.s.b, a.q.s.h, a.q.s.h * (q_heads / heads)}};
+    f.out = {a.out.p, {a.out.s.b, a.out.s.h, a.out.s.h * (q_heads / heads)}};
+    f.k = a.k; f.v = a.v; f.k_lengths = lengths; f.S = z.S; f.T = z.T; f.B = (int)B;
+    f.q_heads = f.heads = (int)heads; f.group = 1; f.D = (int)D; f.units = (int)(B * heads); f.scale = scale; f.scale2 = scale * LOG2E;
+    f.table = table; f.ldt = ld_table; f.pages = pages; f.page = Divisor::of((uint32_t)page_size);
+    return op_hip(call, launch_cache_blocks(f, z, (hipStream_t)stream));
+  }
   static const int32_t none = 0;
   a.table = table_cols > 0 ? table : &none;   // (without columns no length is above 0, and nothing reads it)
   a.ldt = ld_table; a.pages = pages; a.k_lengths = lengths; a.B = B; a.S = 1;
-  a.T = std::min<int64_t>(table_cols * page_size, (1ll << 31) - 1);
+  a.T = z.T;
   if (!stream_fits(B, 1, a.T, q_heads, heads)) return op_fail(ANTDT_UNSUPPORTED, "%s: B heads table_cols page_size / 32: 2^31 or more", call);
-  a.page = (int)page_size;
-  int shift = 0;
-  while ((1ll << shift) < page_size) ++shift;
-  a.page_shift = 31 + shift;
-  a.page_magic = (uint32_t)((((__int128)1 << (31 + shift)) + page_size - 1) / page_size);
+  a.page = Divisor::of((uint32_t)page_size);
   a.q_heads = (int)q_heads; a.heads = (int)heads; a.group = (int)(q_heads / heads); a.D = (int)D; a.scale2 = scale * LOG2E;
   return op_hip(call, launch_stream(a, dtype, workspace, (hipStream_t)stream));
 }

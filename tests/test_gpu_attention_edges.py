@@ -7,7 +7,8 @@ import torch
 
 import attention_formulas as F
 import paper_2404_09679_amd as A
-from test_gpu_attention import DEV, DT, NAN, append_formula, cache_of, check_cross, check_decode, cross, cross_inputs, host, ints, normal, within
+from test_gpu_attention import (DEV, DT, NAN, append_formula, cache_of, check_cross, check_decode, cross, cross_inputs, decode_inputs, host, ints,
+                                normal, within)
 
 pytestmark = pytest.mark.gpu
 
@@ -197,3 +198,32 @@ def test_rows_far_apart(S, far):
     assert room.stride(0) == far
     q2, k2, v2, g2 = (room[:x.shape[1], i * 256:i * 256 + x[0, 0].numel()].view(1, x.shape[1], *x.shape[2:]).copy_(x) for i, x in enumerate((q, k, v, g)))
     assert all(torch.equal(x, y) for x, y in zip(cross(q2, k2, v2, g2, None, None), want))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("lengths,page,HQ,H,D", [([1, 64, 0, 33, 31], 16, 4, 4, 64), ([130, 7, 100], 5, 12, 2, 128), ([300, 299, 0, 1], 1, 66, 2, 32),
+                                                 ([65] * 30, 32, 8, 1, 96), ([450, 12], 100, 3, 1, 8), ([40], 16, 40, 1, 40)])
+def test_small_and_large_caches(lengths, page, HQ, H, D, dtype):
+    """The same tokens in a cache with room for hardly more, and in tables of thousands of pages; some of the pages are none."""
+    rng = np.random.default_rng(D)
+    kc, vc, table, dense, q = decode_inputs(rng, lengths, page, HQ, H, D, dtype, std=2.0)
+    gone = [(b, i) for b in range(len(lengths)) for i in range(-(-lengths[b] // page)) if lengths[b] > 64 and rng.random() < 0.2]
+    for n, (b, i) in enumerate(gone):
+        table[b, i] = (-1, len(kc), -2 ** 31, 2 ** 31 - 1)[n % 4]
+    for b, n in enumerate(lengths):
+        keep = torch.as_tensor([t for t in range(n) if (b, t // page) not in gone], dtype=torch.int64, device=DEV)
+        dense[b] = tuple(x[keep] for x in dense[b])
+    for cols in (0, 2050):
+        wide = np.pad(table, ((0, 0), (0, max(0, cols - table.shape[1]))), constant_values=-1)
+        got = A.cache_attention(q, kc, vc, ints(wide), ints(lengths))
+        check_decode(got, q, dense, dtype, D ** -0.5, cols)
+        assert torch.equal(A.cache_attention(q, kc, vc, ints(wide), ints(lengths), out=torch.full_like(q, 7.0)), got)
+    k, v = (torch.randn(3, 16, H, D, device=DEV).to(kc.dtype) for _ in range(2))      # scores of -infinity and NaN
+    k[0], k[2, 3] = -float("inf"), NAN
+    q = q[:1].abs() + 0.5
+    for cols in (3, 2050):
+        t = np.full((1, cols), -1)
+        t[0, :3] = [0, 1, 2]
+        out = [A.cache_attention(q, k, v, ints(t), ints([n])) for n in (16, 32, 48)]
+        assert not out[0].any() and bool(out[2].isnan().all())
+        check_decode(out[1], q, [(k[1], v[1])], dtype, D ** -0.5, "infinity")
