@@ -1,4 +1,5 @@
-// Attention of few queries over many keys: one new token of each user over a paged cache, or a few queries over an encoded history.
+// Attention of few queries over many keys: one new token of each user over a paged cache, or a few queries over an encoded history (where there are few
+// keys, by the blocks of attention.hip: cross_streams, cache_streams).
 //
 // Every wavefront reads an equal share of all the keys and values there are, whoever they belong to: the work is the list of 32-key tiles of all
 // sequences, heads and 32s of queries, cut into equal pieces (lengths are known to the device only, and differ).  A wavefront works alone: it moves
@@ -524,6 +525,7 @@ int antdt_cache_attention(const void* q, int64_t ldq, int64_t ldq_head, const vo
   if (B == 0) return ANTDT_OK;
   OP_TRY(op_workspace(call, workspace, workspace_bytes, stream_bytes(B, 1, q_heads, heads, D)));
   const Shape z = cache_shape(B, std::min<int64_t>(table_cols * page_size, (1ll << 31) - 1), q_heads, heads, D, dtype);
+  if (!stream_fits(B, 1, z.T, q_heads, heads)) return op_fail(ANTDT_UNSUPPORTED, "%s: B heads table_cols page_size / 32: 2^31 or more", call);
   if (!cache_streams(z, page_size)) {
     CrossArgs f = {};
     f.q = {a.q.p, {a.q.s.b, a.q.s.h, a.q.s.h * (q_heads / heads)}};
@@ -537,7 +539,6 @@ int antdt_cache_attention(const void* q, int64_t ldq, int64_t ldq_head, const vo
   a.table = table_cols > 0 ? table : &none;   // (without columns no length is above 0, and nothing reads it)
   a.ldt = ld_table; a.pages = pages; a.k_lengths = lengths; a.B = B; a.S = 1;
   a.T = z.T;
-  if (!stream_fits(B, 1, a.T, q_heads, heads)) return op_fail(ANTDT_UNSUPPORTED, "%s: B heads table_cols page_size / 32: 2^31 or more", call);
   a.page = Divisor::of((uint32_t)page_size);
   a.q_heads = (int)q_heads; a.heads = (int)heads; a.group = (int)(q_heads / heads); a.D = (int)D; a.scale2 = scale * LOG2E;
   return op_hip(call, launch_stream(a, dtype, workspace, (hipStream_t)stream));

@@ -299,3 +299,11 @@ def test_heads_without_columns():
     for name in ("antdt_cache_attention_bytes", "antdt_cross_attention_bytes"):
         assert getattr(lib, name)(1, *((1, 1) if "cross" in name else ()), 1, 1, 0, 0, C.byref(C.c_size_t())) == UNSUPPORTED
     assert T._scale(None, 0) == 1.0 and T._scale(None, 64) == 0.125 and T._scale(0.5, 64) == 0.5
+
+
+def test_caches_of_too_much_room():
+    """Few large pages or many: one limit."""
+    for page, cols in ((1 << 30, 2), (16, 1 << 27)):
+        rc = lib.antdt_cache_attention(PTR, 512, 64, PTR, PTR, page * 512, 512, 64, 5, page, PTR, cols, 8, cols, PTR, 8, 8, 64, 1, 0.125, 2 * PTR, 512, 64, PTR, 1 << 30,
+                                       None)
+        assert rc == UNSUPPORTED and "2^31" in message()
