@@ -6,7 +6,7 @@
 // its tiles to LDS, several ahead, and keeps the running maximum, sum and output of a softmax over its part of a sequence.  Where a sequence lies
 // in one piece, that is the result; else the pieces' are joined by a second launch:
 //   m = max m_i,  l = sum l_i 2^(m_i - m),  out = sum o_i 2^(m_i - m) / l.
-// Bound by memory, a key head's queries share what is read of it: one user's 131072 tokens (8 heads of 128 bf16 columns, 537 MB) 90 us (6.0 TB/s) and 5.5 to
+// Bound by memory, a key head's queries share what is read of it: one user's 131072 tokens (8 heads of 128 bf16 columns, 537 MB) 92 us (5.8 TB/s) and 5.5 to
 // join; 64 users of 16 to 8192 tokens (178 MB) 39 and 5.  Where there is little to read, by the chain of a wavefront's loads (lengths, page, rows) and
 // by its code's: one tile takes 10 us.
 #include "cross.h"
