@@ -1,0 +1,42 @@
+"""Attention over a user's history at the largest sizes that it takes and over many users, against its definitions in 64 bits
+(attention_formulas.py)."""
+import ctypes as C
+
+import numpy as np
+import pytest
+import torch
+
+import attention_formulas as F
+import paper_2404_09679_amd as A
+from test_gpu_attention import DEV, check_cross, cross, host, ints
+
+pytestmark = pytest.mark.gpu
+
+
+def check_entries(got, operands, ql, kl, entries, what):
+    """check_cross of some entries of a batch; got: (out,) or with the gradients, operands: q, k, v, g."""
+    at = torch.as_tensor(entries, device=DEV)
+    check_cross([x[at] for x in got], *(x[at] for x in operands), [ql[b] for b in entries], [kl[b] for b in entries], operands[0].shape[3] ** -0.5, "bf16", what)
+
+
+def test_more_queries_than_a_launch_has_threads_for():
+    """2^25 queries of heads, joined by a block of 128 threads each: 2^32 threads."""
+    B, S, T, HQ, H, D = 65536, 16, 100, 32, 4, 8
+    n = C.c_size_t()
+    assert A.lib.antdt_cross_attention_bytes(B, S, T, HQ, H, D, 1, C.byref(n)) == 0 and n.value > 0      # (equal shares and a join)
+    assert B * S * HQ * 128 == 2 ** 32
+    torch.manual_seed(1)
+    q, k, v = (torch.randn(B, r, h, D, device=DEV, dtype=torch.bfloat16) for r, h in ((S, HQ), (T, H), (T, H)))
+    kl = torch.randint(1, T + 1, (B,), device=DEV, dtype=torch.int32)
+    kl[3] = kl[-2] = 0
+    out = A.cross_attention(q, k, v, k_lengths=kl, out=torch.full_like(q, 7.0))
+    lengths = kl.tolist()
+    border = 2 ** 22 // (S * HQ)                                  # (the entry that starts the launch's second row)
+    check_entries([out], (q, k, v, q), [S] * B, lengths, [0, 1, 3, border - 1, border, border + 1, B // 2, B - 3, B - 2, B - 1], "entries")
+    # every entry, from calls of a part of the batch: both are within two roundings of the largest value from the definition, and (scores of at most 70, from
+    # operands below 5) 4096 u
+    most = v.abs().amax(1).repeat_interleave(HQ // H, 1)[:, None].float()
+    for b in range(0, B, 4096):
+        part = slice(b, b + 4096)
+        x = A.cross_attention(q[part], k[part], v[part], k_lengths=kl[part])
+        assert bool(((x.float() - out[part].float()).abs() <= 2 * (2 * F.HALF["bf16"] + 4096 * F.U) * most[part]).all()), b
