@@ -354,7 +354,16 @@ hipError_t launch_backward(CrossArgs a, const Shape& z, hipStream_t s) {
   const hipError_t e = allow_lds(cross_backward_kernel<WQ, WK, HELD>, LDS, 0, allowed);
   if (e != hipSuccess) return e;
   a.longest_first = longest_first(z, a.k_lengths || a.q_lengths, a.keys.blocks + a.queries.blocks, 256 * std::min(WQ::PER_CU, WK::PER_CU));
-  hipLaunchKernelGGL((cross_backward_kernel<WQ, WK, HELD>), dim3((unsigned)(div_up(a.keys.blocks, 8) * 8 + a.queries.blocks)), dim3(256), LDS, s, a);
+  const auto go = [&](const CrossArgs& x, int64_t blocks) { hipLaunchKernelGGL((cross_backward_kernel<WQ, WK, HELD>), dim3((unsigned)blocks), dim3(256), LDS, s, x); };
+  const int64_t both = div_up(a.keys.blocks, 8) * 8 + a.queries.blocks;
+  if (both < 1 << 24) {
+    go(a, both);
+  } else {   // (2^32 threads are the most; each kind's blocks are fewer than 2^24)
+    CrossArgs keys = a, queries = a;
+    keys.queries.blocks = queries.keys.blocks = 0;
+    if (a.keys.blocks) go(keys, a.keys.blocks);
+    if (a.queries.blocks) go(queries, a.queries.blocks);
+  }
   return hipGetLastError();
 }
 // Floats of the parts' sums.

@@ -307,3 +307,13 @@ def test_caches_of_too_much_room():
         rc = lib.antdt_cache_attention(PTR, 512, 64, PTR, PTR, page * 512, 512, 64, 5, page, PTR, cols, 8, cols, PTR, 8, 8, 64, 1, 0.125, 2 * PTR, 512, 64, PTR, 1 << 30,
                                        None)
         assert rc == UNSUPPORTED and "2^31" in message()
+
+
+def test_the_most_blocks():
+    """2^24 blocks of rows of one kind are refused, one fewer are not."""
+    n = C.c_size_t()
+    for f in (lib.antdt_cross_attention_bytes, lib.antdt_cross_attention_backward_bytes):
+        for S, T_ in ((1, 1), (1, 128), (128, 1)):
+            assert f((1 << 24) - 1, S, T_, 1, 1, 8, 1, C.byref(n)) == OK and f(1 << 24, S, T_, 1, 1, 8, 1, C.byref(n)) == UNSUPPORTED
+            assert "2^24" in message()
+        assert f(1 << 23, 1, 129, 1, 1, 8, 1, C.byref(n)) == UNSUPPORTED and f((1 << 23) - 1, 129, 1, 1, 1, 8, 1, C.byref(n)) == OK

@@ -40,3 +40,23 @@ def test_more_queries_than_a_launch_has_threads_for():
         part = slice(b, b + 4096)
         x = A.cross_attention(q[part], k[part], v[part], k_lengths=kl[part])
         assert bool(((x.float() - out[part].float()).abs() <= 2 * (2 * F.HALF["bf16"] + 4096 * F.U) * most[part]).all()), b
+
+
+@pytest.mark.parametrize("B,S,T,HQ,H", [(2 ** 19, 1, 2, 16, 16), (2 ** 20, 1, 10, 8, 8), (2 ** 20 - 1, 2, 3, 15, 3)])
+def test_gradients_of_more_blocks_than_a_launch_has_threads_for(B, S, T, HQ, H):
+    """Blocks of keys and blocks of queries are 2^24 together, and more."""
+    D = 8
+    assert B * HQ < 2 ** 24 <= B * (HQ + H)
+    torch.manual_seed(2)
+    q, k, v, g = (torch.randn(B, r, h, D, device=DEV, dtype=torch.bfloat16) for r, h in ((S, HQ), (T, H), (T, H), (S, HQ)))
+    kl = torch.randint(0, T + 1, (B,), device=DEV, dtype=torch.int32)
+    ql = torch.randint(0, S + 1, (B,), device=DEV, dtype=torch.int32)
+    kl[-1], ql[-1] = T, S
+    got = cross(q, k, v, g, ql, kl)
+    entries = [0, 1, 2, 3, B // 2 - 1, B // 2, B - 9, B - 3, B - 2, B - 1]
+    check_entries(got, (q, k, v, g), ql.tolist(), kl.tolist(), entries, (B, T))
+    # every entry, from calls of a part of the batch
+    for b in range(0, B, 2 ** 17):
+        part = slice(b, b + 2 ** 17)
+        for x, y in zip(cross(q[part], k[part], v[part], g[part], ql[part], kl[part]), got):
+            assert torch.equal(x, y[part]), b
