@@ -350,7 +350,7 @@ __global__ __launch_bounds__(64 * WAVES, (Stream<T, DP, R>::PER_CU)) void stream
     const bool stored = part ? lane % R < a.rows : query < a.S;
     if (part && stored && group == 0) *reinterpret_cast<float2*>(a.top_sum + 2 * at_part) = make_float2(m == -INFINITY ? -INFINITY : top2, l);
     if (!part && stored && group == 0 && a.stats) a.stats[(b * a.q_heads + hq) * a.S + query] = m == -INFINITY || !there ? INFINITY : top2 + log2_(l);
-    const float f = part ? 1.0f : m == -INFINITY ? 0.0f : 1.0f / l;   // (scores beyond fp32: l is 0 or infinite, and NaN comes out)
+    const float f = part ? 1.0f : m == -INFINITY ? 0.0f : 1.0f / l;   // (a largest score beyond fp32: l is 0 or infinite, and NaN comes out)
     float* to_part = a.partial + at_part * DP;
     T* to = reinterpret_cast<T*>(reinterpret_cast<char*>(const_cast<void*>(a.out.p)) + b * a.out.s.b + query * a.out.s.l + hq * a.out.s.h);
 #pragma unroll

@@ -8,7 +8,7 @@ import torch
 
 import attention_formulas as F
 import paper_2404_09679_amd as A
-from test_gpu_attention import DEV, check_cross, cross, host, ints
+from test_gpu_attention import DEV, check_cross, cross, host, within
 
 pytestmark = pytest.mark.gpu
 
@@ -60,3 +60,31 @@ def test_gradients_of_more_blocks_than_a_launch_has_threads_for(B, S, T, HQ, H):
         part = slice(b, b + 2 ** 17)
         for x, y in zip(cross(q[part], k[part], v[part], g[part], ql[part], kl[part]), got):
             assert torch.equal(x, y[part]), b
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("S,T", [(1, 40), (200, 40), (1, 6000), (5, 9000)])
+def test_scores_below_the_range(S, T, dtype):
+    """Products of finite operands below fp32's range are -infinity: their keys have no weight, and a query that has no others has zeros and passes no
+    gradient.  Where the scale takes the largest score there, NaN."""
+    D, n = 8, C.c_size_t()
+    assert A.lib.antdt_cross_attention_bytes(1, S, T, 2, 2, D, int(dtype is torch.bfloat16), C.byref(n)) == 0 and (n.value > 0) == (T > 40)
+    torch.manual_seed(S)
+    q, k = torch.zeros(1, S, 2, D, device=DEV, dtype=dtype), torch.zeros(1, T, 2, D, device=DEV, dtype=dtype)
+    v, g = (torch.randn(1, r, 2, D, device=DEV).to(dtype) for r in (T, S))
+    q[..., 0], k[..., 0] = -2e19, 2e19
+    stats = A.cross_attention_stats(q)
+    out = A.cross_attention(q, k, v, stats=stats, out=torch.full_like(q, 7.0))
+    assert not out.any() and bool((stats == float("inf")).all())
+    assert not any(x.any() for x in A.cross_attention_backward(g, q, k, v, out, stats))
+    some = torch.rand(T, device=DEV) < 0.3                        # (scores of 0)
+    k[0, some] = 0
+    got = cross(q, k, v, g, None, None)
+    x = host(v)[0, some.cpu().numpy()]
+    e = (len(x) + 8) * F.U * np.abs(x).mean(0)
+    half = F.HALF["bf16"] if dtype is torch.bfloat16 else F.HALF["f32"]
+    want = np.broadcast_to(x.mean(0), got[0][0].shape)
+    within(got[0][0], want, e + half * (np.abs(want) + e), "the others' mean")
+    assert all(bool(x.isfinite().all()) for x in got) and not got[3][0, ~some].any()
+    k[..., 0] = 1e19                                              # (products of -2e38)
+    assert bool(A.cross_attention(q, k, v, scale=4.0).isnan().all())
