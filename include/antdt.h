@@ -507,8 +507,8 @@ int antdt_token_logprobs_gradient(const void* logits, int64_t ld, int64_t N, int
  *  - lengths: DEVICE int32 [B], of a sequence's rows; what lies outside 0 .. the size is taken as the nearer end.  Rows behind a length
  *    are never read into a result, whatever they hold, and are zeros in one.
  *  - attention: D a multiple of 8, at most ANTDT_MAX_ATTENTION_DIM, heads that start at multiples of 16 bytes (ANTDT_UNSUPPORTED otherwise).  Scores, the
- *    softmax and sums are fp32.  Of bf16 heads the probabilities, and in the backward pass the scores' gradients, are rounded to bf16 as the matrix cores'
- *    operands.  scale is 1e-30 or more (finite times log2(e)).  A query without keys has zeros and passes no gradient.  A product q k^T below fp32's range is
+ *    softmax and sums are fp32.  Of bf16 heads cache attention has its probabilities to 2^-15; cross attention rounds them, and in the backward pass the scores'
+ *    gradients, to bf16 as the matrix cores' operands (the probabilities of few queries, where antdt_cross_attention has a workspace, to 2^-15).  scale is 1e-30 or more (finite times log2(e)).  A query without keys has zeros and passes no gradient.  A product q k^T below fp32's range is
  *    -infinity, whatever the operands, and its key has no weight.  A query all of whose products are -infinity has zeros, too, and passes no gradient (but
  *    infinite operands times its scores' gradients, which are zeros, are NaN); one with a product of NaN, +infinity or above fp32's range, or whose largest
  *    score, scale times the product, is beyond that range on either side, has NaN.

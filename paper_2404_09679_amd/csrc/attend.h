@@ -24,15 +24,36 @@ struct Core<bf16_t> {
   // c += A B^T, 32 x 32
   static __device__ __forceinline__ void multiply(const Fragment& a, const Fragment& b, f32x16& c) { c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
   // Contraction slots STEP i .. of what a product left.
-  static __device__ __forceinline__ Fragment pack(const f32x16& x, int i) {
-    union {
-      uint32_t w[4];
-      Fragment f;
-    } u;
+  template <typename X>
+  static __device__ __forceinline__ Fragment pack(const X& x, int i) {
+    Words u;
 #pragma unroll
     for (int e = 0; e < 4; ++e) u.w[e] = f2bf2(x[8 * i + 2 * e], x[8 * i + 2 * e + 1]);
     return u.f;
   }
+  // The same of x >= 0 in two parts, off by 2^-15 of x together: x cut off, and what that took away, rounded.  The last bit of x counts as set, so that there
+  // is a second part of every x: a zero, or a part of the other sign, times an infinite value would be NaN.
+  static constexpr int PARTS = 2;
+  template <typename X>
+  static __device__ __forceinline__ void pack(const X& x, int i, Fragment (&f)[2]) {
+    Words u[2];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const uint32_t a = __float_as_uint(x[8 * i + 2 * e]) | 1, b = __float_as_uint(x[8 * i + 2 * e + 1]) | 1, a1 = a & 0xFFFF0000u, b1 = b & 0xFFFF0000u;
+      u[0].w[e] = a1 >> 16 | b1;
+      u[1].w[e] = f2bf2(__uint_as_float(a) - __uint_as_float(a1), __uint_as_float(b) - __uint_as_float(b1));
+    }
+    f[0] = u[0].f;
+    f[1] = u[1].f;
+  }
+  template <typename X>
+  static __device__ __forceinline__ void pack(const X& x, int i, Fragment (&f)[1]) { f[0] = pack(x, i); }
+
+ private:
+  union Words {
+    uint32_t w[4];
+    Fragment f;
+  };
 };
 template <>
 struct Core<float> {
@@ -42,7 +63,11 @@ struct Core<float> {
 #pragma unroll
     for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[e], b[e], c, 0, 0, 0);
   }
-  static __device__ __forceinline__ Fragment pack(const f32x16& x, int i) { return Fragment{x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]}; }
+  static constexpr int PARTS = 1;
+  template <typename X>
+  static __device__ __forceinline__ Fragment pack(const X& x, int i) { return Fragment{x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]}; }
+  template <typename X>
+  static __device__ __forceinline__ void pack(const X& x, int i, Fragment (&f)[1]) { f[0] = pack(x, i); }
 };
 
 // Rows of DP columns in LDS.

@@ -8,14 +8,15 @@ namespace {
 // vector units (maximum, exponential, sum) for each over the matrix core, about as long; two wavefronts on a SIMD have them at the same time.  8 ragged
 // histories of 2048 queries and 4096 keys, 16 and 4 heads of 128 bf16 columns: 381 GFLOP in 400-430 us (by the clock that
 // power leaves), an eighth of it the last blocks, when not all compute units have one.
-// PAGED: keys and values are a cache's, the user's pages looked up before the first tile.
+// PAGED: keys and values are a cache's, the user's pages looked up before the first tile; probabilities in two parts, see stream.hip (16 users of 100 and
+// 1000 tokens, 16 and 4 heads of 64 bf16 columns, all of it in the caches: 5.0 -> 5.1 us, 12.4 -> 13.5).
 template <typename W, bool PAGED>
 __global__ __launch_bounds__(W::THREADS, W::PER_CU) void cross_forward_kernel(CrossArgs a) {
   typedef typename W::T T;
   typedef typename W::Tile Tile;
   typedef Core<T> C;
   typedef KeyTiles<W> F;
-  constexpr int BT = W::TILE;
+  constexpr int BT = W::TILE, PARTS = PAGED ? C::PARTS : 1;   // (of the probabilities)
   extern __shared__ __attribute__((aligned(1024))) char lds[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
   int unit, block;
@@ -132,10 +133,11 @@ __global__ __launch_bounds__(W::THREADS, W::PER_CU) void cross_forward_kernel(Cr
         s[j][e] = exp2_(fmaf(s[j][e], a.scale2, -mc));
         l += s[j][e];
       }
-    typename C::Fragment p;
+    typename C::Fragment p[PARTS];
     values.run(value, [&](int i, const typename C::Fragment& x) {
-      if (i % W::DT == 0) p = C::pack(s[i / (W::DT * W::PACKS)], i / W::DT % W::PACKS);
-      C::multiply(x, p, o[i % W::DT]);
+      if (i % W::DT == 0) C::pack(s[i / (W::DT * W::PACKS)], i / W::DT % W::PACKS, p);
+#pragma unroll
+      for (const typename C::Fragment& part : p) C::multiply(x, part, o[i % W::DT]);
     });
   }
   arrive<0, true>();   // (the buffers are free)

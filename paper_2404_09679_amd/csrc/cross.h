@@ -5,7 +5,9 @@
 // 2^(z log2 e), so that p = 2^(z log2 e - L) again.  With g the gradient of out and d = sum of g out over a row's columns:
 //   dP = g v^T,  dZ = p (dP - d),  dQ = scale dZ k,  dK = scale dZ^T q,  dV = p^T g,
 // dQ in blocks of queries and dK, dV in blocks of keys: each forms p and dP anew (14 products for the 10 there are), and every sum has one order.
-// Of bf16 heads p and dZ are rounded to bf16 as the matrix cores' operands.
+// Of bf16 heads p and dZ are rounded to bf16 as the matrix cores' operands (results off by 0.0025 of their norm, of which their own rounding is 0.0017):
+// in two parts, as over a cache, they would take more products, which bound these kernels (8 ragged histories of 2048 queries and 4096 keys, 16 and 4 heads of
+// 128 columns: forward 433 -> 547 us, gradients 1317 -> 1690).
 #pragma once
 
 #include "attend.h"

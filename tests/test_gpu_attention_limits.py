@@ -8,9 +8,10 @@ import torch
 
 import attention_formulas as F
 import paper_2404_09679_amd as A
-from test_gpu_attention import DEV, check_cross, cross, host, within
+from test_gpu_attention import DEV, check_cross, cross, cross_inputs, decode_inputs, host, ints, within
 
 pytestmark = pytest.mark.gpu
+INF = float("inf")
 
 
 def check_entries(got, operands, ql, kl, entries, what):
@@ -88,3 +89,57 @@ def test_scores_below_the_range(S, T, dtype):
     assert all(bool(x.isfinite().all()) for x in got) and not got[3][0, ~some].any()
     k[..., 0] = 1e19                                              # (products of -2e38)
     assert bool(A.cross_attention(q, k, v, scale=4.0).isnan().all())
+
+
+TWO_PARTS = 2.0 ** -15                                            # a bf16 number cut off takes 2^-7 away, of which rounding loses 2^-8
+
+
+def check_two_parts(got, q, k, v, scale, what):
+    """Rows q [S, D], got [S, D] of a head over k, v [T, D], all of bf16: only the result is rounded to bf16."""
+    f = F.attend(host(q), host(k), host(v), scale, TWO_PARTS)
+    within(host(got), f["out"], f["e"] + F.HALF["bf16"] * (np.abs(f["out"]) + f["e"]), what)
+
+
+@pytest.mark.parametrize("lengths,page,HQ,H,D", [([100, 33, 64, 7], 16, 4, 2, 64), ([500, 90], 7, 40, 2, 128), ([300, 0, 70], 64, 8, 8, 96), ([150, 0, 31], 16, 4, 1, 40),
+                                                 ([130] * 40, 16, 3, 1, 32)])
+@pytest.mark.parametrize("room", [0, 2050])
+def test_probabilities_over_a_cache_are_not_rounded_to_bf16(lengths, page, HQ, H, D, room):
+    rng = np.random.default_rng(D)
+    kc, vc, table, dense, q = decode_inputs(rng, lengths, page, HQ, H, D, "bf16")
+    table = np.pad(table, ((0, 0), (0, max(0, room - table.shape[1]))), constant_values=-1)
+    got = A.cache_attention(q, kc, vc, ints(table), ints(lengths))
+    for b, (k, v) in enumerate(dense):
+        for h in range(H):
+            of = slice(h * HQ // H, (h + 1) * HQ // H)
+            check_two_parts(got[b, of], q[b, of], k[:, h], v[:, h], D ** -0.5, (b, h))
+
+
+@pytest.mark.parametrize("S,T,HQ,H,D", [(1, 6000, 4, 4, 64), (3, 9000, 8, 2, 128), (17, 9000, 4, 2, 96)])
+def test_probabilities_of_few_queries_are_not_rounded_to_bf16(S, T, HQ, H, D):
+    n = C.c_size_t()
+    assert A.lib.antdt_cross_attention_bytes(2, S, T, HQ, H, D, 1, C.byref(n)) == 0 and n.value > 0      # (equal shares)
+    rng = np.random.default_rng(T)
+    q, k, v, _, _, _ = cross_inputs(rng, 2, S, T, HQ, H, D, "", "bf16")
+    kl = [200, 63]                                                # (of few terms: the bound on sums' rounding stays below that on the probabilities')
+    got = A.cross_attention(q, k, v, k_lengths=ints(kl))
+    for b in range(2):
+        for h in range(HQ):
+            check_two_parts(got[b, :, h], q[b, :, h], k[b, :kl[b], h * H // HQ], v[b, :kl[b], h * H // HQ], D ** -0.5, (b, h))
+
+
+@pytest.mark.parametrize("S,T", [(1, 40), (1, 6000), (20, 9000), (0, 60), (0, 5000)])
+def test_infinite_values(S, T):
+    """A value's infinity is the result's, of one sign; S = 0: over a cache.  Probabilities that bf16 holds and such that it does not."""
+    rng = np.random.default_rng(T)
+    H, D = 2, 64
+    q, k, v, _, _, _ = cross_inputs(rng, 1, max(S, 1), T, H, H, D, "", "bf16")
+    k[0, ::2] = 0
+    v[0, 7, 0, 3], v[0, 8, 0, 5], v[0, 8, 1, 9], v[0, 30, 1, 9] = INF, -INF, INF, -INF
+    if S:
+        out = A.cross_attention(q, k, v)[0]
+    else:
+        out = A.cache_attention(q[0], k, v, ints([[0]]), ints([T]))
+    inf = torch.zeros(H, D, device=DEV)
+    inf[0, 3], inf[0, 5], inf[1, 9] = INF, -INF, float("nan")
+    for row in out.float():
+        assert torch.equal(torch.where(row.isfinite(), 0, row).nan_to_num(9, INF, -INF), inf.nan_to_num(9, INF, -INF))
