@@ -262,8 +262,10 @@ inline double tile_us(const Shape& z) {
   return z.dtype == ANTDT_F32 ? F32[columns] : BF16[columns];
 }
 // Results' rows in blocks of 128, or of 32 whose `waves` wavefronts share the other side's rows (`tiles` of 32), or these again in parts.
-//  - Blocks of 32 as long as all of them run at once: `most` of them.  bf16, 1024 queries and keys, 64 columns, us of blocks of 128 / 32: 16 heads 20 / 15,
-//    32 heads 22 / 26; gradient of the queries 24 / 16, 26 / 30; 128 columns, gradient of the keys: 16 heads 60 / 46, 32 heads 63 / 89.
+//  - Blocks of 32 as long as there are no more than `most`: all of them run at once, of fp32 heads above 32 columns in two rounds.  bf16, 1024 queries and
+//    keys, 64 columns, us of blocks of 128 / 32: 16 heads 20 / 15, 32 heads 22 / 26; gradient of the queries 24 / 16, 26 / 30; 128 columns, gradient of the
+//    keys: 16 heads 60 / 46, 32 heads 63 / 89.  Two rounds of fp32, 512 blocks, 1000 rows of the other side, gradients of queries and of keys: 64 columns, 16
+//    heads of 1024 rows 108 / 74 and 153 / 94; 128 columns 224 / 247 and 287 / 306, but 500 heads of 20 rows 466 / 271 and 746 / 495.
 //  - Parts where their shorter way outweighs the launch that adds them up, about 6 us.
 inline Plan cross_plan(int64_t heads, int64_t rows, int64_t tiles, int64_t most, int waves, double us, bool parted) {
   Plan p = {false, (int32_t)div_up(rows, 128), 1, 0};
@@ -282,6 +284,7 @@ inline Plan cross_plan(int64_t heads, int64_t rows, int64_t tiles, int64_t most,
 }
 inline int64_t delta_bytes(const Shape& z) { return div_up(z.B * z.S * z.q_heads * 4, 256) * 256; }
 inline bool wide(const Shape& z) { return z.dtype == ANTDT_BF16 && z.D > 64; }          // (a block of 32 fills a compute unit's LDS)
+inline int at_once(const Shape& z) { return z.D > (z.dtype == ANTDT_BF16 ? 64 : 32) ? 256 : 512; }   // blocks of 32
 inline int key_waves(const Shape& z) { return z.dtype == ANTDT_F32 && z.D > 64 ? 2 : 4; }
 inline Plan forward_plan(const Shape& z) { return cross_plan(z.B * z.q_heads, z.S, div_up(z.T, 32), wide(z) ? 256 : 512, key_waves(z), tile_us(z), false); }
 inline Plan dq_plan(const Shape& z) { return cross_plan(z.B * z.q_heads, z.S, div_up(z.T, 32), wide(z) ? 256 : 512, key_waves(z), 1.6 * tile_us(z), true); }
@@ -292,15 +295,19 @@ inline bool longest_first(const Shape& z, bool ragged, int64_t blocks, int at_on
   const double rounds = (double)blocks / at_once;
   return ragged && z.B > 1 && rounds > 1.0 && tile_us(z) * div_up(std::max(z.S, z.T), 32) > 3.0 * rounds;
 }
-// Whether an equal share of all keys to each wavefront (stream.hip) takes less time than the forward pass's blocks: it has a second launch, `fixed` us in all, and
-// tiles that nobody else reads, each `share` times tile_us on one of 1024 SIMDs; a block's take `own` times that.
+// Whether an equal share of all keys to each wavefront (stream.hip) takes less time than the forward pass's blocks: it has a second launch, `fixed` us in all
+// (and in fp32 0.9 for 1000 rows), and tiles that nobody else reads, each `share` times tile_us on one of 1024 SIMDs; a block's take `own` times that, in as
+// many rounds as there are.  Two rounds of fp32, us by blocks / shares: 70 users' caches, 4 heads of 64 columns, 200 and 500 tokens 21 / 14, 40 / 24; 128 users of
+// 128 columns, 100 tokens 35 / 23; 300 keys of 64 columns, 260 heads of 2 queries 28 / 18; of 128 columns, 16 heads of 1024 queries, 100 and 1000 keys 31 / 43,
+// 167 / 134.
 inline bool by_shares(const Shape& z, double fixed, double share, double own) {
   if (z.B == 0 || z.S == 0 || !stream_fits(z.B, z.S, z.T, z.q_heads, z.heads)) return false;
   const int64_t tiles = div_up(z.T, 32), rows = z.S * (z.q_heads / z.heads), row_tiles = rows <= 16 ? 1 : div_up(rows, 32);
   const Plan p = forward_plan(z);
-  const double blocks = p.split ? div_up(tiles, key_waves(z)) * (p.blocks < 128 ? 1.0 : 1.25) : std::max(1.0, p.blocks / 512.0) * tiles;
+  const double blocks = p.split ? div_up(tiles, key_waves(z)) * (p.blocks < 128 ? 1.0 : 1.25) * div_up(p.blocks, at_once(z)) : std::max(1.0, p.blocks / 512.0) * tiles;
   const double shares = (double)z.B * z.heads * row_tiles * tiles / 1024;
-  return fixed + tile_us(z) * share * shares < 4.5 + tile_us(z) * own * blocks;
+  const double joined = z.dtype == ANTDT_F32 ? 0.0009 * z.B * z.S * z.q_heads : 0.0;
+  return fixed + joined + tile_us(z) * share * shares < 4.5 + tile_us(z) * own * blocks;
 }
 // us by blocks / shares of 500, 2000 and 8000 keys, 8 heads: 64 bf16 columns, 1 query 7 / 18, 16 / 17, 49 / 21; 4 x 128 queries 8 / 21, 17 / 27, 61 / 55; 128
 // columns 10 / 17, 25 / 17, 84 / 22 and 12 / 25, 29 / 41, 96 / 97; 64 fp32 columns 16 / 18, 49 / 16, 184 / 17 and 17 / 26, 55 / 46, 195 / 114.

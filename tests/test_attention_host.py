@@ -317,3 +317,15 @@ def test_the_most_blocks():
             assert f((1 << 24) - 1, S, T_, 1, 1, 8, 1, C.byref(n)) == OK and f(1 << 24, S, T_, 1, 1, 8, 1, C.byref(n)) == UNSUPPORTED
             assert "2^24" in message()
         assert f(1 << 23, 1, 129, 1, 1, 8, 1, C.byref(n)) == UNSUPPORTED and f((1 << 23) - 1, 129, 1, 1, 1, 8, 1, C.byref(n)) == OK
+
+
+def test_blocks_in_two_rounds():
+    """fp32 heads above 32 columns, a block of which fills a compute unit: more of them than compute units take twice as long, and equal shares of the keys
+    less (they need a workspace); many rows of few keys stay with the blocks."""
+    def shares(heads, S, keys, D, dtype=0):
+        n = C.c_size_t()
+        assert lib.antdt_cross_attention_bytes(1, S, keys, heads, heads, D, dtype, C.byref(n)) == OK
+        return n.value > 0
+
+    assert shares(260, 2, 300, 64) and shares(400, 9, 300, 128) and shares(16, 1024, 1000, 128)
+    assert not shares(250, 2, 300, 64) and not shares(260, 2, 300, 32) and not shares(16, 1024, 100, 128) and not shares(260, 2, 300, 64, 1)
