@@ -186,7 +186,7 @@ hipError_t launch_forward(CrossArgs a, const Shape& z, const Plan& pl, hipStream
 
 hipError_t launch_cache_blocks(const CrossArgs& a, const Shape& z, hipStream_t s) {
   return by_columns(z.dtype, (int)z.D, [&](auto way, auto cols) {
-    return launch_forward<typename decltype(way)::template SplitKeys<decltype(cols)::value>, true>(a, z, forward_plan(z), s);
+    return launch_forward<typename decltype(way)::template SplitKeys<decltype(cols)::value>, true>(a, z, cache_plan(z), s);
   });
 }
 }  // namespace antdt

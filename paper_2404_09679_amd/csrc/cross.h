@@ -267,11 +267,11 @@ inline double tile_us(const Shape& z) {
 //    keys: 16 heads 60 / 46, 32 heads 63 / 89.  Two rounds of fp32, 512 blocks, 1000 rows of the other side, gradients of queries and of keys: 64 columns, 16
 //    heads of 1024 rows 108 / 74 and 153 / 94; 128 columns 224 / 247 and 287 / 306, but 500 heads of 20 rows 466 / 271 and 746 / 495.
 //  - Parts where their shorter way outweighs the launch that adds them up, about 6 us.
-inline Plan cross_plan(int64_t heads, int64_t rows, int64_t tiles, int64_t most, int waves, double us, bool parted) {
+inline Plan cross_plan(int64_t heads, int64_t rows, int64_t tiles, int64_t most, int waves, double us, bool parted, int64_t least = 2) {
   Plan p = {false, (int32_t)div_up(rows, 128), 1, 0};
   p.blocks = heads * p.tiles;
   const int64_t split = heads * div_up(rows, 32);
-  if (split == 0 || split > most || tiles < 2) return p;
+  if (split == 0 || split > most || tiles < least) return p;
   p.split = true;
   p.tiles = (int32_t)div_up(rows, 32);
   p.blocks = split;
@@ -300,10 +300,9 @@ inline bool longest_first(const Shape& z, bool ragged, int64_t blocks, int at_on
 // many rounds as there are.  Two rounds of fp32, us by blocks / shares: 70 users' caches, 4 heads of 64 columns, 200 and 500 tokens 21 / 14, 40 / 24; 128 users of
 // 128 columns, 100 tokens 35 / 23; 300 keys of 64 columns, 260 heads of 2 queries 28 / 18; of 128 columns, 16 heads of 1024 queries, 100 and 1000 keys 31 / 43,
 // 167 / 134.
-inline bool by_shares(const Shape& z, double fixed, double share, double own) {
+inline bool by_shares(const Shape& z, const Plan& p, double fixed, double share, double own) {
   if (z.B == 0 || z.S == 0 || !stream_fits(z.B, z.S, z.T, z.q_heads, z.heads)) return false;
   const int64_t tiles = div_up(z.T, 32), rows = z.S * (z.q_heads / z.heads), row_tiles = rows <= 16 ? 1 : div_up(rows, 32);
-  const Plan p = forward_plan(z);
   const double blocks = p.split ? div_up(tiles, key_waves(z)) * (p.blocks < 128 ? 1.0 : 1.25) * div_up(p.blocks, at_once(z)) : std::max(1.0, p.blocks / 512.0) * tiles;
   const double shares = (double)z.B * z.heads * row_tiles * tiles / 1024;
   const double joined = z.dtype == ANTDT_F32 ? 0.0009 * z.B * z.S * z.q_heads : 0.0;
@@ -311,7 +310,7 @@ inline bool by_shares(const Shape& z, double fixed, double share, double own) {
 }
 // us by blocks / shares of 500, 2000 and 8000 keys, 8 heads: 64 bf16 columns, 1 query 7 / 18, 16 / 17, 49 / 21; 4 x 128 queries 8 / 21, 17 / 27, 61 / 55; 128
 // columns 10 / 17, 25 / 17, 84 / 22 and 12 / 25, 29 / 41, 96 / 97; 64 fp32 columns 16 / 18, 49 / 16, 184 / 17 and 17 / 26, 55 / 46, 195 / 114.
-inline bool cross_streams(const Shape& z) { return by_shares(z, 16.0, z.dtype == ANTDT_F32 ? 1.3 : 2.0, 1.0); }
+inline bool cross_streams(const Shape& z) { return by_shares(z, forward_plan(z), 16.0, z.dtype == ANTDT_F32 ? 1.3 : 2.0, 1.0); }
 // The same for one token of each user over a cache of room for T: the tokens of a key's heads are one block's rows, which looks up the user's pages once.
 // us of 100, 500, 1000 and 2000 tokens in pages of 16: 16 users, 16 and 4 heads of 64 bf16 columns 5.5 / 16, 9 / 16, 13 / 17, 23 / 17; 64 users of 128
 // columns 8 / 15, 17 / 20, 28 / 29, 49 / 50; fp32, 64 users of 64 columns 8 / 17, 23 / 21, 40 / 30, 72 / 52.
@@ -319,8 +318,15 @@ constexpr int TABLE = 2048;   // pages of a user, at most
 inline Shape cache_shape(int64_t B, int64_t T, int64_t q_heads, int64_t heads, int64_t D, int32_t dtype) {
   return Shape{B, q_heads / heads, T, heads, heads, D, dtype};
 }
+// Blocks of 32 for a single tile, too, where all of them run at once (us by shares / blocks of 20 tokens: 16 users, 16 and 4 heads of 64 bf16 columns 7.7 / 5.0, fp32
+// 8.8 / 7.3; 200 users, 8 and 2 heads of 64 fp32 columns, two rounds, 10.0 / 13.2).
+inline Plan cache_plan(const Shape& z) {
+  const int most = z.T <= 32 ? at_once(z) : wide(z) ? 256 : 512;
+  return cross_plan(z.B * z.q_heads, z.S, div_up(z.T, 32), most, key_waves(z), tile_us(z), false, 1);
+}
 inline bool cache_streams(const Shape& z, int64_t page) {
-  return !forward_plan(z).split || div_up(z.T, page) > TABLE || by_shares(z, 15.0, z.dtype == ANTDT_F32 ? 1.0 : 1.5, 1.5);
+  const Plan p = cache_plan(z);
+  return !p.split || div_up(z.T, page) > TABLE || by_shares(z, p, 15.0, z.dtype == ANTDT_F32 ? 1.0 : 1.5, 1.5);
 }
 hipError_t launch_cache_blocks(const CrossArgs& a, const Shape& z, hipStream_t s);
 

@@ -8,7 +8,7 @@ import torch
 
 import attention_formulas as F
 import paper_2404_09679_amd as A
-from test_gpu_attention import DEV, check_cross, cross, cross_inputs, decode_inputs, host, ints, within
+from test_gpu_attention import DEV, check_cross, check_decode, cross, cross_inputs, decode_inputs, host, ints, within
 
 pytestmark = pytest.mark.gpu
 INF = float("inf")
@@ -143,3 +143,25 @@ def test_infinite_values(S, T):
     inf[0, 3], inf[0, 5], inf[1, 9] = INF, -INF, float("nan")
     for row in out.float():
         assert torch.equal(torch.where(row.isfinite(), 0, row).nan_to_num(9, INF, -INF), inf.nan_to_num(9, INF, -INF))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("B,page,cols,HQ,H,D", [(1, 32, 1, 8, 8, 64), (7, 16, 2, 6, 2, 128), (70, 5, 6, 40, 1, 24), (200, 1, 3, 8, 2, 64), (16, 7, 1, 4, 4, 96),
+                                                (3, 33, 1, 4, 2, 40)])
+def test_caches_of_one_tile(B, page, cols, HQ, H, D, dtype):
+    """Room for at most 32 tokens, and one more; pages that there are not, lengths of 0 and beyond the room."""
+    rng = np.random.default_rng(B + page)
+    room = page * cols
+    lengths = rng.integers(0, room + 1, B).tolist()
+    lengths[-1] = room
+    kc, vc, table, dense, q = decode_inputs(rng, lengths, page, HQ, H, D, dtype)
+    table = np.pad(table, ((0, 0), (0, cols - table.shape[1])), constant_values=-1)
+    gone = rng.integers(0, B)
+    if B > 1 and lengths[gone] > page:
+        table[gone, 0] = len(kc)
+        dense[gone] = tuple(x[page:] for x in dense[gone])
+    given = [n + 1000 if n == room else n - 5 if n == 0 else n for n in lengths]
+    got = A.cache_attention(q, kc, vc, ints(table), ints(given), out=torch.full_like(q, 7.0))
+    check_decode(got, q, dense, dtype, D ** -0.5, "")
+    wide = np.pad(table, ((0, 0), (0, 2050)), constant_values=-1)
+    check_decode(A.cache_attention(q, kc, vc, ints(wide), ints(lengths)), q, dense, dtype, D ** -0.5, "in a large table")
