@@ -8,7 +8,8 @@ import torch
 
 import attention_formulas as F
 import paper_2404_09679_amd as A
-from test_gpu_attention import DEV, check_cross, check_decode, cross, cross_inputs, decode_inputs, host, ints, within
+from test_gpu_attention import (DEV, DT, NAN, check_cross, check_decode, cross, cross_inputs, decode_inputs, host, ints, normal,
+                                within)
 
 pytestmark = pytest.mark.gpu
 INF = float("inf")
@@ -165,3 +166,59 @@ def test_caches_of_one_tile(B, page, cols, HQ, H, D, dtype):
     check_decode(got, q, dense, dtype, D ** -0.5, "")
     wide = np.pad(table, ((0, 0), (0, 2050)), constant_values=-1)
     check_decode(A.cache_attention(q, kc, vc, ints(wide), ints(lengths)), q, dense, dtype, D ** -0.5, "in a large table")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("B,longest,page,HQ,H,D", [(1000, 90, 16, 4, 2, 32), (4097, 40, 5, 2, 1, 16), (20000, 9, 4, 3, 1, 8)])
+def test_caches_of_many_users(B, longest, page, HQ, H, D, dtype):
+    """Several sequences to a lane of the wavefronts that look for theirs; many without tokens, alone and side by side."""
+    rng = np.random.default_rng(B)
+    lengths = rng.integers(0, longest + 1, B)
+    lengths[rng.random(B) < 0.3] = 0
+    lengths[100:400] = lengths[-50:] = 0
+    pages = -(-lengths // page)
+    order, start = rng.permutation(int(pages.sum())), np.cumsum(pages) - pages
+    table = np.full((B, -(-longest // page)), -1)
+    for b in range(B):
+        table[b, :pages[b]] = order[start[b]:start[b] + pages[b]]
+    kc, vc = (torch.full((len(order), page, H, D), NAN, device=DEV, dtype=DT[dtype]) for _ in range(2))
+    seq = np.repeat(np.arange(B), lengths)
+    t = np.arange(len(seq)) - np.repeat(np.cumsum(lengths) - lengths, lengths)
+    slot = torch.as_tensor(table[seq, t // page], device=DEV), torch.as_tensor(t % page, device=DEV)
+    dense = torch.zeros(2, B, longest, H, D, device=DEV, dtype=torch.float64)
+    for c, x in zip((kc, vc), dense):
+        c[slot] = normal(rng, len(seq), H, D, dtype=dtype)
+        x[torch.as_tensor(seq, device=DEV), torch.as_tensor(t, device=DEV)] = c[slot].double()
+    q = normal(rng, B, HQ, D, dtype=dtype)
+    got = A.cache_attention(q, kc, vc, ints(table), ints(lengths), out=torch.full_like(q, 7.0))
+    some = np.flatnonzero(lengths)[[0, 1, 2, 30, 300, -3, -2, -1]]
+    check_decode(got[torch.as_tensor(some, device=DEV)], q[torch.as_tensor(some, device=DEV)], [tuple(x[b, :lengths[b]] for x in dense) for b in some], dtype,
+                 D ** -0.5, "some")
+    # all of them in 64 bits, and the bound with the largest values in the place of their mean: scores of at most 70, as in attention_formulas.attend
+    k, v = (x.repeat_interleave(HQ // H, 2) for x in dense)
+    z = torch.where(torch.arange(longest, device=DEV)[None, None] < ints(lengths)[:, None, None], (q.double()[:, None] * k).sum(3).transpose(1, 2) * D ** -0.5, -INF)
+    want = (torch.softmax(z, 2).nan_to_num(0)[..., None] * v.transpose(1, 2)).sum(2)
+    e = ((2 * (D + 14) * 70 + longest + 16) * F.U + (TWO_PARTS if dtype == "bf16" else 0)) * v.abs().amax(1) + F.HALF[dtype] * (want.abs() * 1.01)
+    assert float(z[z > -INF].abs().max()) < 70
+    assert bool(((got.double() - want).abs() <= e).all())
+    assert torch.equal(A.cache_attention(q, kc, vc, ints(table), ints(lengths)), got)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("B,S,T,HQ,H,D", [(3000, 2, 40, 4, 1, 16), (1100, 1, 300, 2, 2, 32), (700, 40, 33, 2, 1, 8)])
+def test_many_histories(B, S, T, HQ, H, D, dtype):
+    rng = np.random.default_rng(B)
+    q, k, v, g = (normal(rng, B, n, h, D, dtype=dtype) for n, h in ((S, HQ), (T, H), (T, H), (S, HQ)))
+    ql, kl = rng.integers(0, S + 1, B), rng.integers(0, T + 1, B)
+    kl[rng.random(B) < 0.3] = 0
+    ql[-1], kl[-1], kl[60:200] = S, T, 0
+    for x, n in ((q, ql), (g, ql), (k, kl), (v, kl)):
+        x[torch.arange(x.shape[1], device=DEV)[None] >= ints(n)[:, None]] = NAN
+    got = cross(q, k, v, g, ints(ql), ints(kl))
+    at = np.concatenate([np.arange(64), np.arange(B // 2, B // 2 + 32), np.arange(B - 64, B), rng.choice(B, 100, False)])
+    on = torch.as_tensor(at, device=DEV)
+    check_cross([x[on] for x in got], q[on], k[on], v[on], g[on], ql[at].tolist(), kl[at].tolist(), D ** -0.5, dtype, "")
+    assert not any(bool(x.isnan().any()) for x in got)
+    for x, n in zip(got, (ql, ql, kl, kl)):
+        assert not x[torch.arange(x.shape[1], device=DEV)[None] >= ints(n)[:, None]].any()
+    assert all(torch.equal(x, y) for x, y in zip(cross(q, k, v, g, ints(ql), ints(kl)), got))
