@@ -267,6 +267,7 @@ struct StreamArgs {
   int32_t q_heads, heads, group, D;
   int32_t row_tile, row_tiles, rows;   // a key head's queries (row r: query r / group of head r mod group) in 16s or 32s; rows of a partial result
   int32_t waves;               // of the launch
+  uint32_t first;              // query of a head that a launch of the join begins with
   float scale2;
   uint32_t* before;            // [B + 1] tiles of 32 keys of the sequences before, of a single head and tile of rows
   float* top_sum;              // [waves, 2, rows, 2] maximum and sum of the partial results, and

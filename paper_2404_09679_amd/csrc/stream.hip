@@ -362,17 +362,15 @@ __global__ __launch_bounds__(64 * WAVES, (Stream<T, DP, R>::PER_CU)) void stream
   }
 }
 
-// One query of one head to a block: its parts, THREADS / (DP / 4) of them at a time, each thread's in the order of the wavefronts.  ROWS of them along the
-// grid, whose threads are fewer than 2^32 in a dimension.
-constexpr uint32_t ROWS = 1 << 22;
+// One query of one head to a block: its parts, THREADS / (DP / 4) of them at a time, each thread's in the order of the wavefronts.
+constexpr int64_t ROWS_OF_A_JOIN = 1 << 22;   // (2^32 threads are the most)
 template <typename T, int DP, int THREADS>
 __global__ __launch_bounds__(THREADS) void stream_join_kernel(StreamArgs a) {
   constexpr int LANES = DP / 4, GROUPS = THREADS / LANES;
   __shared__ float4 sums[GROUPS][LANES];
   __shared__ float2 parts[GROUPS];   // maximum and sum
-  const uint32_t id = blockIdx.y * ROWS + blockIdx.x, bh = id / (uint32_t)a.S, query = id - bh * (uint32_t)a.S;   // (below 2^31)
+  const uint32_t id = a.first + blockIdx.x, bh = id / (uint32_t)a.S, query = id - bh * (uint32_t)a.S;   // (below 2^31)
   const uint32_t b = bh / (uint32_t)a.q_heads, hq = bh - b * (uint32_t)a.q_heads, h = hq / (uint32_t)a.group, row = query * a.group + hq - h * a.group;
-  if (b >= a.B) return;   // (behind the last row)
   const uint32_t n = a.before[b + 1] - a.before[b], times = a.heads * a.row_tiles;
   const bool there = n > 0 && query < length_of(a.q_lengths, b, a.S);
   const int lane = threadIdx.x % LANES, group = threadIdx.x / LANES;
@@ -447,9 +445,13 @@ hipError_t launch(StreamArgs a, hipStream_t s) {
   hipLaunchKernelGGL((stream_kernel<T, DP, COLS, R, PAGED>), dim3(a.waves / WAVES), dim3(64 * WAVES), F::LDS, s, a);
   // (few sequences and heads: many parts each.  One user's 131072 tokens, 8 heads, us of 128 / 512 threads: 11.1 / 6.4; 64 users, 4 heads 5.1 / 6.1)
   const int64_t n = a.B * a.S * a.q_heads;   // (below 2^31: 128 queries to a block of the other way, whose blocks are below 2^24)
-  const dim3 rows((unsigned)std::min<int64_t>(n, ROWS), (unsigned)div_up(n, ROWS));
-  if (a.B * a.heads * a.row_tiles <= 64) hipLaunchKernelGGL((stream_join_kernel<T, DP, 512>), rows, dim3(512), 0, s, a);
-  else hipLaunchKernelGGL((stream_join_kernel<T, DP, 128>), rows, dim3(128), 0, s, a);
+  const bool few = a.B * a.heads * a.row_tiles <= 64;
+  for (int64_t first = 0; first < n; first += ROWS_OF_A_JOIN) {
+    a.first = (uint32_t)first;
+    const dim3 rows((unsigned)std::min(n - first, ROWS_OF_A_JOIN));
+    if (few) hipLaunchKernelGGL((stream_join_kernel<T, DP, 512>), rows, dim3(512), 0, s, a);
+    else hipLaunchKernelGGL((stream_join_kernel<T, DP, 128>), rows, dim3(128), 0, s, a);
+  }
   return hipGetLastError();
 }
 

@@ -33,7 +33,7 @@ def test_more_queries_than_a_launch_has_threads_for():
     kl[3] = kl[-2] = 0
     out = A.cross_attention(q, k, v, k_lengths=kl, out=torch.full_like(q, 7.0))
     lengths = kl.tolist()
-    border = 2 ** 22 // (S * HQ)                                  # (the entry that starts the launch's second row)
+    border = 2 ** 22 // (S * HQ)                                  # (the entry that a second launch starts with)
     check_entries([out], (q, k, v, q), [S] * B, lengths, [0, 1, 3, border - 1, border, border + 1, B // 2, B - 3, B - 2, B - 1], "entries")
     # every entry, from calls of a part of the batch: both are within two roundings of the largest value from the definition, and (scores of at most 70, from
     # operands below 5) 4096 u
