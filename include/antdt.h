@@ -508,10 +508,13 @@ int antdt_token_logprobs_gradient(const void* logits, int64_t ld, int64_t N, int
  *    are never read into a result, whatever they hold, and are zeros in one.
  *  - attention: D a multiple of 8, at most ANTDT_MAX_ATTENTION_DIM, heads that start at multiples of 16 bytes (ANTDT_UNSUPPORTED otherwise).  Scores, the
  *    softmax and sums are fp32.  Of bf16 heads cache attention has its probabilities to 2^-15; cross attention rounds them, and in the backward pass the scores'
- *    gradients, to bf16 as the matrix cores' operands (the probabilities of few queries, where antdt_cross_attention has a workspace, to 2^-15).  scale is 1e-30 or more (finite times log2(e)).  A query without keys has zeros and passes no gradient.  A product q k^T below fp32's range is
- *    -infinity, whatever the operands, and its key has no weight.  A query all of whose products are -infinity has zeros, too, and passes no gradient (but
- *    infinite operands times its scores' gradients, which are zeros, are NaN); one with a product of NaN, +infinity or above fp32's range, or whose largest
- *    score, scale times the product, is beyond that range on either side, has NaN.
+ *    gradients, to bf16 as the matrix cores' operands (the probabilities of few queries, where antdt_cross_attention has a workspace, to 2^-15).  A call
+ *    repeated has the same result bit for bit; an entry in another batch may have its sums added up in another order.  scale is 1e-30 or more (finite times
+ *    log2(e)).
+ *  - what is no number: a query without keys has zeros and passes no gradient.  A product q k^T below fp32's range is -infinity, whatever the operands, and
+ *    its key has no weight.  A query all of whose products are -infinity has zeros, too, and passes no gradient (but infinite operands times its scores'
+ *    gradients, which are zeros, are NaN); one with a product of NaN, +infinity or above fp32's range, or whose largest score, scale times the product, is
+ *    beyond that range on either side, has NaN.
  */
 #define ANTDT_MAX_HEAD_DIM 256
 #define ANTDT_MAX_ATTENTION_DIM 128
@@ -545,7 +548,8 @@ int antdt_rotary(const void* x, int64_t ldx, int64_t ldx_head, int64_t N, int64_
  * n = offsets[b] .. offsets[b + 1] - 1 (DEVICE int32 [B + 1], ascending), or, offsets NULL, n = b.  lengths (DEVICE int32 [B]) count them in: the last
  * one's position is lengths[b] - 1.  A token of a position below 0 (length 0: a place of the batch that is not in use), in no sequence, or beyond the
  * table's pages is not appended.  q, q_out: DEVICE [N, q_heads, D], the same tokens' queries, turned likewise to q_out (which may be q with the same
- * strides), zeros for tokens without a position; q_heads may be 0.  Sequences share no page that is appended to.  D, heads as antdt_rotary.
+ * strides), zeros for tokens without a position; q_heads may be 0.  Sequences share no page that is appended to.  D, heads as antdt_rotary (attention over
+ * the cache takes fewer: see above).
  */
 int antdt_cache_append(const void* q, int64_t ldq, int64_t ldq_head, void* q_out, int64_t ldqo, int64_t ldqo_head, const void* k, int64_t ldk,
                        int64_t ldk_head, const void* v, int64_t ldv, int64_t ldv_head, int64_t N, int64_t q_heads, int64_t heads, int64_t D, int32_t dtype,
@@ -572,7 +576,8 @@ int antdt_cross_attention(const void* q, int64_t ldq_batch, int64_t ldq, int64_t
                           int64_t D, int32_t dtype, const int32_t* q_lengths, const int32_t* k_lengths, float scale, void* out, int64_t ldo_batch,
                           int64_t ldo, int64_t ldo_head, float* stats, void* workspace, size_t workspace_bytes, void* stream);
 /* Its gradients, from dout = that of out: dq [B, S, q_heads, D] (or NULL), dk and dv [B, T, heads, D] (both or neither NULL), of `dtype`; a repeated
- * operand's gradient is that of each repetition.  q, k, v, out, stats and lengths as antdt_cross_attention was given and left them. */
+ * operand's gradient is that of each repetition.  q, k, v, out, stats and lengths as antdt_cross_attention was given and left them; of entries of more than 64
+ * keys the sum of dout out over a row's columns is formed of out as it was rounded. */
 int antdt_cross_attention_backward_bytes(int64_t B, int64_t S, int64_t T, int64_t q_heads, int64_t heads, int64_t D, int32_t dtype, size_t* bytes);
 int antdt_cross_attention_backward(const void* dout, int64_t lddo_batch, int64_t lddo, int64_t lddo_head, const void* q, int64_t ldq_batch, int64_t ldq,
                                    int64_t ldq_head, const void* k, int64_t ldk_batch, int64_t ldk, int64_t ldk_head, const void* v, int64_t ldv_batch,

@@ -6,7 +6,7 @@ namespace {
 
 // A block has queries of a head; tiles of keys and values go through LDS, the next one's loads under way.  A wavefront's 32 queries take a pass over the
 // vector units (maximum, exponential, sum) for each over the matrix core, about as long; two wavefronts on a SIMD have them at the same time.  8 ragged
-// histories of 2048 queries and 4096 keys, 16 and 4 heads of 128 bf16 columns: 381 GFLOP in 400-430 us (by the clock that
+// histories of 2048 queries and 4096 keys, 16 and 4 heads of 128 bf16 columns: 381 GFLOP in 426-441 us (by the clock that
 // power leaves), an eighth of it the last blocks, when not all compute units have one.
 // PAGED: keys and values are a cache's, the user's pages looked up before the first tile; probabilities in two parts, see stream.hip (16 users of 100 and
 // 1000 tokens, 16 and 4 heads of 64 bf16 columns, all of it in the caches: 5.0 -> 5.1 us, 12.4 -> 13.5).

@@ -6,8 +6,8 @@
 // its tiles to LDS, several ahead, and keeps the running maximum, sum and output of a softmax over its part of a sequence.  Where a sequence lies
 // in one piece, that is the result; else the pieces' are joined by a second launch:
 //   m = max m_i,  l = sum l_i 2^(m_i - m),  out = sum o_i 2^(m_i - m) / l.
-// Bound by memory, a key head's queries share what is read of it: one user's 131072 tokens (8 heads of 128 bf16 columns, 537 MB) 92 us (5.8 TB/s) and 5.5 to
-// join; 64 users of 16 to 8192 tokens (178 MB) 39 and 5.  Where there is little to read, by the chain of a wavefront's loads (lengths, page, rows) and
+// Bound by memory, a key head's queries share what is read of it: one user's 131072 tokens (8 heads of 128 bf16 columns, 537 MB) 92 us (5.8 TB/s) and 5.3 to
+// join; 64 users of 16 to 8192 tokens (178 MB) 39 and 5.1.  Where there is little to read, by the chain of a wavefront's loads (lengths, page, rows) and
 // by its code's: one tile takes 10 us.
 // Probabilities of bf16 heads are multiplied in two parts: rounded to bf16 they would take results off by 0.0025 of their norm instead of the 0.0017 of the
 // results' own rounding, and the matrix cores are busy 6 % of the time (131072 tokens 92.5 -> 92.9 us, 64 users 39.1 -> 39.5).
