@@ -319,7 +319,8 @@ inline Shape cache_shape(int64_t B, int64_t T, int64_t q_heads, int64_t heads, i
   return Shape{B, q_heads / heads, T, heads, heads, D, dtype};
 }
 // Blocks of 32 for a single tile, too, where all of them run at once (us by shares / blocks of 20 tokens: 16 users, 16 and 4 heads of 64 bf16 columns 7.7 / 5.0, fp32
-// 8.8 / 7.3; 200 users, 8 and 2 heads of 64 fp32 columns, two rounds, 10.0 / 13.2).
+// 8.8 / 7.3; 200 users, 8 and 2 heads of 64 fp32 columns, two rounds, 10.0 / 13.2).  Many rounds read less evenly: 4096 users of 100 tokens, 8 heads of 64 bf16
+// columns 215 / 309, of 128 344 / 731, fp32 391 / 836; but one head of 64 bf16 columns 79 / 41, where most of the shares' time goes into the users' lengths.
 inline Plan cache_plan(const Shape& z) {
   const int most = z.T <= 32 ? at_once(z) : wide(z) ? 256 : 512;
   return cross_plan(z.B * z.q_heads, z.S, div_up(z.T, 32), most, key_waves(z), tile_us(z), false, 1);
